@@ -140,7 +140,8 @@ def prepare(case, seed):
         rows, n = case["rows"], case["n"]
         z = 2.5 * torch.randn((rows, n), device=DEV, generator=g)
         top = torch.randint(0, n, (rows, 40), device=DEV, generator=g)
-        z.scatter_(1, top, 8.0 + 4.0 * torch.rand((rows, 40), device=DEV, generator=g))
+        # (an entry that is drawn twice gets the larger value: which of two writes comes last is not the seed's)
+        z.scatter_reduce_(1, top, 8.0 + 4.0 * torch.rand((rows, 40), device=DEV, generator=g), "amax")
         if case["masked"]:
             z.masked_fill_(torch.rand((rows, n), device=DEV, generator=g) < case["masked"], -math.inf)
         if case["empty"]:
