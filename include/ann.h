@@ -61,7 +61,8 @@ extern "C" {
 
 #define ANN_NONE 0xFFFFFFFFu
 
-typedef enum { ANN_U8 = 0, ANN_I8 = 1, ANN_F32 = 2 } ann_dtype;
+/* (ANN_F16 and ANN_BF16: the calls on 4-bit rows and ann_sample only) */
+typedef enum { ANN_U8 = 0, ANN_I8 = 1, ANN_F32 = 2, ANN_F16 = 3, ANN_BF16 = 4 } ann_dtype;
 typedef enum { ANN_L2SQ = 0, ANN_MIPS = 1 } ann_metric;
 
 typedef enum {
@@ -474,6 +475,116 @@ int ann_hcnng_tree_edges(const void* points_dev, uint64_t n, uint32_t d, ann_dty
 int ann_hcnng_leaf_knn(const void* points_dev, uint64_t n, uint32_t d, ann_dtype dtype, ann_metric metric,
                        uint32_t Ls, uint32_t l, uint64_t seed, uint32_t tree, void* stream, uint32_t* perm_host,
                        uint64_t* leaf_off_host, uint64_t* nleaves, uint32_t* knn_ids_host, void* knn_dists_host);
+
+/* ------------------------------------------------------------------------
+ * Microscaled 4-bit rows (the OCP MX format MXFP4): a quarter of the memory of
+ * 16-bit rows, and operands of the scaled matrix instructions.  Elements are
+ * E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives); every 32 consecutive
+ * ones share a power of two, kept as an E8M0 byte b = exponent + 127.
+ *   storage     a row of d elements takes T = ceil(d / 128) steps: 64 T bytes
+ *               of codes (element 2i in the low half of byte i, 2i+1 in the
+ *               high half) and 4 T scale bytes, rows without gaps.  The
+ *               padding up to 128 T elements holds codes 0 and scales 0;
+ *               rows from elsewhere must hold it so too.
+ *   alignment   codes 16 bytes, scales 4; the other matrices of these calls
+ *               that of their element, with a row stride of their own (`ld`,
+ *               in elements, at least the row's length)
+ *   sizes       1 <= d <= 65536; rows < 2^31; a count of zero rows: ANN_OK,
+ *               nothing is done and no pointer is read
+ * All calls are asynchronous on `stream`, allocate nothing, keep nothing and
+ * can be captured into a graph.  Arguments they cannot serve: ANN_EINVAL.
+ * ------------------------------------------------------------------------ */
+
+/* Rows to 4 bits.  Of each 32 elements, with m their largest magnitude:
+ * e = max(floor(log2 m) - 2, -127), code = x / 2^e to the nearest E2M1 value,
+ * ties to even, magnitudes above 6 to 6.  Where one of them is infinite or NaN
+ * the scale byte is 255, and all 32 stand for NaN.
+ *   x_dev      n x d elements of any ann_dtype, rows ldx elements apart
+ *   norms_dev  n floats: the sum of the squares of the values that the row's
+ *              codes stand for (for ann_mx_search with ANN_L2SQ); may be NULL */
+int ann_mx_quantize(const void* x_dev, uint64_t n, uint32_t d, ann_dtype dtype, uint64_t ldx, uint8_t* codes_dev,
+                    uint8_t* scales_dev, float* norms_dev, void* stream);
+
+/* The values that 4-bit rows stand for, as ANN_F32 (exact), ANN_F16 or ANN_BF16
+ * (rounded once) rows of d elements, ldo elements apart.                     */
+int ann_mx_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev,
+                      ann_dtype dtype, uint64_t ldo, void* stream);
+
+/* out[i][j] = sum over the d elements of x[i] * value(row j): every row of a
+ * batch times every 4-bit row, summed in fp32 and rounded once to out_dtype
+ * (ANN_F32, ANN_F16 or ANN_BF16).
+ *   x_dev  nx x d of ANN_F32, ANN_F16 or ANN_BF16, ldx apart, taken whole
+ *          (f32 and f16 as the sum of three and two bf16 numbers, exact but
+ *          for parts below 2^-126)
+ *   n      4-bit rows; out_dev is nx x n, rows ldo >= n apart               */
+int ann_mx_product(const void* x_dev, uint64_t nx, ann_dtype xdtype, uint64_t ldx, const uint8_t* codes_dev,
+                   const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev, ann_dtype out_dtype, uint64_t ldo,
+                   void* stream);
+
+/* The same with a batch that is 4-bit rows too (xcodes, xscales: nx rows of
+ * d elements from ann_mx_quantize).                                          */
+int ann_mx_product_mx(const uint8_t* xcodes_dev, const uint8_t* xscales_dev, uint64_t nx, const uint8_t* codes_dev,
+                      const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev, ann_dtype out_dtype, uint64_t ldo,
+                      void* stream);
+
+/* The k nearest of n 4-bit rows to each of nq 4-bit queries, by scoring all of
+ * them.  With s = sum of q * x over the elements, in fp32,
+ *   ANN_MIPS  distance -s
+ *   ANN_L2SQ  distance max(0, |q|^2 - 2 (s - |x|^2 / 2)), from the norms that
+ *             ann_mx_quantize wrote (norms_dev, qnorms_dev; unused for MIPS)
+ * ordered by (s or s - |x|^2 / 2 downwards, id).  Where the products' exponents
+ * stay within 2^11 of each other, as those of rows of one kind do, all sums
+ * are exact and this is the order of (distance, id).
+ *   ids_dev, dists_dev  nq x k uint32 / float; ANN_NONE / +inf where there are
+ *               fewer than k rows.  Rows whose distance is NaN or +inf are
+ *               never returned.
+ *   scratch_dev at least what ann_mx_search_scratch says, 16-byte aligned; its
+ *               contents need not outlive the call's work on the stream
+ * 1 <= k <= 128.                                                             */
+int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const float* norms_dev, uint64_t n, uint32_t d,
+                  ann_metric metric, const uint8_t* qcodes_dev, const uint8_t* qscales_dev, const float* qnorms_dev,
+                  uint64_t nq, uint32_t k, uint32_t* ids_dev, float* dists_dev, void* scratch_dev, uint64_t scratch_bytes,
+                  void* stream);
+int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint64_t* bytes);
+
+/* ------------------------------------------------------------------------
+ * One id drawn for each row of scores.  A row's candidates are its entries
+ * other than NaN and -inf, sorted by (score downwards, id); weights are
+ * w = exp((score - best) / temperature) (1 where the scores are equal, so +inf
+ * shares the draw among the +inf entries), in fp64.  Kept, in this order:
+ *   top_k  > 0: the first top_k candidates
+ *   top_p  in (0, 1): the shortest prefix of those with at least that share of
+ *          their mass (the comparison is made on weights rounded to multiples
+ *          of 2^-(62 - ceil(log2 n)) of the largest)
+ *   min_p  > 0: those with w >= min(min_p, 1)
+ * and other values switch a rule off.  The id drawn is the smallest kept one,
+ * in id order, whose running mass exceeds uniform * mass.  A temperature that
+ * is not above zero takes the best candidate.  The result depends on the
+ * arguments only.
+ *   scores_dev    rows x n of ANN_F32, ANN_F16 or ANN_BF16, ld apart; n < 2^31
+ *   uniform_dev   rows floats in [0, 1); what is below or NaN counts as 0, from 1 on the last kept id is drawn
+ *   ids_dev       rows uint32; ANN_NONE for a row without candidates
+ *   logprobs_dev  rows floats: log(w / mass) of the id drawn, -inf for a row
+ *                 without candidates; may be NULL
+ *   opts          NULL: temperature 1, no rule.  Every setting is one value
+ *                 for all rows or, where the pointer is given, a device array
+ *                 with one value for each row.
+ *   scratch_dev   at least what ann_sample_scratch says, 16-byte aligned
+ * Asynchronous on `stream`, allocates nothing, can be captured into a graph. */
+typedef struct {
+  float temperature;
+  uint32_t top_k;
+  float top_p;
+  float min_p;
+  const float* temperature_dev;
+  const uint32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+} ann_sample_opts;
+int ann_sample(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtype, uint64_t ld, const ann_sample_opts* opts,
+               const float* uniform_dev, uint32_t* ids_dev, float* logprobs_dev, void* scratch_dev, uint64_t scratch_bytes,
+               void* stream);
+int ann_sample_scratch(uint64_t rows, uint64_t n, uint64_t* bytes);
 
 /* Thread-local description of the last error on this thread ("" if none).   */
 const char* ann_last_error(void);

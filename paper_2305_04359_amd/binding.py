@@ -14,7 +14,7 @@ import numpy as np
 from . import build as _build
 
 NONE = 0xFFFFFFFF
-U8, I8, F32 = 0, 1, 2
+U8, I8, F32, F16, BF16 = 0, 1, 2, 3, 4
 L2SQ, MIPS = 0, 1
 
 
@@ -68,6 +68,12 @@ class HcnngOpts(C.Structure):
     _fields_ = [("alloc", C.c_void_p), ("free", C.c_void_p), ("alloc_user", C.c_void_p)]
 
 
+class SampleOpts(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_uint32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p),
+                ("min_p_dev", C.c_void_p)]
+
+
 class HnswInfo(C.Structure):
     _fields_ = [("n", C.c_uint64), ("d", C.c_uint32), ("m", C.c_uint32), ("dtype", C.c_uint32),
                 ("metric", C.c_uint32), ("top", C.c_uint32), ("entry", C.c_uint32), ("rounds", C.c_uint64)]
@@ -81,6 +87,8 @@ EXPORTS = [
     "ann_hnsw_build", "ann_hnsw_insert_points", "ann_hnsw_from_host", "ann_hnsw_search", "ann_hnsw_info", "ann_hnsw_copy_levels", "ann_hnsw_layer_size",
     "ann_hnsw_copy_layer", "ann_hnsw_get_stats", "ann_hnsw_free",
     "ann_hcnng_build", "ann_hcnng_build_with", "ann_hcnng_tree_edges", "ann_hcnng_leaf_knn",
+    "ann_mx_quantize", "ann_mx_dequantize", "ann_mx_product", "ann_mx_product_mx", "ann_mx_search", "ann_mx_search_scratch",
+    "ann_sample", "ann_sample_scratch",
 ]
 
 _lib = None
@@ -171,6 +179,22 @@ def lib():
         L.ann_hcnng_leaf_knn.restype = C.c_int
         L.ann_hcnng_leaf_knn.argtypes = [vp, u64, u32, C.c_int, C.c_int, u32, u32, u64, u32, vp, vp, vp,
                                          C.POINTER(u64), vp, vp]
+        L.ann_mx_quantize.restype = C.c_int
+        L.ann_mx_quantize.argtypes = [vp, u64, u32, C.c_int, u64, vp, vp, vp, vp]
+        L.ann_mx_dequantize.restype = C.c_int
+        L.ann_mx_dequantize.argtypes = [vp, vp, u64, u32, vp, C.c_int, u64, vp]
+        L.ann_mx_product.restype = C.c_int
+        L.ann_mx_product.argtypes = [vp, u64, C.c_int, u64, vp, vp, u64, u32, vp, C.c_int, u64, vp]
+        L.ann_mx_product_mx.restype = C.c_int
+        L.ann_mx_product_mx.argtypes = [vp, vp, u64, vp, vp, u64, u32, vp, C.c_int, u64, vp]
+        L.ann_mx_search.restype = C.c_int
+        L.ann_mx_search.argtypes = [vp, vp, vp, u64, u32, C.c_int, vp, vp, vp, u64, u32, vp, vp, vp, u64, vp]
+        L.ann_mx_search_scratch.restype = C.c_int
+        L.ann_mx_search_scratch.argtypes = [u64, u32, u64, u32, C.POINTER(u64)]
+        L.ann_sample.restype = C.c_int
+        L.ann_sample.argtypes = [vp, u64, u64, C.c_int, u64, C.POINTER(SampleOpts), vp, vp, vp, vp, u64, vp]
+        L.ann_sample_scratch.restype = C.c_int
+        L.ann_sample_scratch.argtypes = [u64, u64, C.POINTER(u64)]
         L.ann_last_error.restype = C.c_char_p
         L.ann_last_error.argtypes = []
         _lib = L
@@ -618,3 +642,180 @@ def ann_hcnng_leaf_knn(points, Ls, l, seed, tree, metric=L2SQ):
                                     off.ctypes.data_as(C.c_void_p), C.byref(nl), ids.ctypes.data_as(C.c_void_p),
                                     dists.ctypes.data_as(C.c_void_p)))
     return perm, off[:nl.value + 1].astype(np.int64), ids, dists
+
+
+_ELEMENT_CODES = {}
+
+
+def _element_code(t) -> int:
+    """The ann_dtype of a tensor among the types that the calls on 4-bit rows and ann_sample take."""
+    if not _ELEMENT_CODES:
+        torch = _torch()
+        _ELEMENT_CODES.update({torch.uint8: U8, torch.int8: I8, torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    try:
+        return _ELEMENT_CODES[t.dtype]
+    except KeyError:
+        raise TypeError(f"unsupported dtype {t.dtype}") from None
+
+
+def _rows2d(t, name):
+    """A 2-D device tensor whose rows are contiguous, and the distance between them in elements."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D device tensor")
+    n, d = t.shape
+    if n == 0 or d == 0:
+        return t, d
+    if (d > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < d):
+        raise ValueError(f"the rows of {name} must be contiguous and must not overlap")
+    return t, (t.stride(0) if n > 1 else d)
+
+
+def _one_value_per_row(t, name, dtype, rows, device):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != rows or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {rows} {dtype} on {device}")
+    return t
+
+
+class MxRows:
+    """Microscaled 4-bit rows (see ann.h): codes (n, 64 T) and scales (n, 4 T), uint8, T = ceil(d / 128), the row
+    length d, and the rows' squared norms (n, float32) or None."""
+
+    __slots__ = ("codes", "scales", "d", "norms")
+
+    def __init__(self, codes, scales, d, norms=None):
+        steps = (int(d) + 127) // 128
+        torch = _torch()
+        for t, width, name in ((codes, 64 * steps, "codes"), (scales, 4 * steps, "scales")):
+            if not t.is_cuda or t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != width or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous (n, {width}) uint8 device tensor for rows of {d} elements")
+        if codes.shape[0] != scales.shape[0] or codes.device != scales.device:
+            raise ValueError("codes and scales must have the same rows on the same device")
+        if norms is not None:
+            _one_value_per_row(norms, "norms", torch.float32, codes.shape[0], codes.device)
+        self.codes, self.scales, self.d, self.norms = codes, scales, int(d), norms
+
+    @property
+    def n(self) -> int:
+        return self.codes.shape[0]
+
+
+def ann_mx_quantize(x, norms=False) -> MxRows:
+    """Rows of a 2-D device tensor (uint8, int8, float32, float16 or bfloat16) as microscaled 4-bit rows."""
+    torch = _torch()
+    x, ld = _rows2d(x, "x")
+    n, d = x.shape
+    steps = (d + 127) // 128
+    out = MxRows.__new__(MxRows)
+    out.codes = torch.empty((n, 64 * steps), dtype=torch.uint8, device=x.device)
+    out.scales = torch.empty((n, 4 * steps), dtype=torch.uint8, device=x.device)
+    out.norms = torch.empty(n, dtype=torch.float32, device=x.device) if norms else None
+    out.d = d
+    _check(lib().ann_mx_quantize(x.data_ptr(), n, d, _element_code(x), ld, out.codes.data_ptr(), out.scales.data_ptr(),
+                                 out.norms.data_ptr() if norms else None, _stream_ptr()))
+    return out
+
+
+def ann_mx_dequantize(rows: MxRows, dtype=None, out=None):
+    """The values that 4-bit rows stand for: (n, d), float32 unless `dtype` or `out` says otherwise."""
+    torch = _torch()
+    if out is None:
+        out = torch.empty((rows.n, rows.d), dtype=dtype or torch.float32, device=rows.codes.device)
+    out, ld = _rows2d(out, "out")
+    if tuple(out.shape) != (rows.n, rows.d) or out.device != rows.codes.device or dtype not in (None, out.dtype):
+        raise ValueError(f"out must be ({rows.n}, {rows.d}) on {rows.codes.device}")
+    _check(lib().ann_mx_dequantize(rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.d, out.data_ptr(),
+                                   _element_code(out), ld, _stream_ptr()))
+    return out
+
+
+def ann_mx_product(x, rows: MxRows, dtype=None, out=None):
+    """Every row of `x` (a float32, float16 or bfloat16 tensor, or MxRows) times every 4-bit row: (len(x), n), float32
+    unless `dtype` or `out` says otherwise."""
+    torch = _torch()
+    packed = isinstance(x, MxRows)
+    nx, d, device = (x.n, x.d, x.codes.device) if packed else (*_rows2d(x, "x")[0].shape, x.device)
+    if d != rows.d or device != rows.codes.device:
+        raise ValueError("x and rows must have the same row length and device")
+    if out is None:
+        out = torch.empty((nx, rows.n), dtype=dtype or torch.float32, device=device)
+    out, ldo = _rows2d(out, "out")
+    if tuple(out.shape) != (nx, rows.n) or out.device != device or dtype not in (None, out.dtype):
+        raise ValueError(f"out must be ({nx}, {rows.n}) on {device}")
+    if packed:
+        _check(lib().ann_mx_product_mx(x.codes.data_ptr(), x.scales.data_ptr(), nx, rows.codes.data_ptr(),
+                                       rows.scales.data_ptr(), rows.n, d, out.data_ptr(), _element_code(out), ldo,
+                                       _stream_ptr()))
+    else:
+        _check(lib().ann_mx_product(x.data_ptr(), nx, _element_code(x), _rows2d(x, "x")[1], rows.codes.data_ptr(),
+                                    rows.scales.data_ptr(), rows.n, d, out.data_ptr(), _element_code(out), ldo,
+                                    _stream_ptr()))
+    return out
+
+
+def _scratch(given, need, device):
+    torch = _torch()
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if not given.is_cuda or given.device != device or not given.is_contiguous() or given.numel() * given.element_size() < need:
+        raise ValueError(f"scratch must be a contiguous tensor of at least {need} bytes on {device}")
+    return given
+
+
+def ann_mx_search(rows: MxRows, queries: MxRows, k, metric=L2SQ, ids_out=None, dists_out=None, scratch=None):
+    """The k nearest of all 4-bit rows to each 4-bit query; returns (ids, dists) device tensors.  L2SQ needs the norms
+    of both."""
+    torch = _torch()
+    device = rows.codes.device
+    if queries.d != rows.d or queries.codes.device != device:
+        raise ValueError("queries must match rows in row length and device")
+    nq = queries.n
+    need = C.c_uint64(0)
+    _check(lib().ann_mx_search_scratch(rows.n, rows.d, nq, k, C.byref(need)))
+    scratch = _scratch(scratch, need.value, device)
+    if ids_out is None:
+        ids_out = torch.empty((nq, k), dtype=torch.int32, device=device)
+    if dists_out is None:
+        dists_out = torch.empty((nq, k), dtype=torch.float32, device=device)
+    for t, dtype, name in ((ids_out, torch.int32, "ids_out"), (dists_out, torch.float32, "dists_out")):
+        if tuple(t.shape) != (nq, k) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous ({nq}, {k}) tensor of {dtype} on {device}")
+    _check(lib().ann_mx_search(rows.codes.data_ptr(), rows.scales.data_ptr(),
+                               rows.norms.data_ptr() if rows.norms is not None else None, rows.n, rows.d, int(metric),
+                               queries.codes.data_ptr(), queries.scales.data_ptr(),
+                               queries.norms.data_ptr() if queries.norms is not None else None, nq, k,
+                               ids_out.data_ptr(), dists_out.data_ptr(), scratch.data_ptr(),
+                               scratch.numel() * scratch.element_size(), _stream_ptr()))
+    return ids_out, dists_out
+
+
+def ann_sample(scores, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ids_out=None, logprobs_out=None, scratch=None):
+    """One id drawn for each row of `scores` (float32, float16 or bfloat16) by the rules of ann_sample in ann.h, from one
+    number in [0, 1) for each row; returns (ids, logprobs).  Every setting is one number, or a tensor with one for each
+    row (float32; top_k int32)."""
+    torch = _torch()
+    scores, ld = _rows2d(scores, "scores")
+    rows, n = scores.shape
+    device = scores.device
+    _one_value_per_row(uniform, "uniform", torch.float32, rows, device)
+    o = SampleOpts()
+    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(value, torch.Tensor):
+            setattr(o, name + "_dev", _one_value_per_row(value, name, dtype, rows, device).data_ptr())
+        else:
+            if name == "top_k" and not 0 <= value < 2 ** 32:
+                raise ValueError("top_k must be 0 (off) or above")
+            setattr(o, name, value)
+    need = C.c_uint64(0)
+    _check(lib().ann_sample_scratch(rows, n, C.byref(need)))
+    scratch = _scratch(scratch, need.value, device)
+    if ids_out is None:
+        ids_out = torch.empty(rows, dtype=torch.int32, device=device)
+    if logprobs_out is None:
+        logprobs_out = torch.empty(rows, dtype=torch.float32, device=device)
+    _one_value_per_row(ids_out, "ids_out", torch.int32, rows, device)
+    _one_value_per_row(logprobs_out, "logprobs_out", torch.float32, rows, device)
+    _check(lib().ann_sample(scores.data_ptr(), rows, n, _element_code(scores), ld, C.byref(o), uniform.data_ptr(),
+                            ids_out.data_ptr(), logprobs_out.data_ptr(), scratch.data_ptr(),
+                            scratch.numel() * scratch.element_size(), _stream_ptr()))
+    return ids_out, logprobs_out

@@ -1,0 +1,156 @@
+"""ann_sample against its definition in 64 bits."""
+import numpy as np
+import pytest
+
+import mx_plain as P
+from helpers import dev
+
+pytestmark = pytest.mark.gpu
+
+
+def check(torch, A, scores, u, **settings):
+    """Ids equal; log-probabilities within their rounding to fp32 and the sums' own (n terms in fp64)."""
+    ids, logprobs = A.ann_sample(scores, u, **settings)
+    z, uh = scores.double().cpu().numpy(), u.double().cpu().numpy()
+    rows = len(z)
+    per = {k: v.double().cpu().numpy() if isinstance(v, torch.Tensor) else np.full(rows, np.float32(v), np.float64) for k, v in settings.items()}
+    for r in range(rows):
+        s = {k: (int(v[r]) if k == "top_k" else float(v[r])) for k, v in per.items()}
+        i, lp = P.draw(np.where(np.isnan(z[r]), -np.inf, z[r]), uh[r], **s)
+        assert int(ids[r]) == i, (r, s, i, int(ids[r]))
+        got = float(logprobs[r])
+        assert got == lp or abs(got - lp) <= 2.0 ** -24 * abs(lp) + 1e-12 + 2.0 ** -149, (r, s, lp, got)
+    return ids
+
+
+def scores_of(torch, rng, rows, n, dtype, masked=0.0):
+    z = 3.0 * rng.standard_normal((rows, n))
+    z[rng.random((rows, n)) < masked] = -np.inf
+    return dev(torch, z).to(getattr(torch, dtype))
+
+
+def uniform(torch, rng, rows):
+    return dev(torch, rng.random(rows).astype(np.float32) * np.float32(1 - 2.0 ** -24))
+
+
+RULES = ({}, dict(temperature=0.7), dict(temperature=1.5, top_k=1), dict(top_k=50), dict(top_p=0.9, temperature=0.8), dict(min_p=0.05),
+         dict(top_k=40, top_p=0.8, min_p=0.02, temperature=1.3), dict(temperature=0.0), dict(top_k=10 ** 9, top_p=0.999999), dict(top_p=1e-6),
+         dict(min_p=1.0), dict(min_p=5.0), dict(temperature=1e-30), dict(temperature=float("inf"), top_p=0.5), dict(temperature=float("nan")))
+
+
+@pytest.mark.parametrize("dtype", ("float32", "float16", "bfloat16"))
+@pytest.mark.parametrize("rows,n", [(1, 1), (2, 2), (5, 63), (3, 64), (7, 1000), (4, 1025), (2, 5003), (1, 40_000), (130, 257)])
+def test_rules(env, dtype, rows, n):
+    torch, A, _ = env
+    rng = np.random.default_rng(rows * n)
+    for i, rule in enumerate(RULES):
+        z = scores_of(torch, rng, rows, n, dtype, masked=(0.0, 0.3, 0.97)[i % 3])
+        check(torch, A, z, uniform(torch, rng, rows), **rule)
+
+
+@pytest.mark.parametrize("rows,n", [(1, 128_000), (3, 200_003)])
+def test_long_rows(env, rows, n):
+    torch, A, _ = env
+    rng = np.random.default_rng(n)
+    for dtype, rule in (("float32", {}), ("bfloat16", dict(top_p=0.95)), ("float16", dict(top_k=64, min_p=0.01)), ("float32", dict(top_p=0.5, temperature=2.0))):
+        check(torch, A, scores_of(torch, rng, rows, n, dtype), uniform(torch, rng, rows), **rule)
+
+
+def test_settings_of_each_row(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(5)
+    rows, n = 60, 3001
+    t = dev(torch, rng.choice([0.0, 0.3, 1.0, 2.0, -1.0], rows).astype(np.float32))
+    k = dev(torch, rng.choice([0, 1, 7, 500, 3001, 10_000], rows).astype(np.int32))
+    p = dev(torch, rng.choice([0.0, 0.2, 0.9, 1.0, 2.0], rows).astype(np.float32))
+    m = dev(torch, rng.choice([0.0, 0.001, 0.2, 1.0], rows).astype(np.float32))
+    for dtype in ("float32", "bfloat16"):
+        check(torch, A, scores_of(torch, rng, rows, n, dtype, 0.1), uniform(torch, rng, rows), temperature=t, top_k=k, top_p=p, min_p=m)
+
+
+def test_equal_scores(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(6)
+    for n in (3, 64, 1024, 5000):
+        z = dev(torch, rng.integers(0, 3, (20, n)).astype(np.float32))
+        for rule in ({}, dict(top_k=n // 3 + 1), dict(top_p=0.5), dict(top_p=0.25, top_k=n // 2 + 1), dict(min_p=0.9)):
+            check(torch, A, z, uniform(torch, rng, 20), **rule)
+        check(torch, A, torch.zeros((20, n), device="cuda:0"), uniform(torch, rng, 20), top_p=0.75, top_k=n - 1)
+
+
+def test_masks_infinities_and_nan(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(7)
+    inf, low = float("inf"), float(np.finfo(np.float32).min)
+    z = 2.0 * rng.standard_normal((16, 1500)).astype(np.float32)
+    z[0] = -inf                      # nothing to draw from
+    z[1] = np.nan
+    z[2, 5:] = -inf
+    z[3] = low                       # the type's lowest value masks nothing when it is all there is
+    z[4, 100:] = low
+    z[5, [7, 900]] = inf             # infinite scores share the draw
+    z[6, 3] = inf
+    z[7, ::2] = np.nan
+    z[8, 1:] = np.nan
+    z[9, :] = -inf
+    z[9, 1499] = -3.0
+    z[10, 0] = 88.0                  # one candidate takes nearly all the mass
+    z[11] = -0.0
+    z[11, 700:] = 0.0                # zeros of either sign are equal
+    z[12] *= 1e-42                   # subnormal scores
+    z[13, 20] = 3.4e38
+    z[13, 21] = -3.4e38
+    z[14, :700] = 1e30
+    z[15] = np.where(rng.random(1500) < 0.5, np.nan, -inf)
+    for rule in RULES:
+        for dtype in (torch.float32, torch.bfloat16, torch.float16):
+            ids = check(torch, A, dev(torch, z).to(dtype), uniform(torch, rng, 16), **rule)
+            assert ids[0] == -1 and ids[1] == -1 and ids[15] == -1
+
+
+def test_ends_of_the_unit_interval(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(8)
+    z = scores_of(torch, rng, 6, 2000, "float32", 0.5)
+    z[:, 0] = -float("inf")
+    z[:, 1999] = -200.0  # a weight that rounding loses in the sum
+    for v in (0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -3.0):
+        for rule in ({}, dict(top_k=3), dict(top_p=0.5)):
+            check(torch, A, z, torch.full((6,), v, device="cuda:0"), **rule)
+
+
+def test_rows_with_a_stride(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(9)
+    for dtype, pad, at in (("float32", 3, 1), ("bfloat16", 8, 0), ("float16", 1, 1)):
+        wide = scores_of(torch, rng, 9, 1001 + pad, dtype)
+        u = uniform(torch, rng, 9)
+        wide[:, :at] = 1e4
+        wide[:, at + 1001:] = float("nan")
+        check(torch, A, wide[:, at:at + 1001], u, top_p=0.9)
+        check(torch, A, wide[:, at:at + 1001], u, top_k=5)
+
+
+def test_frequencies(env):
+    """A hundred thousand draws from one row: counts within five standard deviations of the probabilities."""
+    torch, A, _ = env
+    n = 100_000
+    z = torch.tensor([1.0, 0.0, -1.0, 2.0, -float("inf"), 0.5], device="cuda:0")
+    ids, logprobs = A.ann_sample(z.repeat(n, 1), torch.rand(n, device="cuda:0", generator=torch.Generator(device="cuda:0").manual_seed(3)))
+    p = torch.softmax(z.double(), 0).cpu().numpy()
+    c = torch.bincount(ids, minlength=6).cpu().numpy()
+    assert (np.abs(c - n * p) <= 5 * np.sqrt(n * p * (1 - p)) + 1e-9).all()
+    assert torch.allclose(logprobs.double(), torch.log_softmax(z.double(), 0)[ids], atol=1e-6)
+
+
+def test_scores_beyond_32_bits(env):
+    """Rows that start more than 4 GiB into the scores."""
+    torch, A, _ = env
+    rows, n = 17_000, 131_073
+    z = torch.zeros((rows, n), dtype=torch.float16, device="cuda:0")
+    tail = scores_of(torch, np.random.default_rng(1), 8, n, "float16")
+    z[-8:] = tail
+    u = torch.rand(rows, device="cuda:0")
+    ids, logprobs = A.ann_sample(z, u, top_p=0.9)
+    i, lp = A.ann_sample(tail, u[-8:].contiguous(), top_p=0.9)
+    assert torch.equal(ids[-8:], i) and torch.equal(logprobs[-8:], lp)
