@@ -12,19 +12,23 @@ struct ProductArgs {
   char* out;
   u64 ldo;
   u32 wide;  // four results can be written at once
+  u32 wide_x;  // eight elements of the batch can be read at once
 };
 
-// The 64 x 64 results of a wave: rows of `w` in the matrix instruction's rows, so that a lane holds four results
-// that follow each other in `out`.
-template <typename OUT>
-__device__ __forceinline__ void store_results(const ProductArgs& a, const v4f (&acc)[4][4], u64 w0, u64 x0) {
+constexpr size_t FEW_LDS = 160 * 1024;    // of a compute unit
+constexpr size_t FEW_BATCH = 96 * 1024;   // most of it that a batch may take
+
+// The 16 WF x 16 XF results of a wave: rows of `w` in the matrix instruction's rows, so that a lane holds four
+// results that follow each other in `out`.
+template <typename OUT, int WF, int XF>
+__device__ __forceinline__ void store_results(const ProductArgs& a, const v4f (&acc)[WF][XF], u64 w0, u64 x0) {
   const u32 lane = threadIdx.x % 64;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < XF; ++j) {
     const u64 x = x0 + 16 * j + lane % 16;
     if (x >= a.nx) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WF; ++i) {
       const u64 w = w0 + 16 * i + lane / 16 * 4;
       OUT* to = reinterpret_cast<OUT*>(a.out) + x * a.ldo + w;
       if (a.wide && w + 4 <= a.w.n) {
@@ -75,7 +79,7 @@ __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 til
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = mx_mfma(w[i].codes, x[j].codes, acc[i][j], w[i].scale, x[j].scale);
     }
-    store_results<OUT>(a, acc, w0, x0);
+    store_results<OUT, 4, 4>(a, acc, w0, x0);
   }
 }
 
@@ -102,70 +106,295 @@ constexpr int parts_of() {
   return sizeof(T) == 4 ? 3 : __is_same(T, __half) ? 2 : 1;
 }
 
-// 4-bit rows against rows of 16 or 32 bits: codes become bf16 numbers times their scale, exactly; the batch is the
-// sum of one, two or three bf16 numbers.  Within a step the elements are taken in the order that a lane holds
-// them: 8 at a time of the lane's 32, the same ones on both sides.
-template <typename T, typename OUT>
-__global__ __launch_bounds__(256) void mx_product16_kernel(ProductArgs a, u32 tiles_w, u64 tiles) {
+// Eight elements of a row of the batch from `at` on; what lies past d is 0, and rows past the last are read as it.
+template <typename T>
+__device__ __forceinline__ Pack<T, 8> load_batch(const ProductArgs& a, u64 row, u32 at) {
+  const T* from = reinterpret_cast<const T*>(a.x) + min(row, (u64)a.nx - 1) * a.ldx + at;
+  if (a.wide_x && at + 8 <= a.d) return *reinterpret_cast<const Pack<T, 8>*>(from);
+  Pack<T, 8> p;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p.v[e] = at + e < a.d ? from[e] : T(0.0f);
+  return p;
+}
+template <typename T, int PARTS>
+__device__ __forceinline__ void split_pack(const Pack<T, 8>& p, v8bf (&out)[PARTS]) {
+  if constexpr (PARTS == 1) {
+    out[0] = __builtin_bit_cast(v8bf, p);
+    return;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      __bf16 part[PARTS];
+      split<PARTS>(mx_float(p.v[e]), part);
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) out[i][e] = part[i];
+    }
+  }
+}
+
+// Eight codes as bf16 numbers times their scale, exactly.  The conversion reads the exponent bits of its scale
+// alone, so that a scale byte needs no care at its ends: 0 is 2^-127 and 255 is NaN.
+__device__ __forceinline__ v8bf unpack(u32 codes, u32 scale_byte) {
+  const float scale = __uint_as_float(scale_byte << 23);
+  const v2bf p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3)};
+  return v8bf{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
+}
+
+// Few rows of 16 or 32 bits against all 4-bit rows: the batch stays in LDS, as one, two or three bf16 numbers for
+// each element, and the 4-bit rows stream past it, each byte read once.  A wave takes 32 of them.  Long rows are
+// summed in RUNS runs of steps, which are added up in their order, by one wave or, where 4-bit rows are few, by
+// a wave each: the sums do not depend on that.  Within a step the elements are taken in the order that a lane
+// holds them (8 at a time of its 32, the same ones on both sides).
+constexpr u32 FEW_THREADS = 512;
+constexpr u32 FEW_ROWS = 32;
+constexpr u32 FEW_AHEAD = 4;  // steps whose codes a wave asks for at once
+
+template <typename T, typename OUT, int G>
+__global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs a, u32 tiles, u32 runs, u32 share) {
   constexpr int PARTS = parts_of<T>();
-  const u32 wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  for (u64 t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const u64 w0 = t % tiles_w * 128 + (wave & 1) * 64, x0 = t / tiles_w * 128 + (wave >> 1) * 64;
-    if (w0 >= a.w.n || x0 >= a.nx) continue;
-    v4f acc[4][4] = {};
-    for (u32 s = 0; s < a.w.steps; ++s) {
-      Fragment w[4];
+  extern __shared__ __align__(16) char lds[];
+  const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  // 16 bytes more for each row than its elements take: the rows' pieces then lie in different banks
+  const u32 row_bytes = a.w.steps * MX_STEP * 2 + 16, part_bytes = a.nx * row_bytes;
+  const u32 pieces = a.w.steps * 16;
+  for (u32 i = threadIdx.x; i < a.nx * pieces; i += FEW_THREADS) {
+    const u32 row = i / pieces, at = i % pieces;
+    v8bf x[PARTS];
+    split_pack<T, PARTS>(load_batch<T>(a, row, at * 8), x);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = load_fragment(a.w, w0 + 16 * i, s);
+    for (int p = 0; p < PARTS; ++p) *reinterpret_cast<v8bf*>(lds + p * part_bytes + row * row_bytes + at * 16) = x[p];
+  }
+  __syncthreads();
+  const u32 teams = FEW_THREADS / 64 / share;  // of waves that share rows
+  const u32 first_run = wave % share * (runs / share), last_run = first_run + runs / share;
+  const char* xs[G];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        v8bf wv[4];
+  for (int j = 0; j < G; ++j) xs[j] = lds + min(16u * j + lane % 16, a.nx - 1) * row_bytes + lane / 16 * 64;
+  for (u32 t0 = blockIdx.x * teams; t0 < tiles; t0 += gridDim.x * teams) {
+    const u32 t = t0 + wave / share;
+    const u64 w0 = (u64)t * FEW_ROWS;
+    v4f sum[2][G] = {};
+    if (t < tiles) {
+      const uint8_t* codes[2];
+      const u32* scales[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float scale = mx_scale((u32)w[i].scale);
-          const v2bf p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((u32)w[i].codes[c], scale, 0),
-                             __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((u32)w[i].codes[c], scale, 1),
-                             __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((u32)w[i].codes[c], scale, 2),
-                             __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((u32)w[i].codes[c], scale, 3)};
-          wv[i] = v8bf{p[0].x, p[0].y, p[1].x, p[1].y, p[2].x, p[2].y, p[3].x, p[3].y};
-        }
-        const u32 at = s * MX_STEP + lane / 16 * 32 + c * 8;
+      for (int i = 0; i < 2; ++i) {
+        const u64 row = min(w0 + 16 * i + lane % 16, (u64)a.w.n - 1);
+        codes[i] = a.w.codes + row * a.w.steps * MX_STEP_BYTES + lane / 16 * 16;
+        scales[i] = reinterpret_cast<const u32*>(a.w.scales) + row * a.w.steps;
+      }
+      for (u32 run = first_run; run < last_run; ++run) {
+        const u32 s0 = a.w.steps * run / runs, s1 = a.w.steps * (run + 1) / runs;
+        v4f acc[2][G] = {};
+        for (u32 first = s0; first < s1; first += FEW_AHEAD) {
+          v4i w[FEW_AHEAD][2];
+          u32 b[FEW_AHEAD][2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u64 row = min(x0 + 16 * j + lane % 16, (u64)a.nx - 1);
-          const T* from = reinterpret_cast<const T*>(a.x) + row * a.ldx + at;
-          v8bf xv[PARTS];
+          for (u32 u = 0; u < FEW_AHEAD; ++u)  // all on their way before the first is used
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            __bf16 part[PARTS];
-            split<PARTS>(at + e < a.d ? mx_float(from[e]) : 0.0f, part);
+            for (int i = 0; i < 2; ++i) {
+              const u32 s = min(first + u, s1 - 1);
+              w[u][i] = *reinterpret_cast<const v4i*>(codes[i] + (u64)s * MX_STEP_BYTES);
+              b[u][i] = scales[i][s];
+            }
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) xv[p][e] = part[p];
+          for (u32 u = 0; u < FEW_AHEAD; ++u) {
+            if (first + u >= s1) break;
+            const u32 b0 = b[u][0] >> (lane / 16 * 8) & 255, b1 = b[u][1] >> (lane / 16 * 8) & 255;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const v8bf wv[2] = {unpack((u32)w[u][0][c], b0), unpack((u32)w[u][1][c], b1)};
+#pragma unroll
+              for (int j = 0; j < G; ++j)
+#pragma unroll
+                for (int p = PARTS - 1; p >= 0; --p) {
+                  const v8bf x = *reinterpret_cast<const v8bf*>(xs[j] + p * part_bytes + (first + u) * (MX_STEP * 2) + c * 16);
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], x, acc[i][j], 0, 0, 0);
+                }
+            }
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], xv[p], acc[i][j], 0, 0, 0);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < G; ++j) sum[i][j] += acc[i][j];
       }
     }
-    store_results<OUT>(a, acc, w0, x0);
+    if (share > 1) {  // (a run each) they meet in the team's first wave
+      char* sums = lds + PARTS * part_bytes + wave * (2 * G * 1024) + lane * 16;
+      if (wave % share)
+#pragma unroll
+        for (int i = 0; i < 2 * G; ++i) *reinterpret_cast<v4f*>(sums + i * 1024) = sum[i / G][i % G];
+      __syncthreads();
+      if (wave % share == 0)
+        for (u32 o = 1; o < share; ++o)
+#pragma unroll
+          for (int i = 0; i < 2 * G; ++i) sum[i / G][i % G] += *reinterpret_cast<const v4f*>(sums + o * (2 * G * 1024) + i * 1024);
+      __syncthreads();
+      if (wave % share) continue;
+    }
+    if (t < tiles) store_results<OUT, 2, G>(a, sum, w0, 0);
   }
+}
+
+// Many rows: 256 4-bit rows x 64 XF rows of the batch a workgroup of eight waves, 128 x 16 XF a wave.  Halves of a
+// step (64 elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for
+// its turn and the one after is on its way.  The codes become bf16 numbers on their way from LDS to the matrix
+// cores, four conversions for each fragment of 16 rows x 32 elements, which serves XF x PARTS products.
+constexpr u32 MANY_THREADS = 512;
+constexpr u32 MANY_ROWS = 256;
+
+template <typename T, typename OUT, int XF>
+__global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductArgs a, u32 tiles_w, u32 tiles) {
+  constexpr int PARTS = parts_of<T>();
+  constexpr u32 X_ROWS = 64 * XF;
+  constexpr u32 W_BYTES = MANY_ROWS * 32, X_BYTES = X_ROWS * 128, STAGE = W_BYTES + PARTS * X_BYTES;
+  extern __shared__ __align__(16) char lds[];  // two stages, then the scales of two steps
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  // Chiplets take workgroups in turn: each gets a run of tiles that share rows.
+  const u32 per = (tiles + 7) / 8, t = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (t >= tiles) return;
+  const u32 tiles_x = tiles / tiles_w;
+  const u64 w0 = (u64)(t / tiles_x) * MANY_ROWS, x0 = (u64)(t % tiles_x) * X_ROWS;
+  const u32 ww = wave % 2 * 128, wx = wave / 2 * (16 * XF);  // the wave's part of the tile
+
+  // what this thread brings to LDS: half the codes of a row, XF pieces of eight elements, a row's scales
+  const uint8_t* codes = a.w.codes + min(w0 + tid / 2, (u64)a.w.n - 1) * a.w.steps * MX_STEP_BYTES + tid % 2 * 16;
+  const u32* scales = reinterpret_cast<const u32*>(a.w.scales) + min(w0 + tid % MANY_ROWS, (u64)a.w.n - 1) * a.w.steps;
+  v4i next_w;
+  u32 next_scale = 0;
+  Pack<T, 8> next_x[XF];
+  const u32 halves = a.w.steps * 2;
+  auto fetch = [&](u32 h) {
+    next_w = *reinterpret_cast<const v4i*>(codes + (u64)h * 32);
+    if (h % 2 == 0) next_scale = scales[h / 2];
+#pragma unroll
+    for (int i = 0; i < XF; ++i) next_x[i] = load_batch<T>(a, x0 + tid / 8 + 64 * i, h * 64 + tid % 8 * 8);
+  };
+  auto keep = [&](u32 h) {
+    char* stage = lds + h % 2 * STAGE;
+    const u32 row = tid / 2;
+#pragma unroll
+    for (u32 e = 0; e < 2; ++e) {  // units of eight bytes, dealt over the banks by the row
+      const u32 unit = (tid % 2 * 2 + e + row / 4) % 4;
+      *reinterpret_cast<long*>(stage + row * 32 + unit * 8) = e ? (long)(u32)next_w[3] << 32 | (u32)next_w[2] : (long)(u32)next_w[1] << 32 | (u32)next_w[0];
+    }
+    if (h % 2 == 0 && tid < MANY_ROWS) reinterpret_cast<u32*>(lds + 2 * STAGE)[h / 2 % 2 * MANY_ROWS + tid] = next_scale;
+#pragma unroll
+    for (int i = 0; i < XF; ++i) {
+      v8bf x[PARTS];
+      split_pack<T, PARTS>(next_x[i], x);
+      const u32 r = tid / 8 + 64 * i;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) *reinterpret_cast<v8bf*>(stage + W_BYTES + p * X_BYTES + r * 128 + (tid % 8 ^ r % 8) * 16) = x[p];
+    }
+  };
+  v4f acc[8][XF] = {};
+  fetch(0);
+  keep(0);
+  if (halves > 1) fetch(1);
+  u32 scale[8];
+  for (u32 h = 0; h < halves; ++h) {
+    __syncthreads();
+    if (h + 1 < halves) keep(h + 1);
+    if (h + 2 < halves) fetch(h + 2);
+    const char* stage = lds + h % 2 * STAGE;
+    long w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const u32 row = ww + 16 * i + lane % 16;
+      w[i] = *reinterpret_cast<const long*>(stage + row * 32 + (lane / 16 + row / 4) % 4 * 8);
+      scale[i] = reinterpret_cast<const u32*>(lds + 2 * STAGE)[h / 2 % 2 * MANY_ROWS + row] >> (h % 2 * 16 + lane / 32 * 8) & 255;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      v8bf x[XF][PARTS];
+#pragma unroll
+      for (int j = 0; j < XF; ++j) {
+        const u32 r = wx + 16 * j + lane % 16;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+          x[j][p] = *reinterpret_cast<const v8bf*>(stage + W_BYTES + p * X_BYTES + r * 128 + ((lane / 16 * 2 + c) ^ r % 8) * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const v8bf wv = unpack((u32)(w[i] >> (32 * c)), scale[i]);
+#pragma unroll
+        for (int j = 0; j < XF; ++j)
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, x[j][p], acc[i][j], 0, 0, 0);
+      }
+    }
+  }
+  store_results<OUT, 8, XF>(a, acc, w0 + ww, x0 + wx);
+}
+
+template <typename T, typename OUT, int G>
+hipError_t launch_few(const ProductArgs& a, size_t batch_bytes, hipStream_t s) {
+  const u32 tiles = (u32)(((u64)a.w.n + FEW_ROWS - 1) / FEW_ROWS);
+  // runs of four steps and more; waves share rows where there is less than one tile for each of 1,024 SIMDs
+  const u32 runs = a.w.steps >= 32 ? 8 : a.w.steps >= 16 ? 4 : a.w.steps >= 8 ? 2 : 1;
+  const u32 share = tiles < 1024 ? runs : 1;
+  const size_t lds = batch_bytes + (share > 1 ? (size_t)FEW_THREADS / 64 * 2 * G * 1024 : 0);
+  const auto kernel = mx_product_few_kernel<T, OUT, G>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  const u32 per = FEW_THREADS / 64 / share, blocks = (tiles + per - 1) / per;
+  const u32 room = (u32)(FEW_LDS / lds);  // workgroups that a compute unit holds at once
+  const u32 most = 256 * (room > 4 ? 4 : room < 1 ? 1 : room);
+  hipLaunchKernelGGL(kernel, dim3(blocks < most ? blocks : most), dim3(FEW_THREADS), lds, s, a, tiles, runs, share);
+  return hipGetLastError();
+}
+
+template <typename T, typename OUT, int XF>
+hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
+  constexpr int PARTS = parts_of<T>();
+  constexpr int lds = 2 * (MANY_ROWS * 32 + PARTS * 64 * XF * 128) + 2 * MANY_ROWS * 4;
+  const auto kernel = mx_product_many_kernel<T, OUT, XF>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  // (launches are counted in threads of 32 bits: long batches go in parts)
+  const u32 tiles_w = (u32)(((u64)a.w.n + MANY_ROWS - 1) / MANY_ROWS);
+  u64 part = (1u << 22) / tiles_w * (64ull * XF);
+  if (part == 0) part = 64 * XF;
+  for (u64 at = 0; at < a.nx; at += part) {
+    ProductArgs b = a;
+    b.nx = (u32)(a.nx - at < part ? a.nx - at : part);
+    b.x = a.x + at * a.ldx * sizeof(T);
+    b.out = a.out + at * a.ldo * sizeof(OUT);
+    const u32 tiles = tiles_w * (u32)(((u64)b.nx + 64 * XF - 1) / (64 * XF));
+    hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(MANY_THREADS), lds, s, b, tiles_w, tiles);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
+}
+
+template <typename T, typename OUT>
+hipError_t launch_product16(const ProductArgs& a, hipStream_t s) {
+  constexpr int PARTS = parts_of<T>();
+  const size_t batch = (size_t)a.nx * (a.w.steps * MX_STEP * 2 + 16) * PARTS;
+  if (a.nx <= 64 && batch <= FEW_BATCH) {
+    if (a.nx <= 16) return launch_few<T, OUT, 1>(a, batch, s);
+    if (a.nx <= 32) return launch_few<T, OUT, 2>(a, batch, s);
+    return launch_few<T, OUT, 4>(a, batch, s);
+  }
+  if (a.nx <= 64) return launch_many<T, OUT, 1>(a, s);
+  if (a.nx <= 128 || PARTS > 1) return launch_many<T, OUT, 2>(a, s);
+  if constexpr (PARTS == 1) return launch_many<T, OUT, 4>(a, s);
 }
 
 template <typename OUT>
 hipError_t launch_product(const ProductArgs& a, int xdtype, hipStream_t s) {
+  if (xdtype == ANN_F32) return launch_product16<float, OUT>(a, s);
+  if (xdtype == ANN_F16) return launch_product16<__half, OUT>(a, s);
+  if (xdtype == ANN_BF16) return launch_product16<__bf16, OUT>(a, s);
   const u32 tiles_w = (u32)(((u64)a.w.n + 127) / 128);
   const u64 tiles = tiles_w * (((u64)a.nx + 127) / 128);
   const dim3 grid((u32)(tiles < (1u << 20) ? tiles : (1u << 20)));
-  if (xdtype < 0)
-    hipLaunchKernelGGL(mx_product4_kernel<OUT>, grid, dim3(256), 0, s, a, tiles_w, tiles);
-  else if (xdtype == ANN_F32)
-    hipLaunchKernelGGL((mx_product16_kernel<float, OUT>), grid, dim3(256), 0, s, a, tiles_w, tiles);
-  else if (xdtype == ANN_F16)
-    hipLaunchKernelGGL((mx_product16_kernel<__half, OUT>), grid, dim3(256), 0, s, a, tiles_w, tiles);
-  else
-    hipLaunchKernelGGL((mx_product16_kernel<__bf16, OUT>), grid, dim3(256), 0, s, a, tiles_w, tiles);
+  hipLaunchKernelGGL(mx_product4_kernel<OUT>, grid, dim3(256), 0, s, a, tiles_w, tiles);
   return hipGetLastError();
 }
 
@@ -212,6 +441,7 @@ int ann_mx_product(const void* x_dev, uint64_t nx, ann_dtype xdtype, uint64_t ld
   a.w = {codes_dev, scales_dev, 0, mx_steps(d)};
   a.x = static_cast<const char*>(x_dev);
   a.ldx = ldx;
+  a.wide_x = aligned_to(x_dev, 8 * esz) && ldx % 8 == 0;
   a.d = d;
   return product(a, xdtype, nx, n, out_dev, out_dtype, ldo, stream);
 } catch (...) {
