@@ -11,6 +11,7 @@ struct ProductArgs {
   u32 nx, d;
   char* out;
   u64 ldo;
+  int odtype;
   u32 wide;  // four results can be written at once
   u32 wide_x;  // eight elements of the batch can be read at once
 };
@@ -18,31 +19,52 @@ struct ProductArgs {
 constexpr size_t FEW_LDS = 160 * 1024;    // of a compute unit
 constexpr size_t FEW_BATCH = 96 * 1024;   // most of it that a batch may take
 
-// The 16 WF x 16 XF results of a wave: rows of `w` in the matrix instruction's rows, so that a lane holds four
-// results that follow each other in `out`.
+// The 16 WF x 16 XF results of a wave.  They lie in the matrix instruction's order (a lane holds four neighbours of a
+// row of `out`); through LDS of the wave's own they get into runs of a whole row's part, so that stores fill lines
+// wherever a row of `out` begins.
+template <int WF>
+constexpr u32 store_room() {
+  return 16 * (16 * WF + 4) * 4;  // bytes of LDS for a wave: the four floats more keep rows in different banks
+}
 template <typename OUT, int WF, int XF>
-__device__ __forceinline__ void store_results(const ProductArgs& a, const v4f (&acc)[WF][XF], u64 w0, u64 x0) {
+__device__ __forceinline__ void store_as(const ProductArgs& a, const v4f (&acc)[WF][XF], u64 w0, u64 x0, float* room) {
+  constexpr u32 ROW = 16 * WF, STRIDE = ROW + 4;
   const u32 lane = threadIdx.x % 64;
 #pragma unroll
   for (int j = 0; j < XF; ++j) {
-    const u64 x = x0 + 16 * j + lane % 16;
-    if (x >= a.nx) continue;
+    if (x0 + 16 * j >= a.nx) break;
 #pragma unroll
-    for (int i = 0; i < WF; ++i) {
-      const u64 w = w0 + 16 * i + lane / 16 * 4;
-      OUT* to = reinterpret_cast<OUT*>(a.out) + x * a.ldo + w;
-      if (a.wide && w + 4 <= a.w.n) {
+    for (int i = 0; i < WF; ++i) *reinterpret_cast<v4f*>(room + lane % 16 * STRIDE + 16 * i + lane / 16 * 4) = acc[i][j];
+    OUT* out = reinterpret_cast<OUT*>(a.out) + (x0 + 16 * j) * a.ldo + w0;
+    const u32 xs = (u32)min((u64)16, a.nx - (x0 + 16 * j)), ws = (u32)min((u64)ROW, a.w.n - w0);
+    if (a.wide && ws == ROW) {
+#pragma unroll
+      for (u32 k = 0; k < 16 * ROW / 256; ++k) {
+        const u32 r = (k * 256 + lane * 4) / ROW, at = (k * 256 + lane * 4) % ROW;
+        const v4f v = *reinterpret_cast<const v4f*>(room + r * STRIDE + at);
         Pack<OUT, 4> p;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p.v[r] = mx_round<OUT>(acc[i][j][r]);
-        *reinterpret_cast<Pack<OUT, 4>*>(to) = p;
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (w + r < a.w.n) to[r] = mx_round<OUT>(acc[i][j][r]);
+        for (int e = 0; e < 4; ++e) p.v[e] = mx_round<OUT>(v[e]);
+        if (r < xs) *reinterpret_cast<Pack<OUT, 4>*>(out + r * a.ldo + at) = p;
+      }
+    } else {
+#pragma unroll 4
+      for (u32 k = 0; k < 16 * ROW / 64; ++k) {
+        const u32 r = (k * 64 + lane) / ROW, at = (k * 64 + lane) % ROW;
+        const float v = room[r * STRIDE + at];
+        if (r < xs && at < ws) out[r * a.ldo + at] = mx_round<OUT>(v);
       }
     }
   }
+}
+template <int WF, int XF>
+__device__ __forceinline__ void store_results(const ProductArgs& a, const v4f (&acc)[WF][XF], u64 w0, u64 x0, char* room) {
+  if (a.odtype == ANN_F32)
+    store_as<float, WF, XF>(a, acc, w0, x0, reinterpret_cast<float*>(room));
+  else if (a.odtype == ANN_F16)
+    store_as<__half, WF, XF>(a, acc, w0, x0, reinterpret_cast<float*>(room));
+  else
+    store_as<__bf16, WF, XF>(a, acc, w0, x0, reinterpret_cast<float*>(room));
 }
 
 struct Fragment {  // 16 rows x 128 elements of 4 bits, a lane's share
@@ -60,8 +82,8 @@ __device__ __forceinline__ Fragment load_fragment(const MxRows& m, u64 row0, u32
 }
 
 // 128 x 128 results a workgroup, 64 x 64 a wave; both sides from memory, step by step.
-template <typename OUT>
 __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 tiles_w, u64 tiles) {
+  __shared__ __align__(16) char room[4 * store_room<4>()];
   const u32 wave = threadIdx.x / 64;
   for (u64 t = blockIdx.x; t < tiles; t += gridDim.x) {
     const u64 w0 = t % tiles_w * 128 + (wave & 1) * 64, x0 = t / tiles_w * 128 + (wave >> 1) * 64;
@@ -79,7 +101,7 @@ __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 til
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = mx_mfma(w[i].codes, x[j].codes, acc[i][j], w[i].scale, x[j].scale);
     }
-    store_results<OUT, 4, 4>(a, acc, w0, x0);
+    store_results<4, 4>(a, acc, w0, x0, room + wave * store_room<4>());
   }
 }
 
@@ -106,15 +128,23 @@ constexpr int parts_of() {
   return sizeof(T) == 4 ? 3 : __is_same(T, __half) ? 2 : 1;
 }
 
-// Eight elements of a row of the batch from `at` on; what lies past d is 0, and rows past the last are read as it.
-template <typename T>
+// Eight elements of a row of the batch from `at` on.  Rows past the last are read as it, and what lies past d as
+// elements before it; `mask_batch` makes those zeros, later, so that no branch waits for a load.
+template <typename T, bool WIDE>
 __device__ __forceinline__ Pack<T, 8> load_batch(const ProductArgs& a, u64 row, u32 at) {
-  const T* from = reinterpret_cast<const T*>(a.x) + min(row, (u64)a.nx - 1) * a.ldx + at;
-  if (a.wide_x && at + 8 <= a.d) return *reinterpret_cast<const Pack<T, 8>*>(from);
+  const T* from = reinterpret_cast<const T*>(a.x) + min(row, (u64)a.nx - 1) * a.ldx;
+  if (WIDE) return *reinterpret_cast<const Pack<T, 8>*>(from + (at < a.d ? at : 0));  // (d is a multiple of eight)
   Pack<T, 8> p;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) p.v[e] = at + e < a.d ? from[e] : T(0.0f);
+  for (int e = 0; e < 8; ++e) p.v[e] = from[min(at + e, a.d - 1)];
   return p;
+}
+template <typename T, bool WIDE>
+__device__ __forceinline__ void mask_batch(const ProductArgs& a, Pack<T, 8>& p, u32 at) {
+  if (at + 8 <= a.d) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (at + e >= a.d) p.v[e] = T(0.0f);
 }
 template <typename T, int PARTS>
 __device__ __forceinline__ void split_pack(const Pack<T, 8>& p, v8bf (&out)[PARTS]) {
@@ -142,17 +172,22 @@ __device__ __forceinline__ v8bf unpack(u32 codes, u32 scale_byte) {
 }
 
 // Few rows of 16 or 32 bits against all 4-bit rows: the batch stays in LDS, as one, two or three bf16 numbers for
-// each element, and the 4-bit rows stream past it, each byte read once.  A wave takes 32 of them.  Long rows are
-// summed in RUNS runs of steps, which are added up in their order, by one wave or, where 4-bit rows are few, by
-// a wave each: the sums do not depend on that.  Within a step the elements are taken in the order that a lane
-// holds them (8 at a time of its 32, the same ones on both sides).
+// each element, and the 4-bit rows stream past it, each byte read once.  A wave takes 16 WF of them and always has
+// the next AHEAD steps on their way while it multiplies the present ones.  Long rows (LONG) are summed in runs of
+// groups of AHEAD steps, which are added up in their order, by one wave or, where 4-bit rows are few, by a wave
+// each: the sums do not depend on that.  Within a step the elements are taken in the order that a lane holds
+// them (8 at a time of its 32, the same ones on both sides).
 constexpr u32 FEW_THREADS = 512;
-constexpr u32 FEW_ROWS = 32;
-constexpr u32 FEW_AHEAD = 4;  // steps whose codes a wave asks for at once
 
-template <typename T, typename OUT, int G>
+template <int G, int WF>
+constexpr u32 few_room(u32 share) {  // bytes of LDS of a wave's own
+  return share > 1 && WF * G * 1024 > store_room<WF>() ? WF * G * 1024 : store_room<WF>();
+}
+
+template <typename T, int G, int WF, int AHEAD, bool LONG>
 __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs a, u32 tiles, u32 runs, u32 share) {
   constexpr int PARTS = parts_of<T>();
+  const u32 room_bytes = few_room<G, WF>(share);
   extern __shared__ __align__(16) char lds[];
   const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   // 16 bytes more for each row than its elements take: the rows' pieces then lie in different banks
@@ -160,82 +195,101 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
   const u32 pieces = a.w.steps * 16;
   for (u32 i = threadIdx.x; i < a.nx * pieces; i += FEW_THREADS) {
     const u32 row = i / pieces, at = i % pieces;
+    Pack<T, 8> piece = a.wide_x ? load_batch<T, true>(a, row, at * 8) : load_batch<T, false>(a, row, at * 8);
+    mask_batch<T, false>(a, piece, at * 8);
     v8bf x[PARTS];
-    split_pack<T, PARTS>(load_batch<T>(a, row, at * 8), x);
+    split_pack<T, PARTS>(piece, x);
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) *reinterpret_cast<v8bf*>(lds + p * part_bytes + row * row_bytes + at * 16) = x[p];
   }
   __syncthreads();
+  char* room = lds + PARTS * part_bytes + wave * room_bytes;
   const u32 teams = FEW_THREADS / 64 / share;  // of waves that share rows
-  const u32 first_run = wave % share * (runs / share), last_run = first_run + runs / share;
+  const u32 first_run = LONG ? wave % share * (runs / share) : 0, last_run = LONG ? first_run + runs / share : 1;
+  const u32 groups = (a.w.steps + AHEAD - 1) / AHEAD;
+  const u32 g_first = LONG ? groups * first_run / runs : 0, g_last = LONG ? groups * last_run / runs : groups;
   const char* xs[G];
 #pragma unroll
   for (int j = 0; j < G; ++j) xs[j] = lds + min(16u * j + lane % 16, a.nx - 1) * row_bytes + lane / 16 * 64;
-  for (u32 t0 = blockIdx.x * teams; t0 < tiles; t0 += gridDim.x * teams) {
-    const u32 t = t0 + wave / share;
-    const u64 w0 = (u64)t * FEW_ROWS;
-    v4f sum[2][G] = {};
+
+  struct Ahead {
+    v4i w[AHEAD][WF];
+    u32 b[WF][AHEAD];
+  } next;
+  auto ask = [&](u32 tile, u32 group) {
+    const u32 s0 = group * AHEAD;
+#pragma unroll
+    for (int i = 0; i < WF; ++i) {
+      const u64 row = min((u64)tile * (16 * WF) + 16 * i + lane % 16, (u64)a.w.n - 1) * a.w.steps;
+      const u32* scales = reinterpret_cast<const u32*>(a.w.scales) + row;
+      const uint8_t* codes = a.w.codes + row * MX_STEP_BYTES + lane / 16 * 16;
+#pragma unroll
+      for (u32 u = 0; u < AHEAD; ++u) next.b[i][u] = scales[min(s0 + u, a.w.steps - 1)];
+#pragma unroll
+      for (u32 u = 0; u < AHEAD; ++u) next.w[u][i] = *reinterpret_cast<const v4i*>(codes + (u64)min(s0 + u, a.w.steps - 1) * MX_STEP_BYTES);
+    }
+  };
+  u32 t = blockIdx.x * teams + wave / share;
+  const u32 stride = gridDim.x * teams;
+  if (t < tiles) ask(t, g_first);
+  for (; t - wave / share < tiles; t += stride) {  // (all waves of a workgroup alike: they may have to meet)
+    v4f sum[WF][G] = {};
     if (t < tiles) {
-      const uint8_t* codes[2];
-      const u32* scales[2];
+      v4f acc[WF][G] = {};
+      u32 run = first_run, g_run = LONG ? groups * (run + 1) / runs : groups;
+      for (u32 g = g_first; g < g_last; ++g) {
+        const Ahead now = next;
+        const bool more = g + 1 < g_last;  // of this tile
+        ask(more ? t : min(t + stride, tiles - 1), more ? g + 1 : g_first);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const u64 row = min(w0 + 16 * i + lane % 16, (u64)a.w.n - 1);
-        codes[i] = a.w.codes + row * a.w.steps * MX_STEP_BYTES + lane / 16 * 16;
-        scales[i] = reinterpret_cast<const u32*>(a.w.scales) + row * a.w.steps;
-      }
-      for (u32 run = first_run; run < last_run; ++run) {
-        const u32 s0 = a.w.steps * run / runs, s1 = a.w.steps * (run + 1) / runs;
-        v4f acc[2][G] = {};
-        for (u32 first = s0; first < s1; first += FEW_AHEAD) {
-          v4i w[FEW_AHEAD][2];
-          u32 b[FEW_AHEAD][2];
+        for (u32 u = 0; u < AHEAD; ++u) {
+          const u32 s = g * AHEAD + u;
+          if (s >= a.w.steps) break;
 #pragma unroll
-          for (u32 u = 0; u < FEW_AHEAD; ++u)  // all on their way before the first is used
+          for (int c = 0; c < 4; ++c) {
+            // (or all the batch's pieces of a step would be read at once, into more registers than there are)
+            __builtin_amdgcn_sched_barrier(0);
+            v8bf wv[WF];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const u32 s = min(first + u, s1 - 1);
-              w[u][i] = *reinterpret_cast<const v4i*>(codes[i] + (u64)s * MX_STEP_BYTES);
-              b[u][i] = scales[i][s];
-            }
+            for (int i = 0; i < WF; ++i) wv[i] = unpack((u32)now.w[u][i][c], now.b[i][u] >> (lane / 16 * 8) & 255);
 #pragma unroll
-          for (u32 u = 0; u < FEW_AHEAD; ++u) {
-            if (first + u >= s1) break;
-            const u32 b0 = b[u][0] >> (lane / 16 * 8) & 255, b1 = b[u][1] >> (lane / 16 * 8) & 255;
+            for (int j = 0; j < G; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const v8bf wv[2] = {unpack((u32)w[u][0][c], b0), unpack((u32)w[u][1][c], b1)};
+              for (int p = PARTS - 1; p >= 0; --p) {
+                const v8bf x = *reinterpret_cast<const v8bf*>(xs[j] + p * part_bytes + s * (MX_STEP * 2) + c * 16);
 #pragma unroll
-              for (int j = 0; j < G; ++j)
-#pragma unroll
-                for (int p = PARTS - 1; p >= 0; --p) {
-                  const v8bf x = *reinterpret_cast<const v8bf*>(xs[j] + p * part_bytes + (first + u) * (MX_STEP * 2) + c * 16);
-#pragma unroll
-                  for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], x, acc[i][j], 0, 0, 0);
-                }
-            }
+                for (int i = 0; i < WF; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], x, acc[i][j], 0, 0, 0);
+              }
           }
         }
+        if (LONG && g + 1 == g_run) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < WF; ++i)
 #pragma unroll
-          for (int j = 0; j < G; ++j) sum[i][j] += acc[i][j];
+            for (int j = 0; j < G; ++j) sum[i][j] += acc[i][j], acc[i][j] = v4f{};
+          ++run;
+          g_run = groups * (run + 1) / runs;
+        }
       }
+      if (!LONG)
+#pragma unroll
+        for (int i = 0; i < WF; ++i)
+#pragma unroll
+          for (int j = 0; j < G; ++j) sum[i][j] = acc[i][j];
     }
-    if (share > 1) {  // (a run each) they meet in the team's first wave
-      char* sums = lds + PARTS * part_bytes + wave * (2 * G * 1024) + lane * 16;
+    if (LONG && share > 1) {  // (a run each) they meet in the team's first wave
+      char* mine = room + lane * 16;
       if (wave % share)
 #pragma unroll
-        for (int i = 0; i < 2 * G; ++i) *reinterpret_cast<v4f*>(sums + i * 1024) = sum[i / G][i % G];
+        for (int i = 0; i < WF * G; ++i) *reinterpret_cast<v4f*>(mine + i * 1024) = sum[i / G][i % G];
       __syncthreads();
       if (wave % share == 0)
         for (u32 o = 1; o < share; ++o)
 #pragma unroll
-          for (int i = 0; i < 2 * G; ++i) sum[i / G][i % G] += *reinterpret_cast<const v4f*>(sums + o * (2 * G * 1024) + i * 1024);
+          for (int i = 0; i < WF * G; ++i) sum[i / G][i % G] += *reinterpret_cast<const v4f*>(mine + o * room_bytes + i * 1024);
       __syncthreads();
-      if (wave % share) continue;
     }
-    if (t < tiles) store_results<OUT, 2, G>(a, sum, w0, 0);
+    if (t < tiles && wave % share == 0) store_results<WF, G>(a, sum, (u64)t * (16 * WF), 0, room);
   }
 }
 
@@ -246,7 +300,7 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
 constexpr u32 MANY_THREADS = 512;
 constexpr u32 MANY_ROWS = 256;
 
-template <typename T, typename OUT, int XF>
+template <typename T, int XF, bool WIDE>
 __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductArgs a, u32 tiles_w, u32 tiles) {
   constexpr int PARTS = parts_of<T>();
   constexpr u32 X_ROWS = 64 * XF;
@@ -271,7 +325,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
     next_w = *reinterpret_cast<const v4i*>(codes + (u64)h * 32);
     if (h % 2 == 0) next_scale = scales[h / 2];
 #pragma unroll
-    for (int i = 0; i < XF; ++i) next_x[i] = load_batch<T>(a, x0 + tid / 8 + 64 * i, h * 64 + tid % 8 * 8);
+    for (int i = 0; i < XF; ++i) next_x[i] = load_batch<T, WIDE>(a, x0 + tid / 8 + 64 * i, h * 64 + tid % 8 * 8);
   };
   auto keep = [&](u32 h) {
     char* stage = lds + h % 2 * STAGE;
@@ -284,6 +338,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
     if (h % 2 == 0 && tid < MANY_ROWS) reinterpret_cast<u32*>(lds + 2 * STAGE)[h / 2 % 2 * MANY_ROWS + tid] = next_scale;
 #pragma unroll
     for (int i = 0; i < XF; ++i) {
+      mask_batch<T, WIDE>(a, next_x[i], h * 64 + tid % 8 * 8);
       v8bf x[PARTS];
       split_pack<T, PARTS>(next_x[i], x);
       const u32 r = tid / 8 + 64 * i;
@@ -298,8 +353,6 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
   u32 scale[8];
   for (u32 h = 0; h < halves; ++h) {
     __syncthreads();
-    if (h + 1 < halves) keep(h + 1);
-    if (h + 2 < halves) fetch(h + 2);
     const char* stage = lds + h % 2 * STAGE;
     long w[8];
 #pragma unroll
@@ -310,6 +363,10 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
+      if (c == 1) {  // behind the first products: they run while the next half is put away
+        if (h + 1 < halves) keep(h + 1);
+        if (h + 2 < halves) fetch(h + 2);
+      }
       v8bf x[XF][PARTS];
 #pragma unroll
       for (int j = 0; j < XF; ++j) {
@@ -328,31 +385,33 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
       }
     }
   }
-  store_results<OUT, 8, XF>(a, acc, w0 + ww, x0 + wx);
+  __syncthreads();
+  if (w0 + ww < a.w.n) store_results<8, XF>(a, acc, w0 + ww, x0 + wx, lds + wave * store_room<8>());
 }
 
-template <typename T, typename OUT, int G>
-hipError_t launch_few(const ProductArgs& a, size_t batch_bytes, hipStream_t s) {
-  const u32 tiles = (u32)(((u64)a.w.n + FEW_ROWS - 1) / FEW_ROWS);
-  // runs of four steps and more; waves share rows where there is less than one tile for each of 1,024 SIMDs
-  const u32 runs = a.w.steps >= 32 ? 8 : a.w.steps >= 16 ? 4 : a.w.steps >= 8 ? 2 : 1;
-  const u32 share = tiles < 1024 ? runs : 1;
-  const size_t lds = batch_bytes + (share > 1 ? (size_t)FEW_THREADS / 64 * 2 * G * 1024 : 0);
-  const auto kernel = mx_product_few_kernel<T, OUT, G>;
+template <typename T, int G, int WF, int AHEAD, bool LONG>
+hipError_t launch_few(const ProductArgs& a, size_t batch_bytes, u32 runs, hipStream_t s) {
+  const u32 tiles = (u32)(((u64)a.w.n + 16 * WF - 1) / (16 * WF));
+  // waves share rows where there is less than one tile for each of 1,024 SIMDs
+  const u32 share = LONG && tiles < 1024 ? runs : 1;
+  constexpr u32 WAVES = FEW_THREADS / 64;
+  const size_t lds = batch_bytes + WAVES * few_room<G, WF>(share);
+  const auto kernel = mx_product_few_kernel<T, G, WF, AHEAD, LONG>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  const u32 per = FEW_THREADS / 64 / share, blocks = (tiles + per - 1) / per;
+  const u32 per = WAVES / share, blocks = (tiles + per - 1) / per;
   const u32 room = (u32)(FEW_LDS / lds);  // workgroups that a compute unit holds at once
   const u32 most = 256 * (room > 4 ? 4 : room < 1 ? 1 : room);
   hipLaunchKernelGGL(kernel, dim3(blocks < most ? blocks : most), dim3(FEW_THREADS), lds, s, a, tiles, runs, share);
   return hipGetLastError();
 }
 
-template <typename T, typename OUT, int XF>
+template <typename T, int XF>
 hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
   constexpr int PARTS = parts_of<T>();
-  constexpr int lds = 2 * (MANY_ROWS * 32 + PARTS * 64 * XF * 128) + 2 * MANY_ROWS * 4;
-  const auto kernel = mx_product_many_kernel<T, OUT, XF>;
+  constexpr int stages = 2 * (MANY_ROWS * 32 + PARTS * 64 * XF * 128) + 2 * MANY_ROWS * 4, room = MANY_THREADS / 64 * store_room<8>();
+  constexpr int lds = stages > room ? stages : room;
+  const auto kernel = a.wide_x ? mx_product_many_kernel<T, XF, true> : mx_product_many_kernel<T, XF, false>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   // (launches are counted in threads of 32 bits: long batches go in parts)
@@ -363,7 +422,7 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
     ProductArgs b = a;
     b.nx = (u32)(a.nx - at < part ? a.nx - at : part);
     b.x = a.x + at * a.ldx * sizeof(T);
-    b.out = a.out + at * a.ldo * sizeof(OUT);
+    b.out = a.out + at * a.ldo * dtype_bytes(a.odtype);
     const u32 tiles = tiles_w * (u32)(((u64)b.nx + 64 * XF - 1) / (64 * XF));
     hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(MANY_THREADS), lds, s, b, tiles_w, tiles);
     const hipError_t err = hipGetLastError();
@@ -372,29 +431,37 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-template <typename T, typename OUT>
+template <typename T, int G>
+hipError_t launch_few_rows(const ProductArgs& a, size_t batch, hipStream_t s) {
+  // runs of one group of four steps and more
+  const u32 runs = a.w.steps >= 32 ? 8 : a.w.steps >= 16 ? 4 : a.w.steps >= 8 ? 2 : 1;
+  if (runs > 1) return launch_few<T, G, 2, G == 1 ? 4 : 2, true>(a, batch, runs, s);
+  return launch_few<T, G, G == 1 ? 2 : 4, 2, false>(a, batch, 1, s);
+}
+
+template <typename T>
 hipError_t launch_product16(const ProductArgs& a, hipStream_t s) {
   constexpr int PARTS = parts_of<T>();
   const size_t batch = (size_t)a.nx * (a.w.steps * MX_STEP * 2 + 16) * PARTS;
   if (a.nx <= 64 && batch <= FEW_BATCH) {
-    if (a.nx <= 16) return launch_few<T, OUT, 1>(a, batch, s);
-    if (a.nx <= 32) return launch_few<T, OUT, 2>(a, batch, s);
-    return launch_few<T, OUT, 4>(a, batch, s);
+    if (a.nx <= 16) return launch_few_rows<T, 1>(a, batch, s);
+    if (a.nx <= 32) return launch_few_rows<T, 2>(a, batch, s);
+    if (a.nx <= 48) return launch_few_rows<T, 3>(a, batch, s);
+    return launch_few_rows<T, 4>(a, batch, s);
   }
-  if (a.nx <= 64) return launch_many<T, OUT, 1>(a, s);
-  if (a.nx <= 128 || PARTS > 1) return launch_many<T, OUT, 2>(a, s);
-  if constexpr (PARTS == 1) return launch_many<T, OUT, 4>(a, s);
+  if (a.nx <= 64) return launch_many<T, 1>(a, s);
+  if (a.nx <= 128 || PARTS > 1) return launch_many<T, 2>(a, s);
+  if constexpr (PARTS == 1) return launch_many<T, 4>(a, s);
 }
 
-template <typename OUT>
 hipError_t launch_product(const ProductArgs& a, int xdtype, hipStream_t s) {
-  if (xdtype == ANN_F32) return launch_product16<float, OUT>(a, s);
-  if (xdtype == ANN_F16) return launch_product16<__half, OUT>(a, s);
-  if (xdtype == ANN_BF16) return launch_product16<__bf16, OUT>(a, s);
+  if (xdtype == ANN_F32) return launch_product16<float>(a, s);
+  if (xdtype == ANN_F16) return launch_product16<__half>(a, s);
+  if (xdtype == ANN_BF16) return launch_product16<__bf16>(a, s);
   const u32 tiles_w = (u32)(((u64)a.w.n + 127) / 128);
   const u64 tiles = tiles_w * (((u64)a.nx + 127) / 128);
   const dim3 grid((u32)(tiles < (1u << 20) ? tiles : (1u << 20)));
-  hipLaunchKernelGGL(mx_product4_kernel<OUT>, grid, dim3(256), 0, s, a, tiles_w, tiles);
+  hipLaunchKernelGGL(mx_product4_kernel, grid, dim3(256), 0, s, a, tiles_w, tiles);
   return hipGetLastError();
 }
 
@@ -411,12 +478,8 @@ int product(ProductArgs a, int xdtype, u64 nx, u64 n, void* out, int odtype, u64
   a.out = static_cast<char*>(out);
   a.ldo = ldo;
   a.wide = aligned_to(out, 4 * osz) && ldo % 4 == 0;
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  switch (odtype) {
-    case ANN_F16: HIP_TRY(launch_product<__half>(a, xdtype, st)); break;
-    case ANN_BF16: HIP_TRY(launch_product<__bf16>(a, xdtype, st)); break;
-    default: HIP_TRY(launch_product<float>(a, xdtype, st)); break;
-  }
+  a.odtype = odtype;
+  HIP_TRY(launch_product(a, xdtype, static_cast<hipStream_t>(stream)));
   return ANN_OK;
 }
 
@@ -441,7 +504,7 @@ int ann_mx_product(const void* x_dev, uint64_t nx, ann_dtype xdtype, uint64_t ld
   a.w = {codes_dev, scales_dev, 0, mx_steps(d)};
   a.x = static_cast<const char*>(x_dev);
   a.ldx = ldx;
-  a.wide_x = aligned_to(x_dev, 8 * esz) && ldx % 8 == 0;
+  a.wide_x = aligned_to(x_dev, 8 * esz) && ldx % 8 == 0 && d % 8 == 0;
   a.d = d;
   return product(a, xdtype, nx, n, out_dev, out_dtype, ldo, stream);
 } catch (...) {
