@@ -223,8 +223,21 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
       const u64 row = min((u64)tile * (16 * WF) + 16 * i + lane % 16, (u64)a.w.n - 1) * a.w.steps;
       const u32* scales = reinterpret_cast<const u32*>(a.w.scales) + row;
       const uint8_t* codes = a.w.codes + row * MX_STEP_BYTES + lane / 16 * 16;
+      if (LONG) {  // one load for the group; the last one may begin before s0
+        const u32 from = min(s0, a.w.steps - AHEAD), skip = s0 - from;
+        using Scales = u32 __attribute__((ext_vector_type(AHEAD), aligned(4)));
+        const Scales some = *reinterpret_cast<const Scales*>(scales + from);
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) next.b[i][u] = scales[min(s0 + u, a.w.steps - 1)];
+        for (u32 u = 0; u < AHEAD; ++u) {
+          next.b[i][u] = some[u];
+#pragma unroll
+          for (u32 k = 1; k + u < AHEAD; ++k)
+            if (skip == k) next.b[i][u] = some[u + k];
+        }
+      } else {
+#pragma unroll
+        for (u32 u = 0; u < AHEAD; ++u) next.b[i][u] = scales[min(s0 + u, a.w.steps - 1)];
+      }
 #pragma unroll
       for (u32 u = 0; u < AHEAD; ++u) next.w[u][i] = *reinterpret_cast<const v4i*>(codes + (u64)min(s0 + u, a.w.steps - 1) * MX_STEP_BYTES);
     }
@@ -435,7 +448,7 @@ template <typename T, int G>
 hipError_t launch_few_rows(const ProductArgs& a, size_t batch, hipStream_t s) {
   // runs of one group of four steps and more
   const u32 runs = a.w.steps >= 32 ? 8 : a.w.steps >= 16 ? 4 : a.w.steps >= 8 ? 2 : 1;
-  if (runs > 1) return launch_few<T, G, 2, G == 1 ? 4 : 2, true>(a, batch, runs, s);
+  if (runs > 1) return launch_few<T, G, G == 1 ? 1 : 2, G == 1 ? 4 : 2, true>(a, batch, runs, s);
   return launch_few<T, G, G == 1 ? 2 : 4, 2, false>(a, batch, 1, s);
 }
 
