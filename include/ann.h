@@ -555,7 +555,7 @@ int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint6
  *   top_k  > 0: the first top_k candidates
  *   top_p  in (0, 1): the shortest prefix of those with at least that share of
  *          their mass (the comparison is made on weights rounded to multiples
- *          of 2^-(62 - ceil(log2 n)) of the largest)
+ *          of 2^-min(50, 62 - ceil(log2 n)) of the largest)
  *   min_p  > 0: those with w >= min(min_p, 1)
  * and other values switch a rule off.  The id drawn is the smallest kept one,
  * in id order, whose running mass exceeds uniform * mass.  A temperature that

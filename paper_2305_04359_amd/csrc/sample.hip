@@ -1,15 +1,18 @@
 // One id drawn for each row of scores, by temperature, top-k, top-p and min-p.
 //
 // All three rules keep a prefix of the candidates sorted by (score downwards, id), so the kept ones are told by a
-// cut: every key above it, and the first `ties` of those at it.  The cut of top-k comes from counts of keys, the
-// cut of top-p from masses, both by a radix selection, eight bits of the key at a time.  Masses are sums of
-// weights rounded to multiples of a power of two: whole numbers, whose sums depend on no order.  The draw then
-// sums the kept weights in fp64 in a fixed order.
+// cut: every key above it, and the first `ties` of those at it.  The cuts of top-k (by counts) and top-p (by
+// masses) are found by histograms over ever shorter ranges of keys.  Masses are sums of weights rounded to multiples
+// of a power of two: whole numbers, whose sums depend on no order.  The draw sums the kept weights in fp64 in a
+// fixed order.
 #include "mx.hpp"
 
 namespace annmi {
 
 constexpr u32 SAMPLE_THREADS = 1024;
+constexpr u32 SAMPLE_WAVES = SAMPLE_THREADS / 64;
+constexpr u32 SAMPLE_BINS = 1024;  // one for each thread
+constexpr u32 SAMPLE_FEW = 1024;   // so many kept by top-k are sorted in LDS, and the row is not read again
 
 struct SampleArgs {
   const char* scores;
@@ -24,276 +27,421 @@ struct SampleArgs {
 
 constexpr u32 SAMPLE_LEAST = 0x007FFFFFu;  // float_key(-inf): candidates have larger keys
 
+// low bits of a key that are the same in all values of one sign of a type
 template <typename T>
-__device__ __forceinline__ u32 score_key(const T* row, u64 i) {
-  return float_key(mx_float(row[i]));
+constexpr u32 key_grain() {
+  return sizeof(T) == 4 ? 0 : __is_same(T, __half) ? 13 : 16;
 }
 
-struct RowRules {
-  double best, inverse;  // of the temperature
+// exp((score - best) / temperature) to a few units of the last place: 2^(j / 256) from a table, the rest, below
+// ln 2 / 512, by its series.
+struct Weights {
+  double best, scale;  // scale: 256 / (temperature ln 2)
   u32 best_key;
-  __device__ double weight(u32 key) const {
-    return key == best_key ? 1.0 : exp((static_cast<double>(key_float(key)) - best) * inverse);
+  const double* table;
+  __device__ __forceinline__ double of(u32 key) const {
+    if (key == best_key) return 1.0;
+    double y = (static_cast<double>(key_float(key)) - best) * scale;
+    y = y > -300000.0 ? y : -300000.0;  // (2^-1171: 0)
+    const double whole = __builtin_rint(y), r = (y - whole) * 0.0027076061740622863;  // ln 2 / 256
+    const int e = static_cast<int>(whole);
+    const double p = __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(r, 1.0 / 24, 1.0 / 6), r, 0.5), r, 1.0), r, 1.0);
+    return ldexp(table[e & 255] * p, e >> 8);
+  }
+  // in units of 2^-unit, to the nearest; unit <= 50: adding 2^52 leaves the whole number in the low bits
+  __device__ __forceinline__ u64 units(u32 key, double unit) const {
+    return static_cast<u64>(__double_as_longlong(__builtin_fma(of(key), unit, 4503599627370496.0)) & 0xFFFFFFFFFFFFFll);
   }
 };
 
-// the sum of `v` over the workgroup, the same in every thread; the order of the sum is fixed
-__device__ double block_sum(double v, double* shared) {
+// f(id, key) for the row's entries from..to, dealt to `ranks` threads: 16 bytes at a time, four loads on their way
+// at once; before the first and after the last whole piece one by one.
+template <typename T, typename F>
+__device__ __forceinline__ void each(const T* row, u64 from, u64 to, u32 rank, u32 ranks, F f) {
+  constexpr u32 V = 16 / sizeof(T), AHEAD = 4;
+  const u64 skew = reinterpret_cast<uintptr_t>(row + from) % 16 / sizeof(T);
+  const u64 head = min(to, from + (V - skew) % V);
+  const u64 pieces = (to - head) / V, tail = head + pieces * V;
+  for (u64 i = from + rank; i < head; i += ranks) f(i, float_key(mx_float(row[i])));
+  for (u64 p = rank; p < pieces; p += (u64)ranks * AHEAD) {
+    Pack<T, V> x[AHEAD];
 #pragma unroll
-  for (int w = 1; w < 64; w *= 2) v += __shfl_xor(v, w);
+    for (u32 u = 0; u < AHEAD; ++u) x[u] = *reinterpret_cast<const Pack<T, V>*>(row + head + min(p + (u64)u * ranks, pieces - 1) * V);
+#pragma unroll
+    for (u32 u = 0; u < AHEAD; ++u) {
+      __builtin_amdgcn_sched_barrier(0);  // (or the weights of several pieces would be taken at once, in too many registers)
+      if (p + (u64)u * ranks < pieces)
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) f(head + (p + (u64)u * ranks) * V + e, float_key(mx_float(x[u].v[e])));
+    }
+  }
+  for (u64 i = tail + rank; i < to; i += ranks) f(i, float_key(mx_float(row[i])));
+}
+
+struct SampleLds {
+  u64 hist[SAMPLE_BINS];    // counts or masses; sorted candidates
+  u64 weight[SAMPLE_BINS];  // of the candidates that are sorted (bits of doubles)
+  double table[256];
+  u64 wave[SAMPLE_WAVES];
+  u64 word;
+  u32 count, bin;
+};
+
+// sums over the workgroup in a fixed order, the same in every thread: of all, and of this thread's and those before
+template <typename V>
+__device__ V block_scan(V v, SampleLds& s, V* upto) {
+  const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) {
+    const V x = __shfl_up(v, w);
+    if (lane >= (u32)w) v += x;
+  }
   __syncthreads();
-  if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
+  if (lane == 63) s.wave[wave] = __builtin_bit_cast(u64, v);
   __syncthreads();
-  double sum = 0.0;
-  for (u32 i = 0; i < SAMPLE_THREADS / 64; ++i) sum += shared[i];
+  V sum = V(0), before = V(0);
+  for (u32 w = 0; w < SAMPLE_WAVES; ++w) {
+    if (w == wave) before = sum;
+    sum += __builtin_bit_cast(V, s.wave[w]);
+  }
+  *upto = before + v;
   return sum;
+}
+
+// s.hist[0 .. size) upwards; size: a power of two
+__device__ void block_sort(SampleLds& s, u32 size) {
+  for (u32 run = 2; run <= size; run *= 2)
+    for (u32 gap = run / 2; gap > 0; gap /= 2) {
+      __syncthreads();
+      const u32 i = threadIdx.x;
+      if (i < size / 2) {
+        const u32 lo = i / gap * 2 * gap + i % gap, hi = lo + gap;
+        const u64 x = s.hist[lo], y = s.hist[hi];
+        if ((x > y) == ((lo & run) == 0)) s.hist[lo] = y, s.hist[hi] = x;
+      }
+    }
+  __syncthreads();
 }
 
 struct Cut {
   u32 key;
   u64 ties;  // how many of the candidates at `key` are kept, the first ones by id
+  u64 at;    // how many there are (top-k only)
 };
 
-// A workgroup per row.
+// A workgroup per row.  The row is read once for its best score, once to three times for each cut, once for the draw
+// (and a sixteenth of it, and so on, to find the draw's place); all but the first time from the caches.
 template <typename T>
 __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
-  __shared__ unsigned long long hist[256];
-  __shared__ double sums[SAMPLE_THREADS / 64];
-  __shared__ unsigned long long s_best, s_left, s_before, s_ties[SAMPLE_THREADS / 64];
-  __shared__ u32 s_prefix;
+  __shared__ SampleLds s;
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  constexpr u32 GRAIN = key_grain<T>();
+  if (tid < 256) s.table[tid] = exp2(tid / 256.0);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
     const float temperature = a.o.temperature_dev ? a.o.temperature_dev[r] : a.o.temperature;
     const u32 top_k = a.o.top_k_dev ? a.o.top_k_dev[r] : a.o.top_k;
     const float top_p = a.o.top_p_dev ? a.o.top_p_dev[r] : a.o.top_p;
     const float min_p = a.o.min_p_dev ? a.o.min_p_dev[r] : a.o.min_p;
+    auto all = [&](auto f) { each(row, 0, a.n, tid, SAMPLE_THREADS, f); };
+
+    u32 best = 0;
+    all([&](u64, u32 key) { best = max(best, key); });
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) best = max(best, (u32)__shfl_xor((int)best, w));
     __syncthreads();
-    if (tid == 0) s_best = 0;
+    if (lane == 0) s.wave[wave] = best;
     __syncthreads();
-    // the best candidate: largest key, smallest id
-    unsigned long long best = 0;
-    for (u64 i = tid; i < a.n; i += SAMPLE_THREADS) {
-      const u64 k = (u64)score_key(row, i) << 32 | (u32)~(u32)i;
-      best = max(best, (unsigned long long)k);
-    }
-    atomicMax(&s_best, best);
-    __syncthreads();
-    best = s_best;
-    RowRules rules;
-    rules.best_key = (u32)(best >> 32);
-    const u32 first = ~(u32)best;
-    if (rules.best_key <= SAMPLE_LEAST || !(temperature > 0.0f)) {  // (the same in all threads)
+    for (u32 w = 0; w < SAMPLE_WAVES; ++w) best = max(best, (u32)s.wave[w]);
+    if (best <= SAMPLE_LEAST) {  // (the same in all threads)
       if (tid == 0) {
-        const bool none = rules.best_key <= SAMPLE_LEAST;
-        a.ids[r] = none ? ANN_NONE : first;
-        if (a.logprobs) a.logprobs[r] = none ? -__builtin_inff() : 0.0f;
+        a.ids[r] = ANN_NONE;
+        if (a.logprobs) a.logprobs[r] = -__builtin_inff();
       }
       continue;
     }
-    rules.best = static_cast<double>(key_float(rules.best_key));
-    // (an infinite temperature has inverse 0; next to an infinite best score any other has weight 0 all the same)
-    rules.inverse = rules.best < __builtin_inf() ? 1.0 / static_cast<double>(temperature) : 1.0;
-    Cut cut = {SAMPLE_LEAST + 1, ~0ull};
+    if (!(temperature > 0.0f)) {
+      if (tid == 0) s.word = ~0ull;
+      __syncthreads();
+      u64 first = ~0ull;
+      all([&](u64 i, u32 key) {
+        if (key == best) first = min(first, i);
+      });
+      if (first != ~0ull) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)first);
+      __syncthreads();
+      if (tid == 0) {
+        a.ids[r] = (u32)s.word;
+        if (a.logprobs) a.logprobs[r] = 0.0f;
+      }
+      continue;
+    }
+    Weights w;
+    w.best_key = best;
+    w.best = static_cast<double>(key_float(best));
+    // (an infinite temperature has scale 0; next to an infinite best score any other has weight 0 all the same)
+    w.scale = w.best < __builtin_inf() ? 369.3299304675746 / static_cast<double>(temperature) : 1.0;
+    w.table = s.table;
+    const double unit = ldexp(1.0, (int)a.unit);
+    Cut cut = {SAMPLE_LEAST + 1, ~0ull, ~0ull};
 
-    // Radix selection: the key at which the running count (mass), from the largest key down, reaches `aim`.
-    auto select = [&](unsigned long long aim, bool mass, u32 limit_key, unsigned long long limit_ties) {
-      // (limit: only the prefix up to it counts; its ties enter by number, since equal keys have equal weights)
-      if (tid == 0) s_prefix = 0, s_left = aim;
-      for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+    // The first histogram is linear in the score, 32 bins for each unit of max(temperature, 1) below the best, the
+    // last one open; equal scores share a bin, and the bins fall with the score.
+    const float per_score = 32.0f / (temperature > 1.0f ? temperature : 1.0f), best_score = key_float(best);
+    auto linear_bin = [&](u32 key) {
+      const float z = (best_score - key_float(key)) * per_score;
+      return key == best ? 0u : z < (float)(SAMPLE_BINS - 1) ? (u32)z : SAMPLE_BINS - 1;
+    };
+    // Finds the key at which the running count (or mass), from the best key down, reaches `aim(total)`; candidates
+    // below floor.key do not count, and of those at it floor.ties do.  False: the total is 0 or below the aim.
+    auto select = [&](const Cut& floor, bool mass, auto aim, Cut* found, u64* rest) -> bool {
+      u32 hi = best, lo = floor.key, shift = 0;
+      u64 want = 0;
+      const bool some_ties = mass && floor.ties != ~0ull;  // counted by number: equal keys have equal weights
+      for (int level = 0;; ++level) {
         __syncthreads();
-        const u32 prefix = s_prefix;
-        for (u64 i = tid; i < a.n; i += SAMPLE_THREADS) {
-          const u32 key = score_key(row, i);
-          if (key <= SAMPLE_LEAST || key < limit_key || (shift < 24 && key >> (shift + 8) != prefix)) continue;
-          if (!mass)
-            atomicAdd(&hist[key >> shift & 255], 1ull);
-          else if (key > limit_key)
-            atomicAdd(&hist[key >> shift & 255], (unsigned long long)__builtin_rint(ldexp(rules.weight(key), (int)a.unit)));
+        s.hist[tid] = 0;
+        __syncthreads();
+        all([&](u64, u32 key) {
+          if (key < lo || key > hi || (some_ties && key == floor.key)) return;
+          const u32 b = level ? (hi - key) >> shift : linear_bin(key);
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[b]), (unsigned long long)(mass ? w.units(key, unit) : 1ull));
+        });
+        __syncthreads();
+        if (tid == 0 && some_ties && floor.key >= lo)
+          s.hist[level ? (hi - floor.key) >> shift : linear_bin(floor.key)] += floor.ties * w.units(floor.key, unit);
+        __syncthreads();
+        const u64 mine = s.hist[tid];
+        u64 upto;
+        const u64 total = block_scan<u64>(mine, s, &upto);
+        if (level == 0) {
+          want = aim(total);
+          if (want == 0 || want > total) return false;
         }
+        if (upto >= want && upto - mine < want) s.bin = tid, s.word = want - (upto - mine);
         __syncthreads();
-        if (tid == 0) {
-          if (mass && limit_ties && (shift == 24 || limit_key >> (shift + 8) == prefix))
-            hist[limit_key >> shift & 255] += limit_ties * (unsigned long long)__builtin_rint(ldexp(rules.weight(limit_key), (int)a.unit));
-          unsigned long long left = s_left;
-          u32 b = 255;
-          while (b > 0 && hist[b] < left) left -= hist[b--];
-          s_left = left;
-          s_prefix = prefix << 8 | b;
+        const u32 b = s.bin;
+        want = s.word;
+        found->at = s.hist[b];
+        if (level == 0) {
+          // the keys of the bin, by bisection: the bins fall with the key
+          u32 x = lo, y = hi;
+          while (x < y) {  // the largest key whose bin is b or above
+            const u32 mid = x + (y - x + 1) / 2;
+            if (linear_bin(mid) >= b)
+              x = mid;
+            else
+              y = mid - 1;
+          }
+          const u32 top = x;
+          x = lo, y = top;
+          while (x < y) {  // the smallest key whose bin is b
+            const u32 mid = x + (y - x) / 2;
+            if (linear_bin(mid) <= b)
+              y = mid;
+            else
+              x = mid + 1;
+          }
+          hi = top, lo = x;
+        } else {
+          hi -= b << shift;
+          lo = max(lo, hi - ((1u << shift) - 1));
         }
-        __syncthreads();
+        // The type's values are the keys whose low bits are 0 (not negative) or 1 (negative): up to the end of the
+        // block of the largest value that is not above hi.
+        constexpr u32 LOW = (1u << GRAIN) - 1;
+        hi = (hi >> 31) || (hi & LOW) == LOW ? hi | LOW : (hi & ~LOW) - 1;
+        if (hi >> GRAIN == lo >> GRAIN) {  // one value
+          found->key = hi >> 31 ? hi & ~LOW : hi;
+          *rest = want;
+          return true;
+        }
+        const u32 bits = 32 - __builtin_clz(hi - lo);
+        shift = bits > 10 + GRAIN ? bits - 10 : GRAIN;
       }
     };
 
-    auto count_at = [&](u32 key, bool above) {
-      __syncthreads();
-      if (tid == 0) s_before = 0;
-      __syncthreads();
-      unsigned long long mine = 0;
-      for (u64 i = tid; i < a.n; i += SAMPLE_THREADS) {
-        const u32 k = score_key(row, i);
-        mine += above ? k > key : k == key;
-      }
-      atomicAdd(&s_before, mine);
-      __syncthreads();
-      const u64 c = s_before;
-      __syncthreads();
-      return c;
-    };
     if (top_k > 0 && top_k < a.n) {
-      const u64 candidates = count_at(SAMPLE_LEAST, true);
-      if (top_k < candidates) {
-        select(top_k, false, SAMPLE_LEAST + 1, 0);
-        cut.key = s_prefix;
-        cut.ties = s_left;
-        __syncthreads();
+      Cut found;
+      u64 ties;
+      if (select(cut, false, [&](u64 total) { return (u64)top_k < total ? (u64)top_k : 0; }, &found, &ties)) {
+        cut = found;
+        cut.ties = ties;
       }
     }
-    if (top_p > 0.0f && top_p < 1.0f) {
-      // the mass of what is kept so far, in whole units
-      const u64 at_cut = min(cut.ties, (u64)count_at(cut.key, false));
+    double u = static_cast<double>(a.uniform[r]);
+    // (1 and above: no running mass exceeds it, so that the last kept one is taken; below 0 and NaN count as 0)
+    u = !(u >= 0.0) ? 0.0 : u < 1.0 ? u : __builtin_inf();
+    const double floor_w = min_p < 1.0f ? static_cast<double>(min_p) : 1.0;
+
+    if (cut.ties != ~0ull && top_k - cut.ties + cut.at <= SAMPLE_FEW) {
+      // Few: sorted by (key downwards, id), cut, then sorted by id and drawn from, a thread for each.
       __syncthreads();
-      if (tid == 0) s_before = 0;
+      if (tid == 0) s.count = 0;
       __syncthreads();
-      unsigned long long mine = 0;
-      for (u64 i = tid; i < a.n; i += SAMPLE_THREADS) {
-        const u32 key = score_key(row, i);
-        if (key > cut.key) mine += (unsigned long long)__builtin_rint(ldexp(rules.weight(key), (int)a.unit));
+      all([&](u64 i, u32 key) {
+        if (key >= cut.key) s.hist[atomicAdd(&s.count, 1u)] = (u64)~key << 32 | i;
+      });
+      __syncthreads();
+      u32 size = 2;
+      while (size < s.count) size *= 2;
+      if (tid >= s.count && tid < size) s.hist[tid] = ~0ull;
+      block_sort(s, size);
+      const bool mine = tid < top_k;
+      const u64 entry = mine ? s.hist[tid] : 0;
+      const u32 key = ~(u32)(entry >> 32);
+      const double weight = mine ? w.of(key) : 0.0;
+      u64 upto;
+      const u64 units = mine ? w.units(key, unit) : 0;
+      const u64 total = block_scan<u64>(units, s, &upto);
+      bool keep = mine;
+      if (top_p > 0.0f && top_p < 1.0f) keep = keep && (tid == 0 || (double)(upto - units) < static_cast<double>(top_p) * static_cast<double>(total));
+      if (min_p > 0.0f) keep = keep && weight >= floor_w;
+      __syncthreads();
+      if (tid < size) s.hist[tid] = keep ? (entry & 0xFFFFFFFFull) << 32 | tid : ~0ull;
+      s.weight[tid] = __builtin_bit_cast(u64, weight);
+      block_sort(s, size);
+      const bool there = tid < size && s.hist[tid] != ~0ull;
+      const u32 from = there ? (u32)s.hist[tid] : 0;
+      const double x = there ? __builtin_bit_cast(double, s.weight[from]) : 0.0;
+      double run, others;
+      const double sum = block_scan<double>(x, s, &run);
+      // the mass without this one, not as a difference from the whole where it is the best: it may be all the mass
+      double rest = block_scan<double>(from == 0 ? 0.0 : x, s, &others);
+      const double aim = u * sum;
+      if (tid == 0) s.word = ~0ull, s.count = 0;
+      __syncthreads();
+      if (x > 0.0) {
+        if (run > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
+        atomicMax(&s.count, tid);
       }
-      atomicAdd(&s_before, mine);
       __syncthreads();
-      const unsigned long long total = s_before + at_cut * (unsigned long long)__builtin_rint(ldexp(rules.weight(cut.key), (int)a.unit));
-      __syncthreads();
-      unsigned long long aim = (unsigned long long)ceil(static_cast<double>(top_p) * static_cast<double>(total));
-      if (aim < 1) aim = 1;
-      if (aim > total) aim = total;
-      select(aim, true, cut.key, at_cut);
-      const u32 key = s_prefix;
-      const unsigned long long left = s_left;
-      __syncthreads();
-      const unsigned long long w = (unsigned long long)__builtin_rint(ldexp(rules.weight(key), (int)a.unit));
-      const u64 need = w ? (left + w - 1) / w : ~0ull;
-      cut.ties = key == cut.key ? min(cut.ties, need) : need;
-      cut.key = key;
+      const u32 at = s.word != ~0ull ? (u32)s.word : s.count;
+      if (tid == at) {
+        a.ids[r] = (u32)(s.hist[tid] >> 32);
+        if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((from == 0 ? rest : 1.0 + rest - x) / x));
+      }
+      continue;
+    }
+
+    if (top_p > 0.0f && top_p < 1.0f) {
+      Cut found;
+      u64 left;
+      if (select(cut, true,
+                 [&](u64 total) {
+                   const u64 aim = (u64)ceil(static_cast<double>(top_p) * static_cast<double>(total));
+                   return aim < 1 ? 1 : aim > total ? total : aim;
+                 },
+                 &found, &left)) {
+        const u64 each_one = w.units(found.key, unit);
+        const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull;
+        cut.ties = found.key == cut.key ? min(cut.ties, need) : need;
+        cut.key = found.key;
+      }
     }
     if (min_p > 0.0f) {
-      const double floor_w = min_p < 1.0f ? static_cast<double>(min_p) : 1.0;
       // weights fall with the key: the smallest key whose weight reaches the floor
-      u32 lo = cut.key, hi = rules.best_key;  // hi reaches it
+      u32 lo = cut.key, hi = best;  // hi reaches it
       while (lo < hi) {
         const u32 mid = lo + (hi - lo) / 2;
-        if (rules.weight(mid) >= floor_w)
+        if (w.of(mid) >= floor_w)
           hi = mid;
         else
           lo = mid + 1;
       }
       if (hi > cut.key) cut.key = hi, cut.ties = ~0ull;
     }
-    // The draw.  The mass other than the first candidate's is kept apart, so that a mass that is nearly all its own
-    // loses nothing.
-    const u64 at_cut = count_at(cut.key, false);
-    const bool all_ties = cut.ties >= at_cut;
-    // where only some of the ties are kept: they are the first ones by id, up to and without `tie_end`
+    // Where only some of those at the cut are kept, they are the first ones by id: those below `tie_end`.
     u64 tie_end = a.n;
-    if (!all_ties) {
-      // find the id of the tie number cut.ties, block by block
+    if (cut.ties != ~0ull) {
       u64 seen = 0;
       for (u64 i0 = 0; i0 < a.n; i0 += SAMPLE_THREADS) {
         const u64 i = i0 + tid;
-        const bool tie = i < a.n && score_key(row, i) == cut.key;
+        const bool tie = i < a.n && float_key(mx_float(row[i])) == cut.key;
         const u64 votes = __ballot(tie);
         __syncthreads();
-        if (lane == 0) s_ties[wave] = (unsigned long long)__popcll(votes);
-        if (tid == 0) s_left = ~0ull;
+        if (lane == 0) s.wave[wave] = (u64)__popcll(votes);
+        if (tid == 0) s.word = ~0ull;
         __syncthreads();
-        u64 before = seen, all = 0;
-        for (u32 w = 0; w < SAMPLE_THREADS / 64; ++w) {
-          if (w < wave) before += s_ties[w];
-          all += s_ties[w];
+        u64 before = seen, here = 0;
+        for (u32 v = 0; v < SAMPLE_WAVES; ++v) {
+          if (v < wave) before += s.wave[v];
+          here += s.wave[v];
         }
         before += __popcll(votes & ((1ull << lane) - 1));
-        if (tie && before == cut.ties) s_left = i;
+        if (tie && before == cut.ties) s.word = i;
         __syncthreads();
-        if (s_left != ~0ull) {
-          tie_end = s_left;
+        if (s.word != ~0ull) {
+          tie_end = s.word;
           break;
         }
-        seen += all;
+        seen += here;
       }
-      __syncthreads();
     }
-    auto kept_weight = [&](u64 i) {
-      const u32 key = score_key(row, i);
-      return key > cut.key || (key == cut.key && i < tie_end) ? rules.weight(key) : 0.0;
-    };
-    // Narrow the span that holds the draw: it is dealt to the waves in runs, whose sums tell which run it is.
+    // The draw: the span that holds it is dealt to the waves in runs, whose masses tell which run it is.  The best
+    // candidates' weights, 1 each, are kept apart, so that a mass that is nearly all the drawn one's loses nothing.
     u64 lo = 0, hi = a.n;
-    double rest = 0.0;  // mass other than the first candidate's
-    {
-      double mine = 0.0;
-      for (u64 i = tid; i < a.n; i += SAMPLE_THREADS)
-        if (i != first) mine += kept_weight(i);
-      rest = block_sum(mine, sums);
-    }
-    double u = static_cast<double>(a.uniform[r]);
-    // (1 and above: no running mass exceeds it, so that the last kept one is taken; below 0 and NaN count as 0)
-    u = !(u >= 0.0) ? 0.0 : u < 1.0 ? u : __builtin_inf();
-    double aim = u * (1.0 + rest);
-    constexpr u32 WAVES = SAMPLE_THREADS / 64;
-    while (hi - lo > SAMPLE_THREADS) {
-      const u64 run = (hi - lo + WAVES - 1) / WAVES;
-      const u64 from = lo + wave * run, to = min(hi, from + run);
-      double mine = 0.0;
-      for (u64 i = from + lane; i < to; i += 64) mine += kept_weight(i);
+    double others = 0.0, bests = 0.0, aim = 0.0;
+    while (true) {
+      const bool whole = lo == 0 && hi == a.n;
+      u64 run = (hi - lo + SAMPLE_WAVES - 1) / SAMPLE_WAVES;
+      run = (run + 63) / 64 * 64;
+      const u64 from = min(hi, lo + wave * run), to = min(hi, from + run);
+      double mine = 0.0, ones = 0.0;
+      each(row, from, to, lane, 64, [&](u64 i, u32 key) {
+        if (key > cut.key || (key == cut.key && i < tie_end)) {
+          if (key == best)
+            ones += 1.0;
+          else
+            mine += w.of(key);
+        }
+      });
 #pragma unroll
-      for (int w = 1; w < 64; w *= 2) mine += __shfl_xor(mine, w);
+      for (int v = 1; v < 64; v *= 2) mine += __shfl_xor(mine, v), ones += __shfl_xor(ones, v);
       __syncthreads();
-      if (lane == 0) sums[wave] = mine;
+      if (lane == 0) s.wave[wave] = __builtin_bit_cast(u64, mine), s.hist[wave] = __builtin_bit_cast(u64, ones);
       __syncthreads();
-      u32 w = 0, last = 0;
+      if (whole) {
+        others = bests = 0.0;
+        for (u32 v = 0; v < SAMPLE_WAVES; ++v) others += __builtin_bit_cast(double, s.wave[v]), bests += __builtin_bit_cast(double, s.hist[v]);
+        aim = u * (bests + others);
+      }
+      u32 at = 0, last = 0;
       double before = 0.0, before_last = 0.0;
       bool found = false;
-      for (w = 0; w < WAVES; ++w) {
-        if (sums[w] > 0.0) {
-          last = w;
+      for (at = 0; at < SAMPLE_WAVES; ++at) {
+        const double mass = __builtin_bit_cast(double, s.wave[at]) + __builtin_bit_cast(double, s.hist[at]);
+        if (mass > 0.0) {
+          last = at;
           before_last = before;
-          if (before + sums[w] > aim) {
+          if (before + mass > aim) {
             found = true;
             break;
           }
         }
-        before += sums[w];
+        before += mass;
       }
-      if (!found) w = last, before = before_last;  // rounding: the last run that holds anything
+      if (!found) at = last, before = before_last;  // rounding: the last run that holds anything
       aim -= before;
-      lo = lo + w * run;
+      lo += at * run;
       hi = min(hi, lo + run);
+      if (hi - lo <= SAMPLE_THREADS) break;
     }
     // the last span, a thread for each entry
     const u64 i = lo + tid;
-    const double mine = i < hi ? kept_weight(i) : 0.0;
-    double run = mine;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) {
-      const double x = __shfl_up(run, w);
-      if (lane >= (u32)w) run += x;
-    }
+    const u32 key = i < hi ? float_key(mx_float(row[i])) : 0;
+    const double mine = i < hi && (key > cut.key || (key == cut.key && i < tie_end)) ? w.of(key) : 0.0;
+    double run;
+    block_scan<double>(mine, s, &run);
+    if (tid == 0) s.word = ~0ull, s.count = 0;
     __syncthreads();
-    if (lane == 63) sums[wave] = run;
-    if (tid == 0) s_left = ~0ull, s_before = 0;
-    __syncthreads();
-    for (u32 w = 0; w < wave; ++w) run += sums[w];
     if (mine > 0.0) {
-      if (run > aim) atomicMin(&s_left, (unsigned long long)i);
-      atomicMax(&s_before, (unsigned long long)i);
+      if (run > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
+      atomicMax(&s.count, tid);
     }
     __syncthreads();
-    if (tid == 0) {
-      const u64 id = s_left != ~0ull ? s_left : s_before;
-      a.ids[r] = (u32)id;
-      const double w = kept_weight(id);
-      if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((id == first ? rest : 1.0 + rest - w) / w));
+    if (tid == (s.word != ~0ull ? (u32)s.word : s.count)) {
+      a.ids[r] = (u32)i;
+      if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((key == best ? bests - 1.0 + others : bests + others - mine) / mine));
     }
   }
 }
@@ -335,6 +483,7 @@ int ann_sample(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtyp
   a.rows = (u32)rows;
   a.unit = 62;
   while ((1ull << (62 - a.unit)) < n) --a.unit;
+  if (a.unit > 50) a.unit = 50;
   a.o.temperature = 1.0f;
   if (opts) a.o = *opts;
   a.uniform = uniform_dev;
