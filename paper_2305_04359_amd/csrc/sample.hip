@@ -5,6 +5,8 @@
 // masses) are found by histograms over ever shorter ranges of keys.  Masses are sums of weights rounded to multiples
 // of a power of two: whole numbers, whose sums depend on no order.  The draw sums the kept weights in fp64 in a
 // fixed order.
+#include <type_traits>
+
 #include "mx.hpp"
 
 namespace annmi {
@@ -33,55 +35,82 @@ constexpr u32 key_grain() {
   return sizeof(T) == 4 ? 0 : __is_same(T, __half) ? 13 : 16;
 }
 
-// exp((score - best) / temperature) to a few units of the last place: 2^(j / 256) from a table, the rest, below
-// ln 2 / 512, by its series.
+constexpr u32 TABLE_BITS = 9;
+constexpr u32 TABLE = 1u << TABLE_BITS;
+
+// exp((score - best) / temperature), within 1e-14 of itself: a power of two, times 2^(j / 512) from a table, times
+// the rest, whose logarithm is below ln 2 / 1024, by three terms of its series.  Adding 1.5 * 2^52 leaves the
+// whole number of 512ths of an octave in the low bits of the sum.
 struct Weights {
-  double best, scale;  // scale: 256 / (temperature ln 2)
-  u32 best_key;
+  float most;          // the best score
+  double best, scale;  // as the sums take it; 512 / (temperature ln 2)
   const double* table;
-  __device__ __forceinline__ double of(u32 key) const {
-    if (key == best_key) return 1.0;
-    double y = (static_cast<double>(key_float(key)) - best) * scale;
-    y = y > -300000.0 ? y : -300000.0;  // (2^-1171: 0)
-    const double whole = __builtin_rint(y), r = (y - whole) * 0.0027076061740622863;  // ln 2 / 256
-    const int e = static_cast<int>(whole);
-    const double p = __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(r, 1.0 / 24, 1.0 / 6), r, 0.5), r, 1.0), r, 1.0);
-    return ldexp(table[e & 255] * p, e >> 8);
+  __device__ __forceinline__ double raw(float score) const {  // (not of +inf); 2^-1000 for all that is smaller
+    constexpr double MAGIC = 6755399441055744.0, C = 0.0013538030870311431;  // C: ln 2 / 512
+    const double d = __builtin_fmax((static_cast<double>(score) - best) * scale, -512000.0);
+    const double t = d + MAGIC;
+    const double r = d - (t - MAGIC);
+    const int n = static_cast<int>(__double_as_longlong(t));
+    const double p = __builtin_fma(__builtin_fma(__builtin_fma(r, C * C * C / 6, C * C / 2), r, C), r, 1.0);
+    const double v = table[n & (TABLE - 1)] * p;
+    return __hiloint2double(__double2hiint(v) + ((n >> TABLE_BITS) << 20), __double2loint(v));
+  }
+  __device__ __forceinline__ double of(float score) const {
+    const double v = raw(score);
+    return score == most ? 1.0 : v > 1e-300 ? v : 0.0;
   }
   // in units of 2^-unit, to the nearest; unit <= 50: adding 2^52 leaves the whole number in the low bits
-  __device__ __forceinline__ u64 units(u32 key, double unit) const {
-    return static_cast<u64>(__double_as_longlong(__builtin_fma(of(key), unit, 4503599627370496.0)) & 0xFFFFFFFFFFFFFll);
+  __device__ __forceinline__ u64 units(float score, double unit) const { return in_units(of(score), unit); }
+  __device__ __forceinline__ u64 in_units(double weight, double unit) const {
+    const double v = __builtin_fma(weight, unit, 4503599627370496.0);
+    return (u64)((u32)__double2hiint(v) & 0xFFFFFu) << 32 | (u32)__double2loint(v);
   }
 };
 
-// f(id, key) for the row's entries from..to, dealt to `ranks` threads: 16 bytes at a time, four loads on their way
-// at once; before the first and after the last whole piece one by one.
-template <typename T, typename F>
+using True = std::integral_constant<bool, true>;
+using False = std::integral_constant<bool, false>;
+
+// Keeps the compiler from taking a value only where it is used: the values of a piece are to be taken side by side.
+__device__ __forceinline__ void taken(double& v) { asm volatile("" : "+v"(v)); }
+
+// f(id, scores) for the row's entries from..to, dealt to `ranks` threads in pieces of 16 bytes, AHEAD of them on
+// their way at once.  What the first and last piece lack of a whole one is -inf, as are no candidates.
+template <int AHEAD, typename T, typename F>
 __device__ __forceinline__ void each(const T* row, u64 from, u64 to, u32 rank, u32 ranks, F f) {
-  constexpr u32 V = 16 / sizeof(T), AHEAD = 4;
+  constexpr u32 V = 16 / sizeof(T);
+  using Piece = Pack<T, V>;
   const u64 skew = reinterpret_cast<uintptr_t>(row + from) % 16 / sizeof(T);
   const u64 head = min(to, from + (V - skew) % V);
-  const u64 pieces = (to - head) / V, tail = head + pieces * V;
-  for (u64 i = from + rank; i < head; i += ranks) f(i, float_key(mx_float(row[i])));
-  for (u64 p = rank; p < pieces; p += (u64)ranks * AHEAD) {
-    Pack<T, V> x[AHEAD];
+  const u32 pieces = (u32)((to - head) / V);
+  const u64 tail = head + (u64)pieces * V;
+  const Piece* at = reinterpret_cast<const Piece*>(row + head);
+  for (u32 p = rank; p < pieces; p += AHEAD * ranks) {
+    Piece x[AHEAD];
 #pragma unroll
-    for (u32 u = 0; u < AHEAD; ++u) x[u] = *reinterpret_cast<const Pack<T, V>*>(row + head + min(p + (u64)u * ranks, pieces - 1) * V);
+    for (u32 u = 0; u < AHEAD; ++u) x[u] = at[min(p + u * ranks, pieces - 1)];
 #pragma unroll
     for (u32 u = 0; u < AHEAD; ++u) {
-      __builtin_amdgcn_sched_barrier(0);  // (or the weights of several pieces would be taken at once, in too many registers)
-      if (p + (u64)u * ranks < pieces)
+      __builtin_amdgcn_sched_barrier(0);  // (or several pieces would be worked on at once, in too many registers)
+      if (p + u * ranks >= pieces) break;
+      float v[V];
 #pragma unroll
-        for (u32 e = 0; e < V; ++e) f(head + (p + (u64)u * ranks) * V + e, float_key(mx_float(x[u].v[e])));
+      for (u32 e = 0; e < V; ++e) v[e] = mx_float(x[u].v[e]);
+      f(head + (u64)(p + u * ranks) * V, v);
     }
   }
-  for (u64 i = tail + rank; i < to; i += ranks) f(i, float_key(mx_float(row[i])));
+  if (rank < 2 && ranks > 1) {
+    const u64 lo = rank ? tail : from, hi = rank ? to : head;
+    float v[V];
+#pragma unroll
+    for (u32 e = 0; e < V; ++e) v[e] = lo + e < hi ? mx_float(row[lo + e]) : -__builtin_inff();
+    if (lo < hi) f(lo, v);
+  }
 }
 
 struct SampleLds {
   u64 hist[SAMPLE_BINS];    // counts or masses; sorted candidates
   u64 weight[SAMPLE_BINS];  // of the candidates that are sorted (bits of doubles)
-  double table[256];
+  double table[TABLE];
   u64 wave[SAMPLE_WAVES];
   u64 word;
   u32 count, bin;
@@ -99,13 +128,15 @@ __device__ V block_scan(V v, SampleLds& s, V* upto) {
   __syncthreads();
   if (lane == 63) s.wave[wave] = __builtin_bit_cast(u64, v);
   __syncthreads();
-  V sum = V(0), before = V(0);
-  for (u32 w = 0; w < SAMPLE_WAVES; ++w) {
-    if (w == wave) before = sum;
-    sum += __builtin_bit_cast(V, s.wave[w]);
+  V sums = __builtin_bit_cast(V, s.wave[lane % SAMPLE_WAVES]);
+#pragma unroll
+  for (u32 w = 1; w < SAMPLE_WAVES; w *= 2) {
+    const V x = __shfl_up(sums, w, SAMPLE_WAVES);
+    if (lane % SAMPLE_WAVES >= w) sums += x;
   }
-  *upto = before + v;
-  return sum;
+  const V before = __shfl(sums, (int)(wave + 63) % 64);
+  *upto = wave ? before + v : v;
+  return __shfl(sums, SAMPLE_WAVES - 1);
 }
 
 // s.hist[0 .. size) upwards; size: a power of two
@@ -126,7 +157,7 @@ __device__ void block_sort(SampleLds& s, u32 size) {
 struct Cut {
   u32 key;
   u64 ties;  // how many of the candidates at `key` are kept, the first ones by id
-  u64 at;    // how many there are (top-k only)
+  u64 at;    // how many there are, where `ties` is a number
 };
 
 // A workgroup per row.  The row is read once for its best score, once to three times for each cut, once for the draw
@@ -136,23 +167,29 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   __shared__ SampleLds s;
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   constexpr u32 GRAIN = key_grain<T>();
-  if (tid < 256) s.table[tid] = exp2(tid / 256.0);
+  if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
     const float temperature = a.o.temperature_dev ? a.o.temperature_dev[r] : a.o.temperature;
     const u32 top_k = a.o.top_k_dev ? a.o.top_k_dev[r] : a.o.top_k;
     const float top_p = a.o.top_p_dev ? a.o.top_p_dev[r] : a.o.top_p;
     const float min_p = a.o.min_p_dev ? a.o.min_p_dev[r] : a.o.min_p;
-    auto all = [&](auto f) { each(row, 0, a.n, tid, SAMPLE_THREADS, f); };
+    auto all = [&](auto f) { each<4>(row, 0, a.n, tid, SAMPLE_THREADS, f); };
+    constexpr u32 V = 16 / sizeof(T);
 
-    u32 best = 0;
-    all([&](u64, u32 key) { best = max(best, key); });
+    float most = -__builtin_inff();
+    each<8>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
 #pragma unroll
-    for (int w = 1; w < 64; w *= 2) best = max(best, (u32)__shfl_xor((int)best, w));
+      for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
+    });
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w));
     __syncthreads();
-    if (lane == 0) s.wave[wave] = best;
+    if (lane == 0) s.wave[wave] = __float_as_uint(most);
     __syncthreads();
-    for (u32 w = 0; w < SAMPLE_WAVES; ++w) best = max(best, (u32)s.wave[w]);
+    for (u32 w = 0; w < SAMPLE_WAVES; ++w) most = __builtin_fmaxf(most, __uint_as_float((u32)s.wave[w]));
+    const u32 best = float_key(most);
+    most = key_float(best);  // (+0 for -0)
     if (best <= SAMPLE_LEAST) {  // (the same in all threads)
       if (tid == 0) {
         a.ids[r] = ANN_NONE;
@@ -164,8 +201,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       if (tid == 0) s.word = ~0ull;
       __syncthreads();
       u64 first = ~0ull;
-      all([&](u64 i, u32 key) {
-        if (key == best) first = min(first, i);
+      all([&](u64 i, const float (&v)[V]) {
+#pragma unroll
+        for (u32 e = 0; e < V; ++e)
+          if (v[e] == most) first = min(first, i + e);
       });
       if (first != ~0ull) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)first);
       __syncthreads();
@@ -176,20 +215,22 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       continue;
     }
     Weights w;
-    w.best_key = best;
-    w.best = static_cast<double>(key_float(best));
     // (an infinite temperature has scale 0; next to an infinite best score any other has weight 0 all the same)
-    w.scale = w.best < __builtin_inf() ? 369.3299304675746 / static_cast<double>(temperature) : 1.0;
+    const bool finite = most < __builtin_inff();
+    w.most = most;
+    w.best = finite ? static_cast<double>(most) : 1e300;
+    w.scale = finite ? 738.6598609351493 / static_cast<double>(temperature) : 1.0;
     w.table = s.table;
     const double unit = ldexp(1.0, (int)a.unit);
     Cut cut = {SAMPLE_LEAST + 1, ~0ull, ~0ull};
 
     // The first histogram is linear in the score, 32 bins for each unit of max(temperature, 1) below the best, the
     // last one open; equal scores share a bin, and the bins fall with the score.
-    const float per_score = 32.0f / (temperature > 1.0f ? temperature : 1.0f), best_score = key_float(best);
-    auto linear_bin = [&](u32 key) {
-      const float z = (best_score - key_float(key)) * per_score;
-      return key == best ? 0u : z < (float)(SAMPLE_BINS - 1) ? (u32)z : SAMPLE_BINS - 1;
+    const float per_score = 32.0f / (temperature > 1.0f ? temperature : 1.0f);
+    auto linear_bin = [&](float v) {
+      // (the smaller of 1023 and a NaN is 1023: inf * 0, or +inf next to a best of +inf, which is put right)
+      const float z = __builtin_fminf((most - v) * per_score, (float)(SAMPLE_BINS - 1));
+      return v == most ? 0u : (u32)z;
     };
     // Finds the key at which the running count (or mass), from the best key down, reaches `aim(total)`; candidates
     // below floor.key do not count, and of those at it floor.ties do.  False: the total is 0 or below the aim.
@@ -201,14 +242,32 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         __syncthreads();
         s.hist[tid] = 0;
         __syncthreads();
-        all([&](u64, u32 key) {
-          if (key < lo || key > hi || (some_ties && key == floor.key)) return;
-          const u32 b = level ? (hi - key) >> shift : linear_bin(key);
-          atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[b]), (unsigned long long)(mass ? w.units(key, unit) : 1ull));
-        });
+        const float lowest = key_float(lo), highest = key_float(hi);
+        const float none = some_ties ? key_float(floor.key) : -__builtin_inff();
+        auto count = [&](auto first, auto masses) {
+          all([&](u64, const float (&v)[V]) {
+            bool in[V], any = false;
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) any |= in[e] = v[e] >= lowest && v[e] <= highest && v[e] != none;
+            if (!any) return;
+            double raw[V];
+            if (masses)
+#pragma unroll
+              for (u32 e = 0; e < V; ++e) raw[e] = w.raw(v[e]), taken(raw[e]);
+#pragma unroll
+            for (u32 e = 0; e < V; ++e)
+              if (in[e])
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[first ? linear_bin(v[e]) : (hi - float_key(v[e])) >> shift]),
+                          (unsigned long long)(masses ? w.in_units(v[e] == most ? 1.0 : raw[e], unit) : 1ull));
+          });
+        };
+        if (level == 0)
+          mass ? count(True(), True()) : count(True(), False());
+        else
+          mass ? count(False(), True()) : count(False(), False());
         __syncthreads();
         if (tid == 0 && some_ties && floor.key >= lo)
-          s.hist[level ? (hi - floor.key) >> shift : linear_bin(floor.key)] += floor.ties * w.units(floor.key, unit);
+          s.hist[level ? (hi - floor.key) >> shift : linear_bin(key_float(floor.key))] += floor.ties * w.units(key_float(floor.key), unit);
         __syncthreads();
         const u64 mine = s.hist[tid];
         u64 upto;
@@ -227,7 +286,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           u32 x = lo, y = hi;
           while (x < y) {  // the largest key whose bin is b or above
             const u32 mid = x + (y - x + 1) / 2;
-            if (linear_bin(mid) >= b)
+            if (linear_bin(key_float(mid)) >= b)
               x = mid;
             else
               y = mid - 1;
@@ -236,7 +295,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           x = lo, y = top;
           while (x < y) {  // the smallest key whose bin is b
             const u32 mid = x + (y - x) / 2;
-            if (linear_bin(mid) <= b)
+            if (linear_bin(key_float(mid)) <= b)
               y = mid;
             else
               x = mid + 1;
@@ -278,8 +337,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       __syncthreads();
       if (tid == 0) s.count = 0;
       __syncthreads();
-      all([&](u64 i, u32 key) {
-        if (key >= cut.key) s.hist[atomicAdd(&s.count, 1u)] = (u64)~key << 32 | i;
+      const float lowest = key_float(cut.key);
+      all([&](u64 i, const float (&v)[V]) {
+#pragma unroll
+        for (u32 e = 0; e < V; ++e)
+          if (v[e] >= lowest) s.hist[atomicAdd(&s.count, 1u)] = (u64)~float_key(v[e]) << 32 | (i + e);
       });
       __syncthreads();
       u32 size = 2;
@@ -288,10 +350,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       block_sort(s, size);
       const bool mine = tid < top_k;
       const u64 entry = mine ? s.hist[tid] : 0;
-      const u32 key = ~(u32)(entry >> 32);
-      const double weight = mine ? w.of(key) : 0.0;
+      const float score = key_float(~(u32)(entry >> 32));
+      const double weight = mine ? w.of(score) : 0.0;
       u64 upto;
-      const u64 units = mine ? w.units(key, unit) : 0;
+      const u64 units = mine ? w.units(score, unit) : 0;
       const u64 total = block_scan<u64>(units, s, &upto);
       bool keep = mine;
       if (top_p > 0.0f && top_p < 1.0f) keep = keep && (tid == 0 || (double)(upto - units) < static_cast<double>(top_p) * static_cast<double>(total));
@@ -332,10 +394,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
                    return aim < 1 ? 1 : aim > total ? total : aim;
                  },
                  &found, &left)) {
-        const u64 each_one = w.units(found.key, unit);
-        const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull;
-        cut.ties = found.key == cut.key ? min(cut.ties, need) : need;
-        cut.key = found.key;
+        const u64 each_one = w.units(key_float(found.key), unit);
+        const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull, at = each_one ? found.at / each_one : ~0ull;
+        if (found.key != cut.key || cut.ties == ~0ull)
+          cut = {found.key, need, at};
+        else if (need < cut.ties)  // (`at` of top-k counts the ones that it dropped as well)
+          cut.ties = need;
       }
     }
     if (min_p > 0.0f) {
@@ -343,7 +407,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       u32 lo = cut.key, hi = best;  // hi reaches it
       while (lo < hi) {
         const u32 mid = lo + (hi - lo) / 2;
-        if (w.of(mid) >= floor_w)
+        if (w.of(key_float(mid)) >= floor_w)
           hi = mid;
         else
           lo = mid + 1;
@@ -352,30 +416,35 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     }
     // Where only some of those at the cut are kept, they are the first ones by id: those below `tie_end`.
     u64 tie_end = a.n;
-    if (cut.ties != ~0ull) {
-      u64 seen = 0;
-      for (u64 i0 = 0; i0 < a.n; i0 += SAMPLE_THREADS) {
-        const u64 i = i0 + tid;
-        const bool tie = i < a.n && float_key(mx_float(row[i])) == cut.key;
-        const u64 votes = __ballot(tie);
+    const float lowest = key_float(cut.key);
+    if (cut.ties < cut.at) {
+      // narrowed down like the draw below: runs of the span, counted by a wave each
+      u64 lo = 0, hi = a.n, before = 0;
+      while (hi - lo > SAMPLE_THREADS) {
+        const u64 run = ((hi - lo + SAMPLE_WAVES - 1) / SAMPLE_WAVES + 63) / 64 * 64;
+        const u64 from = min(hi, lo + wave * run), to = min(hi, from + run);
+        u32 mine = 0;
+        each<4>(row, from, to, lane, 64, [&](u64, const float (&v)[V]) {
+#pragma unroll
+          for (u32 e = 0; e < V; ++e) mine += v[e] == lowest;
+        });
+#pragma unroll
+        for (int v = 1; v < 64; v *= 2) mine += (u32)__shfl_xor((int)mine, v);
         __syncthreads();
-        if (lane == 0) s.wave[wave] = (u64)__popcll(votes);
-        if (tid == 0) s.word = ~0ull;
+        if (lane == 0) s.wave[wave] = mine;
         __syncthreads();
-        u64 before = seen, here = 0;
-        for (u32 v = 0; v < SAMPLE_WAVES; ++v) {
-          if (v < wave) before += s.wave[v];
-          here += s.wave[v];
-        }
-        before += __popcll(votes & ((1ull << lane) - 1));
-        if (tie && before == cut.ties) s.word = i;
-        __syncthreads();
-        if (s.word != ~0ull) {
-          tie_end = s.word;
-          break;
-        }
-        seen += here;
+        u32 at = 0;
+        while (at + 1 < SAMPLE_WAVES && before + s.wave[at] <= cut.ties) before += s.wave[at++];
+        lo += at * run;
+        hi = min(hi, lo + run);
       }
+      const u64 i = lo + tid;
+      const u64 tie = i < hi && mx_float(row[i]) == lowest;
+      u64 upto;
+      block_scan<u64>(tie, s, &upto);
+      if (tie && before + upto - 1 == cut.ties) s.word = i;
+      __syncthreads();
+      tie_end = s.word;
     }
     // The draw: the span that holds it is dealt to the waves in runs, whose masses tell which run it is.  The best
     // candidates' weights, 1 each, are kept apart, so that a mass that is nearly all the drawn one's loses nothing.
@@ -386,50 +455,59 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       u64 run = (hi - lo + SAMPLE_WAVES - 1) / SAMPLE_WAVES;
       run = (run + 63) / 64 * 64;
       const u64 from = min(hi, lo + wave * run), to = min(hi, from + run);
-      double mine = 0.0, ones = 0.0;
-      each(row, from, to, lane, 64, [&](u64 i, u32 key) {
-        if (key > cut.key || (key == cut.key && i < tie_end)) {
-          if (key == best)
-            ones += 1.0;
-          else
-            mine += w.of(key);
+      double mine = 0.0;
+      u32 ones = 0;
+      each<2>(row, from, to, lane, 64, [&](u64 i, const float (&v)[V]) {
+        bool keep[V], any = false;
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) {
+          keep[e] = v[e] >= lowest;
+          if (v[e] == lowest) keep[e] = i + e < tie_end;
+          any |= keep[e];
+        }
+        if (!any) return;
+        double raw[V];
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) raw[e] = w.raw(keep[e] && v[e] != most ? v[e] : -__builtin_inff()), taken(raw[e]);
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) {
+          ones += keep[e] && v[e] == most;
+          mine += raw[e] > 1e-300 ? raw[e] : 0.0;
         }
       });
 #pragma unroll
-      for (int v = 1; v < 64; v *= 2) mine += __shfl_xor(mine, v), ones += __shfl_xor(ones, v);
+      for (int v = 1; v < 64; v *= 2) mine += __shfl_xor(mine, v), ones += (u32)__shfl_xor((int)ones, v);
       __syncthreads();
-      if (lane == 0) s.wave[wave] = __builtin_bit_cast(u64, mine), s.hist[wave] = __builtin_bit_cast(u64, ones);
+      if (lane == 0) s.wave[wave] = __builtin_bit_cast(u64, mine), s.hist[wave] = ones;
       __syncthreads();
+      // (every wave alike, a lane for each run)
+      const double rest = __builtin_bit_cast(double, s.wave[lane % SAMPLE_WAVES]), one = static_cast<double>(s.hist[lane % SAMPLE_WAVES]);
       if (whole) {
-        others = bests = 0.0;
-        for (u32 v = 0; v < SAMPLE_WAVES; ++v) others += __builtin_bit_cast(double, s.wave[v]), bests += __builtin_bit_cast(double, s.hist[v]);
+        others = rest, bests = one;
+#pragma unroll
+        for (int v = 1; v < (int)SAMPLE_WAVES; v *= 2) others += __shfl_xor(others, v, SAMPLE_WAVES), bests += __shfl_xor(bests, v, SAMPLE_WAVES);
         aim = u * (bests + others);
       }
-      u32 at = 0, last = 0;
-      double before = 0.0, before_last = 0.0;
-      bool found = false;
-      for (at = 0; at < SAMPLE_WAVES; ++at) {
-        const double mass = __builtin_bit_cast(double, s.wave[at]) + __builtin_bit_cast(double, s.hist[at]);
-        if (mass > 0.0) {
-          last = at;
-          before_last = before;
-          if (before + mass > aim) {
-            found = true;
-            break;
-          }
-        }
-        before += mass;
+      const double mass = rest + one;
+      double upto = mass;
+#pragma unroll
+      for (int v = 1; v < (int)SAMPLE_WAVES; v *= 2) {
+        const double x = __shfl_up(upto, v, SAMPLE_WAVES);
+        if (lane % SAMPLE_WAVES >= (u32)v) upto += x;
       }
-      if (!found) at = last, before = before_last;  // rounding: the last run that holds anything
-      aim -= before;
+      const u64 above = __ballot(lane < SAMPLE_WAVES && mass > 0.0 && upto > aim), some = __ballot(lane < SAMPLE_WAVES && mass > 0.0);
+      // (none above, by rounding: the last run that holds anything)
+      const u32 at = above ? (u32)__builtin_ctzll(above) : 63u - (u32)__builtin_clzll(some);
+      const double before = __shfl(upto, (int)(at + 63) % 64);
+      aim -= at ? before : 0.0;
       lo += at * run;
       hi = min(hi, lo + run);
       if (hi - lo <= SAMPLE_THREADS) break;
     }
     // the last span, a thread for each entry
     const u64 i = lo + tid;
-    const u32 key = i < hi ? float_key(mx_float(row[i])) : 0;
-    const double mine = i < hi && (key > cut.key || (key == cut.key && i < tie_end)) ? w.of(key) : 0.0;
+    const float v = i < hi ? mx_float(row[i]) : -__builtin_inff();
+    const double mine = v > lowest || (v == lowest && i < tie_end) ? w.of(v) : 0.0;
     double run;
     block_scan<double>(mine, s, &run);
     if (tid == 0) s.word = ~0ull, s.count = 0;
@@ -441,7 +519,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     __syncthreads();
     if (tid == (s.word != ~0ull ? (u32)s.word : s.count)) {
       a.ids[r] = (u32)i;
-      if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((key == best ? bests - 1.0 + others : bests + others - mine) / mine));
+      if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((v == most ? bests - 1.0 + others : bests + others - mine) / mine));
     }
   }
 }
