@@ -11,7 +11,7 @@ namespace annmi {
 
 constexpr u32 SEARCH_GROUP = 64;
 constexpr u32 SEARCH_MOST_K = 128;
-constexpr u64 SEARCH_SCRATCH_FLOATS = 1ull << 26;  // of group maxima held at a time, where 64 queries fit in them
+constexpr u64 SEARCH_SCRATCH_FLOATS = 1ull << 28;  // of group maxima held at a time, where 64 queries fit in them
 constexpr u64 SEARCH_MOST_AT_ONCE = 1ull << 22;   // queries of a launch: its threads are counted in 32 bits
 
 struct MxSearchArgs {
@@ -19,8 +19,8 @@ struct MxSearchArgs {
   const float* norms;   // null: inner products
   const float* qnorms;
   u32 q0, nq;           // the queries of this launch
-  u32 groups, k;
-  float* most;          // (nq, groups)
+  u32 groups, pitch, k; // pitch: floats from one query's maxima to the next's
+  float* most;          // (nq, pitch)
   u32* ids;
   float* dists;
 };
@@ -32,17 +32,219 @@ __device__ __forceinline__ int load_scale(const MxRows& m, u64 row, u32 step) {
   return m.scales[(row * m.steps + step) * MX_STEP_SCALES + threadIdx.x % 64 / 16];
 }
 
-// what the sums of rows row0 .. row0 + 3 start from: 0, or - |x|^2 / 2
-__device__ __forceinline__ v4f first_sum(const MxSearchArgs& a, u64 row0) {
-  v4f c = {};
-  if (a.norms)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = -0.5f * a.norms[min(row0 + r, (u64)a.w.n - 1)];
-  return c;
+// what the sum of a row starts from: 0, or - |x|^2 / 2, and -inf past the last row, which no maximum takes
+__device__ __forceinline__ float first_sum(const MxSearchArgs& a, u64 row) {
+  return row >= a.w.n ? -__builtin_inff() : a.norms ? -0.5f * a.norms[row] : 0.0f;
+}
+__device__ __forceinline__ v4f first_sums(const MxSearchArgs& a, u64 row0) {
+  return v4f{first_sum(a, row0), first_sum(a, row0 + 1), first_sum(a, row0 + 2), first_sum(a, row0 + 3)};
 }
 
-// A wave: 64 rows (a group) x 64 queries.
-__global__ __launch_bounds__(256) void mx_group_most_kernel(MxSearchArgs a, u64 tiles) {
+__device__ __forceinline__ float most_of(float m, v4f v) {
+  return __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(m, v[0]), v[1]), __builtin_fmaxf(v[2], v[3]));
+}
+
+// The maxima of four columns groups over the four lanes that share a column: lane l gets the one of group
+// ((l / 32) | (l / 16 % 2 * 2)), column l % 16.
+__device__ __forceinline__ float join_four(float m0, float m1, float m2, float m3) {
+  using v2u = u32 __attribute__((ext_vector_type(2)));
+  auto both = [](auto p) {
+    const v2u v = __builtin_bit_cast(v2u, p);
+    return __builtin_fmaxf(__uint_as_float(v.x), __uint_as_float(v.y));
+  };
+  const float a = both(__builtin_amdgcn_permlane32_swap(__float_as_uint(m0), __float_as_uint(m1), false, false));
+  const float b = both(__builtin_amdgcn_permlane32_swap(__float_as_uint(m2), __float_as_uint(m3), false, false));
+  return both(__builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false));
+}
+__device__ __forceinline__ u32 joined_group(u32 lane) { return lane / 32 | lane / 16 % 2 * 2; }
+
+// The queries' fragments, held by a wave for good; the scales of a query's steps share a register.
+template <int STEPS, int QF>
+struct Queries {
+  v4i codes[QF][STEPS];
+  int scales[QF];
+  __device__ __forceinline__ void load(const MxSearchArgs& a, u64 first) {
+#pragma unroll
+    for (int j = 0; j < QF; ++j) {
+      const u64 row = a.q0 + min(first + 16 * j + threadIdx.x % 16, (u64)a.nq - 1);
+      u32 b = 0;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        codes[j][s] = load_codes(a.q, row, s);
+        b |= (u32)load_scale(a.q, row, s) << (8 * s);
+      }
+      scales[j] = (int)b;
+    }
+  }
+};
+
+template <int BYTE>
+__device__ __forceinline__ v4f mx_mfma_byte(v4i a, v4i b, v4f c, int scale_a, int scale_b) {
+  const v8i x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, BYTE, scale_a, BYTE, scale_b);
+}
+template <int STEPS, int QF, int S = 0>
+__device__ __forceinline__ void score_tile(const v4i (&w)[STEPS], int scales, const Queries<STEPS, QF>& q, v4f first, v4f (&acc)[QF]) {
+#pragma unroll
+  for (int j = 0; j < QF; ++j) acc[j] = mx_mfma_byte<S>(w[S], q.codes[j][S], S == 0 ? first : acc[j], scales, q.scales[j]);
+  if constexpr (S + 1 < STEPS) score_tile<STEPS, QF, S + 1>(w, scales, q, first, acc);
+}
+
+// Up to 16 QF queries: every wave scores groups of its own, whose rows it asks for one group ahead.  Bound by the
+// memory that the rows come from.
+template <int STEPS, int QF>
+__global__ __launch_bounds__(256) void mx_group_few_kernel(MxSearchArgs a) {
+  const u32 lane = threadIdx.x % 64;
+  const u32 waves = gridDim.x * 4;
+  u32 g = blockIdx.x * 4 + threadIdx.x / 64;
+  Queries<STEPS, QF> q;
+  q.load(a, 0);
+  struct Ahead {
+    v4i w[4][STEPS];
+    u32 b[4][STEPS];
+    v4f first[4];
+  } next;
+  auto ask = [&](u32 group) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u64 row0 = (u64)group * SEARCH_GROUP + 16 * i;
+      const u64 row = min(row0 + lane % 16, (u64)a.w.n - 1);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        next.w[i][s] = load_codes(a.w, row, s);
+        next.b[i][s] = reinterpret_cast<const u32*>(a.w.scales)[row * a.w.steps + s];
+      }
+      next.first[i] = first_sums(a, row0 + lane / 16 * 4);
+    }
+  };
+  if (g < a.groups) ask(g);
+  for (; g < a.groups; g += waves) {
+    const Ahead now = next;
+    ask(min(g + waves, a.groups - 1));
+    float m[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u32 scales = 0;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) scales |= (now.b[i][s] >> (lane / 16 * 8) & 255) << (8 * s);
+      v4f acc[QF];
+      score_tile<STEPS, QF>(now.w[i], (int)scales, q, now.first[i], acc);
+#pragma unroll
+      for (int j = 0; j < QF; ++j) m[j] = most_of(m[j], acc[j]);
+    }
+    const float joined = join_four(m[0], m[1], m[2], m[3]);
+    const u32 x = joined_group(lane) * 16 + lane % 16;
+    if (x < a.nq) a.most[(u64)x * a.pitch + g] = joined;
+  }
+}
+
+// Many queries: eight waves, WR of which share the 16 QF queries they hold and take groups in turn; all rows pass
+// through LDS, in stages of four groups (two where rows are long), laid out as the fragments are read.  Bound by the
+// matrix cores: beside a product of 16 x 16 scores and 128 elements stand two instructions that take its maximum.
+constexpr u32 SEARCH_THREADS = 512;
+template <int STEPS>
+constexpr u32 stage_groups() {
+  return STEPS <= 2 ? 4 : 2;
+}
+
+template <int STEPS, int QF, int WR>
+__global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchArgs a, u32 blocks_q, u32 ranges) {
+  constexpr u32 GS = stage_groups<STEPS>(), ROWS = GS * SEARCH_GROUP, TILES = ROWS / 16;
+  constexpr u32 LOADS = ROWS * STEPS * MX_STEP_BYTES / 16 / SEARCH_THREADS;
+  constexpr u32 SCALES = (ROWS * STEPS + SEARCH_THREADS - 1) / SEARCH_THREADS;
+  struct Stage {
+    v4i codes[TILES * STEPS][64];
+    u32 scales[TILES][64];
+    float first[ROWS];
+  };
+  extern __shared__ __align__(16) char lds[];
+  Stage* stages = reinterpret_cast<Stage*>(lds);
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  // Chiplets take workgroups in turn: each gets a run of them that read the same rows.
+  const u32 all = blocks_q * ranges, per = (all + 7) / 8, t = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (t >= all) return;
+  const u32 range = t / blocks_q;
+  const u32 total = (a.groups + GS - 1) / GS;  // stages
+  const u32 s0 = (u32)((u64)total * range / ranges), s1 = (u32)((u64)total * (range + 1) / ranges);
+  const u64 x0 = (u64)(t % blocks_q) * (8 / WR * 16 * QF) + wave / WR * (16 * QF);
+  Queries<STEPS, QF> q;
+  q.load(a, x0);
+
+  v4i next_w[LOADS];
+  u32 next_scale[SCALES];
+  float next_first = 0.0f;
+  auto fetch = [&](u32 stage) {
+    const u64 row0 = (u64)stage * ROWS;
+#pragma unroll
+    for (u32 i = 0; i < LOADS; ++i) {
+      const u32 at = i * SEARCH_THREADS + tid, frag = at / 64, r = frag / STEPS * 16 + at % 16;
+      next_w[i] = *reinterpret_cast<const v4i*>(a.w.codes + (min(row0 + r, (u64)a.w.n - 1) * STEPS + frag % STEPS) * MX_STEP_BYTES + at / 16 % 4 * 16);
+    }
+#pragma unroll
+    for (u32 i = 0; i < SCALES; ++i) {
+      const u32 at = min(i * SEARCH_THREADS + tid, ROWS * STEPS - 1);
+      next_scale[i] = reinterpret_cast<const u32*>(a.w.scales)[min(row0 * STEPS + at, (u64)a.w.n * STEPS - 1)];
+    }
+    next_first = first_sum(a, row0 + tid % ROWS);
+  };
+  auto keep = [&](Stage& to) {
+#pragma unroll
+    for (u32 i = 0; i < LOADS; ++i) (&to.codes[0][0])[i * SEARCH_THREADS + tid] = next_w[i];
+#pragma unroll
+    for (u32 i = 0; i < SCALES; ++i) {
+      const u32 at = i * SEARCH_THREADS + tid, r = at / STEPS, s = at % STEPS;
+      if (at < ROWS * STEPS)
+#pragma unroll
+        for (u32 g = 0; g < 4; ++g) reinterpret_cast<uint8_t*>(&to.scales[r / 16][g * 16 + r % 16])[s] = (uint8_t)(next_scale[i] >> (8 * g));
+    }
+    if (tid < ROWS) to.first[tid] = next_first;
+  };
+  fetch(s0);
+  keep(stages[s0 % 2]);
+  if (s0 + 1 < s1) fetch(s0 + 1);
+  for (u32 st = s0; st < s1; ++st) {
+    __syncthreads();
+    const Stage& here = stages[st % 2];
+    float joined[GS / WR][QF / 4];
+#pragma unroll
+    for (u32 n = 0; n < GS / WR; ++n) {
+      if (n == 1 || GS == WR) {  // behind the first products
+        if (st + 1 < s1) keep(stages[(st + 1) % 2]);
+        if (st + 2 < s1) fetch(st + 2);
+      }
+      const u32 g = n * WR + wave % WR;
+      float m[QF];
+#pragma unroll
+      for (int j = 0; j < QF; ++j) m[j] = -__builtin_inff();
+#pragma unroll
+      for (u32 i = 0; i < 4; ++i) {
+        v4i w[STEPS];
+#pragma unroll
+        for (u32 s = 0; s < STEPS; ++s) w[s] = here.codes[(g * 4 + i) * STEPS + s][lane];
+        v4f acc[QF];
+        score_tile<STEPS, QF>(w, (int)here.scales[g * 4 + i][lane], q, *reinterpret_cast<const v4f*>(&here.first[(g * 4 + i) * 16 + lane / 16 * 4]), acc);
+#pragma unroll
+        for (int j = 0; j < QF; ++j) m[j] = most_of(m[j], acc[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < QF; j += 4) joined[n][j / 4] = join_four(m[j], m[j + 1], m[j + 2], m[j + 3]);
+    }
+#pragma unroll
+    for (int j = 0; j < QF / 4; ++j) {
+      const u64 x = x0 + 64 * j + joined_group(lane) * 16 + lane % 16;
+      if (x >= a.nq) continue;
+      float* to = a.most + x * a.pitch + (u64)st * GS;  // (the pitch has room for a whole last stage)
+      if constexpr (WR == 1 && GS == 4)
+        *reinterpret_cast<v4f*>(to) = v4f{joined[0][j], joined[1][j], joined[2][j], joined[3][j]};
+      else
+#pragma unroll
+        for (u32 n = 0; n < GS / WR; ++n) to[n * WR + wave % WR] = joined[n][j];
+    }
+  }
+}
+
+// Rows of more steps: a wave scores 64 rows (a group) and 64 queries, step by step from memory.
+__global__ __launch_bounds__(256) void mx_group_long_kernel(MxSearchArgs a, u64 tiles) {
   const u32 lane = threadIdx.x % 64;
   const u64 t = (u64)blockIdx.x * 4 + threadIdx.x / 64;
   if (t >= tiles) return;
@@ -51,7 +253,7 @@ __global__ __launch_bounds__(256) void mx_group_most_kernel(MxSearchArgs a, u64 
   v4f acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const v4f c = first_sum(a, w0 + 16 * i + lane / 16 * 4);
+    const v4f c = first_sums(a, w0 + 16 * i + lane / 16 * 4);
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = c;
   }
@@ -71,123 +273,231 @@ __global__ __launch_bounds__(256) void mx_group_most_kernel(MxSearchArgs a, u64 
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = mx_mfma(w[i], x[j], acc[i][j], ws[i], xs[j]);
   }
+  float m[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    float m = -__builtin_inff();
+    m[j] = -__builtin_inff();
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (w0 + 16 * i + lane / 16 * 4 + r < a.w.n) m = __builtin_fmaxf(m, acc[i][j][r]);
-    m = __builtin_fmaxf(m, __shfl_xor(m, 16));
-    m = __builtin_fmaxf(m, __shfl_xor(m, 32));
-    const u64 x = x0 + 16 * j + lane;
-    if (lane < 16 && x < a.nq) a.most[x * a.groups + g] = m;
+    for (int i = 0; i < 4; ++i) m[j] = most_of(m[j], acc[i][j]);
   }
+  const float joined = join_four(m[0], m[1], m[2], m[3]);
+  const u64 x = x0 + joined_group(lane) * 16 + lane % 16;
+  if (x < a.nq) a.most[x * a.pitch + g] = joined;
 }
 
-// A workgroup per query: the first k groups by a radix selection on the keys of their maxima, eight bits at a time;
-// their rows' scores; the k best of those that reach the last group's maximum, sorted.
-__global__ __launch_bounds__(256) void mx_pick_kernel(MxSearchArgs a) {
-  extern __shared__ u64 found[];  // as many as the rows of k groups, up to a power of two for the sort
-  __shared__ u32 hist[256];
-  __shared__ u32 chosen[SEARCH_MOST_K];
-  __shared__ u32 s_prefix, s_left, s_count, s_scan[4];
-  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const u32 q = blockIdx.x;
-  const float* most = a.most + (u64)q * a.groups;
-  const u32 least = float_key(-__builtin_inff());  // keys up to this one are of groups without a score
+// A workgroup per query.  The k-th largest of its threads' maxima over the groups is a bound that k groups at least
+// reach; the few that do are ranked, the first k scored again, and the k best points ranked.
+constexpr u32 PICK_THREADS = 256;
+constexpr u32 PICK_FEW = 512;  // candidates that are ranked by counting the ones before each
 
-  // the k-th largest key
-  if (tid == 0) s_prefix = 0, s_left = min(a.k, a.groups), s_count = 0;
+struct PickLds {
+  u32 hist[PICK_THREADS];
+  u32 chosen[SEARCH_MOST_K];
+  u32 prefix, left, count, bound, scan[PICK_THREADS / 64];
+};
+
+// All groups' keys, by a radix selection of the k-th largest: where too many reach the bound (equal maxima).
+__device__ void choose_groups(const MxSearchArgs& a, const float* most, u32 least, PickLds& s) {
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  if (tid == 0) s.prefix = 0, s.left = min(a.k, a.groups), s.count = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
+    s.hist[tid] = 0;
     __syncthreads();
-    const u32 prefix = s_prefix;
-    for (u32 i = tid; i < a.groups; i += 256) {
+    const u32 prefix = s.prefix;
+    for (u32 i = tid; i < a.groups; i += PICK_THREADS) {
       const u32 key = float_key(most[i]);
-      if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&hist[key >> shift & 255], 1u);
+      if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&s.hist[key >> shift & 255], 1u);
     }
     __syncthreads();
     if (tid == 0) {
-      u32 left = s_left, b = 255;
-      while (b > 0 && hist[b] < left) left -= hist[b--];
-      s_left = left;
-      s_prefix = prefix << 8 | b;
+      u32 left = s.left, b = 255;
+      while (b > 0 && s.hist[b] < left) left -= s.hist[b--];
+      s.left = left;
+      s.prefix = prefix << 8 | b;
     }
     __syncthreads();
   }
-  const u32 cut = s_prefix, ties = s_left;  // groups above the cut, and the first `ties` of those at it
+  const u32 cut = s.prefix, ties = s.left;  // groups above the cut, and the first `ties` of those at it
   __syncthreads();
-  if (tid == 0) s_left = 0;
+  if (tid == 0) s.left = 0, s.bound = cut;
   __syncthreads();
   // in the order of groups, so that the ties taken are the first ones
-  for (u32 i0 = 0; i0 < a.groups; i0 += 256) {
+  for (u32 i0 = 0; i0 < a.groups; i0 += PICK_THREADS) {
     const u32 i = i0 + tid;
     const u32 key = i < a.groups ? float_key(most[i]) : 0u;
     const bool tie = key == cut && key > least;
     const u64 votes = __ballot(tie);
-    if (lane == 0) s_scan[wave] = (u32)__popcll(votes);
+    if (lane == 0) s.scan[wave] = (u32)__popcll(votes);
     __syncthreads();
-    u32 before = s_left + (u32)__popcll(votes & ((1ull << lane) - 1));
-    for (u32 w = 0; w < wave; ++w) before += s_scan[w];
-    if (i < a.groups && ((key > cut && key > least) || (tie && before < ties))) chosen[atomicAdd(&s_count, 1u)] = i;
+    u32 before = s.left + (u32)__popcll(votes & ((1ull << lane) - 1));
+    for (u32 w = 0; w < wave; ++w) before += s.scan[w];
+    if (i < a.groups && ((key > cut && key > least) || (tie && before < ties))) s.chosen[atomicAdd(&s.count, 1u)] = i;
     __syncthreads();
-    if (tid == 0) s_left += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
+    if (tid == 0) s.left += s.scan[0] + s.scan[1] + s.scan[2] + s.scan[3];
     __syncthreads();
-  }
-  const u32 nchosen = s_count;
-  __syncthreads();
-  if (tid == 0) s_count = 0;
-  __syncthreads();
-  // k groups: k points reach the smallest of their maxima, and no other point matters
-  const u32 low = nchosen == a.k ? max(cut, least + 1) : least + 1;
-  const u64 qrow = (u64)a.q0 + q;
-  for (u32 c = wave; c < nchosen * 4; c += 4) {  // 16 rows at a time
-    const u64 w0 = (u64)chosen[c / 4] * SEARCH_GROUP + c % 4 * 16;
-    const u64 wr = min(w0 + lane % 16, (u64)a.w.n - 1);
-    v4f acc = first_sum(a, w0 + lane / 16 * 4);
-    for (u32 s = 0; s < a.w.steps; ++s)
-      acc = mx_mfma(load_codes(a.w, wr, s), load_codes(a.q, qrow, s), acc, load_scale(a.w, wr, s), load_scale(a.q, qrow, s));
-    // (all columns are this query's: one of them is used)
-    if (lane % 16 == 0)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const u64 id = w0 + lane / 16 * 4 + r;
-        const u32 key = float_key(acc[r]);
-        if (id < a.w.n && key >= low) found[atomicAdd(&s_count, 1u)] = (u64)~key << 32 | id;
-      }
-  }
-  __syncthreads();
-  const u32 count = s_count;
-  u32 size = 2;
-  while (size < count) size *= 2;
-  for (u32 i = count + tid; i < size; i += 256) found[i] = ~0ull;
-  __syncthreads();
-  for (u32 run = 2; run <= size; run *= 2)
-    for (u32 gap = run / 2; gap > 0; gap /= 2) {
-      for (u32 i = tid; i < size / 2; i += 256) {
-        const u32 lo = i / gap * 2 * gap + i % gap, hi = lo + gap;
-        const u64 x = found[lo], y = found[hi];
-        if ((x > y) == ((lo & run) == 0)) found[lo] = y, found[hi] = x;
-      }
-      __syncthreads();
-    }
-  for (u32 i = tid; i < a.k; i += 256) {
-    const u64 at = qrow * a.k + i;
-    if (i < count) {
-      const float s = key_float(~(u32)(found[i] >> 32));
-      a.ids[at] = (u32)found[i];
-      a.dists[at] = a.norms ? __builtin_fmaxf(0.0f, __builtin_fmaf(-2.0f, s, a.qnorms[qrow])) : 0.0f - s;
-    } else {
-      a.ids[at] = ANN_NONE;
-      a.dists[at] = __builtin_inff();
-    }
   }
 }
 
-u64 search_queries_at_once(u64 groups, u64 nq) {
-  u64 most = SEARCH_SCRATCH_FLOATS / groups / 64 * 64;
+__global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
+  extern __shared__ u64 found[];  // as many as the rows of k groups, up to a power of two for the sort
+  __shared__ PickLds s;
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const u32 q = blockIdx.x;
+  const float* most = a.most + (u64)q * a.pitch;
+  const u32 least = float_key(-__builtin_inff());  // keys up to this one are of groups without a score
+
+  u32 mine = least;
+  const u32 fours = a.groups / 4;
+  for (u32 i = tid; i < fours; i += PICK_THREADS) {
+    const v4f v = *reinterpret_cast<const v4f*>(most + 4 * i);
+    mine = max(mine, float_key(most_of(-__builtin_inff(), v)));
+  }
+  if (tid < a.groups % 4) mine = max(mine, float_key(most[4 * fours + tid]));
+  s.hist[tid] = mine;
+  if (tid == 0) s.count = 0;
+  __syncthreads();
+  u32 before = 0;
+  for (u32 i = 0; i < PICK_THREADS; ++i) before += s.hist[i] > mine || (s.hist[i] == mine && i < tid);
+  if (before == a.k - 1) s.bound = max(mine, least + 1);
+  __syncthreads();
+  const u32 bound = s.bound;
+  auto take = [&](u32 i, float v) {
+    const u32 key = float_key(v);
+    if (key < bound) return;
+    const u32 at = atomicAdd(&s.count, 1u);
+    if (at < PICK_FEW) found[at] = (u64)~key << 32 | i;
+  };
+  for (u32 i = tid; i < fours; i += PICK_THREADS) {
+    const v4f v = *reinterpret_cast<const v4f*>(most + 4 * i);
+    if (float_key(most_of(-__builtin_inff(), v)) >= bound)
+#pragma unroll
+      for (u32 e = 0; e < 4; ++e) take(4 * i + e, v[e]);
+  }
+  if (tid < a.groups % 4) take(4 * fours + tid, most[4 * fours + tid]);
+  __syncthreads();
+  const u32 reached = s.count;
+  __syncthreads();
+  if (reached <= PICK_FEW) {
+    for (u32 c = tid; c < reached; c += PICK_THREADS) {
+      const u64 key = found[c];
+      u32 rank = 0;
+      for (u32 i = 0; i < reached; ++i) rank += found[i] < key;
+      if (rank < a.k) s.chosen[rank] = (u32)key;
+      if (rank == a.k - 1) s.bound = ~(u32)(key >> 32);
+    }
+    if (tid == 0) s.count = min(reached, a.k);
+    __syncthreads();
+  } else {
+    choose_groups(a, most, least, s);
+  }
+  const u32 nchosen = s.count;
+  // k groups: k points reach the smallest of their maxima, and no other point matters
+  const u32 low = nchosen == a.k ? max(s.bound, least + 1) : least + 1;
+  __syncthreads();
+  if (tid == 0) s.count = 0;
+  __syncthreads();
+  const u64 qrow = (u64)a.q0 + q;
+  for (u32 c = wave; c < nchosen; c += PICK_THREADS / 64) {
+    const u64 w0 = (u64)s.chosen[c] * SEARCH_GROUP;
+    v4f acc[4];
+    u64 row[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      row[i] = min(w0 + 16 * i + lane % 16, (u64)a.w.n - 1);
+      acc[i] = first_sums(a, w0 + 16 * i + lane / 16 * 4);
+    }
+    for (u32 st = 0; st < a.w.steps; ++st) {
+      const v4i x = load_codes(a.q, qrow, st);
+      const int xs = load_scale(a.q, qrow, st);
+      v4i w[4];
+      int ws[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = load_codes(a.w, row[i], st), ws[i] = load_scale(a.w, row[i], st);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = mx_mfma(w[i], x, acc[i], ws[i], xs);
+    }
+    // (all columns are this query's: one of them is used)
+    if (lane % 16 == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const u64 id = w0 + 16 * i + lane / 16 * 4 + r;
+          const u32 key = float_key(acc[i][r]);
+          if (id < a.w.n && key >= low) found[atomicAdd(&s.count, 1u)] = (u64)~key << 32 | id;
+        }
+  }
+  __syncthreads();
+  const u32 count = s.count;
+  auto put = [&](u32 at, u64 key) {
+    const u64 to = qrow * a.k + at;
+    const float score = key_float(~(u32)(key >> 32));
+    a.ids[to] = (u32)key;
+    a.dists[to] = a.norms ? __builtin_fmaxf(0.0f, __builtin_fmaf(-2.0f, score, a.qnorms[qrow])) : 0.0f - score;
+  };
+  if (count <= PICK_FEW) {
+    for (u32 c = tid; c < count; c += PICK_THREADS) {
+      const u64 key = found[c];
+      u32 rank = 0;
+      for (u32 i = 0; i < count; ++i) rank += found[i] < key;
+      if (rank < a.k) put(rank, key);
+    }
+  } else {
+    u32 size = 2;
+    while (size < count) size *= 2;
+    for (u32 i = count + tid; i < size; i += PICK_THREADS) found[i] = ~0ull;
+    __syncthreads();
+    for (u32 run = 2; run <= size; run *= 2)
+      for (u32 gap = run / 2; gap > 0; gap /= 2) {
+        for (u32 i = tid; i < size / 2; i += PICK_THREADS) {
+          const u32 lo = i / gap * 2 * gap + i % gap, hi = lo + gap;
+          const u64 x = found[lo], y = found[hi];
+          if ((x > y) == ((lo & run) == 0)) found[lo] = y, found[hi] = x;
+        }
+        __syncthreads();
+      }
+    for (u32 i = tid; i < a.k; i += PICK_THREADS) put(i, found[i]);
+  }
+  for (u32 i = count + tid; i < a.k; i += PICK_THREADS) {
+    a.ids[qrow * a.k + i] = ANN_NONE;
+    a.dists[qrow * a.k + i] = __builtin_inff();
+  }
+}
+
+template <int STEPS>
+hipError_t launch_groups(const MxSearchArgs& a, hipStream_t s) {
+  if (a.nq <= 64) {
+    const u32 blocks = (a.groups + 3) / 4;
+    const dim3 grid(blocks < 1024 ? blocks : 1024);
+    if (a.nq <= 16)
+      hipLaunchKernelGGL((mx_group_few_kernel<STEPS, 1>), grid, dim3(256), 0, s, a);
+    else if (a.nq <= 32)
+      hipLaunchKernelGGL((mx_group_few_kernel<STEPS, 2>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((mx_group_few_kernel<STEPS, 4>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  constexpr int QF = STEPS <= 2 ? 8 : 4;
+  constexpr u32 GS = stage_groups<STEPS>(), ROWS = GS * SEARCH_GROUP;
+  constexpr u32 lds = 2 * (ROWS * STEPS * MX_STEP_BYTES + ROWS * 4 * 4 + ROWS * 4);
+  // waves that hold the same queries, where there are too few for all eight
+  const bool shared = a.nq <= 16 * QF * 8 / GS;
+  const u32 per = 16 * QF * 8 / (shared ? GS : 1), blocks_q = (a.nq + per - 1) / per;
+  const u32 total = (a.groups + GS - 1) / GS;
+  // one workgroup for each compute unit, as near as whole ranges come to it
+  u32 ranges = blocks_q >= 256 ? 1 : (256 + blocks_q / 2) / blocks_q;
+  if (ranges > total) ranges = total;
+  const auto kernel = shared ? mx_group_many_kernel<STEPS, QF, GS> : mx_group_many_kernel<STEPS, QF, 1>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((blocks_q * ranges + 7) / 8 * 8), dim3(SEARCH_THREADS), lds, s, a, blocks_q, ranges);
+  return hipGetLastError();
+}
+
+constexpr u64 search_pitch(u64 n) { return (n + 4 * SEARCH_GROUP - 1) / (4 * SEARCH_GROUP) * 4; }  // whole stages of groups
+
+u64 search_queries_at_once(u64 pitch, u64 nq) {
+  u64 most = SEARCH_SCRATCH_FLOATS / pitch / 64 * 64;
   if (most < 64) most = 64;
   if (most > SEARCH_MOST_AT_ONCE) most = SEARCH_MOST_AT_ONCE;
   return nq < most ? nq : most;
@@ -201,8 +511,8 @@ int check_search(u64 n, u32 d, u64 nq, u32 k) {
 }
 
 u64 search_scratch(u64 n, u64 nq) {
-  const u64 groups = (n + SEARCH_GROUP - 1) / SEARCH_GROUP;
-  return groups == 0 ? 0 : (search_queries_at_once(groups, nq) * groups * 4 + 15) / 16 * 16;
+  const u64 pitch = search_pitch(n);
+  return pitch == 0 ? 0 : search_queries_at_once(pitch, nq) * pitch * 4;
 }
 
 __global__ void mx_none_kernel(u32* ids, float* dists, u64 count) {
@@ -265,17 +575,28 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
   a.most = static_cast<float*>(scratch_dev);
   a.ids = ids_dev;
   a.dists = dists_dev;
-  const u64 part = search_queries_at_once(a.groups, nq);
-  size_t room = 2;
+  a.pitch = (u32)search_pitch(n);
+  const u64 part = search_queries_at_once(a.pitch, nq);
+  size_t room = PICK_FEW;
   while (room < (size_t)(k < a.groups ? k : a.groups) * SEARCH_GROUP) room *= 2;
   room *= 8;
   HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(mx_pick_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room));
   for (u64 q0 = 0; q0 < nq; q0 += part) {
     a.q0 = (u32)q0;
     a.nq = (u32)(nq - q0 < part ? nq - q0 : part);
-    const u64 tiles = a.groups * (((u64)a.nq + 63) / 64);
-    hipLaunchKernelGGL(mx_group_most_kernel, dim3((u32)((tiles + 3) / 4)), dim3(256), 0, st, a, tiles);
-    HIP_TRY(hipGetLastError());
+    if (a.w.steps == 1) {
+      HIP_TRY(launch_groups<1>(a, st));
+    } else if (a.w.steps == 2) {
+      HIP_TRY(launch_groups<2>(a, st));
+    } else if (a.w.steps == 3) {
+      HIP_TRY(launch_groups<3>(a, st));
+    } else if (a.w.steps == 4) {
+      HIP_TRY(launch_groups<4>(a, st));
+    } else {
+      const u64 tiles = a.groups * (((u64)a.nq + 63) / 64);
+      hipLaunchKernelGGL(mx_group_long_kernel, dim3((u32)((tiles + 3) / 4)), dim3(256), 0, st, a, tiles);
+      HIP_TRY(hipGetLastError());
+    }
     hipLaunchKernelGGL(mx_pick_kernel, dim3(a.nq), dim3(256), room, st, a);
     HIP_TRY(hipGetLastError());
   }

@@ -224,6 +224,33 @@ def test_search(env, n, d, nq, k, dtype, l2):
 
 
 @pytest.mark.parametrize("l2", (True, False))
+@pytest.mark.parametrize("nq", (17, 33, 65, 200, 300, 600, 1100))
+@pytest.mark.parametrize("n,d", [(700, 100), (2049, 130), (1500, 300), (3000, 450), (900, 600)])
+def test_search_of_larger_batches(env, n, d, nq, l2):
+    """Every way that rows and queries are dealt to waves."""
+    torch, A, _ = env
+    rng = np.random.default_rng(n + d + nq)
+    rows = A.ann_mx_quantize(rows_of(torch, rng, n, d, "int8")[0], norms=True)
+    queries = A.ann_mx_quantize(rows_of(torch, rng, nq, d, "int8")[0], norms=True)
+    check_search(A, torch, rows, queries, 10, l2)
+
+
+@pytest.mark.parametrize("l2", (True, False))
+@pytest.mark.parametrize("nq", (3, 100, 700))
+def test_search_equal_rows(env, nq, l2):
+    """All rows equal: the first k ids; and only every other row with a distance."""
+    torch, A, _ = env
+    x = torch.ones((70_000, 100), device="cuda:0")
+    queries = A.ann_mx_quantize(torch.ones((nq, 100), device="cuda:0"), norms=True)
+    for k in (1, 10, 100):
+        ids, dists = A.ann_mx_search(A.ann_mx_quantize(x, norms=True), queries, k, metric=A.L2SQ if l2 else A.MIPS)
+        assert (ids.cpu() == torch.arange(k, dtype=torch.int32)).all() and (dists == (0.0 if l2 else -100.0)).all()
+    x[::2, 40] = float("inf")
+    ids, _ = A.ann_mx_search(A.ann_mx_quantize(x, norms=True), queries, 50, metric=A.L2SQ if l2 else A.MIPS)
+    assert (ids.cpu() == torch.arange(1, 101, 2, dtype=torch.int32)).all()
+
+
+@pytest.mark.parametrize("l2", (True, False))
 def test_search_ties_and_rows_without_a_distance(env, l2):
     torch, A, _ = env
     rng = np.random.default_rng(1)
