@@ -41,7 +41,7 @@ __device__ __forceinline__ v4f first_sums(const MxSearchArgs& a, u64 row0) {
 }
 
 __device__ __forceinline__ float most_of(float m, v4f v) {
-  return __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(m, v[0]), v[1]), __builtin_fmaxf(v[2], v[3]));
+  return __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(m, v[0]), v[1]), v[2]), v[3]);
 }
 
 // The maxima of four columns groups over the four lanes that share a column: lane l gets the one of group
@@ -484,8 +484,13 @@ hipError_t launch_groups(const MxSearchArgs& a, hipStream_t s) {
   const bool shared = a.nq <= 16 * QF * 8 / GS;
   const u32 per = 16 * QF * 8 / (shared ? GS : 1), blocks_q = (a.nq + per - 1) / per;
   const u32 total = (a.groups + GS - 1) / GS;
-  // one workgroup for each compute unit, as near as whole ranges come to it
-  u32 ranges = blocks_q >= 256 ? 1 : (256 + blocks_q / 2) / blocks_q;
+  // A compute unit holds one workgroup: as many ranges as make whole turns of 256 workgroups, or nearly.  (260 of them
+  // take twice as long as 250.)
+  u32 ranges = blocks_q < 256 ? 256 / blocks_q : 1;
+  for (u32 r = ranges, best = 0; r <= total && r <= 8 * ranges && best < 95; ++r) {
+    const u64 groups_of = (u64)blocks_q * r, full = 100 * groups_of / ((groups_of + 255) / 256 * 256);
+    if (full > best) best = (u32)full, ranges = r;
+  }
   if (ranges > total) ranges = total;
   const auto kernel = shared ? mx_group_many_kernel<STEPS, QF, GS> : mx_group_many_kernel<STEPS, QF, 1>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
