@@ -21,6 +21,8 @@ struct MxSearchArgs {
   u32 q0, nq;           // the queries of this launch
   u32 groups, pitch, k; // pitch: floats from one query's maxima to the next's
   float* most;          // (nq, pitch)
+  float* coarse;        // (nq, coarse_pitch): the largest of every `per_coarse` of them, or null
+  u32 coarse_pitch, per_coarse;
   u32* ids;
   float* dists;
 };
@@ -32,12 +34,21 @@ __device__ __forceinline__ int load_scale(const MxRows& m, u64 row, u32 step) {
   return m.scales[(row * m.steps + step) * MX_STEP_SCALES + threadIdx.x % 64 / 16];
 }
 
-// what the sum of a row starts from: 0, or - |x|^2 / 2, and -inf past the last row, which no maximum takes
-__device__ __forceinline__ float first_sum(const MxSearchArgs& a, u64 row) {
-  return row >= a.w.n ? -__builtin_inff() : a.norms ? -0.5f * a.norms[row] : 0.0f;
+// What the sum of a row starts from: 0, or - |x|^2 / 2, and -inf past the last row, which no maximum takes.  Without
+// norms something else of at least that size is read and not used, so that no branch waits for the load.
+__device__ __forceinline__ float load_norm(const MxSearchArgs& a, u64 row) {
+  const float* from = a.norms ? a.norms : reinterpret_cast<const float*>(a.w.scales);
+  return from[min(row, (u64)a.w.n - 1)];
 }
-__device__ __forceinline__ v4f first_sums(const MxSearchArgs& a, u64 row0) {
-  return v4f{first_sum(a, row0), first_sum(a, row0 + 1), first_sum(a, row0 + 2), first_sum(a, row0 + 3)};
+__device__ __forceinline__ float first_sum(const MxSearchArgs& a, u64 row, float norm) {
+  return row >= a.w.n ? -__builtin_inff() : a.norms ? -0.5f * norm : 0.0f;
+}
+// of four rows from row0 + 4 (lane / 16) on, from the lanes that hold the norms of row0 + lane % 16
+__device__ __forceinline__ v4f first_sums(const MxSearchArgs& a, u64 row0, float norm) {
+  const u32 lane = threadIdx.x % 64;
+  const float mine = first_sum(a, row0 + lane % 16, norm);
+  const int from = (int)(lane / 16 * 4);
+  return v4f{__shfl(mine, from), __shfl(mine, from + 1), __shfl(mine, from + 2), __shfl(mine, from + 3)};
 }
 
 __device__ __forceinline__ float most_of(float m, v4f v) {
@@ -102,7 +113,7 @@ __global__ __launch_bounds__(256) void mx_group_few_kernel(MxSearchArgs a) {
   struct Ahead {
     v4i w[4][STEPS];
     u32 b[4][STEPS];
-    v4f first[4];
+    float norm[4];
   } next;
   auto ask = [&](u32 group) {
 #pragma unroll
@@ -114,7 +125,7 @@ __global__ __launch_bounds__(256) void mx_group_few_kernel(MxSearchArgs a) {
         next.w[i][s] = load_codes(a.w, row, s);
         next.b[i][s] = reinterpret_cast<const u32*>(a.w.scales)[row * a.w.steps + s];
       }
-      next.first[i] = first_sums(a, row0 + lane / 16 * 4);
+      next.norm[i] = load_norm(a, row);
     }
   };
   if (g < a.groups) ask(g);
@@ -128,7 +139,7 @@ __global__ __launch_bounds__(256) void mx_group_few_kernel(MxSearchArgs a) {
 #pragma unroll
       for (int s = 0; s < STEPS; ++s) scales |= (now.b[i][s] >> (lane / 16 * 8) & 255) << (8 * s);
       v4f acc[QF];
-      score_tile<STEPS, QF>(now.w[i], (int)scales, q, now.first[i], acc);
+      score_tile<STEPS, QF>(now.w[i], (int)scales, q, first_sums(a, (u64)g * SEARCH_GROUP + 16 * i, now.norm[i]), acc);
 #pragma unroll
       for (int j = 0; j < QF; ++j) m[j] = most_of(m[j], acc[j]);
     }
@@ -172,7 +183,8 @@ __global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchA
 
   v4i next_w[LOADS];
   u32 next_scale[SCALES];
-  float next_first = 0.0f;
+  float next_norm = 0.0f;
+  u64 next_row = 0;
   auto fetch = [&](u32 stage) {
     const u64 row0 = (u64)stage * ROWS;
 #pragma unroll
@@ -185,7 +197,8 @@ __global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchA
       const u32 at = min(i * SEARCH_THREADS + tid, ROWS * STEPS - 1);
       next_scale[i] = reinterpret_cast<const u32*>(a.w.scales)[min(row0 * STEPS + at, (u64)a.w.n * STEPS - 1)];
     }
-    next_first = first_sum(a, row0 + tid % ROWS);
+    next_row = row0 + tid % ROWS;
+    next_norm = load_norm(a, next_row);
   };
   auto keep = [&](Stage& to) {
 #pragma unroll
@@ -197,7 +210,7 @@ __global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchA
 #pragma unroll
         for (u32 g = 0; g < 4; ++g) reinterpret_cast<uint8_t*>(&to.scales[r / 16][g * 16 + r % 16])[s] = (uint8_t)(next_scale[i] >> (8 * g));
     }
-    if (tid < ROWS) to.first[tid] = next_first;
+    if (tid < ROWS) to.first[tid] = first_sum(a, next_row, next_norm);
   };
   fetch(s0);
   keep(stages[s0 % 2]);
@@ -234,6 +247,12 @@ __global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchA
       const u64 x = x0 + 64 * j + joined_group(lane) * 16 + lane % 16;
       if (x >= a.nq) continue;
       float* to = a.most + x * a.pitch + (u64)st * GS;  // (the pitch has room for a whole last stage)
+      if constexpr (WR == 1) {
+        float m = joined[0][j];
+#pragma unroll
+        for (u32 n = 1; n < GS; ++n) m = __builtin_fmaxf(m, joined[n][j]);
+        a.coarse[x * a.coarse_pitch + st] = m;
+      }
       if constexpr (WR == 1 && GS == 4)
         *reinterpret_cast<v4f*>(to) = v4f{joined[0][j], joined[1][j], joined[2][j], joined[3][j]};
       else
@@ -253,7 +272,7 @@ __global__ __launch_bounds__(256) void mx_group_long_kernel(MxSearchArgs a, u64 
   v4f acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const v4f c = first_sums(a, w0 + 16 * i + lane / 16 * 4);
+    const v4f c = first_sums(a, w0 + 16 * i, load_norm(a, w0 + 16 * i + lane % 16));
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = c;
   }
@@ -296,15 +315,16 @@ struct PickLds {
   u32 prefix, left, count, bound, scan[PICK_THREADS / 64];
 };
 
-// All groups' keys, by a radix selection of the k-th largest: where too many reach the bound (equal maxima).
-__device__ void choose_groups(const MxSearchArgs& a, const float* most, u32 least, PickLds& s) {
+// The first k of `count` maxima by (size downwards, place), by a radix selection of the k-th largest key: where too
+// many reach the bound below (equal maxima).
+__device__ void choose_equal(const float* most, u32 count, u32 k, u32 least, PickLds& s) {
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  if (tid == 0) s.prefix = 0, s.left = min(a.k, a.groups), s.count = 0;
+  if (tid == 0) s.prefix = 0, s.left = min(k, count), s.count = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
     s.hist[tid] = 0;
     __syncthreads();
     const u32 prefix = s.prefix;
-    for (u32 i = tid; i < a.groups; i += PICK_THREADS) {
+    for (u32 i = tid; i < count; i += PICK_THREADS) {
       const u32 key = float_key(most[i]);
       if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&s.hist[key >> shift & 255], 1u);
     }
@@ -317,78 +337,122 @@ __device__ void choose_groups(const MxSearchArgs& a, const float* most, u32 leas
     }
     __syncthreads();
   }
-  const u32 cut = s.prefix, ties = s.left;  // groups above the cut, and the first `ties` of those at it
+  const u32 cut = s.prefix, ties = s.left;  // maxima above the cut, and the first `ties` of those at it
   __syncthreads();
   if (tid == 0) s.left = 0, s.bound = cut;
   __syncthreads();
-  // in the order of groups, so that the ties taken are the first ones
-  for (u32 i0 = 0; i0 < a.groups; i0 += PICK_THREADS) {
+  // in the order of places, so that the ties taken are the first ones
+  for (u32 i0 = 0; i0 < count; i0 += PICK_THREADS) {
     const u32 i = i0 + tid;
-    const u32 key = i < a.groups ? float_key(most[i]) : 0u;
+    const u32 key = i < count ? float_key(most[i]) : 0u;
     const bool tie = key == cut && key > least;
     const u64 votes = __ballot(tie);
     if (lane == 0) s.scan[wave] = (u32)__popcll(votes);
     __syncthreads();
     u32 before = s.left + (u32)__popcll(votes & ((1ull << lane) - 1));
     for (u32 w = 0; w < wave; ++w) before += s.scan[w];
-    if (i < a.groups && ((key > cut && key > least) || (tie && before < ties))) s.chosen[atomicAdd(&s.count, 1u)] = i;
+    if (i < count && ((key > cut && key > least) || (tie && before < ties))) s.chosen[atomicAdd(&s.count, 1u)] = i;
     __syncthreads();
     if (tid == 0) s.left += s.scan[0] + s.scan[1] + s.scan[2] + s.scan[3];
     __syncthreads();
   }
 }
 
+// found[0 .. count): keys and places; the first k of them into s.chosen, the k-th key into s.bound
+__device__ __forceinline__ void choose_ranked(const u64* found, u32 count, u32 k, PickLds& s) {
+  for (u32 c = threadIdx.x; c < count; c += PICK_THREADS) {
+    const u64 key = found[c];
+    u32 rank = 0;
+    for (u32 i = 0; i < count; ++i) rank += found[i] < key;
+    if (rank < k) s.chosen[rank] = (u32)key;
+    if (rank == k - 1) s.bound = ~(u32)(key >> 32);
+  }
+  if (threadIdx.x == 0) s.count = min(count, k);
+  __syncthreads();
+}
+
+// The first k of `count` maxima (16-byte aligned) by (size downwards, place): s.count of them in s.chosen; where that
+// is k, s.bound is the last one's key.
+__device__ void choose(const float* most, u32 count, u32 k, u32 least, u64* found, PickLds& s) {
+  constexpr u32 AHEAD = 8;
+  const u32 tid = threadIdx.x, fours = (count + 3) / 4;
+  const v4f* all = reinterpret_cast<const v4f*>(most);
+  v4f x[AHEAD];
+  auto ask = [&](u32 at) {
+#pragma unroll
+    for (u32 u = 0; u < AHEAD; ++u) x[u] = all[min(at + u * PICK_THREADS + tid, fours - 1)];
+  };
+  // (the places past the last are none; a maximum read twice does no harm)
+  auto value = [&](u32 at, u32 u, u32 e) { return (at + u * PICK_THREADS + tid) * 4 + e < count ? x[u][e] : -__builtin_inff(); };
+  float m = -__builtin_inff();
+  for (u32 at = 0; at < fours; at += AHEAD * PICK_THREADS) {
+    ask(at);
+#pragma unroll
+    for (u32 u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (u32 e = 0; e < 4; ++e) m = __builtin_fmaxf(m, value(at, u, e));
+  }
+  const u32 mine = float_key(m);
+  s.hist[tid] = mine;
+  if (tid == 0) s.count = 0;
+  __syncthreads();
+  u32 before = 0;
+#pragma unroll 4
+  for (u32 i = 0; i < PICK_THREADS; i += 4) {
+    using v4u = u32 __attribute__((ext_vector_type(4)));
+    const v4u h = *reinterpret_cast<const v4u*>(&s.hist[i]);
+#pragma unroll
+    for (u32 e = 0; e < 4; ++e) before += h[e] > mine || (h[e] == mine && i + e < tid);
+  }
+  if (before == k - 1) s.bound = max(mine, least + 1);
+  __syncthreads();
+  const u32 bound = s.bound;
+  const float at_least = key_float(bound);
+  for (u32 at = 0; at < fours; at += AHEAD * PICK_THREADS) {
+    if (fours > AHEAD * PICK_THREADS) ask(at);  // (else they are all here)
+#pragma unroll
+    for (u32 u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (u32 e = 0; e < 4; ++e)
+        if (value(at, u, e) >= at_least) {
+          const u32 to = atomicAdd(&s.count, 1u);
+          if (to < PICK_FEW) found[to] = (u64)~float_key(x[u][e]) << 32 | ((at + u * PICK_THREADS + tid) * 4 + e);
+        }
+  }
+  __syncthreads();
+  const u32 reached = s.count;
+  __syncthreads();
+  if (reached <= PICK_FEW)
+    choose_ranked(found, reached, k, s);
+  else
+    choose_equal(most, count, k, least, s);
+}
+
 __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
   extern __shared__ u64 found[];  // as many as the rows of k groups, up to a power of two for the sort
-  __shared__ PickLds s;
+  __shared__ __align__(16) PickLds s;
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const u32 q = blockIdx.x;
   const float* most = a.most + (u64)q * a.pitch;
   const u32 least = float_key(-__builtin_inff());  // keys up to this one are of groups without a score
 
-  u32 mine = least;
-  const u32 fours = a.groups / 4;
-  for (u32 i = tid; i < fours; i += PICK_THREADS) {
-    const v4f v = *reinterpret_cast<const v4f*>(most + 4 * i);
-    mine = max(mine, float_key(most_of(-__builtin_inff(), v)));
-  }
-  if (tid < a.groups % 4) mine = max(mine, float_key(most[4 * fours + tid]));
-  s.hist[tid] = mine;
-  if (tid == 0) s.count = 0;
-  __syncthreads();
-  u32 before = 0;
-  for (u32 i = 0; i < PICK_THREADS; ++i) before += s.hist[i] > mine || (s.hist[i] == mine && i < tid);
-  if (before == a.k - 1) s.bound = max(mine, least + 1);
-  __syncthreads();
-  const u32 bound = s.bound;
-  auto take = [&](u32 i, float v) {
-    const u32 key = float_key(v);
-    if (key < bound) return;
-    const u32 at = atomicAdd(&s.count, 1u);
-    if (at < PICK_FEW) found[at] = (u64)~key << 32 | i;
-  };
-  for (u32 i = tid; i < fours; i += PICK_THREADS) {
-    const v4f v = *reinterpret_cast<const v4f*>(most + 4 * i);
-    if (float_key(most_of(-__builtin_inff(), v)) >= bound)
-#pragma unroll
-      for (u32 e = 0; e < 4; ++e) take(4 * i + e, v[e]);
-  }
-  if (tid < a.groups % 4) take(4 * fours + tid, most[4 * fours + tid]);
-  __syncthreads();
-  const u32 reached = s.count;
-  __syncthreads();
-  if (reached <= PICK_FEW) {
-    for (u32 c = tid; c < reached; c += PICK_THREADS) {
-      const u64 key = found[c];
-      u32 rank = 0;
-      for (u32 i = 0; i < reached; ++i) rank += found[i] < key;
-      if (rank < a.k) s.chosen[rank] = (u32)key;
-      if (rank == a.k - 1) s.bound = ~(u32)(key >> 32);
-    }
-    if (tid == 0) s.count = min(reached, a.k);
+  if (a.coarse) {  // the first k groups are in the first k groups of groups
+    choose(a.coarse + (u64)q * a.coarse_pitch, (a.groups + a.per_coarse - 1) / a.per_coarse, a.k, least, found, s);
+    const u32 parts = s.count * a.per_coarse;
     __syncthreads();
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    for (u32 i = tid; i < parts; i += PICK_THREADS) {
+      const u32 g = s.chosen[i / a.per_coarse] * a.per_coarse + i % a.per_coarse;
+      const u32 key = g < a.groups ? float_key(most[g]) : 0u;
+      if (key > least) found[atomicAdd(&s.count, 1u)] = (u64)~key << 32 | g;
+    }
+    __syncthreads();
+    const u32 reached = s.count;
+    __syncthreads();
+    choose_ranked(found, reached, a.k, s);
   } else {
-    choose_groups(a, most, least, s);
+    choose(most, a.groups, a.k, least, found, s);
   }
   const u32 nchosen = s.count;
   // k groups: k points reach the smallest of their maxima, and no other point matters
@@ -404,7 +468,7 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       row[i] = min(w0 + 16 * i + lane % 16, (u64)a.w.n - 1);
-      acc[i] = first_sums(a, w0 + 16 * i + lane / 16 * 4);
+      acc[i] = first_sums(a, w0 + 16 * i, load_norm(a, w0 + 16 * i + lane % 16));
     }
     for (u32 st = 0; st < a.w.steps; ++st) {
       const v4i x = load_codes(a.q, qrow, st);
@@ -465,8 +529,9 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
 }
 
 template <int STEPS>
-hipError_t launch_groups(const MxSearchArgs& a, hipStream_t s) {
+hipError_t launch_groups(MxSearchArgs& a, hipStream_t s) {
   if (a.nq <= 64) {
+    a.coarse = nullptr;
     const u32 blocks = (a.groups + 3) / 4;
     const dim3 grid(blocks < 1024 ? blocks : 1024);
     if (a.nq <= 16)
@@ -495,11 +560,16 @@ hipError_t launch_groups(const MxSearchArgs& a, hipStream_t s) {
   const auto kernel = shared ? mx_group_many_kernel<STEPS, QF, GS> : mx_group_many_kernel<STEPS, QF, 1>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
+  if (shared) a.coarse = nullptr;
+  a.per_coarse = GS;
   hipLaunchKernelGGL(kernel, dim3((blocks_q * ranges + 7) / 8 * 8), dim3(SEARCH_THREADS), lds, s, a, blocks_q, ranges);
   return hipGetLastError();
 }
 
 constexpr u64 search_pitch(u64 n) { return (n + 4 * SEARCH_GROUP - 1) / (4 * SEARCH_GROUP) * 4; }  // whole stages of groups
+
+// the largest of the maxima of a stage, kept apart by launches of many queries (a stage has two groups at least)
+constexpr u64 search_coarse_pitch(u64 n) { return (search_pitch(n) / 2 + 3) / 4 * 4; }
 
 u64 search_queries_at_once(u64 pitch, u64 nq) {
   u64 most = SEARCH_SCRATCH_FLOATS / pitch / 64 * 64;
@@ -517,7 +587,7 @@ int check_search(u64 n, u32 d, u64 nq, u32 k) {
 
 u64 search_scratch(u64 n, u64 nq) {
   const u64 pitch = search_pitch(n);
-  return pitch == 0 ? 0 : search_queries_at_once(pitch, nq) * pitch * 4;
+  return pitch == 0 ? 0 : search_queries_at_once(pitch, nq) * (pitch + search_coarse_pitch(n)) * 4;
 }
 
 __global__ void mx_none_kernel(u32* ids, float* dists, u64 count) {
@@ -582,13 +652,15 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
   a.dists = dists_dev;
   a.pitch = (u32)search_pitch(n);
   const u64 part = search_queries_at_once(a.pitch, nq);
-  size_t room = PICK_FEW;
+  size_t room = PICK_FEW;  // (four groups of each of the first k groups of groups as well)
   while (room < (size_t)(k < a.groups ? k : a.groups) * SEARCH_GROUP) room *= 2;
   room *= 8;
   HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(mx_pick_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room));
   for (u64 q0 = 0; q0 < nq; q0 += part) {
     a.q0 = (u32)q0;
     a.nq = (u32)(nq - q0 < part ? nq - q0 : part);
+    a.coarse = a.most + part * a.pitch;
+    a.coarse_pitch = (u32)search_coarse_pitch(n);
     if (a.w.steps == 1) {
       HIP_TRY(launch_groups<1>(a, st));
     } else if (a.w.steps == 2) {
@@ -599,6 +671,7 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
       HIP_TRY(launch_groups<4>(a, st));
     } else {
       const u64 tiles = a.groups * (((u64)a.nq + 63) / 64);
+      a.coarse = nullptr;
       hipLaunchKernelGGL(mx_group_long_kernel, dim3((u32)((tiles + 3) / 4)), dim3(256), 0, st, a, tiles);
       HIP_TRY(hipGetLastError());
     }
