@@ -306,25 +306,26 @@ __global__ __launch_bounds__(256) void mx_group_long_kernel(MxSearchArgs a, u64 
 
 // A workgroup per query.  The k-th largest of its threads' maxima over the groups is a bound that k groups at least
 // reach; the few that do are ranked, the first k scored again, and the k best points ranked.
-constexpr u32 PICK_THREADS = 256;
+constexpr u32 PICK_BOUNDS = 256;  // maxima, of one or four threads each, of which the k-th largest is the bound
 constexpr u32 PICK_FEW = 512;  // candidates that are ranked by counting the ones before each
 
 struct PickLds {
-  u32 hist[PICK_THREADS];
+  u32 hist[PICK_BOUNDS];
   u32 chosen[SEARCH_MOST_K];
-  u32 prefix, left, count, bound, scan[PICK_THREADS / 64];
+  u32 prefix, left, count, bound, scan[16];
 };
 
 // The first k of `count` maxima by (size downwards, place), by a radix selection of the k-th largest key: where too
 // many reach the bound below (equal maxima).
+template <u32 THREADS>
 __device__ void choose_equal(const float* most, u32 count, u32 k, u32 least, PickLds& s) {
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   if (tid == 0) s.prefix = 0, s.left = min(k, count), s.count = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    s.hist[tid] = 0;
+    if (tid < 256) s.hist[tid] = 0;
     __syncthreads();
     const u32 prefix = s.prefix;
-    for (u32 i = tid; i < count; i += PICK_THREADS) {
+    for (u32 i = tid; i < count; i += THREADS) {
       const u32 key = float_key(most[i]);
       if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&s.hist[key >> shift & 255], 1u);
     }
@@ -342,7 +343,7 @@ __device__ void choose_equal(const float* most, u32 count, u32 k, u32 least, Pic
   if (tid == 0) s.left = 0, s.bound = cut;
   __syncthreads();
   // in the order of places, so that the ties taken are the first ones
-  for (u32 i0 = 0; i0 < count; i0 += PICK_THREADS) {
+  for (u32 i0 = 0; i0 < count; i0 += THREADS) {
     const u32 i = i0 + tid;
     const u32 key = i < count ? float_key(most[i]) : 0u;
     const bool tie = key == cut && key > least;
@@ -353,14 +354,16 @@ __device__ void choose_equal(const float* most, u32 count, u32 k, u32 least, Pic
     for (u32 w = 0; w < wave; ++w) before += s.scan[w];
     if (i < count && ((key > cut && key > least) || (tie && before < ties))) s.chosen[atomicAdd(&s.count, 1u)] = i;
     __syncthreads();
-    if (tid == 0) s.left += s.scan[0] + s.scan[1] + s.scan[2] + s.scan[3];
+    if (tid == 0)
+      for (u32 w = 0; w < THREADS / 64; ++w) s.left += s.scan[w];
     __syncthreads();
   }
 }
 
 // found[0 .. count): keys and places; the first k of them into s.chosen, the k-th key into s.bound
+template <u32 THREADS>
 __device__ __forceinline__ void choose_ranked(const u64* found, u32 count, u32 k, PickLds& s) {
-  for (u32 c = threadIdx.x; c < count; c += PICK_THREADS) {
+  for (u32 c = threadIdx.x; c < count; c += THREADS) {
     const u64 key = found[c];
     u32 rank = 0;
     for (u32 i = 0; i < count; ++i) rank += found[i] < key;
@@ -373,62 +376,69 @@ __device__ __forceinline__ void choose_ranked(const u64* found, u32 count, u32 k
 
 // The first k of `count` maxima (16-byte aligned) by (size downwards, place): s.count of them in s.chosen; where that
 // is k, s.bound is the last one's key.
+template <u32 THREADS>
 __device__ void choose(const float* most, u32 count, u32 k, u32 least, u64* found, PickLds& s) {
-  constexpr u32 AHEAD = 8;
+  constexpr u32 AHEAD = THREADS == 256 ? 8 : 4, SHARE = THREADS / PICK_BOUNDS;
   const u32 tid = threadIdx.x, fours = (count + 3) / 4;
   const v4f* all = reinterpret_cast<const v4f*>(most);
   v4f x[AHEAD];
   auto ask = [&](u32 at) {
 #pragma unroll
-    for (u32 u = 0; u < AHEAD; ++u) x[u] = all[min(at + u * PICK_THREADS + tid, fours - 1)];
+    for (u32 u = 0; u < AHEAD; ++u) x[u] = all[min(at + u * THREADS + tid, fours - 1)];
   };
   // (the places past the last are none; a maximum read twice does no harm)
-  auto value = [&](u32 at, u32 u, u32 e) { return (at + u * PICK_THREADS + tid) * 4 + e < count ? x[u][e] : -__builtin_inff(); };
+  auto value = [&](u32 at, u32 u, u32 e) { return (at + u * THREADS + tid) * 4 + e < count ? x[u][e] : -__builtin_inff(); };
   float m = -__builtin_inff();
-  for (u32 at = 0; at < fours; at += AHEAD * PICK_THREADS) {
+  for (u32 at = 0; at < fours; at += AHEAD * THREADS) {
     ask(at);
 #pragma unroll
     for (u32 u = 0; u < AHEAD; ++u)
 #pragma unroll
       for (u32 e = 0; e < 4; ++e) m = __builtin_fmaxf(m, value(at, u, e));
   }
-  const u32 mine = float_key(m);
-  s.hist[tid] = mine;
+#pragma unroll
+  for (u32 v = 1; v < SHARE; v *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, (int)v));
+  const u32 mine = float_key(m), place = tid / SHARE;
+  if (tid % SHARE == 0) s.hist[place] = mine;
   if (tid == 0) s.count = 0;
   __syncthreads();
+  // (the threads that share a maximum rank it against a part of the others each)
   u32 before = 0;
 #pragma unroll 4
-  for (u32 i = 0; i < PICK_THREADS; i += 4) {
+  for (u32 i = tid % SHARE * 4; i < PICK_BOUNDS; i += SHARE * 4) {
     using v4u = u32 __attribute__((ext_vector_type(4)));
     const v4u h = *reinterpret_cast<const v4u*>(&s.hist[i]);
 #pragma unroll
-    for (u32 e = 0; e < 4; ++e) before += h[e] > mine || (h[e] == mine && i + e < tid);
+    for (u32 e = 0; e < 4; ++e) before += h[e] > mine || (h[e] == mine && i + e < place);
   }
+#pragma unroll
+  for (u32 v = 1; v < SHARE; v *= 2) before += (u32)__shfl_xor((int)before, (int)v);
   if (before == k - 1) s.bound = max(mine, least + 1);
   __syncthreads();
   const u32 bound = s.bound;
   const float at_least = key_float(bound);
-  for (u32 at = 0; at < fours; at += AHEAD * PICK_THREADS) {
-    if (fours > AHEAD * PICK_THREADS) ask(at);  // (else they are all here)
+  for (u32 at = 0; at < fours; at += AHEAD * THREADS) {
+    if (fours > AHEAD * THREADS) ask(at);  // (else they are all here)
 #pragma unroll
     for (u32 u = 0; u < AHEAD; ++u)
 #pragma unroll
       for (u32 e = 0; e < 4; ++e)
         if (value(at, u, e) >= at_least) {
           const u32 to = atomicAdd(&s.count, 1u);
-          if (to < PICK_FEW) found[to] = (u64)~float_key(x[u][e]) << 32 | ((at + u * PICK_THREADS + tid) * 4 + e);
+          if (to < PICK_FEW) found[to] = (u64)~float_key(x[u][e]) << 32 | ((at + u * THREADS + tid) * 4 + e);
         }
   }
   __syncthreads();
   const u32 reached = s.count;
   __syncthreads();
   if (reached <= PICK_FEW)
-    choose_ranked(found, reached, k, s);
+    choose_ranked<THREADS>(found, reached, k, s);
   else
-    choose_equal(most, count, k, least, s);
+    choose_equal<THREADS>(most, count, k, least, s);
 }
 
-__global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
+template <u32 THREADS>
+__global__ __launch_bounds__(THREADS, 4) void mx_pick_kernel(MxSearchArgs a) {
   extern __shared__ u64 found[];  // as many as the rows of k groups, up to a power of two for the sort
   __shared__ __align__(16) PickLds s;
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
@@ -437,12 +447,12 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
   const u32 least = float_key(-__builtin_inff());  // keys up to this one are of groups without a score
 
   if (a.coarse) {  // the first k groups are in the first k groups of groups
-    choose(a.coarse + (u64)q * a.coarse_pitch, (a.groups + a.per_coarse - 1) / a.per_coarse, a.k, least, found, s);
+    choose<THREADS>(a.coarse + (u64)q * a.coarse_pitch, (a.groups + a.per_coarse - 1) / a.per_coarse, a.k, least, found, s);
     const u32 parts = s.count * a.per_coarse;
     __syncthreads();
     if (tid == 0) s.count = 0;
     __syncthreads();
-    for (u32 i = tid; i < parts; i += PICK_THREADS) {
+    for (u32 i = tid; i < parts; i += THREADS) {
       const u32 g = s.chosen[i / a.per_coarse] * a.per_coarse + i % a.per_coarse;
       const u32 key = g < a.groups ? float_key(most[g]) : 0u;
       if (key > least) found[atomicAdd(&s.count, 1u)] = (u64)~key << 32 | g;
@@ -450,9 +460,9 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
     __syncthreads();
     const u32 reached = s.count;
     __syncthreads();
-    choose_ranked(found, reached, a.k, s);
+    choose_ranked<THREADS>(found, reached, a.k, s);
   } else {
-    choose(most, a.groups, a.k, least, found, s);
+    choose<THREADS>(most, a.groups, a.k, least, found, s);
   }
   const u32 nchosen = s.count;
   // k groups: k points reach the smallest of their maxima, and no other point matters
@@ -461,7 +471,7 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
   if (tid == 0) s.count = 0;
   __syncthreads();
   const u64 qrow = (u64)a.q0 + q;
-  for (u32 c = wave; c < nchosen; c += PICK_THREADS / 64) {
+  for (u32 c = wave; c < nchosen; c += THREADS / 64) {
     const u64 w0 = (u64)s.chosen[c] * SEARCH_GROUP;
     v4f acc[4];
     u64 row[4];
@@ -470,15 +480,23 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
       row[i] = min(w0 + 16 * i + lane % 16, (u64)a.w.n - 1);
       acc[i] = first_sums(a, w0 + 16 * i, load_norm(a, w0 + 16 * i + lane % 16));
     }
-    for (u32 st = 0; st < a.w.steps; ++st) {
-      const v4i x = load_codes(a.q, qrow, st);
-      const int xs = load_scale(a.q, qrow, st);
-      v4i w[4];
-      int ws[4];
+    for (u32 st = 0; st < a.w.steps; st += 2) {  // two steps' loads on their way at once
+      v4i x[2], w[4][2];
+      int xs[2], ws[4][2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = load_codes(a.w, row[i], st), ws[i] = load_scale(a.w, row[i], st);
+      for (u32 e = 0; e < 2; ++e) {
+        const u32 step = min(st + e, a.w.steps - 1);
+        x[e] = load_codes(a.q, qrow, step);
+        xs[e] = load_scale(a.q, qrow, step);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = mx_mfma(w[i], x, acc[i], ws[i], xs);
+        for (int i = 0; i < 4; ++i) w[i][e] = load_codes(a.w, row[i], step), ws[i][e] = load_scale(a.w, row[i], step);
+      }
+#pragma unroll
+      for (u32 e = 0; e < 2; ++e) {
+        if (st + e >= a.w.steps) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = mx_mfma(w[i][e], x[e], acc[i], ws[i][e], xs[e]);
+      }
     }
     // (all columns are this query's: one of them is used)
     if (lane % 16 == 0)
@@ -500,7 +518,7 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
     a.dists[to] = a.norms ? __builtin_fmaxf(0.0f, __builtin_fmaf(-2.0f, score, a.qnorms[qrow])) : 0.0f - score;
   };
   if (count <= PICK_FEW) {
-    for (u32 c = tid; c < count; c += PICK_THREADS) {
+    for (u32 c = tid; c < count; c += THREADS) {
       const u64 key = found[c];
       u32 rank = 0;
       for (u32 i = 0; i < count; ++i) rank += found[i] < key;
@@ -509,20 +527,20 @@ __global__ __launch_bounds__(PICK_THREADS) void mx_pick_kernel(MxSearchArgs a) {
   } else {
     u32 size = 2;
     while (size < count) size *= 2;
-    for (u32 i = count + tid; i < size; i += PICK_THREADS) found[i] = ~0ull;
+    for (u32 i = count + tid; i < size; i += THREADS) found[i] = ~0ull;
     __syncthreads();
     for (u32 run = 2; run <= size; run *= 2)
       for (u32 gap = run / 2; gap > 0; gap /= 2) {
-        for (u32 i = tid; i < size / 2; i += PICK_THREADS) {
+        for (u32 i = tid; i < size / 2; i += THREADS) {
           const u32 lo = i / gap * 2 * gap + i % gap, hi = lo + gap;
           const u64 x = found[lo], y = found[hi];
           if ((x > y) == ((lo & run) == 0)) found[lo] = y, found[hi] = x;
         }
         __syncthreads();
       }
-    for (u32 i = tid; i < a.k; i += PICK_THREADS) put(i, found[i]);
+    for (u32 i = tid; i < a.k; i += THREADS) put(i, found[i]);
   }
-  for (u32 i = count + tid; i < a.k; i += PICK_THREADS) {
+  for (u32 i = count + tid; i < a.k; i += THREADS) {
     a.ids[qrow * a.k + i] = ANN_NONE;
     a.dists[qrow * a.k + i] = __builtin_inff();
   }
@@ -655,7 +673,10 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
   size_t room = PICK_FEW;  // (four groups of each of the first k groups of groups as well)
   while (room < (size_t)(k < a.groups ? k : a.groups) * SEARCH_GROUP) room *= 2;
   room *= 8;
-  HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(mx_pick_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room));
+  // a thousand threads for a query where there are not enough queries for all compute units
+  const auto pick = part <= 256 ? mx_pick_kernel<1024> : mx_pick_kernel<256>;
+  const u32 pick_threads = part <= 256 ? 1024 : 256;
+  HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(pick), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room));
   for (u64 q0 = 0; q0 < nq; q0 += part) {
     a.q0 = (u32)q0;
     a.nq = (u32)(nq - q0 < part ? nq - q0 : part);
@@ -675,7 +696,7 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
       hipLaunchKernelGGL(mx_group_long_kernel, dim3((u32)((tiles + 3) / 4)), dim3(256), 0, st, a, tiles);
       HIP_TRY(hipGetLastError());
     }
-    hipLaunchKernelGGL(mx_pick_kernel, dim3(a.nq), dim3(256), room, st, a);
+    hipLaunchKernelGGL(pick, dim3(a.nq), dim3(pick_threads), room, st, a);
     HIP_TRY(hipGetLastError());
   }
   return ANN_OK;
