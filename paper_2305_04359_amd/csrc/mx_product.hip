@@ -105,6 +105,94 @@ __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 til
   }
 }
 
+// 4-bit rows on both sides, many: 256 x 256 results a workgroup of eight waves, 128 x 64 a wave.  Pairs of steps (256
+// elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for its turn.
+constexpr u32 BOTH_THREADS = 512;
+constexpr u32 BOTH_ROWS = 256;  // of either side
+
+__global__ __launch_bounds__(BOTH_THREADS) void mx_product4_many_kernel(ProductArgs a, u32 tiles_w, u32 tiles) {
+  constexpr u32 BYTES = BOTH_ROWS * 128;                   // codes of one side of a stage
+  constexpr u32 STAGE = 2 * BYTES + 2 * BOTH_ROWS * 8;     // and the scales of both
+  extern __shared__ __align__(16) char lds[];
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  // Chiplets take workgroups in turn: each gets a run of tiles that share rows.
+  const u32 per = (tiles + 7) / 8, t = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (t >= tiles) return;
+  const u32 tiles_x = tiles / tiles_w;
+  const u64 w0 = (u64)(t / tiles_x) * BOTH_ROWS, x0 = (u64)(t % tiles_x) * BOTH_ROWS;
+  const u32 ww = wave % 2 * 128, wx = wave / 2 * 64;  // the wave's part of the tile
+  const u32 steps = a.w.steps, pairs = (steps + 1) / 2;
+
+  // What this thread brings to LDS: 16 bytes of the pair's 128 of four rows of each side, and the scales of one step
+  // of a row.  A step past the last is read as the last.
+  const u32 unit = tid % 8;
+  v4i next[2][4];
+  u32 next_scale[2];
+  bool there;  // (the 4-bit rows' codes of a step past the last count as 0)
+  auto fetch = [&](u32 p) {
+    const u32 step = min(p * 2 + unit / 4, steps - 1);
+    there = p * 2 + unit / 4 < steps;
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+      const u32 r = tid / 8 + 64 * i;
+      next[0][i] = *reinterpret_cast<const v4i*>(a.w.codes + (min(w0 + r, (u64)a.w.n - 1) * steps + step) * MX_STEP_BYTES + unit % 4 * 16);
+      next[1][i] = *reinterpret_cast<const v4i*>(a.q.codes + (min(x0 + r, (u64)a.q.n - 1) * steps + step) * MX_STEP_BYTES + unit % 4 * 16);
+    }
+    const u32 s = min(p * 2 + tid % 2, steps - 1);
+    next_scale[0] = reinterpret_cast<const u32*>(a.w.scales)[min(w0 + tid / 2, (u64)a.w.n - 1) * steps + s];
+    next_scale[1] = reinterpret_cast<const u32*>(a.q.scales)[min(x0 + tid / 2, (u64)a.q.n - 1) * steps + s];
+  };
+  auto keep = [&](u32 p) {
+    char* stage = lds + p % 2 * STAGE;
+#pragma unroll
+    for (u32 side = 0; side < 2; ++side) {
+#pragma unroll
+      for (u32 i = 0; i < 4; ++i) {
+        const u32 r = tid / 8 + 64 * i;
+        *reinterpret_cast<v4i*>(stage + side * BYTES + r * 128 + (unit ^ r % 8) * 16) = side || there ? next[side][i] : v4i{};
+      }
+      reinterpret_cast<u32*>(stage + 2 * BYTES + side * BOTH_ROWS * 8)[tid] = next_scale[side];
+    }
+  };
+  v4f acc[8][4] = {};
+  fetch(0);
+  keep(0);
+  fetch(min(1u, pairs - 1));
+  for (u32 p = 0; p < pairs; ++p) {
+    __syncthreads();
+    const char* stage = lds + p % 2 * STAGE;
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) {
+      __builtin_amdgcn_sched_barrier(0);  // (or both steps' fragments would be read at once, in too many registers)
+      if (h == 1) {
+        // Behind the first products: they run while the next pair is put away.  At the end a pair too many is, and
+        // not read: at a condition the compiler would move the products behind it.
+        keep(p + 1);
+        fetch(min(p + 2, pairs - 1));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      v4i x[4];
+      int xs[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u32 r = wx + 16 * j + lane % 16;
+        x[j] = *reinterpret_cast<const v4i*>(stage + BYTES + r * 128 + ((h * 4 + lane / 16) ^ r % 8) * 16);
+        xs[j] = (stage + 2 * BYTES + BOTH_ROWS * 8)[r * 8 + h * 4 + lane / 16];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const u32 r = ww + 16 * i + lane % 16;
+        const v4i w = *reinterpret_cast<const v4i*>(stage + r * 128 + ((h * 4 + lane / 16) ^ r % 8) * 16);
+        const int ws = (stage + 2 * BYTES)[r * 8 + h * 4 + lane / 16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = mx_mfma(w, x[j], acc[i][j], ws, xs[j]);
+      }
+    }
+  }
+  __syncthreads();
+  if (w0 + ww < a.w.n) store_results<8, 4>(a, acc, w0 + ww, x0 + wx, lds + wave * store_room<8>());
+}
+
 // A float as bf16 numbers whose sum it is: the upper halves of what is left, without rounding, so that none
 // leaves the range.  Infinities and NaN stay in the first.
 template <int PARTS>
@@ -336,7 +424,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
   const u32 halves = a.w.steps * 2;
   auto fetch = [&](u32 h) {
     next_w = *reinterpret_cast<const v4i*>(codes + (u64)h * 32);
-    if (h % 2 == 0) next_scale = scales[h / 2];
+    next_scale = scales[h / 2];
 #pragma unroll
     for (int i = 0; i < XF; ++i) next_x[i] = load_batch<T, WIDE>(a, x0 + tid / 8 + 64 * i, h * 64 + tid % 8 * 8);
   };
@@ -348,7 +436,8 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
       const u32 unit = (tid % 2 * 2 + e + row / 4) % 4;
       *reinterpret_cast<long*>(stage + row * 32 + unit * 8) = e ? (long)(u32)next_w[3] << 32 | (u32)next_w[2] : (long)(u32)next_w[1] << 32 | (u32)next_w[0];
     }
-    if (h % 2 == 0 && tid < MANY_ROWS) reinterpret_cast<u32*>(lds + 2 * STAGE)[h / 2 % 2 * MANY_ROWS + tid] = next_scale;
+    // (twice for a step and by two threads each, the same value: no branch)
+    reinterpret_cast<u32*>(lds + 2 * STAGE)[h / 2 % 2 * MANY_ROWS + tid % MANY_ROWS] = next_scale;
 #pragma unroll
     for (int i = 0; i < XF; ++i) {
       mask_batch<T, WIDE>(a, next_x[i], h * 64 + tid % 8 * 8);
@@ -362,7 +451,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
   v4f acc[8][XF] = {};
   fetch(0);
   keep(0);
-  if (halves > 1) fetch(1);
+  fetch(1);
   u32 scale[8];
   for (u32 h = 0; h < halves; ++h) {
     __syncthreads();
@@ -376,9 +465,13 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      if (c == 1) {  // behind the first products: they run while the next half is put away
-        if (h + 1 < halves) keep(h + 1);
-        if (h + 2 < halves) fetch(h + 2);
+      if (c == 1) {
+        // Behind the first products: they run while the next half is put away.  At the end a half too many is, and
+        // not read: at a condition the compiler would move the products behind it.
+        __builtin_amdgcn_sched_barrier(0);
+        keep(h + 1);
+        fetch(min(h + 2, halves - 1));
+        __builtin_amdgcn_sched_barrier(0);
       }
       v8bf x[XF][PARTS];
 #pragma unroll
@@ -471,6 +564,15 @@ hipError_t launch_product(const ProductArgs& a, int xdtype, hipStream_t s) {
   if (xdtype == ANN_F32) return launch_product16<float>(a, s);
   if (xdtype == ANN_F16) return launch_product16<__half>(a, s);
   if (xdtype == ANN_BF16) return launch_product16<__bf16>(a, s);
+  const u64 many_w = ((u64)a.w.n + BOTH_ROWS - 1) / BOTH_ROWS, many_x = ((u64)a.nx + BOTH_ROWS - 1) / BOTH_ROWS;
+  if (a.w.steps > 2 && many_w * many_x >= 128 && many_w * many_x < 1u << 22) {
+    constexpr int lds = 2 * (2 * BOTH_ROWS * 128 + 2 * BOTH_ROWS * 8);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx_product4_many_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    const u32 tiles = (u32)(many_w * many_x);
+    hipLaunchKernelGGL(mx_product4_many_kernel, dim3((tiles + 7) / 8 * 8), dim3(BOTH_THREADS), lds, s, a, (u32)many_w, tiles);
+    return hipGetLastError();
+  }
   const u32 tiles_w = (u32)(((u64)a.w.n + 127) / 128);
   const u64 tiles = tiles_w * (((u64)a.nx + 127) / 128);
   const dim3 grid((u32)(tiles < (1u << 20) ? tiles : (1u << 20)));

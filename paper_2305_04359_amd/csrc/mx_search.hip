@@ -214,16 +214,18 @@ __global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchA
   };
   fetch(s0);
   keep(stages[s0 % 2]);
-  if (s0 + 1 < s1) fetch(s0 + 1);
+  fetch(min(s0 + 1, s1 - 1));
   for (u32 st = s0; st < s1; ++st) {
     __syncthreads();
     const Stage& here = stages[st % 2];
     float joined[GS / WR][QF / 4];
 #pragma unroll
     for (u32 n = 0; n < GS / WR; ++n) {
-      if (n == 1 || GS == WR) {  // behind the first products
-        if (st + 1 < s1) keep(stages[(st + 1) % 2]);
-        if (st + 2 < s1) fetch(st + 2);
+      if (n == 1 || GS == WR) {
+        // Behind the first products.  At the end a stage too many is put away, and not read: at a condition the
+        // compiler would move the products behind it.
+        keep(stages[(st + 1) % 2]);
+        fetch(min(st + 2, s1 - 1));
       }
       const u32 g = n * WR + wave % WR;
       float m[QF];
