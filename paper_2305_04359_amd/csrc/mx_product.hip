@@ -1,4 +1,7 @@
 // Products of a batch with microscaled 4-bit rows.
+#include <type_traits>
+#include <utility>
+
 #include "mx.hpp"
 
 namespace annmi {
@@ -106,13 +109,28 @@ __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 til
 }
 
 // 4-bit rows on both sides, many: 256 x 256 results a workgroup of eight waves, 128 x 64 a wave.  Pairs of steps (256
-// elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for its turn.
+// elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for its turn.  The
+// scales lie in LDS so that a lane reads those of all its fragments' rows at once; the instruction picks the byte.
 constexpr u32 BOTH_THREADS = 512;
 constexpr u32 BOTH_ROWS = 256;  // of either side
 
+template <int... I, typename F>
+__device__ __forceinline__ void unroll(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unroll(F f) {
+  unroll(std::make_integer_sequence<int, N>(), f);
+}
+template <int BYTE_A, int BYTE_B>
+__device__ __forceinline__ v4f mx_mfma_bytes(v4i a, v4i b, v4f c, int scales_a, int scales_b) {
+  const v8i x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, BYTE_A, scales_a, BYTE_B, scales_b);
+}
+
 __global__ __launch_bounds__(BOTH_THREADS) void mx_product4_many_kernel(ProductArgs a, u32 tiles_w, u32 tiles) {
-  constexpr u32 BYTES = BOTH_ROWS * 128;                   // codes of one side of a stage
-  constexpr u32 STAGE = 2 * BYTES + 2 * BOTH_ROWS * 8;     // and the scales of both
+  constexpr u32 BYTES = BOTH_ROWS * 128;                // codes of one side of a stage
+  constexpr u32 STAGE = 2 * BYTES + 2 * BOTH_ROWS * 8;  // and the scales of both
   extern __shared__ __align__(16) char lds[];
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   // Chiplets take workgroups in turn: each gets a run of tiles that share rows.
@@ -124,23 +142,31 @@ __global__ __launch_bounds__(BOTH_THREADS) void mx_product4_many_kernel(ProductA
   const u32 steps = a.w.steps, pairs = (steps + 1) / 2;
 
   // What this thread brings to LDS: 16 bytes of the pair's 128 of four rows of each side, and the scales of one step
-  // of a row.  A step past the last is read as the last.
+  // of a row.  A step past the last is read as the one before, and the 4-bit rows' codes of it count as 0.
   const u32 unit = tid % 8;
+  const uint8_t* side_codes[2] = {a.w.codes + w0 * steps * MX_STEP_BYTES, a.q.codes + x0 * steps * MX_STEP_BYTES};
+  const u32* side_scales[2] = {reinterpret_cast<const u32*>(a.w.scales) + w0 * steps, reinterpret_cast<const u32*>(a.q.scales) + x0 * steps};
+  const u32 last_row[2] = {(u32)min((u64)BOTH_ROWS, a.w.n - w0) - 1, (u32)min((u64)BOTH_ROWS, a.q.n - x0) - 1};
+  u32 offset[2][4], scale_at[2];
+#pragma unroll
+  for (u32 side = 0; side < 2; ++side) {
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) offset[side][i] = min(tid / 8 + 64 * i, last_row[side]) * steps * MX_STEP_BYTES + unit % 4 * 16;
+    scale_at[side] = min(tid / 2, last_row[side]) * steps;
+  }
   v4i next[2][4];
   u32 next_scale[2];
-  bool there;  // (the 4-bit rows' codes of a step past the last count as 0)
+  bool there;
   auto fetch = [&](u32 p) {
-    const u32 step = min(p * 2 + unit / 4, steps - 1);
     there = p * 2 + unit / 4 < steps;
+    const u32 second = there ? unit / 4 * MX_STEP_BYTES : 0, scale = min(p * 2 + tid % 2, steps - 1);
 #pragma unroll
-    for (u32 i = 0; i < 4; ++i) {
-      const u32 r = tid / 8 + 64 * i;
-      next[0][i] = *reinterpret_cast<const v4i*>(a.w.codes + (min(w0 + r, (u64)a.w.n - 1) * steps + step) * MX_STEP_BYTES + unit % 4 * 16);
-      next[1][i] = *reinterpret_cast<const v4i*>(a.q.codes + (min(x0 + r, (u64)a.q.n - 1) * steps + step) * MX_STEP_BYTES + unit % 4 * 16);
+    for (u32 side = 0; side < 2; ++side) {
+      const uint8_t* from = side_codes[side] + p * (2 * MX_STEP_BYTES);
+#pragma unroll
+      for (u32 i = 0; i < 4; ++i) next[side][i] = *reinterpret_cast<const v4i*>(from + (offset[side][i] + second));
+      next_scale[side] = side_scales[side][scale_at[side] + scale];
     }
-    const u32 s = min(p * 2 + tid % 2, steps - 1);
-    next_scale[0] = reinterpret_cast<const u32*>(a.w.scales)[min(w0 + tid / 2, (u64)a.w.n - 1) * steps + s];
-    next_scale[1] = reinterpret_cast<const u32*>(a.q.scales)[min(x0 + tid / 2, (u64)a.q.n - 1) * steps + s];
   };
   auto keep = [&](u32 p) {
     char* stage = lds + p % 2 * STAGE;
@@ -151,7 +177,11 @@ __global__ __launch_bounds__(BOTH_THREADS) void mx_product4_many_kernel(ProductA
         const u32 r = tid / 8 + 64 * i;
         *reinterpret_cast<v4i*>(stage + side * BYTES + r * 128 + (unit ^ r % 8) * 16) = side || there ? next[side][i] : v4i{};
       }
-      reinterpret_cast<u32*>(stage + 2 * BYTES + side * BOTH_ROWS * 8)[tid] = next_scale[side];
+      // (step, block, row % 16, row / 16): a lane's fragments are 16 rows apart
+      const u32 row = tid / 2;
+      char* scales = stage + 2 * BYTES + side * BOTH_ROWS * 8 + (tid % 2 * 64 + row % 16) * 16 + row / 16;
+#pragma unroll
+      for (u32 g = 0; g < 4; ++g) scales[g * 256] = (char)(next_scale[side] >> (8 * g));
     }
   };
   v4f acc[8][4] = {};
@@ -171,22 +201,18 @@ __global__ __launch_bounds__(BOTH_THREADS) void mx_product4_many_kernel(ProductA
         fetch(min(p + 2, pairs - 1));
         __builtin_amdgcn_sched_barrier(0);
       }
+      const char* scales = stage + 2 * BYTES + (h * 64 + lane) * 16;
+      using v2i = int __attribute__((ext_vector_type(2)));
+      const v2i ws = *reinterpret_cast<const v2i*>(scales + ww / 16);
+      const int xs = *reinterpret_cast<const int*>(scales + BOTH_ROWS * 8 + wx / 16);
+      const u32 at = ((h * 4 + lane / 16) ^ lane % 8) * 16 + lane % 16 * 128;
       v4i x[4];
-      int xs[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32 r = wx + 16 * j + lane % 16;
-        x[j] = *reinterpret_cast<const v4i*>(stage + BYTES + r * 128 + ((h * 4 + lane / 16) ^ r % 8) * 16);
-        xs[j] = (stage + 2 * BYTES + BOTH_ROWS * 8)[r * 8 + h * 4 + lane / 16];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const u32 r = ww + 16 * i + lane % 16;
-        const v4i w = *reinterpret_cast<const v4i*>(stage + r * 128 + ((h * 4 + lane / 16) ^ r % 8) * 16);
-        const int ws = (stage + 2 * BYTES)[r * 8 + h * 4 + lane / 16];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mx_mfma(w, x[j], acc[i][j], ws, xs[j]);
-      }
+      for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const v4i*>(stage + BYTES + (wx + 16 * j) * 128 + at);
+      unroll<8>([&](auto i) {
+        const v4i w = *reinterpret_cast<const v4i*>(stage + (ww + 16 * i) * 128 + at);
+        unroll<4>([&](auto j) { acc[i][j] = mx_mfma_bytes<i % 4, j>(w, x[j], acc[i][j], ws[i / 4], xs); });
+      });
     }
   }
   __syncthreads();
