@@ -1,4 +1,6 @@
 // Rows to microscaled 4-bit codes and back.
+#include <type_traits>
+
 #include "mx.hpp"
 
 namespace annmi {
@@ -17,134 +19,211 @@ struct QuantizeArgs {
   const char* x;
   u64 ldx;
   u32 n, d, steps;
-  u32 wide;  // every row can be read eight elements at a time
   uint8_t* codes;
   uint8_t* scales;
   float* norms;
 };
 
+// N elements at a multiple of four bytes, for one load or store of all
+template <typename T, int N>
+struct __attribute__((packed, aligned(4))) WordPack {
+  T v[N];
+};
+
+// exchanges inside 16 lanes, by one instruction each
+template <int CTRL>
+__device__ __forceinline__ u32 dpp(u32 v) {
+  return (u32)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true);
+}
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_ROT4 = 0x124, DPP_ROT8 = 0x128;
+template <int CTRL>
+__device__ __forceinline__ float dpp_sum(float v) {
+  return v + __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
+}
+
 // Four lanes take 32 elements, eight each: their largest magnitude by two exchanges, then the codes.  LPR lanes
-// (16, 32 or 64: one, two or four steps) take a row, longer rows in turns; whole waves then read and write
-// runs of memory.  Bound by memory: a byte in for each element at least, 17 bytes out for 32.
-template <typename T, int LPR>
+// (16, 32 or 64: one, two or four steps) take a row, longer rows in turns; a wave asks for four such pieces of rows
+// at once.  Bound by memory: a byte in for each element at least, 17 bytes out for 32.
+// WIDE: every row begins at a multiple of four bytes and has eight elements at least; eight are then read at once,
+// past d too, but in the last row, whose last eight are read where these reach its end.
+template <typename T, int LPR, bool WIDE>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantizeArgs a) {
+  constexpr u32 AHEAD = 4, PER_BLOCK = 256 / LPR;
   const u32 lane = threadIdx.x % LPR;
-  const u32 per_block = 256 / LPR;
-  for (u64 r = (u64)blockIdx.x * per_block + threadIdx.x / LPR; r < a.n; r += (u64)gridDim.x * per_block) {
-    const T* row = reinterpret_cast<const T*>(a.x) + r * a.ldx;
-    float norm = 0.0f;
-    for (u32 s = 0; s < a.steps; s += LPR / 16) {
-      const u32 at = s * MX_STEP + lane * 8;  // the lane's first element
-      float v[8];
-      if (a.wide && at + 8 <= a.d) {
-        const Pack<T, 8> p = *reinterpret_cast<const Pack<T, 8>*>(row + at);
+  const u32 turns = (a.steps + LPR / 16 - 1) / (LPR / 16);  // 1 but for rows of more than four steps
+  // the rows of a pass: of AHEAD turns of one row where rows are long, else of AHEAD rows
+  const bool rows_ahead = turns == 1;
+  const u64 stride = (u64)gridDim.x * PER_BLOCK;
+  for (u64 r0 = (u64)blockIdx.x * PER_BLOCK + threadIdx.x / LPR; r0 < a.n; r0 += rows_ahead ? stride * AHEAD : stride) {
+    float norm[AHEAD] = {};
+    for (u32 s0 = 0; s0 < turns; s0 += AHEAD) {
+      WordPack<T, 8> in[AHEAD];
+      u64 row[AHEAD];
+      u32 at[AHEAD];
+      bool on[AHEAD];
+      u32 early[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = mx_float(p.v[i]);
-      } else {
+      for (u32 u = 0; u < AHEAD; ++u) {
+        row[u] = rows_ahead ? r0 + stride * u : r0;
+        at[u] = (rows_ahead ? 0 : s0 + u) * (LPR / 16 * MX_STEP) + lane * 8;  // the lane's first element
+        on[u] = row[u] < a.n && at[u] < a.steps * MX_STEP;
+        const u64 r = min(row[u], (u64)a.n - 1);
+        const T* from = reinterpret_cast<const T*>(a.x) + r * a.ldx;
+        if (WIDE) {
+          const u32 first = at[u] < a.d ? at[u] : 0;
+          early[u] = (a.n - 1 - r) * a.ldx < 7 && first + 8 > a.d ? first + 8 - a.d : 0;
+          in[u] = *reinterpret_cast<const WordPack<T, 8>*>(from + (first - early[u]));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = at + i < a.d ? mx_float(row[at + i]) : 0.0f;
+          for (u32 e = 0; e < 8; ++e) in[u].v[e] = from[min(at[u] + e, a.d - 1)];
+        }
       }
-      // magnitudes compare like their bits, and so do NaN and infinity
-      u32 most = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-      most = max(most, (u32)__shfl_xor((int)most, 1));
-      most = max(most, (u32)__shfl_xor((int)most, 2));
-      const bool fine = most < 0x7F800000u;
-      const u32 exponent = most >> 23;
-      const u32 byte = !fine ? 255u : exponent > 2 ? exponent - 2 : 0u;
-      const float inverse = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte); of no use where byte is 255
-      u32 code = 0;
-      float sum = 0.0f;
+      for (u32 u = 0; u < AHEAD; ++u) {
+        if (!on[u]) continue;  // (whole rows or steps at a time: 16 lanes alike)
+        float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
+        for (u32 e = 0; e < 8; ++e) v[e] = mx_float(static_cast<T>(in[u].v[e]));
+        if (WIDE && early[u])
+          for (u32 k = 0; k < early[u]; ++k)
+#pragma unroll
+            for (u32 e = 0; e < 7; ++e) v[e] = v[e + 1];
+#pragma unroll
+        for (u32 e = 0; e < 8; ++e) v[e] = at[u] + e < a.d ? v[e] : 0.0f;
+        // magnitudes compare like their bits, and so do NaN and infinity
+        u32 most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        most = max(most, dpp<DPP_XOR1>(most));
+        most = max(most, dpp<DPP_XOR2>(most));
+        const bool fine = most < 0x7F800000u;
+        const u32 exponent = most >> 23;
+        const u32 byte = !fine ? 255u : exponent > 2 ? exponent - 2 : 0u;
+        const float inverse = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte); of no use where byte is 255
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= inverse;
         // (the scale is in the factor: the instruction gets 1)
-        const float lo = v[i] * inverse, hi = v[i + 1] * inverse;
-        if (i == 0) code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, lo, hi, 1.0f, 0);
-        if (i == 2) code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, lo, hi, 1.0f, 1);
-        if (i == 4) code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, lo, hi, 1.0f, 2);
-        if (i == 6) code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, lo, hi, 1.0f, 3);
-      }
-      if (!fine) code = 0;
-      if (a.norms) {
-        using v2f = float __attribute__((ext_vector_type(2)));
-        const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 1),
-                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 3)};
+        u32 code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], 1.0f, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], 1.0f, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], 1.0f, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], 1.0f, 3);
+        if (!fine) code = 0;
+        if (a.norms) {
+          using v2f = float __attribute__((ext_vector_type(2)));
+          const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 1),
+                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 3)};
+          float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum = __builtin_fmaf(p[i].x, p[i].x, __builtin_fmaf(p[i].y, p[i].y, sum));
-        const float scale = mx_scale(byte);
-        norm = __builtin_fmaf(sum * scale, scale, norm);
-      }
-      const u32 step = s + lane / 16;
-      if (step < a.steps) {
-        reinterpret_cast<u32*>(a.codes)[(r * a.steps + step) * 16 + lane % 16] = code;
-        if (lane % 4 == 0) a.scales[(r * a.steps + step) * 4 + lane % 16 / 4] = (uint8_t)(at < a.d ? byte : 0u);
+          for (int i = 0; i < 4; ++i) sum = __builtin_fmaf(p[i].x, p[i].x, __builtin_fmaf(p[i].y, p[i].y, sum));
+          const float scale = mx_scale(byte);
+          float& to = norm[rows_ahead ? u : 0];
+          to = __builtin_fmaf(sum * scale, scale, to);
+        }
+        // a step's four scale bytes meet in one word
+        u32 word = (at[u] < a.d ? byte : 0u) << (lane % 16 / 4 * 8);
+        word |= dpp<DPP_ROT4>(word);
+        word |= dpp<DPP_ROT8>(word);
+        const u64 step = row[u] * a.steps + at[u] / MX_STEP;
+        reinterpret_cast<u32*>(a.codes)[step * 16 + lane % 16] = code;
+        if (lane % 16 == 0) reinterpret_cast<u32*>(a.scales)[step] = word;
       }
     }
     if (a.norms) {
 #pragma unroll
-      for (int w = 1; w < LPR; w *= 2) norm += __shfl_xor(norm, w);
-      if (lane == 0) a.norms[r] = norm;
+      for (u32 u = 0; u < AHEAD; ++u) {
+        float sum = dpp_sum<DPP_XOR1>(norm[u]);
+        sum = dpp_sum<DPP_XOR2>(sum);
+        sum = dpp_sum<DPP_ROT4>(sum);
+        sum = dpp_sum<DPP_ROT8>(sum);
+#pragma unroll
+        for (int w = 16; w < LPR; w *= 2) sum += __shfl_xor(sum, w);
+        const u64 r = r0 + stride * u;
+        if (lane == 0 && (u == 0 || rows_ahead) && r < a.n) a.norms[r] = sum;
+        if (!rows_ahead) break;
+      }
     }
   }
 }
 
-template <typename T>
+template <typename T, bool WIDE>
 hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s) {
   const u32 lpr = a.steps == 1 ? 16 : a.steps == 2 ? 32 : 64;
-  const u64 blocks = ((u64)a.n * lpr + 255) / 256;
+  // four rows for each place, where a turn takes a row
+  const u64 per = 256 / lpr * (a.steps <= 4 ? 4 : 1), blocks = ((u64)a.n + per - 1) / per;
   const u32 grid = (u32)(blocks < (1u << 20) ? blocks : (1u << 20));
   if (lpr == 16)
-    hipLaunchKernelGGL((mx_quantize_kernel<T, 16>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((mx_quantize_kernel<T, 16, WIDE>), dim3(grid), dim3(256), 0, s, a);
   else if (lpr == 32)
-    hipLaunchKernelGGL((mx_quantize_kernel<T, 32>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((mx_quantize_kernel<T, 32, WIDE>), dim3(grid), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((mx_quantize_kernel<T, 64>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((mx_quantize_kernel<T, 64, WIDE>), dim3(grid), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s) {
+  const bool wide = aligned_to(a.x, 4) && a.ldx * sizeof(T) % 4 == 0 && a.d >= 8;
+  return wide ? launch_quantize<T, true>(a, s) : launch_quantize<T, false>(a, s);
 }
 
 struct DequantizeArgs {
   const uint8_t* codes;
   const uint8_t* scales;
-  u64 pieces;  // of eight elements, in all rows (padding included)
+  u64 n;
   u32 steps, d;
   char* out;
   u64 ldo;
-  u32 wide;
+  u32 wide;  // every row of `out` begins at a multiple of 16 bytes
 };
 
-// A lane per eight elements.  Bound by memory.
+// A thread takes 16 bytes of a row of `out`, and the same ones of other rows in turn.  Bound by memory.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(DequantizeArgs a) {
-  for (u64 i = (u64)blockIdx.x * 256 + threadIdx.x; i < a.pieces; i += (u64)gridDim.x * 256) {
-    const u64 r = i / (a.steps * 16);
-    const u32 at = (u32)(i - r * (a.steps * 16)) * 8;
-    if (at >= a.d) continue;
-    const u32 code = reinterpret_cast<const u32*>(a.codes)[i];
-    const float scale = mx_scale(a.scales[i / 4]);
-    using v2f = float __attribute__((ext_vector_type(2)));
-    const v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 1),
-                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 3)};
-    Pack<T, 8> o;
+  constexpr u32 E = 16 / sizeof(T), AHEAD = 4;  // elements; rows at a time
+  using Codes = std::conditional_t<E == 4, unsigned short, u32>;
+  using v2f = float __attribute__((ext_vector_type(2)));
+  const u32 pieces = (a.d + E - 1) / E;
+  const u32 across = pieces < 256 ? pieces : 256, rows = 256 / across;  // of a block
+  const u32 sub = threadIdx.x / across;
+  if (sub >= rows) return;
+  const u64 stride = (u64)gridDim.x * rows;
+  for (u64 r0 = (u64)blockIdx.x * rows + sub; r0 < a.n; r0 += stride * AHEAD) {
+    for (u32 c = threadIdx.x % across; c < pieces; c += across) {
+      u32 code[AHEAD];
+      float scale[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      o.v[2 * j] = mx_round<T>(p[j].x * scale);
-      o.v[2 * j + 1] = mx_round<T>(p[j].y * scale);
-    }
-    T* to = reinterpret_cast<T*>(a.out) + r * a.ldo + at;
-    if (a.wide && at + 8 <= a.d) {
-      *reinterpret_cast<Pack<T, 8>*>(to) = o;
-    } else {
+      for (u32 u = 0; u < AHEAD; ++u) {
+        const u64 r = min(r0 + stride * u, a.n - 1) * a.steps;
+        code[u] = reinterpret_cast<const Codes*>(a.codes + r * MX_STEP_BYTES)[c];
+        scale[u] = mx_scale(a.scales[r * MX_STEP_SCALES + c * E / 32]);
+      }
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (at + j < a.d) to[j] = o.v[j];
+      for (u32 u = 0; u < AHEAD; ++u) {
+        if (r0 + stride * u >= a.n) break;
+        v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 1)};
+        if (E == 8) p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 2), p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 3);
+        Pack<T, E> o;
+#pragma unroll
+        for (u32 j = 0; j < E / 2; ++j) {
+          o.v[2 * j] = mx_round<T>(p[j].x * scale[u]);
+          o.v[2 * j + 1] = mx_round<T>(p[j].y * scale[u]);
+        }
+        T* to = reinterpret_cast<T*>(a.out) + (r0 + stride * u) * a.ldo + c * E;
+        if (a.wide && c * E + E <= a.d) {
+          *reinterpret_cast<Pack<T, E>*>(to) = o;
+        } else {
+#pragma unroll
+          for (u32 j = 0; j < E; ++j)
+            if (c * E + j < a.d) to[j] = o.v[j];
+        }
+      }
     }
   }
 }
 
 template <typename T>
 hipError_t launch_dequantize(const DequantizeArgs& a, hipStream_t s) {
-  const u64 blocks = (a.pieces + 255) / 256;
+  const u32 pieces = (u32)((a.d + 16 / sizeof(T) - 1) / (16 / sizeof(T))), rows = pieces < 256 ? 256 / pieces : 1;
+  const u64 blocks = (a.n + 4 * rows - 1) / (4 * rows);
   hipLaunchKernelGGL(mx_dequantize_kernel<T>, dim3((u32)(blocks < (1u << 20) ? blocks : (1u << 20))), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -165,8 +244,7 @@ int ann_mx_quantize(const void* x_dev, uint64_t n, uint32_t d, ann_dtype dtype, 
   if (n == 0) return ANN_OK;
   if (!x_dev) return fail(ANN_EINVAL, "null argument");
   if (!aligned_to(x_dev, esz) || !aligned_to(norms_dev, 4)) return fail(ANN_EINVAL, "x or norms not aligned to their elements");
-  QuantizeArgs a{static_cast<const char*>(x_dev), ldx, (u32)n, d, mx_steps(d), 0, codes_dev, scales_dev, norms_dev};
-  a.wide = aligned_to(x_dev, 8 * esz) && ldx % 8 == 0;
+  QuantizeArgs a{static_cast<const char*>(x_dev), ldx, (u32)n, d, mx_steps(d), codes_dev, scales_dev, norms_dev};
   hipStream_t st = static_cast<hipStream_t>(stream);
   switch (dtype) {
     case ANN_U8: HIP_TRY(launch_quantize<uint8_t>(a, st)); break;
@@ -190,8 +268,8 @@ int ann_mx_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint6
   if (n == 0) return ANN_OK;
   if (!out_dev) return fail(ANN_EINVAL, "null argument");
   if (!aligned_to(out_dev, esz)) return fail(ANN_EINVAL, "out not aligned to its elements");
-  DequantizeArgs a{codes_dev, scales_dev, n * mx_steps(d) * 16, mx_steps(d), d, static_cast<char*>(out_dev), ldo, 0};
-  a.wide = aligned_to(out_dev, 8 * esz) && ldo % 8 == 0;
+  DequantizeArgs a{codes_dev, scales_dev, n, mx_steps(d), d, static_cast<char*>(out_dev), ldo, 0};
+  a.wide = aligned_to(out_dev, 16) && ldo * esz % 16 == 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   switch (dtype) {
     case ANN_F16: HIP_TRY(launch_dequantize<__half>(a, st)); break;
