@@ -16,6 +16,19 @@ constexpr u32 SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr u32 SAMPLE_BINS = 1024;  // one for each thread
 constexpr u32 SAMPLE_FEW = 1024;   // so many kept by top-k are sorted in LDS, and the row is not read again
 
+// What the launches of a divided call know of a row.
+enum SampleKind : u32 {
+  ROW_DONE,  // drawn
+  ROW_CUT,   // kept: above `lowest`, or at it with an id below tie_end
+  ROW_WHOLE  // left to the kernel that takes whole rows
+};
+struct SampleState {
+  u64 tie_end;
+  u64 before, want, total;  // counts or masses: above the bin of the cut, up to the cut, of all candidates
+  float lowest;
+  u32 kind, bin, few;       // few: all candidates up to the bin are listed, not just the bin's
+};
+
 struct SampleArgs {
   const char* scores;
   u64 ld, n;
@@ -25,6 +38,17 @@ struct SampleArgs {
   const float* uniform;
   u32* ids;
   float* logprobs;
+  // Divided rows (chunks > 0): `groups` workgroups for a row, `per` chunks of `chunk` entries each.  Sums are kept for
+  // each chunk, so that they do not depend on how many rows there are.
+  u32 chunks, chunk, groups, per;
+  u32 rules;           // top-k or top-p may be on
+  float* most;         // (rows, chunks): best scores
+  double* others;      // masses other than the best candidates'
+  u32* ones;           // numbers of best candidates
+  u64* hist;           // (rows, SAMPLE_BINS)
+  u64* list;           // (rows, SAMPLE_FEW): candidates around the cut
+  u32* listed;
+  SampleState* state;
 };
 
 constexpr u32 SAMPLE_LEAST = 0x007FFFFFu;  // float_key(-inf): candidates have larger keys
@@ -117,8 +141,8 @@ struct SampleLds {
 };
 
 // sums over the workgroup in a fixed order, the same in every thread: of all, and of this thread's and those before
-template <typename V>
-__device__ V block_scan(V v, SampleLds& s, V* upto) {
+template <typename V, u32 WAVES = SAMPLE_WAVES>
+__device__ V block_scan(V v, u64* words, V* upto) {
   const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
 #pragma unroll
   for (int w = 1; w < 64; w *= 2) {
@@ -126,17 +150,17 @@ __device__ V block_scan(V v, SampleLds& s, V* upto) {
     if (lane >= (u32)w) v += x;
   }
   __syncthreads();
-  if (lane == 63) s.wave[wave] = __builtin_bit_cast(u64, v);
+  if (lane == 63) words[wave] = __builtin_bit_cast(u64, v);
   __syncthreads();
-  V sums = __builtin_bit_cast(V, s.wave[lane % SAMPLE_WAVES]);
+  V sums = __builtin_bit_cast(V, words[lane % WAVES]);
 #pragma unroll
-  for (u32 w = 1; w < SAMPLE_WAVES; w *= 2) {
-    const V x = __shfl_up(sums, w, SAMPLE_WAVES);
-    if (lane % SAMPLE_WAVES >= w) sums += x;
+  for (u32 w = 1; w < WAVES; w *= 2) {
+    const V x = __shfl_up(sums, w, WAVES);
+    if (lane % WAVES >= w) sums += x;
   }
   const V before = __shfl(sums, (int)(wave + 63) % 64);
   *upto = wave ? before + v : v;
-  return __shfl(sums, SAMPLE_WAVES - 1);
+  return __shfl(sums, WAVES - 1);
 }
 
 // s.hist[0 .. size) upwards; size: a power of two
@@ -160,6 +184,118 @@ struct Cut {
   u64 at;    // how many there are, where `ties` is a number
 };
 
+// A row's settings, and what follows from its best score.
+struct RowRules {
+  float temperature, top_p, min_p, per_score;
+  u32 top_k, best;
+  double u, floor_w;
+  Weights w;
+  bool k_on, p_on;
+  __device__ __forceinline__ RowRules(const SampleArgs& a, u64 r, const double* table) {
+    temperature = a.o.temperature_dev ? a.o.temperature_dev[r] : a.o.temperature;
+    top_k = a.o.top_k_dev ? a.o.top_k_dev[r] : a.o.top_k;
+    top_p = a.o.top_p_dev ? a.o.top_p_dev[r] : a.o.top_p;
+    min_p = a.o.min_p_dev ? a.o.min_p_dev[r] : a.o.min_p;
+    k_on = top_k > 0 && top_k < a.n;
+    p_on = top_p > 0.0f && top_p < 1.0f;
+    floor_w = min_p < 1.0f ? static_cast<double>(min_p) : 1.0;
+    u = static_cast<double>(a.uniform[r]);
+    // (1 and above: no running mass exceeds it, so that the last kept one is taken; below 0 and NaN count as 0)
+    u = !(u >= 0.0) ? 0.0 : u < 1.0 ? u : __builtin_inf();
+    // The first histogram is linear in the score, 32 bins for each unit of max(temperature, 1) below the best, the
+    // last one open; equal scores share a bin, and the bins fall with the score.
+    per_score = 32.0f / (temperature > 1.0f ? temperature : 1.0f);
+    w.table = table;
+  }
+  // false: the row has no candidates
+  __device__ __forceinline__ bool set_best(float most) {
+    best = float_key(most);
+    w.most = key_float(best);  // (+0 for -0)
+    // (an infinite temperature has scale 0; next to an infinite best score any other has weight 0 all the same)
+    const bool finite = w.most < __builtin_inff();
+    w.best = finite ? static_cast<double>(w.most) : 1e300;
+    w.scale = finite ? 738.6598609351493 / static_cast<double>(temperature) : 1.0;
+    return best > SAMPLE_LEAST;
+  }
+  // the share of top-p of a mass in whole units
+  __device__ __forceinline__ u64 wanted_mass(u64 total) const {
+    const u64 want = (u64)ceil(static_cast<double>(top_p) * static_cast<double>(total));
+    return want < 1 ? 1 : want > total ? total : want;
+  }
+  __device__ __forceinline__ bool greedy() const { return !(temperature > 0.0f); }
+  __device__ __forceinline__ u32 linear_bin(float v) const {
+    // (the smaller of 1023 and a NaN is 1023: inf * 0, or +inf next to a best of +inf, which is put right)
+    const float z = __builtin_fminf((w.most - v) * per_score, (float)(SAMPLE_BINS - 1));
+    return v == w.most ? 0u : (u32)z;
+  }
+  // The smallest key not below `from` whose weight reaches the floor of min-p.  Weights fall with the key; 64 keys
+  // around the one that the logarithm gives are tried at once, by whole waves.
+  __device__ __forceinline__ u32 min_p_key(u32 from) const {
+    const u32 lane = threadIdx.x % 64;
+    if (w.most < __builtin_inff() && temperature < __builtin_inff()) {
+      const u32 near = float_key(static_cast<float>(w.best + static_cast<double>(temperature) * log(floor_w)));
+      const u32 first = near > from + 32 ? near - 32 : from;
+      if (best >= 63 && first <= best - 63) {
+        const u64 reach = __ballot(w.of(key_float(first + lane)) >= floor_w);
+        if (reach >> 63 && (first == from || !(reach & 1))) return first + (u32)__builtin_ctzll(reach);
+      }
+    }
+    u32 lo = from, hi = best;  // hi reaches it
+    while (lo < hi) {
+      const u32 mid = lo + (hi - lo) / 2;
+      if (w.of(key_float(mid)) >= floor_w)
+        hi = mid;
+      else
+        lo = mid + 1;
+    }
+    return hi;
+  }
+};
+
+// Few candidates, s.hist[0 .. count): those of rank below `limit` by (key downwards, id) are cut by top-p and min-p,
+// sorted by id and drawn from, a thread for each.
+__device__ void draw_few(const SampleArgs& a, u64 r, const RowRules& rules, u64 limit, u32 count, double unit, SampleLds& s) {
+  const u32 tid = threadIdx.x;
+  u32 size = 2;
+  while (size < count) size *= 2;
+  if (tid >= count && tid < size) s.hist[tid] = ~0ull;
+  block_sort(s, size);
+  const bool mine = tid < limit && tid < count;
+  const u64 entry = mine ? s.hist[tid] : 0;
+  const float score = key_float(~(u32)(entry >> 32));
+  const double weight = mine ? rules.w.of(score) : 0.0;
+  u64 upto;
+  const u64 units = mine ? rules.w.units(score, unit) : 0;
+  const u64 total = block_scan<u64>(units, s.wave, &upto);
+  bool keep = mine;
+  if (rules.p_on) keep = keep && upto - units < rules.wanted_mass(total);
+  if (rules.min_p > 0.0f) keep = keep && weight >= rules.floor_w;
+  __syncthreads();
+  if (tid < size) s.hist[tid] = keep ? (entry & 0xFFFFFFFFull) << 32 | tid : ~0ull;
+  s.weight[tid] = __builtin_bit_cast(u64, weight);
+  block_sort(s, size);
+  const bool there = tid < size && s.hist[tid] != ~0ull;
+  const u32 from = there ? (u32)s.hist[tid] : 0;
+  const double x = there ? __builtin_bit_cast(double, s.weight[from]) : 0.0;
+  double run, others;
+  const double sum = block_scan<double>(x, s.wave, &run);
+  // the mass without this one, not as a difference from the whole where it is the best: it may be all the mass
+  const double rest = block_scan<double>(from == 0 ? 0.0 : x, s.wave, &others);
+  const double aim = rules.u * sum;
+  if (tid == 0) s.word = ~0ull, s.count = 0;
+  __syncthreads();
+  if (x > 0.0) {
+    if (run > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
+    atomicMax(&s.count, tid);
+  }
+  __syncthreads();
+  const u32 at = s.word != ~0ull ? (u32)s.word : s.count;
+  if (tid == at) {
+    a.ids[r] = (u32)(s.hist[tid] >> 32);
+    if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((from == 0 ? rest : 1.0 + rest - x) / x));
+  }
+}
+
 // A workgroup per row.  The row is read once for its best score, once to three times for each cut, once for the draw
 // (and a sixteenth of it, and so on, to find the draw's place); all but the first time from the caches.
 template <typename T>
@@ -170,34 +306,36 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
-    const float temperature = a.o.temperature_dev ? a.o.temperature_dev[r] : a.o.temperature;
-    const u32 top_k = a.o.top_k_dev ? a.o.top_k_dev[r] : a.o.top_k;
-    const float top_p = a.o.top_p_dev ? a.o.top_p_dev[r] : a.o.top_p;
-    const float min_p = a.o.min_p_dev ? a.o.min_p_dev[r] : a.o.min_p;
+    if (a.state && a.rules && a.state[r].kind == ROW_DONE) continue;
+    RowRules rules(a, r, s.table);
     auto all = [&](auto f) { each<4>(row, 0, a.n, tid, SAMPLE_THREADS, f); };
     constexpr u32 V = 16 / sizeof(T);
 
     float most = -__builtin_inff();
-    each<8>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
+    if (a.chunks) {
+      if (tid < a.chunks) most = a.most[r * a.chunks + tid];
+    } else {
+      each<8>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
 #pragma unroll
-      for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
-    });
+        for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
+      });
+    }
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w));
     __syncthreads();
     if (lane == 0) s.wave[wave] = __float_as_uint(most);
     __syncthreads();
     for (u32 w = 0; w < SAMPLE_WAVES; ++w) most = __builtin_fmaxf(most, __uint_as_float((u32)s.wave[w]));
-    const u32 best = float_key(most);
-    most = key_float(best);  // (+0 for -0)
-    if (best <= SAMPLE_LEAST) {  // (the same in all threads)
+    if (!rules.set_best(most)) {  // (the same in all threads)
       if (tid == 0) {
         a.ids[r] = ANN_NONE;
         if (a.logprobs) a.logprobs[r] = -__builtin_inff();
       }
       continue;
     }
-    if (!(temperature > 0.0f)) {
+    const u32 best = rules.best;
+    most = rules.w.most;
+    if (rules.greedy()) {
       if (tid == 0) s.word = ~0ull;
       __syncthreads();
       u64 first = ~0ull;
@@ -214,24 +352,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       }
       continue;
     }
-    Weights w;
-    // (an infinite temperature has scale 0; next to an infinite best score any other has weight 0 all the same)
-    const bool finite = most < __builtin_inff();
-    w.most = most;
-    w.best = finite ? static_cast<double>(most) : 1e300;
-    w.scale = finite ? 738.6598609351493 / static_cast<double>(temperature) : 1.0;
-    w.table = s.table;
+    const Weights& w = rules.w;
     const double unit = ldexp(1.0, (int)a.unit);
     Cut cut = {SAMPLE_LEAST + 1, ~0ull, ~0ull};
 
-    // The first histogram is linear in the score, 32 bins for each unit of max(temperature, 1) below the best, the
-    // last one open; equal scores share a bin, and the bins fall with the score.
-    const float per_score = 32.0f / (temperature > 1.0f ? temperature : 1.0f);
-    auto linear_bin = [&](float v) {
-      // (the smaller of 1023 and a NaN is 1023: inf * 0, or +inf next to a best of +inf, which is put right)
-      const float z = __builtin_fminf((most - v) * per_score, (float)(SAMPLE_BINS - 1));
-      return v == most ? 0u : (u32)z;
-    };
     // Finds the key at which the running count (or mass), from the best key down, reaches `aim(total)`; candidates
     // below floor.key do not count, and of those at it floor.ties do.  False: the total is 0 or below the aim.
     auto select = [&](const Cut& floor, bool mass, auto aim, Cut* found, u64* rest) -> bool {
@@ -257,7 +381,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll
             for (u32 e = 0; e < V; ++e)
               if (in[e])
-                atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[first ? linear_bin(v[e]) : (hi - float_key(v[e])) >> shift]),
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[first ? rules.linear_bin(v[e]) : (hi - float_key(v[e])) >> shift]),
                           (unsigned long long)(masses ? w.in_units(v[e] == most ? 1.0 : raw[e], unit) : 1ull));
           });
         };
@@ -267,11 +391,11 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           mass ? count(False(), True()) : count(False(), False());
         __syncthreads();
         if (tid == 0 && some_ties && floor.key >= lo)
-          s.hist[level ? (hi - floor.key) >> shift : linear_bin(key_float(floor.key))] += floor.ties * w.units(key_float(floor.key), unit);
+          s.hist[level ? (hi - floor.key) >> shift : rules.linear_bin(key_float(floor.key))] += floor.ties * w.units(key_float(floor.key), unit);
         __syncthreads();
         const u64 mine = s.hist[tid];
         u64 upto;
-        const u64 total = block_scan<u64>(mine, s, &upto);
+        const u64 total = block_scan<u64>(mine, s.wave, &upto);
         if (level == 0) {
           want = aim(total);
           if (want == 0 || want > total) return false;
@@ -286,7 +410,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           u32 x = lo, y = hi;
           while (x < y) {  // the largest key whose bin is b or above
             const u32 mid = x + (y - x + 1) / 2;
-            if (linear_bin(key_float(mid)) >= b)
+            if (rules.linear_bin(key_float(mid)) >= b)
               x = mid;
             else
               y = mid - 1;
@@ -295,7 +419,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
           x = lo, y = top;
           while (x < y) {  // the smallest key whose bin is b
             const u32 mid = x + (y - x) / 2;
-            if (linear_bin(key_float(mid)) <= b)
+            if (rules.linear_bin(key_float(mid)) <= b)
               y = mid;
             else
               x = mid + 1;
@@ -319,104 +443,80 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       }
     };
 
-    if (top_k > 0 && top_k < a.n) {
-      Cut found;
-      u64 ties;
-      if (select(cut, false, [&](u64 total) { return (u64)top_k < total ? (u64)top_k : 0; }, &found, &ties)) {
-        cut = found;
-        cut.ties = ties;
-      }
-    }
-    double u = static_cast<double>(a.uniform[r]);
-    // (1 and above: no running mass exceeds it, so that the last kept one is taken; below 0 and NaN count as 0)
-    u = !(u >= 0.0) ? 0.0 : u < 1.0 ? u : __builtin_inf();
-    const double floor_w = min_p < 1.0f ? static_cast<double>(min_p) : 1.0;
-
-    if (cut.ties != ~0ull && top_k - cut.ties + cut.at <= SAMPLE_FEW) {
-      // Few: sorted by (key downwards, id), cut, then sorted by id and drawn from, a thread for each.
-      __syncthreads();
-      if (tid == 0) s.count = 0;
-      __syncthreads();
-      const float lowest = key_float(cut.key);
-      all([&](u64 i, const float (&v)[V]) {
-#pragma unroll
-        for (u32 e = 0; e < V; ++e)
-          if (v[e] >= lowest) s.hist[atomicAdd(&s.count, 1u)] = (u64)~float_key(v[e]) << 32 | (i + e);
-      });
-      __syncthreads();
-      u32 size = 2;
-      while (size < s.count) size *= 2;
-      if (tid >= s.count && tid < size) s.hist[tid] = ~0ull;
-      block_sort(s, size);
-      const bool mine = tid < top_k;
-      const u64 entry = mine ? s.hist[tid] : 0;
-      const float score = key_float(~(u32)(entry >> 32));
-      const double weight = mine ? w.of(score) : 0.0;
-      u64 upto;
-      const u64 units = mine ? w.units(score, unit) : 0;
-      const u64 total = block_scan<u64>(units, s, &upto);
-      bool keep = mine;
-      if (top_p > 0.0f && top_p < 1.0f) keep = keep && (tid == 0 || (double)(upto - units) < static_cast<double>(top_p) * static_cast<double>(total));
-      if (min_p > 0.0f) keep = keep && weight >= floor_w;
-      __syncthreads();
-      if (tid < size) s.hist[tid] = keep ? (entry & 0xFFFFFFFFull) << 32 | tid : ~0ull;
-      s.weight[tid] = __builtin_bit_cast(u64, weight);
-      block_sort(s, size);
-      const bool there = tid < size && s.hist[tid] != ~0ull;
-      const u32 from = there ? (u32)s.hist[tid] : 0;
-      const double x = there ? __builtin_bit_cast(double, s.weight[from]) : 0.0;
-      double run, others;
-      const double sum = block_scan<double>(x, s, &run);
-      // the mass without this one, not as a difference from the whole where it is the best: it may be all the mass
-      double rest = block_scan<double>(from == 0 ? 0.0 : x, s, &others);
-      const double aim = u * sum;
+    u64 tie_end = a.n;
+    float lowest = key_float(cut.key);
+    u64 lo = 0, hi = a.n;
+    double others = 0.0, bests = 0.0, aim = 0.0;
+    if (a.chunks && (!a.rules || a.state[r].kind == ROW_CUT)) {
+      // The masses of the row's chunks are there: the one that holds the draw.
+      if (a.rules)
+        tie_end = a.state[r].tie_end, lowest = a.state[r].lowest;
+      else if (rules.min_p > 0.0f)
+        lowest = key_float(rules.min_p_key(cut.key));
+      const bool chunk = tid < a.chunks;
+      const double other = chunk ? a.others[r * a.chunks + tid] : 0.0, one = chunk ? a.ones[r * a.chunks + tid] : 0.0;
+      double upto;
+      others = block_scan<double>(other, s.wave, &upto);
+      bests = block_scan<double>(one, s.wave, &upto);
+      const double mass = other + one;
+      block_scan<double>(mass, s.wave, &upto);
+      aim = rules.u * (bests + others);
       if (tid == 0) s.word = ~0ull, s.count = 0;
       __syncthreads();
-      if (x > 0.0) {
-        if (run > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
+      if (mass > 0.0) {
+        if (upto > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
         atomicMax(&s.count, tid);
       }
       __syncthreads();
       const u32 at = s.word != ~0ull ? (u32)s.word : s.count;
-      if (tid == at) {
-        a.ids[r] = (u32)(s.hist[tid] >> 32);
-        if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((from == 0 ? rest : 1.0 + rest - x) / x));
+      __syncthreads();
+      if (tid == at) s.word = __builtin_bit_cast(u64, upto - mass);
+      __syncthreads();
+      aim -= at ? __builtin_bit_cast(double, s.word) : 0.0;
+      lo = (u64)at * a.chunk;
+      hi = min(a.n, lo + a.chunk);
+    } else {
+      if (rules.k_on) {
+        Cut found;
+        u64 ties;
+        if (select(cut, false, [&](u64 total) { return (u64)rules.top_k < total ? (u64)rules.top_k : 0; }, &found, &ties)) {
+          cut = found;
+          cut.ties = ties;
+        }
       }
-      continue;
-    }
-
-    if (top_p > 0.0f && top_p < 1.0f) {
-      Cut found;
-      u64 left;
-      if (select(cut, true,
-                 [&](u64 total) {
-                   const u64 aim = (u64)ceil(static_cast<double>(top_p) * static_cast<double>(total));
-                   return aim < 1 ? 1 : aim > total ? total : aim;
-                 },
-                 &found, &left)) {
-        const u64 each_one = w.units(key_float(found.key), unit);
-        const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull, at = each_one ? found.at / each_one : ~0ull;
-        if (found.key != cut.key || cut.ties == ~0ull)
-          cut = {found.key, need, at};
-        else if (need < cut.ties)  // (`at` of top-k counts the ones that it dropped as well)
-          cut.ties = need;
+      if (cut.ties != ~0ull && rules.top_k - cut.ties + cut.at <= SAMPLE_FEW) {
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        lowest = key_float(cut.key);
+        all([&](u64 i, const float (&v)[V]) {
+#pragma unroll
+          for (u32 e = 0; e < V; ++e)
+            if (v[e] >= lowest) s.hist[atomicAdd(&s.count, 1u)] = (u64)~float_key(v[e]) << 32 | (i + e);
+        });
+        __syncthreads();
+        draw_few(a, r, rules, rules.top_k, s.count, unit, s);
+        continue;
       }
-    }
-    if (min_p > 0.0f) {
-      // weights fall with the key: the smallest key whose weight reaches the floor
-      u32 lo = cut.key, hi = best;  // hi reaches it
-      while (lo < hi) {
-        const u32 mid = lo + (hi - lo) / 2;
-        if (w.of(key_float(mid)) >= floor_w)
-          hi = mid;
-        else
-          lo = mid + 1;
+      if (rules.p_on) {
+        Cut found;
+        u64 left;
+        if (select(cut, true, [&](u64 total) { return rules.wanted_mass(total); }, &found, &left)) {
+          const u64 each_one = w.units(key_float(found.key), unit);
+          const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull, at = each_one ? found.at / each_one : ~0ull;
+          if (found.key != cut.key || cut.ties == ~0ull)
+            cut = {found.key, need, at};
+          else if (need < cut.ties)  // (`at` of top-k counts the ones that it dropped as well)
+            cut.ties = need;
+        }
       }
-      if (hi > cut.key) cut.key = hi, cut.ties = ~0ull;
+      if (rules.min_p > 0.0f) {
+        const u32 key = rules.min_p_key(cut.key);
+        if (key > cut.key) cut.key = key, cut.ties = ~0ull;
+      }
+      lowest = key_float(cut.key);
     }
     // Where only some of those at the cut are kept, they are the first ones by id: those below `tie_end`.
-    u64 tie_end = a.n;
-    const float lowest = key_float(cut.key);
     if (cut.ties < cut.at) {
       // narrowed down like the draw below: runs of the span, counted by a wave each
       u64 lo = 0, hi = a.n, before = 0;
@@ -441,17 +541,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       const u64 i = lo + tid;
       const u64 tie = i < hi && mx_float(row[i]) == lowest;
       u64 upto;
-      block_scan<u64>(tie, s, &upto);
+      block_scan<u64>(tie, s.wave, &upto);
       if (tie && before + upto - 1 == cut.ties) s.word = i;
       __syncthreads();
       tie_end = s.word;
     }
     // The draw: the span that holds it is dealt to the waves in runs, whose masses tell which run it is.  The best
     // candidates' weights, 1 each, are kept apart, so that a mass that is nearly all the drawn one's loses nothing.
-    u64 lo = 0, hi = a.n;
-    double others = 0.0, bests = 0.0, aim = 0.0;
-    while (true) {
-      const bool whole = lo == 0 && hi == a.n;
+    bool whole = !a.chunks || (a.rules && a.state[r].kind != ROW_CUT);
+    while (whole || hi - lo > SAMPLE_THREADS) {
       u64 run = (hi - lo + SAMPLE_WAVES - 1) / SAMPLE_WAVES;
       run = (run + 63) / 64 * 64;
       const u64 from = min(hi, lo + wave * run), to = min(hi, from + run);
@@ -486,7 +584,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
         others = rest, bests = one;
 #pragma unroll
         for (int v = 1; v < (int)SAMPLE_WAVES; v *= 2) others += __shfl_xor(others, v, SAMPLE_WAVES), bests += __shfl_xor(bests, v, SAMPLE_WAVES);
-        aim = u * (bests + others);
+        aim = rules.u * (bests + others);
+        whole = false;
       }
       const double mass = rest + one;
       double upto = mass;
@@ -502,14 +601,13 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       aim -= at ? before : 0.0;
       lo += at * run;
       hi = min(hi, lo + run);
-      if (hi - lo <= SAMPLE_THREADS) break;
     }
     // the last span, a thread for each entry
     const u64 i = lo + tid;
     const float v = i < hi ? mx_float(row[i]) : -__builtin_inff();
     const double mine = v > lowest || (v == lowest && i < tie_end) ? w.of(v) : 0.0;
     double run;
-    block_scan<double>(mine, s, &run);
+    block_scan<double>(mine, s.wave, &run);
     if (tid == 0) s.word = ~0ull, s.count = 0;
     __syncthreads();
     if (mine > 0.0) {
@@ -524,6 +622,310 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   }
 }
 
+
+// Divided rows: where rows are long and few, several workgroups share each.  One launch takes the chunks' best scores,
+// one their histograms (added up per row: whole numbers), one lists the candidates around the cut, one finds the cut
+// from these or, where top-k keeps few, draws, one takes the chunks' masses, and the kernel above draws.  Rows whose
+// cut needs more than the list holds are left to that kernel whole.
+constexpr u32 SPLIT_THREADS = 256;
+constexpr u32 SPLIT_CHUNKS = 256;  // most of a row
+constexpr u32 SPLIT_CHUNK = 4096;  // entries of one, where a row has no more than 256 of that size
+
+struct SplitLds {
+  u64 hist[SAMPLE_BINS];
+  double table[TABLE];
+  u64 wave[SPLIT_THREADS / 64];
+  u64 word[3];
+};
+
+struct Part {  // of a row: what a workgroup takes
+  u64 r, from, to;
+  u32 group, c0, c1;
+  __device__ __forceinline__ explicit Part(const SampleArgs& a) {
+    r = blockIdx.x / a.groups;
+    group = blockIdx.x % a.groups;
+    c0 = min(group * a.per, a.chunks), c1 = min(c0 + a.per, a.chunks);
+    from = (u64)c0 * a.chunk, to = min(a.n, (u64)c1 * a.chunk);
+  }
+};
+
+__device__ __forceinline__ float split_max(float v, u64* words) {
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) v = __builtin_fmaxf(v, __shfl_xor(v, w));
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) words[threadIdx.x / 64] = __float_as_uint(v);
+  __syncthreads();
+#pragma unroll
+  for (u32 w = 0; w < SPLIT_THREADS / 64; ++w) v = __builtin_fmaxf(v, __uint_as_float((u32)words[w]));
+  return v;
+}
+__device__ __forceinline__ float row_best(const SampleArgs& a, u64 r, u64* words) {
+  return split_max(threadIdx.x < a.chunks ? a.most[r * a.chunks + threadIdx.x] : -__builtin_inff(), words);
+}
+
+template <typename T>
+__global__ __launch_bounds__(SPLIT_THREADS) void sample_best_kernel(SampleArgs a) {
+  __shared__ u64 words[SPLIT_THREADS / 64];
+  constexpr u32 V = 16 / sizeof(T);
+  const Part p(a);
+  const T* row = reinterpret_cast<const T*>(a.scores) + p.r * a.ld;
+  for (u32 c = p.c0; c < p.c1; ++c) {
+    float most = -__builtin_inff();
+    each<4>(row, (u64)c * a.chunk, min(a.n, (u64)(c + 1) * a.chunk), threadIdx.x, SPLIT_THREADS, [&](u64, const float (&v)[V]) {
+#pragma unroll
+      for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
+    });
+    most = split_max(most, words);
+    if (threadIdx.x == 0) a.most[p.r * a.chunks + c] = most;
+  }
+  if (a.rules) {  // clears the row's histogram, a share each
+    for (u32 b = p.group * SPLIT_THREADS + threadIdx.x; b < SAMPLE_BINS; b += a.groups * SPLIT_THREADS) a.hist[p.r * SAMPLE_BINS + b] = 0;
+    if (p.group == 0 && threadIdx.x == 0) a.listed[p.r] = 0;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(SPLIT_THREADS) void sample_hist_kernel(SampleArgs a) {
+  __shared__ SplitLds s;
+  constexpr u32 V = 16 / sizeof(T);
+  const u32 tid = threadIdx.x;
+  const Part p(a);
+  const T* row = reinterpret_cast<const T*>(a.scores) + p.r * a.ld;
+  RowRules rules(a, p.r, s.table);
+  if (!rules.set_best(row_best(a, p.r, s.wave)) || rules.greedy() || !(rules.k_on || rules.p_on)) return;
+  const bool masses = !rules.k_on;
+  if (masses)
+    for (u32 i = tid; i < TABLE; i += SPLIT_THREADS) s.table[i] = exp2(i / (double)TABLE);
+  for (u32 b = tid; b < SAMPLE_BINS; b += SPLIT_THREADS) s.hist[b] = 0;
+  __syncthreads();
+  const double unit = ldexp(1.0, (int)a.unit);
+  const float most = rules.w.most;
+  auto count = [&](auto of_masses) {
+    each<4>(row, p.from, p.to, tid, SPLIT_THREADS, [&](u64, const float (&v)[V]) {
+      double raw[V];
+      if (of_masses)
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) raw[e] = rules.w.raw(v[e]), taken(raw[e]);
+#pragma unroll
+      for (u32 e = 0; e < V; ++e)
+        if (v[e] > -__builtin_inff())
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[rules.linear_bin(v[e])]),
+                    (unsigned long long)(of_masses ? rules.w.in_units(v[e] == most ? 1.0 : raw[e], unit) : 1ull));
+    });
+  };
+  masses ? count(True()) : count(False());
+  __syncthreads();
+  for (u32 b = tid; b < SAMPLE_BINS; b += SPLIT_THREADS)
+    if (s.hist[b]) atomicAdd(reinterpret_cast<unsigned long long*>(&a.hist[p.r * SAMPLE_BINS + b]), (unsigned long long)s.hist[b]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(SPLIT_THREADS) void sample_list_kernel(SampleArgs a) {
+  __shared__ SplitLds s;
+  constexpr u32 V = 16 / sizeof(T), BINS = SAMPLE_BINS / SPLIT_THREADS;
+  const u32 tid = threadIdx.x;
+  const Part p(a);
+  const T* row = reinterpret_cast<const T*>(a.scores) + p.r * a.ld;
+  RowRules rules(a, p.r, nullptr);
+  SampleState state{};
+  state.kind = ROW_CUT;
+  state.bin = ~0u;
+  if (rules.set_best(row_best(a, p.r, s.wave)) && !rules.greedy() && (rules.k_on || rules.p_on)) {
+    u64 bin[BINS], mine = 0, upto;
+#pragma unroll
+    for (u32 i = 0; i < BINS; ++i) mine += bin[i] = a.hist[p.r * SAMPLE_BINS + tid * BINS + i];
+    const u64 total = block_scan<u64, SPLIT_THREADS / 64>(mine, s.wave, &upto);
+    const u64 want = !rules.k_on ? rules.wanted_mass(total) : rules.top_k < total ? rules.top_k : 0;
+    if (want == 0) {
+      // top-k drops nothing; what top-p keeps then needs masses that were not counted
+      if (rules.p_on) state.kind = ROW_WHOLE;
+    } else {
+      u64 before = upto - mine;
+#pragma unroll
+      for (u32 i = 0; i < BINS; ++i) {
+        if (before < want && before + bin[i] >= want) s.word[0] = tid * BINS + i, s.word[1] = before, s.word[2] = bin[i];
+        before += bin[i];
+      }
+      __syncthreads();
+      state.bin = (u32)s.word[0], state.before = s.word[1], state.want = want, state.total = total;
+      const u64 in_bin = s.word[2];
+      if (rules.k_on) {
+        state.few = state.before + in_bin <= SAMPLE_FEW;
+        if (!state.few && (in_bin > SAMPLE_FEW || rules.p_on)) state.kind = ROW_WHOLE;
+      }
+      if (state.kind == ROW_CUT)
+        each<4>(row, p.from, p.to, tid, SPLIT_THREADS, [&](u64 i, const float (&v)[V]) {
+#pragma unroll
+          for (u32 e = 0; e < V; ++e) {
+            const u32 b = rules.linear_bin(v[e]);
+            if (v[e] > -__builtin_inff() && (b == state.bin || (state.few && b < state.bin))) {
+              const u32 at = atomicAdd(&a.listed[p.r], 1u);
+              if (at < SAMPLE_FEW) a.list[p.r * SAMPLE_FEW + at] = (u64)~float_key(v[e]) << 32 | (i + e);
+            }
+          }
+        });
+    }
+  }
+  if (p.group == 0 && tid == 0) a.state[p.r] = state;
+}
+
+template <typename T>
+__global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a) {
+  __shared__ SampleLds s;
+  const u32 tid = threadIdx.x;
+  const u64 r = blockIdx.x;
+  SampleState state = a.state[r];
+  if (state.kind != ROW_CUT) return;
+  if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
+  RowRules rules(a, r, s.table);
+  float most = tid < a.chunks ? a.most[r * a.chunks + tid] : -__builtin_inff();
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w));
+  if (tid % 64 == 0) s.wave[tid / 64] = __float_as_uint(most);
+  __syncthreads();
+  for (u32 w = 0; w < SAMPLE_WAVES; ++w) most = __builtin_fmaxf(most, __uint_as_float((u32)s.wave[w]));
+  __syncthreads();
+  if (!rules.set_best(most) || rules.greedy()) {  // (the kernel for whole rows has these)
+    if (tid == 0) a.state[r].kind = ROW_WHOLE;
+    return;
+  }
+  u32 lowest = SAMPLE_LEAST + 1;
+  state.tie_end = a.n;
+  if (state.bin != ~0u) {
+    const u32 count = a.listed[r];
+    if (count > SAMPLE_FEW) {
+      if (tid == 0) a.state[r].kind = ROW_WHOLE;
+      return;
+    }
+    if (tid < count) s.hist[tid] = a.list[r * SAMPLE_FEW + tid];
+    const double unit = ldexp(1.0, (int)a.unit);
+    __syncthreads();
+    if (rules.k_on && state.few) {
+      draw_few(a, r, rules, rules.top_k, count, unit, s);
+      if (tid == 0) a.state[r].kind = ROW_DONE;
+      return;
+    }
+    u32 size = 2;
+    while (size < count) size *= 2;
+    if (tid >= count && tid < size) s.hist[tid] = ~0ull;
+    block_sort(s, size);
+    const u64 entry = tid < count ? s.hist[tid] : 0;
+    const u64 amount = tid >= count ? 0 : rules.k_on ? 1 : rules.w.units(key_float(~(u32)(entry >> 32)), unit);
+    u64 upto;
+    block_scan<u64>(amount, s.wave, &upto);
+    // the last one kept: the first at which the count (or mass) is reached
+    if (tid < count && state.before + upto - amount < state.want && state.before + upto >= state.want) s.word = entry;
+    __syncthreads();
+    lowest = ~(u32)(s.word >> 32);
+    state.tie_end = (s.word & 0xFFFFFFFFull) + 1;
+  }
+  if (rules.min_p > 0.0f) {
+    const u32 key = rules.min_p_key(lowest);
+    if (key > lowest) lowest = key, state.tie_end = a.n;
+  }
+  if (tid == 0) {
+    state.lowest = key_float(lowest);
+    a.state[r] = state;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(SPLIT_THREADS) void sample_mass_kernel(SampleArgs a) {
+  __shared__ SplitLds s;
+  constexpr u32 V = 16 / sizeof(T);
+  const u32 tid = threadIdx.x;
+  const Part p(a);
+  if (a.rules && a.state[p.r].kind != ROW_CUT) return;
+  const T* row = reinterpret_cast<const T*>(a.scores) + p.r * a.ld;
+  for (u32 i = tid; i < TABLE; i += SPLIT_THREADS) s.table[i] = exp2(i / (double)TABLE);
+  RowRules rules(a, p.r, s.table);
+  if (!rules.set_best(row_best(a, p.r, s.wave)) || rules.greedy()) return;
+  float lowest = key_float(SAMPLE_LEAST + 1);
+  u64 tie_end = a.n;
+  if (a.rules)
+    lowest = a.state[p.r].lowest, tie_end = a.state[p.r].tie_end;
+  else if (rules.min_p > 0.0f)
+    lowest = key_float(rules.min_p_key(SAMPLE_LEAST + 1));
+  const Weights& w = rules.w;
+  const float most = w.most;
+  for (u32 c = p.c0; c < p.c1; ++c) {
+    double mine = 0.0;
+    u32 ones = 0;
+    each<4>(row, (u64)c * a.chunk, min(a.n, (u64)(c + 1) * a.chunk), tid, SPLIT_THREADS, [&](u64 i, const float (&v)[V]) {
+      bool keep[V], any = false;
+#pragma unroll
+      for (u32 e = 0; e < V; ++e) {
+        keep[e] = v[e] >= lowest;
+        if (v[e] == lowest) keep[e] = i + e < tie_end;
+        any |= keep[e];
+      }
+      if (!any) return;
+      double raw[V];
+#pragma unroll
+      for (u32 e = 0; e < V; ++e) raw[e] = w.raw(keep[e] && v[e] != most ? v[e] : -__builtin_inff()), taken(raw[e]);
+#pragma unroll
+      for (u32 e = 0; e < V; ++e) {
+        ones += keep[e] && v[e] == most;
+        mine += raw[e] > 1e-300 ? raw[e] : 0.0;
+      }
+    });
+    u64 one_upto;
+    double upto;
+    const double sum = block_scan<double, SPLIT_THREADS / 64>(mine, s.wave, &upto);
+    const u64 one = block_scan<u64, SPLIT_THREADS / 64>(ones, s.wave, &one_upto);
+    if (tid == 0) a.others[p.r * a.chunks + c] = sum, a.ones[p.r * a.chunks + c] = (u32)one;
+  }
+}
+
+// Rows from SPLIT_LEAST entries on, in calls of up to SPLIT_ROWS rows.
+constexpr u64 SPLIT_LEAST = 16384, SPLIT_ROWS = 4096;
+
+// fills in what a divided call needs and returns its scratch, or 0 where rows are taken whole
+u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
+  a.chunks = 0;
+  if (n < SPLIT_LEAST || rows > SPLIT_ROWS) return 0;
+  u64 chunk = SPLIT_CHUNK;
+  while ((n + chunk - 1) / chunk > SPLIT_CHUNKS) chunk *= 2;
+  a.chunk = (u32)chunk;
+  a.chunks = (u32)((n + chunk - 1) / chunk);
+  // some two thousand workgroups
+  const u64 groups = (2048 + rows - 1) / rows;
+  a.per = (u32)(groups >= a.chunks ? 1 : (a.chunks + groups - 1) / groups);
+  a.groups = (a.chunks + a.per - 1) / a.per;
+  u64 at = 0;
+  auto take = [&](u64 bytes) {
+    const u64 from = at;
+    at += (bytes + 15) / 16 * 16;
+    return scratch + from;
+  };
+  a.hist = reinterpret_cast<u64*>(take(rows * SAMPLE_BINS * 8));
+  a.list = reinterpret_cast<u64*>(take(rows * SAMPLE_FEW * 8));
+  a.state = reinterpret_cast<SampleState*>(take(rows * sizeof(SampleState)));
+  a.others = reinterpret_cast<double*>(take(rows * a.chunks * 8));
+  a.ones = reinterpret_cast<u32*>(take(rows * a.chunks * 4));
+  a.most = reinterpret_cast<float*>(take(rows * a.chunks * 4));
+  a.listed = reinterpret_cast<u32*>(take(rows * 4));
+  return at;
+}
+
+template <typename T>
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
+  if (a.chunks) {
+    const dim3 parts(a.rows * a.groups), threads(SPLIT_THREADS);
+    hipLaunchKernelGGL(sample_best_kernel<T>, parts, threads, 0, s, a);
+    if (a.rules) {
+      hipLaunchKernelGGL(sample_hist_kernel<T>, parts, threads, 0, s, a);
+      hipLaunchKernelGGL(sample_list_kernel<T>, parts, threads, 0, s, a);
+      hipLaunchKernelGGL(sample_cut_kernel<T>, dim3(a.rows), dim3(SAMPLE_THREADS), 0, s, a);
+    }
+    hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(sample_kernel<T>, dim3(a.rows < (1u << 20) ? a.rows : (1u << 20)), dim3(SAMPLE_THREADS), 0, s, a);
+  return hipGetLastError();
+}
+
 }  // namespace annmi
 
 using namespace annmi;
@@ -533,7 +935,8 @@ extern "C" {
 int ann_sample_scratch(uint64_t rows, uint64_t n, uint64_t* bytes) try {
   if (!bytes) return fail(ANN_EINVAL, "null argument");
   if (rows > MX_MOST_ROWS || n < 1 || n > MX_MOST_ROWS) return fail(ANN_EINVAL, "ann_sample: n must be at least 1, rows and n below 2^31");
-  *bytes = 0;
+  SampleArgs a{};
+  *bytes = plan_split(a, rows, n, nullptr);
   return ANN_OK;
 } catch (...) {
   return annmi::on_exception();
@@ -569,15 +972,16 @@ int ann_sample(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtyp
   a.logprobs = logprobs_dev;
   if (!aligned_to(a.o.temperature_dev, 4) || !aligned_to(a.o.top_k_dev, 4) || !aligned_to(a.o.top_p_dev, 4) || !aligned_to(a.o.min_p_dev, 4))
     return fail(ANN_EINVAL, "settings not aligned to their elements");
+  plan_split(a, rows, n, static_cast<char*>(scratch_dev));
+  // top-k and top-p are off for all rows where single values say so
+  a.rules = a.o.top_k_dev || a.o.top_p_dev || (a.o.top_k > 0 && a.o.top_k < n) || (a.o.top_p > 0.0f && a.o.top_p < 1.0f);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid((u32)(rows < (1u << 20) ? rows : (1u << 20)));
   if (dtype == ANN_F16)
-    hipLaunchKernelGGL(sample_kernel<__half>, grid, dim3(SAMPLE_THREADS), 0, st, a);
+    HIP_TRY(launch_sample<__half>(a, st));
   else if (dtype == ANN_BF16)
-    hipLaunchKernelGGL(sample_kernel<__bf16>, grid, dim3(SAMPLE_THREADS), 0, st, a);
+    HIP_TRY(launch_sample<__bf16>(a, st));
   else
-    hipLaunchKernelGGL(sample_kernel<float>, grid, dim3(SAMPLE_THREADS), 0, st, a);
-  HIP_TRY(hipGetLastError());
+    HIP_TRY(launch_sample<float>(a, st));
   return ANN_OK;
 } catch (...) {
   return annmi::on_exception();

@@ -56,6 +56,52 @@ def test_long_rows(env, rows, n):
         check(torch, A, scores_of(torch, rng, rows, n, dtype), uniform(torch, rng, rows), **rule)
 
 
+@pytest.mark.parametrize("dtype", ("float32", "float16", "bfloat16"))
+@pytest.mark.parametrize("rows,n", [(1, 16_384), (3, 16_383), (5, 20_001), (2, 70_003), (1, 1_100_000)])
+def test_rules_on_long_rows(env, dtype, rows, n):
+    """Rows that several workgroups share, and just shorter ones."""
+    torch, A, _ = env
+    rng = np.random.default_rng(rows * n)
+    for i, rule in enumerate(RULES + (dict(top_k=2000), dict(top_k=900, top_p=0.7), dict(top_k=5000, min_p=0.001), dict(top_k=3000, top_p=0.5))):
+        if n > 10 ** 6 and i % 3:
+            continue
+        z = scores_of(torch, rng, rows, n, dtype, masked=(0.0, 0.3, 0.97)[i % 3])
+        check(torch, A, z, uniform(torch, rng, rows), **rule)
+
+
+def test_settings_of_each_long_row(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(15)
+    rows, n = 60, 17_001
+    t = dev(torch, rng.choice([0.0, 0.3, 1.0, 2.0, -1.0], rows).astype(np.float32))
+    k = dev(torch, rng.choice([0, 1, 7, 500, 1024, 1025, 17_000, 100_000], rows).astype(np.int32))
+    p = dev(torch, rng.choice([0.0, 0.2, 0.9, 1.0, 2.0], rows).astype(np.float32))
+    m = dev(torch, rng.choice([0.0, 0.001, 0.2, 1.0], rows).astype(np.float32))
+    for dtype in ("float32", "bfloat16"):
+        z = scores_of(torch, rng, rows, n, dtype, 0.1)
+        z[3] = -float("inf")
+        z[4, 100:] = -float("inf")
+        z[5] = 2.0
+        z[6, ::3] = 5.0
+        z[7, 1000] = float("inf")
+        z[8, ::2] = float("nan")
+        check(torch, A, z, uniform(torch, rng, rows), temperature=t, top_k=k, top_p=p, min_p=m)
+        # equal scores around every cut
+        z = torch.round(scores_of(torch, rng, rows, n, dtype)).to(z.dtype)
+        check(torch, A, z, uniform(torch, rng, rows), temperature=t, top_k=k, top_p=p, min_p=m)
+
+
+def test_draws_do_not_depend_on_the_other_rows(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(16)
+    z, u = scores_of(torch, rng, 700, 20_000, "bfloat16"), uniform(torch, rng, 700)
+    for rule in ({}, dict(top_p=0.8), dict(top_k=30), dict(min_p=0.02)):
+        ids, logprobs = A.ann_sample(z, u, **rule)
+        for lo, hi in ((0, 1), (3, 5), (100, 400)):
+            i, lp = A.ann_sample(z[lo:hi], u[lo:hi].contiguous(), **rule)
+            assert torch.equal(i, ids[lo:hi]) and torch.equal(lp, logprobs[lo:hi])
+
+
 def test_settings_of_each_row(env):
     torch, A, _ = env
     rng = np.random.default_rng(5)
