@@ -42,6 +42,7 @@ struct SampleArgs {
   // each chunk, so that they do not depend on how many rows there are.
   u32 chunks, chunk, groups, per;
   u32 rules;           // top-k or top-p may be on
+  u32 no_mass;         // rows that are not drawn from their lists are left whole
   float* most;         // (rows, chunks): best scores
   double* others;      // masses other than the best candidates'
   u32* ones;           // numbers of best candidates
@@ -163,18 +164,28 @@ __device__ V block_scan(V v, u64* words, V* upto) {
   return __shfl(sums, WAVES - 1);
 }
 
-// s.hist[0 .. size) upwards; size: a power of two
+// s.hist[0 .. size) upwards, size a power of two of at most a thread each: exchanges inside a wave by shuffles, the
+// others through LDS
 __device__ void block_sort(SampleLds& s, u32 size) {
+  const u32 i = threadIdx.x;
+  __syncthreads();
+  u64 mine = i < size ? s.hist[i] : ~0ull;
   for (u32 run = 2; run <= size; run *= 2)
     for (u32 gap = run / 2; gap > 0; gap /= 2) {
-      __syncthreads();
-      const u32 i = threadIdx.x;
-      if (i < size / 2) {
-        const u32 lo = i / gap * 2 * gap + i % gap, hi = lo + gap;
-        const u64 x = s.hist[lo], y = s.hist[hi];
-        if ((x > y) == ((lo & run) == 0)) s.hist[lo] = y, s.hist[hi] = x;
+      u64 other;
+      if (gap >= 64) {
+        __syncthreads();
+        if (i < size) s.hist[i] = mine;
+        __syncthreads();
+        other = i < size ? s.hist[i ^ gap] : ~0ull;
+      } else {
+        other = __shfl_xor(mine, (int)gap);
       }
+      const bool up = (i & run) == 0, low = (i & gap) == 0;
+      mine = up == low ? min(mine, other) : max(mine, other);
     }
+  __syncthreads();
+  if (i < size) s.hist[i] = mine;
   __syncthreads();
 }
 
@@ -306,7 +317,14 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
-    if (a.state && a.rules && a.state[r].kind == ROW_DONE) continue;
+    SampleState state{};
+    state.kind = a.chunks ? ROW_CUT : ROW_WHOLE;
+    double other = 0.0, one = 0.0;
+    if (a.chunks) {
+      if (a.rules) state = a.state[r];
+      if (tid < a.chunks) other = a.others[r * a.chunks + tid], one = a.ones[r * a.chunks + tid];
+    }
+    if (state.kind == ROW_DONE) continue;
     RowRules rules(a, r, s.table);
     auto all = [&](auto f) { each<4>(row, 0, a.n, tid, SAMPLE_THREADS, f); };
     constexpr u32 V = 16 / sizeof(T);
@@ -447,14 +465,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     float lowest = key_float(cut.key);
     u64 lo = 0, hi = a.n;
     double others = 0.0, bests = 0.0, aim = 0.0;
-    if (a.chunks && (!a.rules || a.state[r].kind == ROW_CUT)) {
+    if (state.kind == ROW_CUT) {
       // The masses of the row's chunks are there: the one that holds the draw.
       if (a.rules)
-        tie_end = a.state[r].tie_end, lowest = a.state[r].lowest;
+        tie_end = state.tie_end, lowest = state.lowest;
       else if (rules.min_p > 0.0f)
         lowest = key_float(rules.min_p_key(cut.key));
-      const bool chunk = tid < a.chunks;
-      const double other = chunk ? a.others[r * a.chunks + tid] : 0.0, one = chunk ? a.ones[r * a.chunks + tid] : 0.0;
       double upto;
       others = block_scan<double>(other, s.wave, &upto);
       bests = block_scan<double>(one, s.wave, &upto);
@@ -548,8 +564,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     }
     // The draw: the span that holds it is dealt to the waves in runs, whose masses tell which run it is.  The best
     // candidates' weights, 1 each, are kept apart, so that a mass that is nearly all the drawn one's loses nothing.
-    bool whole = !a.chunks || (a.rules && a.state[r].kind != ROW_CUT);
-    while (whole || hi - lo > SAMPLE_THREADS) {
+    bool whole = state.kind == ROW_WHOLE;
+    while (whole || hi - lo > 4 * SAMPLE_THREADS) {
       u64 run = (hi - lo + SAMPLE_WAVES - 1) / SAMPLE_WAVES;
       run = (run + 63) / 64 * 64;
       const u64 from = min(hi, lo + wave * run), to = min(hi, from + run);
@@ -602,22 +618,44 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
       lo += at * run;
       hi = min(hi, lo + run);
     }
-    // the last span, a thread for each entry
-    const u64 i = lo + tid;
-    const float v = i < hi ? mx_float(row[i]) : -__builtin_inff();
-    const double mine = v > lowest || (v == lowest && i < tie_end) ? w.of(v) : 0.0;
-    double run;
+    // the last span, a thread for four entries
+    float v[4];
+    double weight[4], mine = 0.0, run;
+    u32 some = 0;  // of the four, which hold anything
+#pragma unroll
+    for (u32 e = 0; e < 4; ++e) {
+      const u64 i = lo + tid * 4 + e;
+      v[e] = i < hi ? mx_float(row[i]) : -__builtin_inff();
+      weight[e] = v[e] > lowest || (v[e] == lowest && i < tie_end) ? w.of(v[e]) : 0.0;
+      mine += weight[e];
+      some |= (weight[e] > 0.0) << e;
+    }
     block_scan<double>(mine, s.wave, &run);
     if (tid == 0) s.word = ~0ull, s.count = 0;
     __syncthreads();
-    if (mine > 0.0) {
+    if (some) {
       if (run > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
       atomicMax(&s.count, tid);
     }
     __syncthreads();
     if (tid == (s.word != ~0ull ? (u32)s.word : s.count)) {
-      a.ids[r] = (u32)i;
-      if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((v == most ? bests - 1.0 + others : bests + others - mine) / mine));
+      double upto = run - mine;
+      u32 at = 31 - __builtin_clz(some);  // (none above the aim, by rounding: the last that holds anything)
+#pragma unroll
+      for (int e = 3; e >= 0; --e) {
+        double before = upto;
+        for (int f = 0; f < e; ++f) before += weight[f];
+        if (weight[e] > 0.0 && before + weight[e] > aim) at = e;
+      }
+      a.ids[r] = (u32)(lo + tid * 4 + at);
+      if (a.logprobs) {
+        float score = v[0];
+        double x = weight[0];
+#pragma unroll
+        for (u32 e = 1; e < 4; ++e)
+          if (at == e) score = v[e], x = weight[e];
+        a.logprobs[r] = static_cast<float>(-log1p((score == most ? bests - 1.0 + others : bests + others - x) / x));
+      }
     }
   }
 }
@@ -636,6 +674,7 @@ struct SplitLds {
   double table[TABLE];
   u64 wave[SPLIT_THREADS / 64];
   u64 word[3];
+  u32 count, place;
 };
 
 struct Part {  // of a row: what a workgroup takes
@@ -753,19 +792,30 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_list_kernel(SampleArgs a
         state.few = state.before + in_bin <= SAMPLE_FEW;
         if (!state.few && (in_bin > SAMPLE_FEW || rules.p_on)) state.kind = ROW_WHOLE;
       }
-      if (state.kind == ROW_CUT)
+      if (state.kind == ROW_CUT) {  // into LDS first, and to the row's list at once
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
         each<4>(row, p.from, p.to, tid, SPLIT_THREADS, [&](u64 i, const float (&v)[V]) {
 #pragma unroll
           for (u32 e = 0; e < V; ++e) {
             const u32 b = rules.linear_bin(v[e]);
             if (v[e] > -__builtin_inff() && (b == state.bin || (state.few && b < state.bin))) {
-              const u32 at = atomicAdd(&a.listed[p.r], 1u);
-              if (at < SAMPLE_FEW) a.list[p.r * SAMPLE_FEW + at] = (u64)~float_key(v[e]) << 32 | (i + e);
+              const u32 at = atomicAdd(&s.count, 1u);
+              if (at < SAMPLE_FEW) s.hist[at] = (u64)~float_key(v[e]) << 32 | (i + e);
             }
           }
         });
+        __syncthreads();
+        const u32 count = s.count;
+        if (tid == 0 && count) s.place = atomicAdd(&a.listed[p.r], count);
+        __syncthreads();
+        for (u32 i = tid; i < count; i += SPLIT_THREADS)  // (too many for the list: its count alone says so)
+          if (i < SAMPLE_FEW && s.place + i < SAMPLE_FEW) a.list[p.r * SAMPLE_FEW + s.place + i] = s.hist[i];
+      }
     }
   }
+  if (a.no_mass && state.kind == ROW_CUT && !state.few) state.kind = ROW_WHOLE;
   if (p.group == 0 && tid == 0) a.state[p.r] = state;
 }
 
@@ -918,7 +968,7 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
       hipLaunchKernelGGL(sample_list_kernel<T>, parts, threads, 0, s, a);
       hipLaunchKernelGGL(sample_cut_kernel<T>, dim3(a.rows), dim3(SAMPLE_THREADS), 0, s, a);
     }
-    hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
+    if (!a.no_mass) hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -976,6 +1026,8 @@ int ann_sample(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtyp
   // top-k and top-p are off for all rows where single values say so
   a.rules = a.o.top_k_dev || a.o.top_p_dev || (a.o.top_k > 0 && a.o.top_k < n) || (a.o.top_p > 0.0f && a.o.top_p < 1.0f);
   hipStream_t st = static_cast<hipStream_t>(stream);
+  // one top-k for all rows of which their lists hold enough, but where many scores are equal or masked
+  a.no_mass = !a.o.top_k_dev && a.o.top_k > 0 && a.o.top_k <= SAMPLE_FEW / 2 && a.o.top_k < n;
   if (dtype == ANN_F16)
     HIP_TRY(launch_sample<__half>(a, st));
   else if (dtype == ANN_BF16)
