@@ -133,7 +133,7 @@ __device__ __forceinline__ void each(const T* row, u64 from, u64 to, u32 rank, u
 }
 
 struct SampleLds {
-  u64 hist[SAMPLE_BINS];    // counts or masses; sorted candidates
+  alignas(16) u64 hist[SAMPLE_BINS];    // counts or masses; sorted candidates
   u64 weight[SAMPLE_BINS];  // of the candidates that are sorted (bits of doubles)
   double table[TABLE];
   u64 wave[SAMPLE_WAVES];
@@ -164,28 +164,40 @@ __device__ V block_scan(V v, u64* words, V* upto) {
   return __shfl(sums, WAVES - 1);
 }
 
-// s.hist[0 .. size) upwards, size a power of two of at most a thread each: exchanges inside a wave by shuffles, the
-// others through LDS
-__device__ void block_sort(SampleLds& s, u32 size) {
+// s.hist[0 .. count) upwards, all of them different, at most one for each thread.  Few are placed by counting the ones
+// before each; more by a bitonic network (256: 0.6 us against 2.6).
+__device__ void block_sort(SampleLds& s, u32 count) {
   const u32 i = threadIdx.x;
   __syncthreads();
-  u64 mine = i < size ? s.hist[i] : ~0ull;
+  if (count <= 256) {
+    const u64 mine = i < count ? s.hist[i] : 0;
+    u32 rank = 0;
+    if (i < count) {
+      using v2l = u64 __attribute__((ext_vector_type(2)));
+      const v2l* all = reinterpret_cast<const v2l*>(s.hist);
+#pragma unroll 4
+      for (u32 j = 0; j < count / 2; ++j) {
+        const v2l x = all[j];
+        rank += (x[0] < mine) + (x[1] < mine);
+      }
+      if (count % 2) rank += s.hist[count - 1] < mine;
+    }
+    __syncthreads();
+    if (i < count) s.hist[rank] = mine;
+    __syncthreads();
+    return;
+  }
+  const u32 size = count <= 512 ? 512 : 1024;
+  if (i >= count && i < size) s.hist[i] = ~0ull;
   for (u32 run = 2; run <= size; run *= 2)
     for (u32 gap = run / 2; gap > 0; gap /= 2) {
-      u64 other;
-      if (gap >= 64) {
-        __syncthreads();
-        if (i < size) s.hist[i] = mine;
-        __syncthreads();
-        other = i < size ? s.hist[i ^ gap] : ~0ull;
-      } else {
-        other = __shfl_xor(mine, (int)gap);
+      __syncthreads();
+      if (i < size / 2) {
+        const u32 lo = i / gap * 2 * gap + i % gap, hi = lo + gap;
+        const u64 x = s.hist[lo], y = s.hist[hi];
+        if ((x > y) == ((lo & run) == 0)) s.hist[lo] = y, s.hist[hi] = x;
       }
-      const bool up = (i & run) == 0, low = (i & gap) == 0;
-      mine = up == low ? min(mine, other) : max(mine, other);
     }
-  __syncthreads();
-  if (i < size) s.hist[i] = mine;
   __syncthreads();
 }
 
@@ -267,10 +279,7 @@ struct RowRules {
 // sorted by id and drawn from, a thread for each.
 __device__ void draw_few(const SampleArgs& a, u64 r, const RowRules& rules, u64 limit, u32 count, double unit, SampleLds& s) {
   const u32 tid = threadIdx.x;
-  u32 size = 2;
-  while (size < count) size *= 2;
-  if (tid >= count && tid < size) s.hist[tid] = ~0ull;
-  block_sort(s, size);
+  block_sort(s, count);
   const bool mine = tid < limit && tid < count;
   const u64 entry = mine ? s.hist[tid] : 0;
   const float score = key_float(~(u32)(entry >> 32));
@@ -281,11 +290,11 @@ __device__ void draw_few(const SampleArgs& a, u64 r, const RowRules& rules, u64 
   bool keep = mine;
   if (rules.p_on) keep = keep && upto - units < rules.wanted_mass(total);
   if (rules.min_p > 0.0f) keep = keep && weight >= rules.floor_w;
-  __syncthreads();
-  if (tid < size) s.hist[tid] = keep ? (entry & 0xFFFFFFFFull) << 32 | tid : ~0ull;
+  const u32 kept = (u32)__syncthreads_count(keep);  // (the first ones)
+  if (keep) s.hist[tid] = (entry & 0xFFFFFFFFull) << 32 | tid;
   s.weight[tid] = __builtin_bit_cast(u64, weight);
-  block_sort(s, size);
-  const bool there = tid < size && s.hist[tid] != ~0ull;
+  block_sort(s, kept);
+  const bool there = tid < kept;
   const u32 from = there ? (u32)s.hist[tid] : 0;
   const double x = there ? __builtin_bit_cast(double, s.weight[from]) : 0.0;
   double run, others;
@@ -317,27 +326,16 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
-    SampleState state{};
-    state.kind = a.chunks ? ROW_CUT : ROW_WHOLE;
-    double other = 0.0, one = 0.0;
-    if (a.chunks) {
-      if (a.rules) state = a.state[r];
-      if (tid < a.chunks) other = a.others[r * a.chunks + tid], one = a.ones[r * a.chunks + tid];
-    }
-    if (state.kind == ROW_DONE) continue;
+    if (a.chunks && a.state[r].kind != ROW_WHOLE) continue;  // (of a divided call)
     RowRules rules(a, r, s.table);
     auto all = [&](auto f) { each<4>(row, 0, a.n, tid, SAMPLE_THREADS, f); };
     constexpr u32 V = 16 / sizeof(T);
 
     float most = -__builtin_inff();
-    if (a.chunks) {
-      if (tid < a.chunks) most = a.most[r * a.chunks + tid];
-    } else {
-      each<8>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
+    each<8>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
 #pragma unroll
-        for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
-      });
-    }
+      for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
+    });
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w));
     __syncthreads();
@@ -465,73 +463,45 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     float lowest = key_float(cut.key);
     u64 lo = 0, hi = a.n;
     double others = 0.0, bests = 0.0, aim = 0.0;
-    if (state.kind == ROW_CUT) {
-      // The masses of the row's chunks are there: the one that holds the draw.
-      if (a.rules)
-        tie_end = state.tie_end, lowest = state.lowest;
-      else if (rules.min_p > 0.0f)
-        lowest = key_float(rules.min_p_key(cut.key));
-      double upto;
-      others = block_scan<double>(other, s.wave, &upto);
-      bests = block_scan<double>(one, s.wave, &upto);
-      const double mass = other + one;
-      block_scan<double>(mass, s.wave, &upto);
-      aim = rules.u * (bests + others);
-      if (tid == 0) s.word = ~0ull, s.count = 0;
-      __syncthreads();
-      if (mass > 0.0) {
-        if (upto > aim) atomicMin(reinterpret_cast<unsigned long long*>(&s.word), (unsigned long long)tid);
-        atomicMax(&s.count, tid);
+    if (rules.k_on) {
+      Cut found;
+      u64 ties;
+      if (select(cut, false, [&](u64 total) { return (u64)rules.top_k < total ? (u64)rules.top_k : 0; }, &found, &ties)) {
+        cut = found;
+        cut.ties = ties;
       }
-      __syncthreads();
-      const u32 at = s.word != ~0ull ? (u32)s.word : s.count;
-      __syncthreads();
-      if (tid == at) s.word = __builtin_bit_cast(u64, upto - mass);
-      __syncthreads();
-      aim -= at ? __builtin_bit_cast(double, s.word) : 0.0;
-      lo = (u64)at * a.chunk;
-      hi = min(a.n, lo + a.chunk);
-    } else {
-      if (rules.k_on) {
-        Cut found;
-        u64 ties;
-        if (select(cut, false, [&](u64 total) { return (u64)rules.top_k < total ? (u64)rules.top_k : 0; }, &found, &ties)) {
-          cut = found;
-          cut.ties = ties;
-        }
-      }
-      if (cut.ties != ~0ull && rules.top_k - cut.ties + cut.at <= SAMPLE_FEW) {
-        __syncthreads();
-        if (tid == 0) s.count = 0;
-        __syncthreads();
-        lowest = key_float(cut.key);
-        all([&](u64 i, const float (&v)[V]) {
-#pragma unroll
-          for (u32 e = 0; e < V; ++e)
-            if (v[e] >= lowest) s.hist[atomicAdd(&s.count, 1u)] = (u64)~float_key(v[e]) << 32 | (i + e);
-        });
-        __syncthreads();
-        draw_few(a, r, rules, rules.top_k, s.count, unit, s);
-        continue;
-      }
-      if (rules.p_on) {
-        Cut found;
-        u64 left;
-        if (select(cut, true, [&](u64 total) { return rules.wanted_mass(total); }, &found, &left)) {
-          const u64 each_one = w.units(key_float(found.key), unit);
-          const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull, at = each_one ? found.at / each_one : ~0ull;
-          if (found.key != cut.key || cut.ties == ~0ull)
-            cut = {found.key, need, at};
-          else if (need < cut.ties)  // (`at` of top-k counts the ones that it dropped as well)
-            cut.ties = need;
-        }
-      }
-      if (rules.min_p > 0.0f) {
-        const u32 key = rules.min_p_key(cut.key);
-        if (key > cut.key) cut.key = key, cut.ties = ~0ull;
-      }
-      lowest = key_float(cut.key);
     }
+    if (cut.ties != ~0ull && rules.top_k - cut.ties + cut.at <= SAMPLE_FEW) {
+      __syncthreads();
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+      lowest = key_float(cut.key);
+      all([&](u64 i, const float (&v)[V]) {
+#pragma unroll
+        for (u32 e = 0; e < V; ++e)
+          if (v[e] >= lowest) s.hist[atomicAdd(&s.count, 1u)] = (u64)~float_key(v[e]) << 32 | (i + e);
+      });
+      __syncthreads();
+      draw_few(a, r, rules, rules.top_k, s.count, unit, s);
+      continue;
+    }
+    if (rules.p_on) {
+      Cut found;
+      u64 left;
+      if (select(cut, true, [&](u64 total) { return rules.wanted_mass(total); }, &found, &left)) {
+        const u64 each_one = w.units(key_float(found.key), unit);
+        const u64 need = each_one ? (left + each_one - 1) / each_one : ~0ull, at = each_one ? found.at / each_one : ~0ull;
+        if (found.key != cut.key || cut.ties == ~0ull)
+          cut = {found.key, need, at};
+        else if (need < cut.ties)  // (`at` of top-k counts the ones that it dropped as well)
+          cut.ties = need;
+      }
+    }
+    if (rules.min_p > 0.0f) {
+      const u32 key = rules.min_p_key(cut.key);
+      if (key > cut.key) cut.key = key, cut.ties = ~0ull;
+    }
+    lowest = key_float(cut.key);
     // Where only some of those at the cut are kept, they are the first ones by id: those below `tie_end`.
     if (cut.ties < cut.at) {
       // narrowed down like the draw below: runs of the span, counted by a wave each
@@ -564,7 +534,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
     }
     // The draw: the span that holds it is dealt to the waves in runs, whose masses tell which run it is.  The best
     // candidates' weights, 1 each, are kept apart, so that a mass that is nearly all the drawn one's loses nothing.
-    bool whole = state.kind == ROW_WHOLE;
+    bool whole = true;
     while (whole || hi - lo > 4 * SAMPLE_THREADS) {
       u64 run = (hi - lo + SAMPLE_WAVES - 1) / SAMPLE_WAVES;
       run = (run + 63) / 64 * 64;
@@ -815,6 +785,7 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_list_kernel(SampleArgs a
       }
     }
   }
+  // (without the launches that follow, rows whose list does not end in a draw: greedy and empty ones among them)
   if (a.no_mass && state.kind == ROW_CUT && !state.few) state.kind = ROW_WHOLE;
   if (p.group == 0 && tid == 0) a.state[p.r] = state;
 }
@@ -835,10 +806,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
   __syncthreads();
   for (u32 w = 0; w < SAMPLE_WAVES; ++w) most = __builtin_fmaxf(most, __uint_as_float((u32)s.wave[w]));
   __syncthreads();
-  if (!rules.set_best(most) || rules.greedy()) {  // (the kernel for whole rows has these)
-    if (tid == 0) a.state[r].kind = ROW_WHOLE;
-    return;
-  }
+  if (!rules.set_best(most) || rules.greedy()) return;  // (the draw needs no cut)
   u32 lowest = SAMPLE_LEAST + 1;
   state.tie_end = a.n;
   if (state.bin != ~0u) {
@@ -855,10 +823,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
       if (tid == 0) a.state[r].kind = ROW_DONE;
       return;
     }
-    u32 size = 2;
-    while (size < count) size *= 2;
-    if (tid >= count && tid < size) s.hist[tid] = ~0ull;
-    block_sort(s, size);
+    block_sort(s, count);
     const u64 entry = tid < count ? s.hist[tid] : 0;
     const u64 amount = tid >= count ? 0 : rules.k_on ? 1 : rules.w.units(key_float(~(u32)(entry >> 32)), unit);
     u64 upto;
@@ -927,6 +892,146 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_mass_kernel(SampleArgs a
   }
 }
 
+// A workgroup per row: the chunk that holds the draw, by the chunks' masses, then the entry.
+template <typename T>
+__global__ __launch_bounds__(SPLIT_THREADS) void sample_draw_kernel(SampleArgs a) {
+  __shared__ SplitLds s;
+  constexpr u32 EACH = SPLIT_CHUNK / SPLIT_THREADS, WAVES = SPLIT_THREADS / 64, V = 16 / sizeof(T);
+  const u32 tid = threadIdx.x;
+  const u64 r = blockIdx.x;
+  const bool chunk = tid < a.chunks;
+  const u64 place = r * a.chunks + (chunk ? tid : 0);
+  const float most_here = a.most[place];
+  const double other = a.others[place];
+  const u32 one = a.ones[place];
+  SampleState state{};
+  state.kind = ROW_CUT;
+  if (a.rules) state = a.state[r];
+  if (state.kind != ROW_CUT) return;
+  for (u32 i = tid; i < TABLE; i += SPLIT_THREADS) s.table[i] = exp2(i / (double)TABLE);
+  RowRules rules(a, r, s.table);
+  const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
+  if (tid == 0) s.word[0] = ~0ull, s.word[1] = ~0ull;
+  if (!rules.set_best(split_max(chunk ? most_here : -__builtin_inff(), s.wave))) {  // (the same in all threads)
+    if (tid == 0) {
+      a.ids[r] = ANN_NONE;
+      if (a.logprobs) a.logprobs[r] = -__builtin_inff();
+    }
+    return;
+  }
+  const Weights& w = rules.w;
+  const float most = w.most;
+  auto* words = reinterpret_cast<unsigned long long*>(s.word);
+  if (rules.greedy()) {
+    if (chunk && most_here == most) atomicMin(&words[0], (unsigned long long)tid);
+    __syncthreads();
+    const u64 lo = s.word[0] * a.chunk, hi = min(a.n, lo + a.chunk);
+    for (u64 i = lo + tid; i < hi; i += SPLIT_THREADS)
+      if (mx_float(row[i]) == most) {
+        atomicMin(&words[1], (unsigned long long)i);
+        break;
+      }
+    __syncthreads();
+    if (tid == 0) {
+      a.ids[r] = (u32)s.word[1];
+      if (a.logprobs) a.logprobs[r] = 0.0f;
+    }
+    return;
+  }
+  float lowest = key_float(SAMPLE_LEAST + 1);
+  u64 tie_end = a.n;
+  if (a.rules)
+    lowest = state.lowest, tie_end = state.tie_end;
+  else if (rules.min_p > 0.0f)
+    lowest = key_float(rules.min_p_key(SAMPLE_LEAST + 1));
+  double upto;
+  const double others = block_scan<double, WAVES>(chunk ? other : 0.0, s.wave, &upto);
+  const double bests = block_scan<double, WAVES>(chunk ? one : 0.0, s.wave, &upto);
+  const double mass = chunk ? other + one : 0.0;
+  block_scan<double, WAVES>(mass, s.wave, &upto);
+  double aim = rules.u * (bests + others);
+  // the first whose running mass is above the aim, or (none, by rounding) the last that holds anything
+  auto first_above = [&](double mine, double run) {
+    if (tid == 0) s.word[0] = ~0ull, s.count = 0;
+    __syncthreads();
+    if (mine > 0.0) {
+      if (run > aim) atomicMin(&words[0], (unsigned long long)tid);
+      atomicMax(&s.count, tid);
+    }
+    __syncthreads();
+    const u32 at = s.word[0] != ~0ull ? (u32)s.word[0] : s.count;
+    if (tid == at) s.word[1] = __builtin_bit_cast(u64, run - mine);
+    __syncthreads();
+    return at;
+  };
+  const u32 at = first_above(mass, upto);
+  aim -= at ? __builtin_bit_cast(double, s.word[1]) : 0.0;
+  u64 lo = (u64)at * a.chunk;
+  const u64 hi = min(a.n, lo + a.chunk);
+
+  // 4,096 entries at a time (longer chunks have several such blocks), sixteen neighbours a thread
+  float v[EACH];
+  auto weigh = [&](u64 from) {
+    const u64 mine = from + tid * EACH;
+    if (reinterpret_cast<uintptr_t>(row) % 16 == 0 && mine + EACH <= hi) {
+      Pack<T, V> x[EACH / V];
+#pragma unroll
+      for (u32 i = 0; i < EACH / V; ++i) x[i] = reinterpret_cast<const Pack<T, V>*>(row + mine)[i];
+#pragma unroll
+      for (u32 e = 0; e < EACH; ++e) v[e] = mx_float(x[e / V].v[e % V]);
+    } else {
+#pragma unroll
+      for (u32 e = 0; e < EACH; ++e) v[e] = mine + e < hi ? mx_float(row[mine + e]) : -__builtin_inff();
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (u32 e = 0; e < EACH; ++e) {
+      const bool keep = v[e] > lowest || (v[e] == lowest && mine + e < tie_end);
+      if (!keep) v[e] = -__builtin_inff();
+      sum += w.of(v[e]);
+    }
+    return sum;
+  };
+  double mine = weigh(lo), run;
+  double block = block_scan<double, WAVES>(mine, s.wave, &run);
+  if (hi - lo > SPLIT_CHUNK) {
+    u64 last = lo;
+    double before = 0.0, before_last = 0.0;
+    while (true) {
+      if (block > 0.0) last = lo, before_last = before;
+      if (before + block > aim || lo + SPLIT_CHUNK >= hi) break;
+      before += block;
+      lo += SPLIT_CHUNK;
+      mine = weigh(lo);
+      block = block_scan<double, WAVES>(mine, s.wave, &run);
+    }
+    if (lo != last) {
+      lo = last;
+      mine = weigh(lo);
+      block_scan<double, WAVES>(mine, s.wave, &run);
+    }
+    aim -= before_last;
+  }
+  if (tid == first_above(mine, run)) {
+    double before = run - mine, x = 0.0;
+    u32 which = 0;
+#pragma unroll
+    for (u32 e = 0; e < EACH; ++e) {  // (the running mass before this one: the last taken is the one that passes the aim)
+      const double next = w.of(v[e]);
+      if (next > 0.0 && !(x > 0.0 && before > aim)) which = e, x = next;
+      before += next;
+    }
+    a.ids[r] = (u32)(lo + tid * EACH + which);
+    if (a.logprobs) {
+      float score = v[0];
+#pragma unroll
+      for (u32 e = 1; e < EACH; ++e)
+        if (which == e) score = v[e];
+      a.logprobs[r] = static_cast<float>(-log1p((score == most ? bests - 1.0 + others : bests + others - x) / x));
+    }
+  }
+}
+
 // Rows from SPLIT_LEAST entries on, in calls of up to SPLIT_ROWS rows.
 constexpr u64 SPLIT_LEAST = 16384, SPLIT_ROWS = 4096;
 
@@ -968,9 +1073,12 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
       hipLaunchKernelGGL(sample_list_kernel<T>, parts, threads, 0, s, a);
       hipLaunchKernelGGL(sample_cut_kernel<T>, dim3(a.rows), dim3(SAMPLE_THREADS), 0, s, a);
     }
-    if (!a.no_mass) hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
+    if (!a.no_mass) {
+      hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
+      hipLaunchKernelGGL(sample_draw_kernel<T>, dim3(a.rows), threads, 0, s, a);
+    }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || !a.rules) return e;
   }
   hipLaunchKernelGGL(sample_kernel<T>, dim3(a.rows < (1u << 20) ? a.rows : (1u << 20)), dim3(SAMPLE_THREADS), 0, s, a);
   return hipGetLastError();
