@@ -257,11 +257,9 @@ struct RowRules {
     const u32 lane = threadIdx.x % 64;
     if (w.most < __builtin_inff() && temperature < __builtin_inff()) {
       const u32 near = float_key(static_cast<float>(w.best + static_cast<double>(temperature) * log(floor_w)));
-      const u32 first = near > from + 32 ? near - 32 : from;
-      if (best >= 63 && first <= best - 63) {
-        const u64 reach = __ballot(w.of(key_float(first + lane)) >= floor_w);
-        if (reach >> 63 && (first == from || !(reach & 1))) return first + (u32)__builtin_ctzll(reach);
-      }
+      const u32 first = max(from, min(near - 32, best - 63));  // (keys of candidates are far above 63)
+      const u64 reach = __ballot(first + lane <= best && w.of(key_float(first + lane)) >= floor_w);
+      if (reach && (first == from || !(reach & 1))) return first + (u32)__builtin_ctzll(reach);
     }
     u32 lo = from, hi = best;  // hi reaches it
     while (lo < hi) {
@@ -1043,8 +1041,8 @@ u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
   while ((n + chunk - 1) / chunk > SPLIT_CHUNKS) chunk *= 2;
   a.chunk = (u32)chunk;
   a.chunks = (u32)((n + chunk - 1) / chunk);
-  // some two thousand workgroups
-  const u64 groups = (2048 + rows - 1) / rows;
+  // some eight thousand workgroups
+  const u64 groups = (8192 + rows - 1) / rows;
   a.per = (u32)(groups >= a.chunks ? 1 : (a.chunks + groups - 1) / groups);
   a.groups = (a.chunks + a.per - 1) / a.per;
   u64 at = 0;
