@@ -47,7 +47,8 @@ struct SampleArgs {
   double* others;      // masses other than the best candidates'
   u32* ones;           // numbers of best candidates
   u64* hist;           // (rows, SAMPLE_BINS)
-  u64* list;           // (rows, SAMPLE_FEW): candidates around the cut
+  u64* list;           // (rows, capacity): candidates around the cut
+  u32 capacity;
   u32* listed;
   SampleState* state;
 };
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
-    if (a.chunks && a.state[r].kind != ROW_WHOLE) continue;  // (of a divided call)
+    if (a.state[r].kind != ROW_WHOLE) continue;
     RowRules rules(a, r, s.table);
     auto all = [&](auto f) { each<4>(row, 0, a.n, tid, SAMPLE_THREADS, f); };
     constexpr u32 V = 16 / sizeof(T);
@@ -635,6 +636,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 // cut needs more than the list holds are left to that kernel whole.
 constexpr u32 SPLIT_THREADS = 256;
 constexpr u32 SPLIT_CHUNKS = 256;  // most of a row
+constexpr u32 SPLIT_LIST = 16384;  // most candidates of a list
 constexpr u32 SPLIT_CHUNK = 4096;  // entries of one, where a row has no more than 256 of that size
 
 struct SplitLds {
@@ -758,28 +760,35 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_list_kernel(SampleArgs a
       const u64 in_bin = s.word[2];
       if (rules.k_on) {
         state.few = state.before + in_bin <= SAMPLE_FEW;
-        if (!state.few && (in_bin > SAMPLE_FEW || rules.p_on)) state.kind = ROW_WHOLE;
+        if (!state.few && (in_bin > a.capacity || rules.p_on)) state.kind = ROW_WHOLE;
       }
-      if (state.kind == ROW_CUT) {  // into LDS first, and to the row's list at once
+      if (state.kind == ROW_CUT) {
+        // Into LDS first, and to the row's list at once; what LDS has no room for goes there by itself.
         __syncthreads();
         if (tid == 0) s.count = 0;
         __syncthreads();
+        auto put = [&](u32 at, u64 entry) {  // (too many for the list: its count alone says so)
+          if (at < a.capacity) a.list[p.r * a.capacity + at] = entry;
+        };
         each<4>(row, p.from, p.to, tid, SPLIT_THREADS, [&](u64 i, const float (&v)[V]) {
 #pragma unroll
           for (u32 e = 0; e < V; ++e) {
             const u32 b = rules.linear_bin(v[e]);
             if (v[e] > -__builtin_inff() && (b == state.bin || (state.few && b < state.bin))) {
+              const u64 entry = (u64)~float_key(v[e]) << 32 | (i + e);
               const u32 at = atomicAdd(&s.count, 1u);
-              if (at < SAMPLE_FEW) s.hist[at] = (u64)~float_key(v[e]) << 32 | (i + e);
+              if (at < SAMPLE_BINS)
+                s.hist[at] = entry;
+              else
+                put(atomicAdd(&a.listed[p.r], 1u), entry);
             }
           }
         });
         __syncthreads();
-        const u32 count = s.count;
+        const u32 count = min(s.count, SAMPLE_BINS);
         if (tid == 0 && count) s.place = atomicAdd(&a.listed[p.r], count);
         __syncthreads();
-        for (u32 i = tid; i < count; i += SPLIT_THREADS)  // (too many for the list: its count alone says so)
-          if (i < SAMPLE_FEW && s.place + i < SAMPLE_FEW) a.list[p.r * SAMPLE_FEW + s.place + i] = s.hist[i];
+        for (u32 i = tid; i < count; i += SPLIT_THREADS) put(s.place + i, s.hist[i]);
       }
     }
   }
@@ -808,13 +817,60 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
   u32 lowest = SAMPLE_LEAST + 1;
   state.tie_end = a.n;
   if (state.bin != ~0u) {
-    const u32 count = a.listed[r];
-    if (count > SAMPLE_FEW) {
+    const u64* list = a.list + r * a.capacity;
+    u32 count = a.listed[r];
+    bool left = count > a.capacity;
+    const double unit = ldexp(1.0, (int)a.unit);
+    if (!left && count > SAMPLE_FEW) {
+      // A long list: entries sort as (key downwards, id) and are all different; the histogram of their range, and of
+      // the part of the cut again, until few are left.
+      u64 lo = ~0ull, hi = 0;
+      for (u32 i = tid; i < count; i += SAMPLE_THREADS) lo = min(lo, list[i]), hi = max(hi, list[i]);
+#pragma unroll
+      for (int w = 1; w < 64; w *= 2) lo = min(lo, __shfl_xor(lo, w)), hi = max(hi, __shfl_xor(hi, w));
+      if (tid % 64 == 0) s.wave[tid / 64] = lo, s.hist[tid / 64] = hi;
+      __syncthreads();
+      for (u32 w = 0; w < SAMPLE_WAVES; ++w) lo = min(lo, s.wave[w]), hi = max(hi, s.hist[w]);
+      u32 some;
+      do {
+        const u32 bits = 64 - __builtin_clzll(hi - lo), shift = bits > 10 ? bits - 10 : 0;
+        __syncthreads();
+        s.hist[tid] = 0;
+        __syncthreads();
+        for (u32 i = tid; i < count; i += SAMPLE_THREADS) {
+          const u64 entry = list[i];
+          if (entry < lo || entry > hi) continue;
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[(entry - lo) >> shift]),
+                    (unsigned long long)(rules.k_on ? 1 : rules.w.units(key_float(~(u32)(entry >> 32)), unit)));
+        }
+        __syncthreads();
+        const u64 mine = s.hist[tid];
+        u64 upto;
+        block_scan<u64>(mine, s.wave, &upto);
+        if (state.before + upto >= state.want && state.before + upto - mine < state.want) s.bin = tid, s.word = upto - mine;
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        lo += (u64)s.bin << shift;
+        hi = min(hi, lo + ((1ull << shift) - 1));
+        state.before += s.word;
+        for (u32 i = tid; i < count; i += SAMPLE_THREADS) {
+          const u64 entry = list[i];
+          if (entry < lo || entry > hi) continue;
+          const u32 at = atomicAdd(&s.count, 1u);
+          if (at < SAMPLE_FEW) s.hist[at] = entry;
+        }
+        __syncthreads();
+        some = s.count;
+      } while (some > SAMPLE_FEW);
+      count = some;
+      __syncthreads();
+    } else if (!left && tid < count) {
+      s.hist[tid] = list[tid];
+    }
+    if (left) {
       if (tid == 0) a.state[r].kind = ROW_WHOLE;
       return;
     }
-    if (tid < count) s.hist[tid] = a.list[r * SAMPLE_FEW + tid];
-    const double unit = ldexp(1.0, (int)a.unit);
     __syncthreads();
     if (rules.k_on && state.few) {
       draw_few(a, r, rules, rules.top_k, count, unit, s);
@@ -1030,13 +1086,191 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_draw_kernel(SampleArgs a
   }
 }
 
-// Rows from SPLIT_LEAST entries on, in calls of up to SPLIT_ROWS rows.
-constexpr u64 SPLIT_LEAST = 16384, SPLIT_ROWS = 4096;
+// Short rows: a workgroup holds a row in its registers, EACH neighbours a thread.
+constexpr u32 SMALL_THREADS = 256;
+template <u32 EACH>
+struct SmallLds {
+  alignas(16) u64 list[SMALL_THREADS * EACH];
+  u64 hist[SAMPLE_BINS];
+  double table[TABLE];
+  u64 wave[SMALL_THREADS / 64];
+  u64 word[3];
+  u32 count;
+};
 
-// fills in what a divided call needs and returns its scratch, or 0 where rows are taken whole
+// list[0 .. count) upwards, all of them different
+template <u32 THREADS>
+__device__ void sort_list(u64* list, u32 count) {
+  const u32 i = threadIdx.x;
+  __syncthreads();
+  if (count <= THREADS) {  // placed by counting the ones before each
+    const u64 mine = i < count ? list[i] : 0;
+    u32 rank = 0;
+    if (i < count)
+      for (u32 j = 0; j < count; ++j) rank += list[j] < mine;
+    __syncthreads();
+    if (i < count) list[rank] = mine;
+    __syncthreads();
+    return;
+  }
+  u32 size = 2;
+  while (size < count) size *= 2;
+  for (u32 j = count + i; j < size; j += THREADS) list[j] = ~0ull;
+  for (u32 run = 2; run <= size; run *= 2)
+    for (u32 gap = run / 2; gap > 0; gap /= 2) {
+      __syncthreads();
+      for (u32 j = i; j < size / 2; j += THREADS) {
+        const u32 lo = j / gap * 2 * gap + j % gap, hi = lo + gap;
+        const u64 x = list[lo], y = list[hi];
+        if ((x > y) == ((lo & run) == 0)) list[lo] = y, list[hi] = x;
+      }
+    }
+  __syncthreads();
+}
+
+template <typename T, u32 EACH>
+__global__ __launch_bounds__(SMALL_THREADS) void sample_short_kernel(SampleArgs a) {
+  __shared__ SmallLds<EACH> s;
+  constexpr u32 WAVES = SMALL_THREADS / 64, BINS = SAMPLE_BINS / SMALL_THREADS;
+  const u32 tid = threadIdx.x, n = (u32)a.n, first = tid * EACH;
+  const double unit = ldexp(1.0, (int)a.unit);
+  auto* words = reinterpret_cast<unsigned long long*>(s.word);
+  for (u32 i = tid; i < TABLE; i += SMALL_THREADS) s.table[i] = exp2(i / (double)TABLE);
+  for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
+    float v[EACH], most = -__builtin_inff();
+#pragma unroll
+    for (u32 e = 0; e < EACH; ++e) v[e] = mx_float(row[min(first + e, n - 1)]);
+    RowRules rules(a, r, s.table);
+#pragma unroll
+    for (u32 e = 0; e < EACH; ++e) {
+      if (!(first + e < n && v[e] == v[e])) v[e] = -__builtin_inff();
+      most = __builtin_fmaxf(most, v[e]);
+    }
+    most = split_max(most, s.wave);
+    __syncthreads();
+    if (tid == 0) s.word[0] = ~0ull;
+    if (!rules.set_best(most)) {  // (the same in all threads)
+      if (tid == 0) {
+        a.ids[r] = ANN_NONE;
+        if (a.logprobs) a.logprobs[r] = -__builtin_inff();
+      }
+      continue;
+    }
+    const Weights& w = rules.w;
+    most = w.most;
+    __syncthreads();
+    if (rules.greedy()) {
+#pragma unroll
+      for (u32 e = EACH; e-- > 0;)
+        if (v[e] == most) atomicMin(&words[0], (unsigned long long)(first + e));
+      __syncthreads();
+      if (tid == 0) {
+        a.ids[r] = (u32)s.word[0];
+        if (a.logprobs) a.logprobs[r] = 0.0f;
+      }
+      __syncthreads();
+      continue;
+    }
+    // Kept: above `lowest`, or at it with an id below tie_end.
+    float lowest = key_float(SAMPLE_LEAST + 1);
+    u32 tie_end = n;
+    auto kept = [&](u32 e) { return v[e] > lowest || (v[e] == lowest && first + e < tie_end); };
+    // Moves the cut to where the count (or mass) of the kept ones, from the best down, reaches `aim(total)`.
+    auto cut = [&](auto masses, auto aim) {
+      __syncthreads();
+#pragma unroll
+      for (u32 i = 0; i < BINS; ++i) s.hist[tid + i * SMALL_THREADS] = 0;
+      if (tid == 0) s.count = 0;
+      __syncthreads();
+#pragma unroll
+      for (u32 e = 0; e < EACH; ++e)
+        if (kept(e)) atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[rules.linear_bin(v[e])]), (unsigned long long)(masses ? w.units(v[e], unit) : 1ull));
+      __syncthreads();
+      u64 bin[BINS], mine = 0, upto;
+#pragma unroll
+      for (u32 i = 0; i < BINS; ++i) mine += bin[i] = s.hist[tid * BINS + i];
+      const u64 total = block_scan<u64, WAVES>(mine, s.wave, &upto), want = aim(total);
+      if (want == 0) return;
+      u64 before = upto - mine;
+#pragma unroll
+      for (u32 i = 0; i < BINS; ++i) {
+        if (before < want && before + bin[i] >= want) s.word[0] = tid * BINS + i, s.word[1] = before;
+        before += bin[i];
+      }
+      __syncthreads();
+      const u32 b = (u32)s.word[0];
+      before = s.word[1];
+#pragma unroll
+      for (u32 e = 0; e < EACH; ++e)
+        if (kept(e) && rules.linear_bin(v[e]) == b) s.list[atomicAdd(&s.count, 1u)] = (u64)~float_key(v[e]) << 32 | (first + e);
+      __syncthreads();
+      const u32 count = s.count;
+      sort_list<SMALL_THREADS>(s.list, count);
+      for (u32 at = 0; at < count; at += SMALL_THREADS) {
+        const u64 entry = at + tid < count ? s.list[at + tid] : 0;
+        const u64 amount = at + tid >= count ? 0 : masses ? w.units(key_float(~(u32)(entry >> 32)), unit) : 1;
+        const u64 sum = block_scan<u64, WAVES>(amount, s.wave, &upto);
+        if (amount && before + upto - amount < want && before + upto >= want) s.word[2] = entry;
+        before += sum;
+        if (before >= want) break;
+      }
+      __syncthreads();
+      lowest = key_float(~(u32)(s.word[2] >> 32));
+      tie_end = (u32)s.word[2] + 1;
+    };
+    if (rules.k_on) cut(False(), [&](u64 total) { return (u64)rules.top_k < total ? (u64)rules.top_k : 0; });
+    if (rules.p_on) cut(True(), [&](u64 total) { return rules.wanted_mass(total); });
+    if (rules.min_p > 0.0f) {
+      const u32 from = float_key(lowest), key = rules.min_p_key(from);
+      if (key > from) lowest = key_float(key), tie_end = n;
+    }
+    double weight[EACH], mine = 0.0, others = 0.0, bests = 0.0, run, upto;
+#pragma unroll
+    for (u32 e = 0; e < EACH; ++e) {
+      weight[e] = kept(e) ? w.of(v[e]) : 0.0;
+      mine += weight[e];
+      if (v[e] == most && weight[e] > 0.0)
+        bests += 1.0;
+      else
+        others += weight[e];
+    }
+    others = block_scan<double, WAVES>(others, s.wave, &upto);
+    bests = block_scan<double, WAVES>(bests, s.wave, &upto);
+    block_scan<double, WAVES>(mine, s.wave, &run);
+    const double aim = rules.u * (bests + others);
+    // the first whose running mass is above the aim, or (none, by rounding) the last that holds anything
+    if (tid == 0) s.word[0] = ~0ull, s.count = 0;
+    __syncthreads();
+    if (mine > 0.0) {
+      if (run > aim) atomicMin(&words[0], (unsigned long long)tid);
+      atomicMax(&s.count, tid);
+    }
+    __syncthreads();
+    if (tid == (s.word[0] != ~0ull ? (u32)s.word[0] : s.count)) {
+      double before = run - mine, x = 0.0;
+      float score = 0.0f;
+      u32 which = 0;
+#pragma unroll
+      for (u32 e = 0; e < EACH; ++e) {  // (the running mass before this one: the last taken is the one that passes the aim)
+        if (weight[e] > 0.0 && !(x > 0.0 && before > aim)) which = e, x = weight[e], score = v[e];
+        before += weight[e];
+      }
+      a.ids[r] = first + which;
+      if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((score == most ? bests - 1.0 + others : bests + others - x) / x));
+    }
+    __syncthreads();
+  }
+}
+
+// Rows above SHORT entries are divided, SPLIT_ROWS of them at a time.
+constexpr u64 SHORT = SMALL_THREADS * 16, SPLIT_ROWS = 4096;
+
+// fills in what a divided call needs and returns its scratch, or 0 where rows are short
 u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
   a.chunks = 0;
-  if (n < SPLIT_LEAST || rows > SPLIT_ROWS) return 0;
+  if (n <= SHORT || rows == 0) return 0;
+  if (rows > SPLIT_ROWS) rows = SPLIT_ROWS;
   u64 chunk = SPLIT_CHUNK;
   while ((n + chunk - 1) / chunk > SPLIT_CHUNKS) chunk *= 2;
   a.chunk = (u32)chunk;
@@ -1045,6 +1279,8 @@ u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
   const u64 groups = (8192 + rows - 1) / rows;
   a.per = (u32)(groups >= a.chunks ? 1 : (a.chunks + groups - 1) / groups);
   a.groups = (a.chunks + a.per - 1) / a.per;
+  // a bin of the histogram has about n / 200 of normal scores near their middle
+  a.capacity = n / 64 < SAMPLE_FEW ? SAMPLE_FEW : n / 64 < SPLIT_LIST ? (u32)(n / 64) : SPLIT_LIST;
   u64 at = 0;
   auto take = [&](u64 bytes) {
     const u64 from = at;
@@ -1052,7 +1288,7 @@ u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
     return scratch + from;
   };
   a.hist = reinterpret_cast<u64*>(take(rows * SAMPLE_BINS * 8));
-  a.list = reinterpret_cast<u64*>(take(rows * SAMPLE_FEW * 8));
+  a.list = reinterpret_cast<u64*>(take(rows * a.capacity * 8));
   a.state = reinterpret_cast<SampleState*>(take(rows * sizeof(SampleState)));
   a.others = reinterpret_cast<double*>(take(rows * a.chunks * 8));
   a.ones = reinterpret_cast<u32*>(take(rows * a.chunks * 4));
@@ -1062,8 +1298,18 @@ u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
 }
 
 template <typename T>
-hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
-  if (a.chunks) {
+hipError_t launch_sample(SampleArgs a, hipStream_t s) {
+  if (a.chunks == 0) {
+    const dim3 grid(a.rows < (1u << 20) ? a.rows : (1u << 20));
+    if (a.n <= SMALL_THREADS * 4)
+      hipLaunchKernelGGL((sample_short_kernel<T, 4>), grid, dim3(SMALL_THREADS), 0, s, a);
+    else
+      hipLaunchKernelGGL((sample_short_kernel<T, 16>), grid, dim3(SMALL_THREADS), 0, s, a);
+    return hipGetLastError();
+  }
+  const u64 all = a.rows;
+  for (u64 row0 = 0; row0 < all; row0 += SPLIT_ROWS) {
+    a.rows = (u32)(all - row0 < SPLIT_ROWS ? all - row0 : SPLIT_ROWS);
     const dim3 parts(a.rows * a.groups), threads(SPLIT_THREADS);
     hipLaunchKernelGGL(sample_best_kernel<T>, parts, threads, 0, s, a);
     if (a.rules) {
@@ -1075,11 +1321,20 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
       hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
       hipLaunchKernelGGL(sample_draw_kernel<T>, dim3(a.rows), threads, 0, s, a);
     }
+    if (a.rules) hipLaunchKernelGGL(sample_kernel<T>, dim3(a.rows), dim3(SAMPLE_THREADS), 0, s, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !a.rules) return e;
+    if (e != hipSuccess) return e;
+    // the next rows
+    a.scores += SPLIT_ROWS * a.ld * sizeof(T);
+    a.uniform += SPLIT_ROWS;
+    a.ids += SPLIT_ROWS;
+    if (a.logprobs) a.logprobs += SPLIT_ROWS;
+    if (a.o.temperature_dev) a.o.temperature_dev += SPLIT_ROWS;
+    if (a.o.top_k_dev) a.o.top_k_dev += SPLIT_ROWS;
+    if (a.o.top_p_dev) a.o.top_p_dev += SPLIT_ROWS;
+    if (a.o.min_p_dev) a.o.min_p_dev += SPLIT_ROWS;
   }
-  hipLaunchKernelGGL(sample_kernel<T>, dim3(a.rows < (1u << 20) ? a.rows : (1u << 20)), dim3(SAMPLE_THREADS), 0, s, a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace annmi

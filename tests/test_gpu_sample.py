@@ -91,6 +91,36 @@ def test_settings_of_each_long_row(env):
         check(torch, A, z, uniform(torch, rng, rows), temperature=t, top_k=k, top_p=p, min_p=m)
 
 
+@pytest.mark.parametrize("rows,n", [(9, 1024), (9, 1025), (5, 4096), (5, 4097), (300, 33), (5000, 5), (4097, 4500)])
+def test_sizes_at_which_rows_are_dealt_otherwise(env, rows, n):
+    torch, A, _ = env
+    rng = np.random.default_rng(rows + n)
+    for i, rule in enumerate((dict(top_k=n // 3 + 1, top_p=0.9), dict(top_p=0.7), dict(min_p=0.1, temperature=0.5))):
+        z = scores_of(torch, rng, rows, n, ("float32", "bfloat16", "float16")[i], 0.1)
+        u = uniform(torch, rng, rows)
+        if rows * n < 10 ** 6:
+            check(torch, A, z, u, **rule)
+        else:  # the last rows against a call of their own
+            ids, logprobs = A.ann_sample(z, u, **rule)
+            check(torch, A, z[-5:], u[-5:].contiguous(), **rule)
+            check(torch, A, z[4090:4096], u[4090:4096].contiguous(), **rule)
+            for lo in (0, 4000, rows - 50):
+                i2, lp2 = A.ann_sample(z[lo:lo + 50], u[lo:lo + 50].contiguous(), **rule)
+                assert torch.equal(i2, ids[lo:lo + 50]) and torch.equal(lp2, logprobs[lo:lo + 50])
+
+
+def test_many_candidates_around_the_cut(env):
+    """Long rows whose scores lie close together, and rows of few different scores."""
+    torch, A, _ = env
+    rng = np.random.default_rng(17)
+    n = 300_000
+    close = dev(torch, rng.standard_normal((3, n)).astype(np.float32) * 0.05)
+    steps = dev(torch, rng.integers(0, 40, (3, n)).astype(np.float32) / 8)
+    for rule in (dict(top_p=0.6), dict(top_k=70_000), dict(top_k=1000), dict(top_k=70_000, top_p=0.5), dict(top_p=0.999, min_p=0.9), {}):
+        for z in (close, close.bfloat16(), steps, steps.half()):
+            check(torch, A, z, uniform(torch, rng, 3), **rule)
+
+
 def test_draws_do_not_depend_on_the_other_rows(env):
     torch, A, _ = env
     rng = np.random.default_rng(16)
