@@ -521,6 +521,123 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
   if (w0 + ww < a.w.n) store_results<8, XF>(a, acc, w0 + ww, x0 + wx, lds + wave * store_room<8>());
 }
 
+// Few tiles of long rows, which would leave most of the chip idle: 32 4-bit rows x 16 G of the batch a workgroup, whose
+// eight waves take an eighth of the steps each, both sides from memory.  Their sums meet in LDS and are added up in
+// the order of the steps.
+struct Packed {};  // a batch of 4-bit rows
+constexpr u32 DEEP_WAVES = 8;
+constexpr u32 DEEP_ROWS = 32, DEEP_STRIDE = DEEP_ROWS + 4;
+
+template <typename T, int G, bool WIDE>
+__global__ __launch_bounds__(64 * DEEP_WAVES) void mx_product_deep_kernel(ProductArgs a, u32 tiles_w) {
+  constexpr bool PACKED = __is_same(T, Packed);
+  __shared__ __align__(16) float sums[DEEP_WAVES][16 * G][DEEP_STRIDE];
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const u64 w0 = (u64)(blockIdx.x % tiles_w) * DEEP_ROWS, x0 = (u64)(blockIdx.x / tiles_w) * (16 * G);
+  const u32 s0 = a.w.steps * wave / DEEP_WAVES, s1 = a.w.steps * (wave + 1) / DEEP_WAVES;
+  v4f acc[2][G] = {};
+  if constexpr (PACKED) {
+    Fragment w[2], x[G];
+    auto ask = [&](u32 s) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[i] = load_fragment(a.w, w0 + 16 * i, s);
+#pragma unroll
+      for (int j = 0; j < G; ++j) x[j] = load_fragment(a.q, x0 + 16 * j, s);
+    };
+    ask(min(s0, a.w.steps - 1));
+    for (u32 s = s0; s < s1; ++s) {
+      Fragment nw[2], nx[G];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) nw[i] = w[i];
+#pragma unroll
+      for (int j = 0; j < G; ++j) nx[j] = x[j];
+      ask(min(s + 1, s1 - 1));
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < G; ++j) acc[i][j] = mx_mfma(nw[i].codes, nx[j].codes, acc[i][j], nw[i].scale, nx[j].scale);
+    }
+  } else {
+    constexpr int PARTS = parts_of<T>();
+    for (u32 s = s0; s < s1; ++s) {
+      Fragment w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[i] = load_fragment(a.w, w0 + 16 * i, s);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const u32 at = s * MX_STEP + lane / 16 * 32 + c * 8;
+        Pack<T, 8> in[G];
+#pragma unroll
+        for (int j = 0; j < G; ++j) in[j] = load_batch<T, WIDE>(a, x0 + 16 * j + lane % 16, at);
+        const v8bf wv[2] = {unpack((u32)w[0].codes[c], (u32)w[0].scale), unpack((u32)w[1].codes[c], (u32)w[1].scale)};
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          mask_batch<T, WIDE>(a, in[j], at);
+          v8bf x[PARTS];
+          split_pack<T, PARTS>(in[j], x);
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], x[p], acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < G; ++j) *reinterpret_cast<v4f*>(&sums[wave][16 * j + lane % 16][16 * i + lane / 16 * 4]) = acc[i][j];
+  __syncthreads();
+  for (u32 at = tid; at < 16 * G * (DEEP_ROWS / 4); at += 64 * DEEP_WAVES) {
+    const u32 r = at / (DEEP_ROWS / 4), c = at % (DEEP_ROWS / 4) * 4;
+    v4f sum = *reinterpret_cast<const v4f*>(&sums[0][r][c]);
+#pragma unroll
+    for (u32 v = 1; v < DEEP_WAVES; ++v) sum += *reinterpret_cast<const v4f*>(&sums[v][r][c]);
+    const u64 x = x0 + r, w = w0 + c;
+    if (x >= a.nx) continue;
+    auto put = [&](auto type) {
+      using OUT = decltype(type);
+      OUT* to = reinterpret_cast<OUT*>(a.out) + x * a.ldo + w;
+      if (a.wide && w + 4 <= a.w.n) {
+        Pack<OUT, 4> p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p.v[e] = mx_round<OUT>(sum[e]);
+        *reinterpret_cast<Pack<OUT, 4>*>(to) = p;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (w + e < a.w.n) to[e] = mx_round<OUT>(sum[e]);
+      }
+    };
+    if (a.odtype == ANN_F32)
+      put(float());
+    else if (a.odtype == ANN_F16)
+      put(__half());
+    else
+      put(__bf16());
+  }
+}
+
+template <typename T, int G>
+hipError_t launch_deep(const ProductArgs& a, hipStream_t s) {
+  const u32 tiles_w = (u32)(((u64)a.w.n + DEEP_ROWS - 1) / DEEP_ROWS), tiles_x = (a.nx + 16 * G - 1) / (16 * G);
+  const auto kernel = a.wide_x ? mx_product_deep_kernel<T, G, true> : mx_product_deep_kernel<T, G, false>;
+  hipLaunchKernelGGL(kernel, dim3(tiles_w * tiles_x), dim3(64 * DEEP_WAVES), 0, s, a, tiles_w);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_deep(const ProductArgs& a, hipStream_t s) {
+  return a.nx <= 16 ? launch_deep<T, 1>(a, s) : a.nx <= 32 ? launch_deep<T, 2>(a, s) : launch_deep<T, 4>(a, s);
+}
+// Whether it is the faster one: its time grows with its tiles, that of the kernels with larger tiles with the row's
+// length alone as long as these do not fill the chip.  4,096 elements of bf16, by 64 x 4,000 and 64 x 30,000: 21 us
+// against 51, and 81 against 55; by 400 x 4,000 and 1,000 x 4,000: 73 against 110, and 159 against 113.
+bool deep_pays(const ProductArgs& a) {
+  const u32 rows = a.nx <= 16 ? 16 : a.nx <= 32 ? 32 : 64;
+  const u64 tiles = (((u64)a.w.n + DEEP_ROWS - 1) / DEEP_ROWS) * (((u64)a.nx + rows - 1) / rows);
+  return a.w.steps >= 8 && tiles * rows <= (a.nx <= 64 ? 512 : 1024) * 64;
+}
+
 template <typename T, int G, int WF, int AHEAD, bool LONG>
 hipError_t launch_few(const ProductArgs& a, size_t batch_bytes, u32 runs, hipStream_t s) {
   const u32 tiles = (u32)(((u64)a.w.n + 16 * WF - 1) / (16 * WF));
@@ -581,6 +698,7 @@ hipError_t launch_product16(const ProductArgs& a, hipStream_t s) {
     if (a.nx <= 48) return launch_few_rows<T, 3>(a, batch, s);
     return launch_few_rows<T, 4>(a, batch, s);
   }
+  if (deep_pays(a)) return launch_deep<T>(a, s);
   if (a.nx <= 64) return launch_many<T, 1>(a, s);
   if (a.nx <= 128 || PARTS > 1) return launch_many<T, 2>(a, s);
   if constexpr (PARTS == 1) return launch_many<T, 4>(a, s);
@@ -590,8 +708,12 @@ hipError_t launch_product(const ProductArgs& a, int xdtype, hipStream_t s) {
   if (xdtype == ANN_F32) return launch_product16<float>(a, s);
   if (xdtype == ANN_F16) return launch_product16<__half>(a, s);
   if (xdtype == ANN_BF16) return launch_product16<__bf16>(a, s);
+  if (deep_pays(a)) return launch_deep<Packed>(a, s);
   const u64 many_w = ((u64)a.w.n + BOTH_ROWS - 1) / BOTH_ROWS, many_x = ((u64)a.nx + BOTH_ROWS - 1) / BOTH_ROWS;
-  if (a.w.steps > 2 && many_w * many_x >= 128 && many_w * many_x < 1u << 22) {
+  const u64 many = many_w * many_x;
+  // Short rows of few tiles are left to the smaller tiles: 400 x 10,000, 80 tiles, of 512 elements in 12 us against 14,
+  // of 4,096 elements in 79 against 39.
+  if (a.w.steps > 2 && many >= (a.w.steps < 8 ? 128 : 24) && many < 1u << 22) {
     constexpr int lds = 2 * (2 * BOTH_ROWS * 128 + 2 * BOTH_ROWS * 8);
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx_product4_many_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
