@@ -24,9 +24,9 @@ struct QuantizeArgs {
   float* norms;
 };
 
-// N elements at a multiple of four bytes, for one load or store of all
+// N elements wherever they begin, for one load or store of all
 template <typename T, int N>
-struct __attribute__((packed, aligned(4))) WordPack {
+struct __attribute__((packed, aligned(alignof(T)))) AnyPack {
   T v[N];
 };
 
@@ -44,8 +44,8 @@ __device__ __forceinline__ float dpp_sum(float v) {
 // Four lanes take 32 elements, eight each: their largest magnitude by two exchanges, then the codes.  LPR lanes
 // (16, 32 or 64: one, two or four steps) take a row, longer rows in turns; a wave asks for four such pieces of rows
 // at once.  Bound by memory: a byte in for each element at least, 17 bytes out for 32.
-// WIDE: every row begins at a multiple of four bytes and has eight elements at least; eight are then read at once,
-// past d too, but in the last row, whose last eight are read where these reach its end.
+// WIDE: every row has eight elements at least; eight are then read at once, past d too, but in the last row, whose
+// last eight are read where these reach its end.
 template <typename T, int LPR, bool WIDE>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantizeArgs a) {
   constexpr u32 AHEAD = 4, PER_BLOCK = 256 / LPR;
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantizeArgs a) {
   for (u64 r0 = (u64)blockIdx.x * PER_BLOCK + threadIdx.x / LPR; r0 < a.n; r0 += rows_ahead ? stride * AHEAD : stride) {
     float norm[AHEAD] = {};
     for (u32 s0 = 0; s0 < turns; s0 += AHEAD) {
-      WordPack<T, 8> in[AHEAD];
+      AnyPack<T, 8> in[AHEAD];
       u64 row[AHEAD];
       u32 at[AHEAD];
       bool on[AHEAD];
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantizeArgs a) {
         if (WIDE) {
           const u32 first = at[u] < a.d ? at[u] : 0;
           early[u] = (a.n - 1 - r) * a.ldx < 7 && first + 8 > a.d ? first + 8 - a.d : 0;
-          in[u] = *reinterpret_cast<const WordPack<T, 8>*>(from + (first - early[u]));
+          in[u] = *reinterpret_cast<const AnyPack<T, 8>*>(from + (first - early[u]));
         } else {
 #pragma unroll
           for (u32 e = 0; e < 8; ++e) in[u].v[e] = from[min(at[u] + e, a.d - 1)];
@@ -161,8 +161,7 @@ hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s) {
 }
 template <typename T>
 hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s) {
-  const bool wide = aligned_to(a.x, 4) && a.ldx * sizeof(T) % 4 == 0 && a.d >= 8;
-  return wide ? launch_quantize<T, true>(a, s) : launch_quantize<T, false>(a, s);
+  return a.d >= 8 ? launch_quantize<T, true>(a, s) : launch_quantize<T, false>(a, s);
 }
 
 struct DequantizeArgs {
@@ -172,7 +171,6 @@ struct DequantizeArgs {
   u32 steps, d;
   char* out;
   u64 ldo;
-  u32 wide;  // every row of `out` begins at a multiple of 16 bytes
 };
 
 // A thread takes 16 bytes of a row of `out`, and the same ones of other rows in turn.  Bound by memory.
@@ -201,15 +199,15 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(DequantizeArgs a) {
         if (r0 + stride * u >= a.n) break;
         v2f p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 1)};
         if (E == 8) p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 2), p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], 1.0f, 3);
-        Pack<T, E> o;
+        AnyPack<T, E> o;
 #pragma unroll
         for (u32 j = 0; j < E / 2; ++j) {
           o.v[2 * j] = mx_round<T>(p[j].x * scale[u]);
           o.v[2 * j + 1] = mx_round<T>(p[j].y * scale[u]);
         }
         T* to = reinterpret_cast<T*>(a.out) + (r0 + stride * u) * a.ldo + c * E;
-        if (a.wide && c * E + E <= a.d) {
-          *reinterpret_cast<Pack<T, E>*>(to) = o;
+        if (c * E + E <= a.d) {
+          *reinterpret_cast<AnyPack<T, E>*>(to) = o;
         } else {
 #pragma unroll
           for (u32 j = 0; j < E; ++j)
@@ -268,8 +266,7 @@ int ann_mx_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint6
   if (n == 0) return ANN_OK;
   if (!out_dev) return fail(ANN_EINVAL, "null argument");
   if (!aligned_to(out_dev, esz)) return fail(ANN_EINVAL, "out not aligned to its elements");
-  DequantizeArgs a{codes_dev, scales_dev, n, mx_steps(d), d, static_cast<char*>(out_dev), ldo, 0};
-  a.wide = aligned_to(out_dev, 16) && ldo * esz % 16 == 0;
+  DequantizeArgs a{codes_dev, scales_dev, n, mx_steps(d), d, static_cast<char*>(out_dev), ldo};
   hipStream_t st = static_cast<hipStream_t>(stream);
   switch (dtype) {
     case ANN_F16: HIP_TRY(launch_dequantize<__half>(a, st)); break;

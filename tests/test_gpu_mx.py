@@ -121,6 +121,42 @@ def test_product_of_packed_rows(env, nx, n, d, out):
     check_product(A, torch, x, w, A.ann_mx_product(x, w, dtype=getattr(torch, out)), xv, wv)
 
 
+@pytest.mark.parametrize("dtype", ("float32", "float16", "bfloat16", "mx"))
+@pytest.mark.parametrize("nx,n,d,pad,out", [(8, 1, 1024, 0, "float32"), (16, 33, 1025, 0, "bfloat16"), (31, 500, 1100, 4, "float16"), (48, 100, 4096, 0, "float32"),
+                                            (65, 31, 2047, 1, "bfloat16"), (300, 129, 1536, 8, "float32"), (520, 64, 1152, 0, "float16")])
+def test_product_of_few_long_rows(env, dtype, nx, n, d, pad, out):
+    torch, A, _ = env
+    rng = np.random.default_rng(nx * n + d)
+    t, x = rows_of(torch, rng, nx, d, "bfloat16" if dtype == "mx" else dtype, pad)
+    w = A.ann_mx_quantize(rows_of(torch, rng, n, d, "float32", spread=4)[0])
+    wv = P.values(w.codes.cpu().numpy(), w.scales.cpu().numpy(), d)
+    if dtype == "mx":
+        t = A.ann_mx_quantize(t)
+        x = P.values(t.codes.cpu().numpy(), t.scales.cpu().numpy(), d)
+    got = A.ann_mx_product(t, w, dtype=getattr(torch, out))
+    check_product(A, torch, t, w, got, x, wv)
+    assert torch.equal(got, A.ann_mx_product(t, w, dtype=getattr(torch, out)))
+
+
+@pytest.mark.parametrize("dtype", ("uint8", "float16", "bfloat16", "float32"))
+@pytest.mark.parametrize("n,d,ld,at", [(9, 31, 31, 0), (50, 33, 35, 1), (3, 8, 9, 1), (21, 333, 337, 3), (1, 129, 131, 1)])
+def test_rows_that_begin_anywhere(env, dtype, n, d, ld, at):
+    """Rows at every alignment that their elements allow, read and written as they are elsewhere."""
+    torch, A, _ = env
+    rng = np.random.default_rng(n * d)
+    t = rows_of(torch, rng, n, d, dtype)[0]
+    wide = torch.zeros((n, ld), dtype=t.dtype, device=t.device)
+    wide[:, at:at + d] = t
+    r, s = A.ann_mx_quantize(t, norms=True), A.ann_mx_quantize(wide[:, at:at + d], norms=True)
+    for a, b in ((r.codes, s.codes), (r.scales, s.scales), (r.norms, s.norms)):
+        assert torch.equal(a, b)
+    if dtype != "uint8":
+        back = torch.full((n, ld), -7.0, dtype=t.dtype, device=t.device)
+        A.ann_mx_dequantize(r, out=back[:, at:at + d])
+        assert torch.equal(back[:, at:at + d], A.ann_mx_dequantize(r, dtype=t.dtype))
+        assert (back[:, :at] == -7.0).all() and (back[:, at + d:] == -7.0).all()
+
+
 def test_product_takes_blocks_apart(env):
     """Every element and every block's scale counts where it belongs: one at a time, exact."""
     torch, A, _ = env
