@@ -24,12 +24,6 @@ struct QuantizeArgs {
   float* norms;
 };
 
-// N elements wherever they begin, for one load or store of all
-template <typename T, int N>
-struct __attribute__((packed, aligned(alignof(T)))) AnyPack {
-  T v[N];
-};
-
 // exchanges inside 16 lanes, by one instruction each
 template <int CTRL>
 __device__ __forceinline__ u32 dpp(u32 v) {

@@ -69,6 +69,11 @@ template <typename T, int N>
 struct alignas(sizeof(T) * N) Pack {
   T v[N];
 };
+// N elements wherever they begin, for one load or store of all
+template <typename T, int N>
+struct __attribute__((packed, aligned(alignof(T)))) AnyPack {
+  T v[N];
+};
 
 // a larger key for a larger float; 0 for NaN
 __device__ __forceinline__ u32 float_key(float f) {

@@ -16,7 +16,7 @@ struct ProductArgs {
   u64 ldo;
   int odtype;
   u32 wide;  // four results can be written at once
-  u32 wide_x;  // eight elements of the batch can be read at once
+  u32 wide_x;  // the batch's rows have eight elements and more
 };
 
 constexpr size_t FEW_LDS = 160 * 1024;    // of a compute unit
@@ -242,12 +242,16 @@ constexpr int parts_of() {
   return sizeof(T) == 4 ? 3 : __is_same(T, __half) ? 2 : 1;
 }
 
-// Eight elements of a row of the batch from `at` on.  Rows past the last are read as it, and what lies past d as
-// elements before it; `mask_batch` makes those zeros, later, so that no branch waits for a load.
+// Eight elements of a row of the batch from `at` on; rows past the last are read as it.  WIDE, for rows of eight
+// elements and more: in one load wherever they begin, and the row's last eight where they would reach past its end.
+// `mask_batch` then brings these to their place and puts zeros behind them, later, so that no branch waits for a load.
+// (Rows that begin at any element against rows at multiples of 16 bytes: 98 us and 94 for 1,000 of 200 by 100,000,
+// where eight loads of an element each took 166.)
 template <typename T, bool WIDE>
 __device__ __forceinline__ Pack<T, 8> load_batch(const ProductArgs& a, u64 row, u32 at) {
   const T* from = reinterpret_cast<const T*>(a.x) + min(row, (u64)a.nx - 1) * a.ldx;
-  if (WIDE) return *reinterpret_cast<const Pack<T, 8>*>(from + (at < a.d ? at : 0));  // (d is a multiple of eight)
+  using Whole = Pack<T, 8>;
+  if (WIDE) return __builtin_bit_cast(Whole, *reinterpret_cast<const AnyPack<T, 8>*>(from + min(at, a.d - 8)));
   Pack<T, 8> p;
 #pragma unroll
   for (int e = 0; e < 8; ++e) p.v[e] = from[min(at + e, a.d - 1)];
@@ -255,7 +259,27 @@ __device__ __forceinline__ Pack<T, 8> load_batch(const ProductArgs& a, u64 row, 
 }
 template <typename T, bool WIDE>
 __device__ __forceinline__ void mask_batch(const ProductArgs& a, Pack<T, 8>& p, u32 at) {
-  if (at + 8 <= a.d) return;
+  if (WIDE) {
+    constexpr u32 WORDS = 2 * sizeof(T);
+    using Words = Pack<u32, WORDS>;
+    // Elements to leave out at the front.  (Written with unsigned numbers, at + 8 > d ? min(at + 8 - d, 8) : 0, the
+    // compiler made it 8 for some constant parts of `at`.)
+    const u32 past = min(max((int)(at + 8 - a.d), 0), 8);
+    Words w = __builtin_bit_cast(Words, p);
+#pragma unroll
+    for (u32 by = 8; by * sizeof(T) >= 4; by /= 2) {
+      const u32 words = by * sizeof(T) / 4;
+#pragma unroll
+      for (u32 i = 0; i < WORDS; ++i) w.v[i] = past & by ? (i + words < WORDS ? w.v[i + words] : 0u) : w.v[i];
+    }
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (u32 i = 0; i < WORDS; ++i) w.v[i] = __builtin_amdgcn_alignbit(i + 1 < WORDS ? w.v[i + 1] : 0u, w.v[i], past % 2 * 16);
+    }
+    using Whole = Pack<T, 8>;
+    p = __builtin_bit_cast(Whole, w);
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if (at + e >= a.d) p.v[e] = T(0.0f);
@@ -310,7 +334,10 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
   for (u32 i = threadIdx.x; i < a.nx * pieces; i += FEW_THREADS) {
     const u32 row = i / pieces, at = i % pieces;
     Pack<T, 8> piece = a.wide_x ? load_batch<T, true>(a, row, at * 8) : load_batch<T, false>(a, row, at * 8);
-    mask_batch<T, false>(a, piece, at * 8);
+    if (a.wide_x)
+      mask_batch<T, true>(a, piece, at * 8);
+    else
+      mask_batch<T, false>(a, piece, at * 8);
     v8bf x[PARTS];
     split_pack<T, PARTS>(piece, x);
 #pragma unroll
@@ -428,7 +455,7 @@ constexpr u32 MANY_THREADS = 512;
 constexpr u32 MANY_ROWS = 256;
 
 template <typename T, int XF, bool WIDE>
-__global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductArgs a, u32 tiles_w, u32 tiles) {
+__global__ __launch_bounds__(MANY_THREADS, XF == 1 ? 4 : 2) void mx_product_many_kernel(ProductArgs a, u32 tiles_w, u32 tiles) {
   constexpr int PARTS = parts_of<T>();
   constexpr u32 X_ROWS = 64 * XF;
   constexpr u32 W_BYTES = MANY_ROWS * 32, X_BYTES = X_ROWS * 128, STAGE = W_BYTES + PARTS * X_BYTES;
@@ -454,7 +481,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
 #pragma unroll
     for (int i = 0; i < XF; ++i) next_x[i] = load_batch<T, WIDE>(a, x0 + tid / 8 + 64 * i, h * 64 + tid % 8 * 8);
   };
-  auto keep = [&](u32 h) {
+  auto keep = [&](u32 h, auto ends) {
     char* stage = lds + h % 2 * STAGE;
     const u32 row = tid / 2;
 #pragma unroll
@@ -466,7 +493,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
     reinterpret_cast<u32*>(lds + 2 * STAGE)[h / 2 % 2 * MANY_ROWS + tid % MANY_ROWS] = next_scale;
 #pragma unroll
     for (int i = 0; i < XF; ++i) {
-      mask_batch<T, WIDE>(a, next_x[i], h * 64 + tid % 8 * 8);
+      if (ends) mask_batch<T, WIDE>(a, next_x[i], h * 64 + tid % 8 * 8);
       v8bf x[PARTS];
       split_pack<T, PARTS>(next_x[i], x);
       const u32 r = tid / 8 + 64 * i;
@@ -476,10 +503,10 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
   };
   v4f acc[8][XF] = {};
   fetch(0);
-  keep(0);
+  keep(0, std::true_type());
   fetch(1);
   u32 scale[8];
-  for (u32 h = 0; h < halves; ++h) {
+  auto turn = [&](u32 h, auto ends) __attribute__((always_inline)) {
     __syncthreads();
     const char* stage = lds + h % 2 * STAGE;
     long w[8];
@@ -495,7 +522,7 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
         // Behind the first products: they run while the next half is put away.  At the end a half too many is, and
         // not read: at a condition the compiler would move the products behind it.
         __builtin_amdgcn_sched_barrier(0);
-        keep(h + 1);
+        keep(h + 1, ends);
         fetch(min(h + 2, halves - 1));
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -516,7 +543,11 @@ __global__ __launch_bounds__(MANY_THREADS) void mx_product_many_kernel(ProductAr
           for (int p = PARTS - 1; p >= 0; --p) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, x[j][p], acc[i][j], 0, 0, 0);
       }
     }
-  }
+  };
+  // the rows' ends are looked for where they can be
+  u32 h = 0;
+  for (; h + 1 < a.d / 64; ++h) turn(h, std::false_type());
+  for (; h < halves; ++h) turn(h, std::true_type());
   __syncthreads();
   if (w0 + ww < a.w.n) store_results<8, XF>(a, acc, w0 + ww, x0 + wx, lds + wave * store_room<8>());
 }
@@ -528,11 +559,11 @@ struct Packed {};  // a batch of 4-bit rows
 constexpr u32 DEEP_WAVES = 8;
 constexpr u32 DEEP_ROWS = 32, DEEP_STRIDE = DEEP_ROWS + 4;
 
-template <typename T, int G, bool WIDE>
-__global__ __launch_bounds__(64 * DEEP_WAVES) void mx_product_deep_kernel(ProductArgs a, u32 tiles_w) {
+template <typename T, int G>
+__global__ __launch_bounds__(64 * DEEP_WAVES, 4) void mx_product_deep_kernel(ProductArgs a, u32 tiles_w) {
   constexpr bool PACKED = __is_same(T, Packed);
   __shared__ __align__(16) float sums[DEEP_WAVES][16 * G][DEEP_STRIDE];
-  const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const u32 tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const u64 w0 = (u64)(blockIdx.x % tiles_w) * DEEP_ROWS, x0 = (u64)(blockIdx.x / tiles_w) * (16 * G);
   const u32 s0 = a.w.steps * wave / DEEP_WAVES, s1 = a.w.steps * (wave + 1) / DEEP_WAVES;
   v4f acc[2][G] = {};
@@ -559,7 +590,7 @@ __global__ __launch_bounds__(64 * DEEP_WAVES) void mx_product_deep_kernel(Produc
     }
   } else {
     constexpr int PARTS = parts_of<T>();
-    for (u32 s = s0; s < s1; ++s) {
+    auto turn = [&](u32 s, auto ends) __attribute__((always_inline)) {
       Fragment w[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) w[i] = load_fragment(a.w, w0 + 16 * i, s);
@@ -568,11 +599,11 @@ __global__ __launch_bounds__(64 * DEEP_WAVES) void mx_product_deep_kernel(Produc
         const u32 at = s * MX_STEP + lane / 16 * 32 + c * 8;
         Pack<T, 8> in[G];
 #pragma unroll
-        for (int j = 0; j < G; ++j) in[j] = load_batch<T, WIDE>(a, x0 + 16 * j + lane % 16, at);
+        for (int j = 0; j < G; ++j) in[j] = load_batch<T, true>(a, x0 + 16 * j + lane % 16, at);
         const v8bf wv[2] = {unpack((u32)w[0].codes[c], (u32)w[0].scale), unpack((u32)w[1].codes[c], (u32)w[1].scale)};
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-          mask_batch<T, WIDE>(a, in[j], at);
+          if (ends) mask_batch<T, true>(a, in[j], at);
           v8bf x[PARTS];
           split_pack<T, PARTS>(in[j], x);
 #pragma unroll
@@ -581,7 +612,10 @@ __global__ __launch_bounds__(64 * DEEP_WAVES) void mx_product_deep_kernel(Produc
             for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i], x[p], acc[i][j], 0, 0, 0);
         }
       }
-    }
+    };
+    u32 s = s0;
+    for (; s < min(s1, a.d / MX_STEP); ++s) turn(s, std::false_type());
+    for (; s < s1; ++s) turn(s, std::true_type());
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -621,8 +655,7 @@ __global__ __launch_bounds__(64 * DEEP_WAVES) void mx_product_deep_kernel(Produc
 template <typename T, int G>
 hipError_t launch_deep(const ProductArgs& a, hipStream_t s) {
   const u32 tiles_w = (u32)(((u64)a.w.n + DEEP_ROWS - 1) / DEEP_ROWS), tiles_x = (a.nx + 16 * G - 1) / (16 * G);
-  const auto kernel = a.wide_x ? mx_product_deep_kernel<T, G, true> : mx_product_deep_kernel<T, G, false>;
-  hipLaunchKernelGGL(kernel, dim3(tiles_w * tiles_x), dim3(64 * DEEP_WAVES), 0, s, a, tiles_w);
+  hipLaunchKernelGGL((mx_product_deep_kernel<T, G>), dim3(tiles_w * tiles_x), dim3(64 * DEEP_WAVES), 0, s, a, tiles_w);
   return hipGetLastError();
 }
 template <typename T>
@@ -631,11 +664,12 @@ hipError_t launch_deep(const ProductArgs& a, hipStream_t s) {
 }
 // Whether it is the faster one: its time grows with its tiles, that of the kernels with larger tiles with the row's
 // length alone as long as these do not fill the chip.  4,096 elements of bf16, by 64 x 4,000 and 64 x 30,000: 21 us
-// against 51, and 81 against 55; by 400 x 4,000 and 1,000 x 4,000: 73 against 110, and 159 against 113.
-bool deep_pays(const ProductArgs& a) {
+// against 51, and 81 against 55; by 400 x 4,000 and 1,000 x 4,000: 73 against 110, and 159 against 113.  Of fp32, of
+// which each product takes three, 32 x 30,000: 132 against 97.
+bool deep_pays(const ProductArgs& a, int xdtype) {
   const u32 rows = a.nx <= 16 ? 16 : a.nx <= 32 ? 32 : 64;
   const u64 tiles = (((u64)a.w.n + DEEP_ROWS - 1) / DEEP_ROWS) * (((u64)a.nx + rows - 1) / rows);
-  return a.w.steps >= 8 && tiles * rows <= (a.nx <= 64 ? 512 : 1024) * 64;
+  return a.w.steps >= 8 && tiles * rows <= (a.nx > 64 ? 1024 : xdtype == ANN_F32 ? 384 : 512) * 64;
 }
 
 template <typename T, int G, int WF, int AHEAD, bool LONG>
@@ -660,7 +694,9 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
   constexpr int PARTS = parts_of<T>();
   constexpr int stages = 2 * (MANY_ROWS * 32 + PARTS * 64 * XF * 128) + 2 * MANY_ROWS * 4, room = MANY_THREADS / 64 * store_room<8>();
   constexpr int lds = stages > room ? stages : room;
-  const auto kernel = a.wide_x ? mx_product_many_kernel<T, XF, true> : mx_product_many_kernel<T, XF, false>;
+  auto kernel = mx_product_many_kernel<T, XF, true>;
+  if constexpr (XF < 4)
+    if (!a.wide_x) kernel = mx_product_many_kernel<T, XF, false>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   // (launches are counted in threads of 32 bits: long batches go in parts)
@@ -689,7 +725,7 @@ hipError_t launch_few_rows(const ProductArgs& a, size_t batch, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_product16(const ProductArgs& a, hipStream_t s) {
+hipError_t launch_product16(const ProductArgs& a, int xdtype, hipStream_t s) {
   constexpr int PARTS = parts_of<T>();
   const size_t batch = (size_t)a.nx * (a.w.steps * MX_STEP * 2 + 16) * PARTS;
   if (a.nx <= 64 && batch <= FEW_BATCH) {
@@ -698,17 +734,17 @@ hipError_t launch_product16(const ProductArgs& a, hipStream_t s) {
     if (a.nx <= 48) return launch_few_rows<T, 3>(a, batch, s);
     return launch_few_rows<T, 4>(a, batch, s);
   }
-  if (deep_pays(a)) return launch_deep<T>(a, s);
+  if (deep_pays(a, xdtype)) return launch_deep<T>(a, s);
   if (a.nx <= 64) return launch_many<T, 1>(a, s);
-  if (a.nx <= 128 || PARTS > 1) return launch_many<T, 2>(a, s);
+  if (a.nx <= 128 || PARTS > 1 || !a.wide_x) return launch_many<T, 2>(a, s);
   if constexpr (PARTS == 1) return launch_many<T, 4>(a, s);
 }
 
 hipError_t launch_product(const ProductArgs& a, int xdtype, hipStream_t s) {
-  if (xdtype == ANN_F32) return launch_product16<float>(a, s);
-  if (xdtype == ANN_F16) return launch_product16<__half>(a, s);
-  if (xdtype == ANN_BF16) return launch_product16<__bf16>(a, s);
-  if (deep_pays(a)) return launch_deep<Packed>(a, s);
+  if (xdtype == ANN_F32) return launch_product16<float>(a, xdtype, s);
+  if (xdtype == ANN_F16) return launch_product16<__half>(a, xdtype, s);
+  if (xdtype == ANN_BF16) return launch_product16<__bf16>(a, xdtype, s);
+  if (deep_pays(a, xdtype)) return launch_deep<Packed>(a, s);
   const u64 many_w = ((u64)a.w.n + BOTH_ROWS - 1) / BOTH_ROWS, many_x = ((u64)a.nx + BOTH_ROWS - 1) / BOTH_ROWS;
   const u64 many = many_w * many_x;
   // Short rows of few tiles are left to the smaller tiles: 400 x 10,000, 80 tiles, of 512 elements in 12 us against 14,
@@ -767,7 +803,7 @@ int ann_mx_product(const void* x_dev, uint64_t nx, ann_dtype xdtype, uint64_t ld
   a.w = {codes_dev, scales_dev, 0, mx_steps(d)};
   a.x = static_cast<const char*>(x_dev);
   a.ldx = ldx;
-  a.wide_x = aligned_to(x_dev, 8 * esz) && ldx % 8 == 0 && d % 8 == 0;
+  a.wide_x = d >= 8;
   a.d = d;
   return product(a, xdtype, nx, n, out_dev, out_dtype, ldo, stream);
 } catch (...) {
