@@ -516,8 +516,11 @@ __global__ __launch_bounds__(THREADS, 4) void mx_pick_kernel(MxSearchArgs a) {
   auto put = [&](u32 at, u64 key) {
     const u64 to = qrow * a.k + at;
     const float score = key_float(~(u32)(key >> 32));
-    a.ids[to] = (u32)key;
-    a.dists[to] = a.norms ? __builtin_fmaxf(0.0f, __builtin_fmaf(-2.0f, score, a.qnorms[qrow])) : 0.0f - score;
+    const float dist = a.norms ? __builtin_fmaf(-2.0f, score, a.qnorms[qrow]) : 0.0f - score;
+    // (|q|^2, or the distance, beyond fp32: distances grow with the place, so that none behind it is finite either)
+    const bool fine = dist < __builtin_inff();
+    a.ids[to] = fine ? (u32)key : ANN_NONE;
+    a.dists[to] = !fine ? __builtin_inff() : a.norms ? __builtin_fmaxf(0.0f, dist) : dist;
   };
   if (count <= PICK_FEW) {
     for (u32 c = tid; c < count; c += THREADS) {

@@ -309,6 +309,23 @@ def test_search_ties_and_rows_without_a_distance(env, l2):
     assert (ids == -1).all() and (dists == float("inf")).all()
 
 
+def test_search_of_norms_beyond_fp32(env):
+    """Squared distances that leave fp32's range are infinite: those rows are not returned, whatever the products are."""
+    torch, A, _ = env
+    x = np.ones((200, 40), np.float32)
+    x[5::20] = 2.0 ** 70
+    q = np.stack([np.ones(40, np.float32), np.full(40, 2.0 ** 70, np.float32), np.full(40, -2.0 ** 60, np.float32)])
+    rows, queries = (A.ann_mx_quantize(dev(torch, v), norms=True) for v in (x, q))
+    assert torch.isinf(queries.norms[1]) and torch.isfinite(queries.norms[2])
+    ids, dists = A.ann_mx_search(rows, queries, 128)
+    ids, dists = ids.cpu().numpy(), dists.cpu().numpy()
+    ones = np.setdiff1d(np.arange(200), np.arange(5, 200, 20))
+    assert (ids[0] == ones[:128]).all() and (dists[0] == 0).all()
+    assert (ids[1] == -1).all() and (dists[1] == np.inf).all()
+    # 2^120 * 40 and 2^60 * 80 + 40, which fp32 rounds away
+    assert (ids[2] == ones[:128]).all() and (dists[2] == np.float32(2.0 ** 120 * 40)).all()
+
+
 def test_search_of_no_rows_or_queries(env):
     torch, A, _ = env
     rows = A.ann_mx_quantize(torch.ones((10, 40), device="cuda:0"), norms=True)
