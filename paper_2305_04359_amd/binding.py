@@ -658,7 +658,6 @@ def _stream_of(t):
     return _raw_stream(t.device.index)
 
 
-
 def _element_code(t) -> int:
     """The ann_dtype of a tensor among the types that the calls on 4-bit rows and ann_sample take."""
     if not _ELEMENT_CODES:
@@ -677,9 +676,10 @@ def _rows2d(t, name):
     n, d = t.shape
     if n == 0 or d == 0:
         return t, d
-    if (d > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < d):
+    ld, step = t.stride()
+    if (d > 1 and step != 1) or (n > 1 and ld < d):
         raise ValueError(f"the rows of {name} must be contiguous and must not overlap")
-    return t, (t.stride(0) if n > 1 else d)
+    return t, (ld if n > 1 else d)
 
 
 def _one_value_per_row(t, name, dtype, rows, device):
@@ -727,14 +727,20 @@ def ann_mx_quantize(x, norms=False) -> MxRows:
     return out
 
 
+def _results(out, n, d, dtype, device):
+    """`out`, or a new (n, d) tensor where it is None, and the distance between its rows."""
+    if out is None:
+        torch = _torch()
+        return torch.empty((n, d), dtype=dtype or torch.float32, device=device), d
+    out, ld = _rows2d(out, "out")
+    if tuple(out.shape) != (n, d) or out.device != device or dtype not in (None, out.dtype):
+        raise ValueError(f"out must be ({n}, {d}) on {device}")
+    return out, ld
+
+
 def ann_mx_dequantize(rows: MxRows, dtype=None, out=None):
     """The values that 4-bit rows stand for: (n, d), float32 unless `dtype` or `out` says otherwise."""
-    torch = _torch()
-    if out is None:
-        out = torch.empty((rows.n, rows.d), dtype=dtype or torch.float32, device=rows.codes.device)
-    out, ld = _rows2d(out, "out")
-    if tuple(out.shape) != (rows.n, rows.d) or out.device != rows.codes.device or dtype not in (None, out.dtype):
-        raise ValueError(f"out must be ({rows.n}, {rows.d}) on {rows.codes.device}")
+    out, ld = _results(out, rows.codes.shape[0], rows.d, dtype, rows.codes.device)
     _check(lib().ann_mx_dequantize(rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.d, out.data_ptr(),
                                    _element_code(out), ld, _stream_of(out)))
     return out
@@ -743,22 +749,21 @@ def ann_mx_dequantize(rows: MxRows, dtype=None, out=None):
 def ann_mx_product(x, rows: MxRows, dtype=None, out=None):
     """Every row of `x` (a float32, float16 or bfloat16 tensor, or MxRows) times every 4-bit row: (len(x), n), float32
     unless `dtype` or `out` says otherwise."""
-    torch = _torch()
     packed = isinstance(x, MxRows)
-    nx, d, device = (x.n, x.d, x.codes.device) if packed else (*_rows2d(x, "x")[0].shape, x.device)
+    if packed:
+        nx, d, device = x.codes.shape[0], x.d, x.codes.device
+    else:
+        x, ldx = _rows2d(x, "x")
+        (nx, d), device = x.shape, x.device
     if d != rows.d or device != rows.codes.device:
         raise ValueError("x and rows must have the same row length and device")
-    if out is None:
-        out = torch.empty((nx, rows.n), dtype=dtype or torch.float32, device=device)
-    out, ldo = _rows2d(out, "out")
-    if tuple(out.shape) != (nx, rows.n) or out.device != device or dtype not in (None, out.dtype):
-        raise ValueError(f"out must be ({nx}, {rows.n}) on {device}")
+    out, ldo = _results(out, nx, rows.codes.shape[0], dtype, device)
     if packed:
         _check(lib().ann_mx_product_mx(x.codes.data_ptr(), x.scales.data_ptr(), nx, rows.codes.data_ptr(),
                                        rows.scales.data_ptr(), rows.n, d, out.data_ptr(), _element_code(out), ldo,
                                        _stream_of(out)))
     else:
-        _check(lib().ann_mx_product(x.data_ptr(), nx, _element_code(x), _rows2d(x, "x")[1], rows.codes.data_ptr(),
+        _check(lib().ann_mx_product(x.data_ptr(), nx, _element_code(x), ldx, rows.codes.data_ptr(),
                                     rows.scales.data_ptr(), rows.n, d, out.data_ptr(), _element_code(out), ldo,
                                     _stream_of(out)))
     return out
@@ -784,13 +789,13 @@ def ann_mx_search(rows: MxRows, queries: MxRows, k, metric=L2SQ, ids_out=None, d
     need = C.c_uint64(0)
     _check(lib().ann_mx_search_scratch(rows.n, rows.d, nq, k, C.byref(need)))
     scratch = _scratch(scratch, need.value, device)
+    for t, dtype, name in ((ids_out, torch.int32, "ids_out"), (dists_out, torch.float32, "dists_out")):
+        if t is not None and (tuple(t.shape) != (nq, k) or t.dtype != dtype or t.device != device or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous ({nq}, {k}) tensor of {dtype} on {device}")
     if ids_out is None:
         ids_out = torch.empty((nq, k), dtype=torch.int32, device=device)
     if dists_out is None:
         dists_out = torch.empty((nq, k), dtype=torch.float32, device=device)
-    for t, dtype, name in ((ids_out, torch.int32, "ids_out"), (dists_out, torch.float32, "dists_out")):
-        if tuple(t.shape) != (nq, k) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous ({nq}, {k}) tensor of {dtype} on {device}")
     _check(lib().ann_mx_search(rows.codes.data_ptr(), rows.scales.data_ptr(),
                                rows.norms.data_ptr() if rows.norms is not None else None, rows.n, rows.d, int(metric),
                                queries.codes.data_ptr(), queries.scales.data_ptr(),
@@ -814,19 +819,21 @@ def ann_sample(scores, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
                                ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
         if isinstance(value, torch.Tensor):
             setattr(o, name + "_dev", _one_value_per_row(value, name, dtype, rows, device).data_ptr())
+        elif name == "top_k" and not 0 <= value < 2 ** 32:
+            raise ValueError("top_k must be 0 (off) or above")
         else:
-            if name == "top_k" and not 0 <= value < 2 ** 32:
-                raise ValueError("top_k must be 0 (off) or above")
             setattr(o, name, value)
     need = C.c_uint64(0)
     _check(lib().ann_sample_scratch(rows, n, C.byref(need)))
     scratch = _scratch(scratch, need.value, device)
     if ids_out is None:
         ids_out = torch.empty(rows, dtype=torch.int32, device=device)
+    else:
+        _one_value_per_row(ids_out, "ids_out", torch.int32, rows, device)
     if logprobs_out is None:
         logprobs_out = torch.empty(rows, dtype=torch.float32, device=device)
-    _one_value_per_row(ids_out, "ids_out", torch.int32, rows, device)
-    _one_value_per_row(logprobs_out, "logprobs_out", torch.float32, rows, device)
+    else:
+        _one_value_per_row(logprobs_out, "logprobs_out", torch.float32, rows, device)
     _check(lib().ann_sample(scores.data_ptr(), rows, n, _element_code(scores), ld, C.byref(o), uniform.data_ptr(),
                             ids_out.data_ptr(), logprobs_out.data_ptr(), scratch.data_ptr(),
                             scratch.numel() * scratch.element_size(), _stream_of(scores)))
