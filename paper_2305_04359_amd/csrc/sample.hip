@@ -15,6 +15,7 @@ constexpr u32 SAMPLE_THREADS = 1024;
 constexpr u32 SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr u32 SAMPLE_BINS = 1024;  // one for each thread
 constexpr u32 SAMPLE_FEW = 1024;   // so many kept by top-k are sorted in LDS, and the row is not read again
+constexpr u32 SAMPLE_TOPS = 1024;  // most of the best scores of a row's parts
 
 // What the launches of a divided call know of a row.
 enum SampleKind : u32 {
@@ -42,14 +43,20 @@ struct SampleArgs {
   // each chunk, so that they do not depend on how many rows there are.
   u32 chunks, chunk, groups, per;
   u32 rules;           // top-k or top-p may be on
+  u32 no_hist;         // a bound serves all rows
   u32 no_mass;         // rows that are not drawn from their lists are left whole
+  u32 top_lanes;       // so many lanes share one of `tops`
+  u32 tops_of_row;     // 256 / top_lanes for each chunk
   float* most;         // (rows, chunks): best scores
+  float* tops;         // (rows, tops_of_row): of parts of the chunks
   double* others;      // masses other than the best candidates'
   u32* ones;           // numbers of best candidates
   u64* hist;           // (rows, SAMPLE_BINS)
   u64* list;           // (rows, capacity): candidates around the cut
   u32 capacity;
   u32* listed;
+  float* bound;        // (rows): of those whose k best are told by one
+  double* table;       // of the weights: TABLE entries
   SampleState* state;
 };
 
@@ -63,6 +70,12 @@ constexpr u32 key_grain() {
 
 constexpr u32 TABLE_BITS = 9;
 constexpr u32 TABLE = 1u << TABLE_BITS;
+__device__ __forceinline__ double table_entry(u32 i) { return exp2(i / (double)TABLE); }
+// (a copy: to work it out anew takes a divided call's workgroups longer than all else that they do but once)
+template <u32 THREADS>
+__device__ __forceinline__ void take_table(const double* from, double* to) {
+  for (u32 i = threadIdx.x; i < TABLE; i += THREADS) to[i] = from[i];
+}
 
 // exp((score - best) / temperature), within 1e-14 of itself: a power of two, times 2^(j / 512) from a table, times
 // the rest, whose logarithm is below ln 2 / 1024, by three terms of its series.  Adding 1.5 * 2^52 leaves the
@@ -99,38 +112,55 @@ using False = std::integral_constant<bool, false>;
 // Keeps the compiler from taking a value only where it is used: the values of a piece are to be taken side by side.
 __device__ __forceinline__ void taken(double& v) { asm volatile("" : "+v"(v)); }
 
-// f(id, scores) for the row's entries from..to, dealt to `ranks` threads in pieces of 16 bytes, AHEAD of them on
-// their way at once.  What the first and last piece lack of a whole one is -inf, as are no candidates.
-template <int AHEAD, typename T, typename F>
-__device__ __forceinline__ void each(const T* row, u64 from, u64 to, u32 rank, u32 ranks, F f) {
-  constexpr u32 V = 16 / sizeof(T);
+// A row's entries from..to, dealt to `ranks` threads in pieces of 16 bytes, AHEAD of them on their way at once: the
+// first ones from where the reader is made, so that what stands between that and `run` hides their way.  run(f) calls
+// f(id, scores) for each; what the first and last piece lack of a whole one is -inf, as are no candidates.
+template <int AHEAD, typename T>
+struct Reader {
+  static constexpr u32 V = 16 / sizeof(T);
   using Piece = Pack<T, V>;
-  const u64 skew = reinterpret_cast<uintptr_t>(row + from) % 16 / sizeof(T);
-  const u64 head = min(to, from + (V - skew) % V);
-  const u32 pieces = (u32)((to - head) / V);
-  const u64 tail = head + (u64)pieces * V;
-  const Piece* at = reinterpret_cast<const Piece*>(row + head);
-  for (u32 p = rank; p < pieces; p += AHEAD * ranks) {
-    Piece x[AHEAD];
+  const T* row;
+  u64 from, to, head, tail;
+  u32 rank, ranks, pieces;
+  Piece x[AHEAD];
+  __device__ __forceinline__ void ask(u32 p) {
+    const Piece* at = reinterpret_cast<const Piece*>(row + head);
 #pragma unroll
     for (u32 u = 0; u < AHEAD; ++u) x[u] = at[min(p + u * ranks, pieces - 1)];
+  }
+  __device__ __forceinline__ Reader(const T* row_, u64 from_, u64 to_, u32 rank_, u32 ranks_) : row(row_), from(from_), to(to_), rank(rank_), ranks(ranks_) {
+    const u64 skew = reinterpret_cast<uintptr_t>(row + from) % 16 / sizeof(T);
+    head = min(to, from + (V - skew) % V);
+    pieces = (u32)((to - head) / V);
+    tail = head + (u64)pieces * V;
+    if (pieces) ask(rank);
+  }
+  template <typename F>
+  __device__ __forceinline__ void run(F f) {
+    for (u32 p = rank; p < pieces; p += AHEAD * ranks) {
+      if (p != rank) ask(p);
 #pragma unroll
-    for (u32 u = 0; u < AHEAD; ++u) {
-      __builtin_amdgcn_sched_barrier(0);  // (or several pieces would be worked on at once, in too many registers)
-      if (p + u * ranks >= pieces) break;
+      for (u32 u = 0; u < AHEAD; ++u) {
+        __builtin_amdgcn_sched_barrier(0);  // (or several pieces would be worked on at once, in too many registers)
+        if (p + u * ranks >= pieces) break;
+        float v[V];
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) v[e] = mx_float(x[u].v[e]);
+        f(head + (u64)(p + u * ranks) * V, v);
+      }
+    }
+    if (rank < 2) {
+      const u64 lo = rank ? tail : from, hi = rank ? to : head;
       float v[V];
 #pragma unroll
-      for (u32 e = 0; e < V; ++e) v[e] = mx_float(x[u].v[e]);
-      f(head + (u64)(p + u * ranks) * V, v);
+      for (u32 e = 0; e < V; ++e) v[e] = lo + e < hi ? mx_float(row[lo + e]) : -__builtin_inff();
+      if (lo < hi) f(lo, v);
     }
   }
-  if (rank < 2 && ranks > 1) {
-    const u64 lo = rank ? tail : from, hi = rank ? to : head;
-    float v[V];
-#pragma unroll
-    for (u32 e = 0; e < V; ++e) v[e] = lo + e < hi ? mx_float(row[lo + e]) : -__builtin_inff();
-    if (lo < hi) f(lo, v);
-  }
+};
+template <int AHEAD, typename T, typename F>
+__device__ __forceinline__ void each(const T* row, u64 from, u64 to, u32 rank, u32 ranks, F f) {
+  Reader<AHEAD, T>(row, from, to, rank, ranks).run(f);
 }
 
 struct SampleLds {
@@ -252,6 +282,19 @@ struct RowRules {
     const float z = __builtin_fminf((w.most - v) * per_score, (float)(SAMPLE_BINS - 1));
     return v == w.most ? 0u : (u32)z;
   }
+  // The largest key of a candidate whose bin is b or above, or SAMPLE_LEAST: the bins fall with the key.  64 keys are
+  // tried at once, by whole waves.
+  __device__ __forceinline__ u32 last_of(u32 b) const {
+    const u32 lane = threadIdx.x % 64;
+    u64 lo = SAMPLE_LEAST, hi = (u64)best + 1;  // at or below lo: b or above; from hi on: below b
+    while (hi - lo > 1) {
+      const u64 step = (hi - lo + 63) / 64, x = lo + step * (lane + 1);
+      const u64 reach = __ballot(x < hi && linear_bin(key_float((u32)x)) >= b);
+      lo += step * (u32)__popcll(reach);
+      hi = min(hi, lo + step);
+    }
+    return (u32)lo;
+  }
   // The smallest key not below `from` whose weight reaches the floor of min-p.  Weights fall with the key; 64 keys
   // around the one that the logarithm gives are tried at once, by whole waves.
   __device__ __forceinline__ u32 min_p_key(u32 from) const {
@@ -315,6 +358,59 @@ __device__ void draw_few(const SampleArgs& a, u64 r, const RowRules& rules, u64 
   }
 }
 
+// The same for at most 64 candidates, `entry` of each lane, by one wave without the others: same sums in the same
+// order.  `room`: 64 places of LDS of the wave's own.
+__device__ void draw_by_wave(const SampleArgs& a, u64 r, const RowRules& rules, u64 limit, u32 count, u64 entry, double unit, u64* room) {
+  const u32 lane = threadIdx.x % 64;
+  // the lane's entry becomes the one whose rank it is, among those of the first `among` lanes
+  auto sort = [&](u64 mine, u32 among) {
+    using v2l = u64 __attribute__((ext_vector_type(2)));
+    room[lane] = lane < among ? mine : ~0ull;
+    u32 rank = 0;
+#pragma unroll 4
+    for (u32 j = 0; j < among; j += 2) {
+      const v2l x = *reinterpret_cast<const v2l*>(room + j);
+      rank += (x[0] < mine) + (x[1] < mine);
+    }
+    if (lane < among) room[rank] = mine;
+    return room[lane];
+  };
+  auto scan = [&](auto v) {
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) {
+      const auto x = __shfl_up(v, w);
+      if (lane >= (u32)w) v += x;
+    }
+    return v;
+  };
+  entry = sort(entry, count);
+  const bool mine = lane < limit && lane < count;
+  const float score = key_float(~(u32)(entry >> 32));
+  const double weight = mine ? rules.w.of(score) : 0.0;
+  bool keep = mine;
+  if (rules.p_on) {
+    const u64 units = mine ? rules.w.units(score, unit) : 0, upto = scan(units);
+    const u64 want = rules.wanted_mass(__shfl(upto, 63));  // (by all lanes)
+    keep = keep && upto - units < want;
+  }
+  if (rules.min_p > 0.0f) keep = keep && weight >= rules.floor_w;
+  const u32 kept = (u32)__popcll(__ballot(keep));  // (the first ones)
+  const u64 by_id = sort((entry & 0xFFFFFFFFull) << 32 | lane, kept);
+  const bool there = lane < kept;
+  const u32 from = there ? (u32)by_id & 63 : 0;
+  const double there_weight = __shfl(weight, (int)from);
+  const double x = there ? there_weight : 0.0;
+  const double run = scan(x), sum = __shfl(run, 63);
+  // the mass without this one, not as a difference from the whole where it is the best: it may be all the mass
+  const double rest = __shfl(scan(from == 0 ? 0.0 : x), 63);
+  const u64 above = __ballot(x > 0.0 && run > rules.u * sum), some = __ballot(x > 0.0);
+  const u32 at = above ? (u32)__builtin_ctzll(above) : 63u - (u32)__builtin_clzll(some);
+  if (lane == at) {
+    a.ids[r] = (u32)(by_id >> 32);
+    if (a.logprobs) a.logprobs[r] = static_cast<float>(-log1p((from == 0 ? rest : 1.0 + rest - x) / x));
+  }
+}
+
 // A workgroup per row.  The row is read once for its best score, once to three times for each cut, once for the draw
 // (and a sixteenth of it, and so on, to find the draw's place); all but the first time from the caches.
 template <typename T>
@@ -322,16 +418,17 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
   __shared__ SampleLds s;
   const u32 tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   constexpr u32 GRAIN = key_grain<T>();
-  if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
     if (a.state[r].kind != ROW_WHOLE) continue;
+    __syncthreads();
+    take_table<SAMPLE_THREADS>(a.table, s.table);
     RowRules rules(a, r, s.table);
     auto all = [&](auto f) { each<4>(row, 0, a.n, tid, SAMPLE_THREADS, f); };
     constexpr u32 V = 16 / sizeof(T);
 
     float most = -__builtin_inff();
-    each<8>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
+    each<4>(row, 0, a.n, tid, SAMPLE_THREADS, [&](u64, const float (&v)[V]) {
 #pragma unroll
       for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
     });
@@ -672,6 +769,33 @@ __device__ __forceinline__ float row_best(const SampleArgs& a, u64 r, u64* words
   return split_max(threadIdx.x < a.chunks ? a.most[r * a.chunks + threadIdx.x] : -__builtin_inff(), words);
 }
 
+// Whether the k best are told by a bound.  Where k parts of a row have a score of at least some value, so have k
+// candidates; that value is the k-th largest of the parts' best scores.  With k up to half of the parts, some 1.4 k
+// candidates reach it where good scores lie in no order, and no histogram is needed.
+constexpr u32 BOUND_MOST_K = SAMPLE_FEW / 2;
+__host__ __device__ __forceinline__ bool bound_serves(u32 top_k, u32 tops_of_row) { return top_k > 0 && top_k <= BOUND_MOST_K && top_k <= tops_of_row / 2; }
+// A value that k of the tops reach and none that is much larger does: the upper 20 bits of the k-th largest key, found
+// bit by bit, by one wave for a row.  (By one of each workgroup that lists: 66 us against 36 for 500 rows.)
+__device__ __forceinline__ float kth_top(const float* tops, u32 count, u32 k) {
+  constexpr u32 EACH = SAMPLE_TOPS / 64;
+  const u32 lane = threadIdx.x % 64;
+  u32 key[EACH], found = 0;
+#pragma unroll
+  for (u32 i = 0; i < EACH; ++i) key[i] = __float_as_uint(tops[min(i * 64 + lane, count - 1)]);  // (all on their way at once)
+#pragma unroll
+  for (u32 i = 0; i < EACH; ++i) key[i] = i * 64 + lane < count ? float_key(__uint_as_float(key[i])) : 0u;
+  for (u32 bit = 1u << 31; bit >= 1u << 12; bit >>= 1) {
+    u32 reach = 0;
+#pragma unroll
+    for (u32 i = 0; i < EACH; ++i) {
+      if (i * 64 >= count) break;
+      reach += (u32)__popcll(__ballot(key[i] >= (found | bit)));
+    }
+    if (reach >= k) found |= bit;
+  }
+  return key_float(max(found, SAMPLE_LEAST));
+}
+
 template <typename T>
 __global__ __launch_bounds__(SPLIT_THREADS) void sample_best_kernel(SampleArgs a) {
   __shared__ u64 words[SPLIT_THREADS / 64];
@@ -684,13 +808,28 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_best_kernel(SampleArgs a
 #pragma unroll
       for (u32 e = 0; e < V; ++e) most = __builtin_fmaxf(most, v[e]);  // (passes over NaN)
     });
+    if (a.rules) {
+      float top = most;
+      for (u32 w = 1; w < a.top_lanes; w *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, (int)w));
+      if (threadIdx.x % a.top_lanes == 0) a.tops[p.r * a.tops_of_row + (c * SPLIT_THREADS + threadIdx.x) / a.top_lanes] = top;
+    }
     most = split_max(most, words);
     if (threadIdx.x == 0) a.most[p.r * a.chunks + c] = most;
   }
+  if (blockIdx.x == 0)
+    for (u32 i = threadIdx.x; i < TABLE; i += SPLIT_THREADS) a.table[i] = table_entry(i);
   if (a.rules) {  // clears the row's histogram, a share each
     for (u32 b = p.group * SPLIT_THREADS + threadIdx.x; b < SAMPLE_BINS; b += a.groups * SPLIT_THREADS) a.hist[p.r * SAMPLE_BINS + b] = 0;
     if (p.group == 0 && threadIdx.x == 0) a.listed[p.r] = 0;
   }
+}
+
+__global__ __launch_bounds__(64) void sample_bound_kernel(SampleArgs a) {
+  const u64 r = blockIdx.x;
+  const u32 top_k = a.o.top_k_dev ? a.o.top_k_dev[r] : a.o.top_k;
+  if (!bound_serves(top_k, a.tops_of_row)) return;
+  const float bound = kth_top(a.tops + r * a.tops_of_row, a.tops_of_row, top_k);
+  if (threadIdx.x == 0) a.bound[r] = bound;
 }
 
 template <typename T>
@@ -701,16 +840,19 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_hist_kernel(SampleArgs a
   const Part p(a);
   const T* row = reinterpret_cast<const T*>(a.scores) + p.r * a.ld;
   RowRules rules(a, p.r, s.table);
-  if (!rules.set_best(row_best(a, p.r, s.wave)) || rules.greedy() || !(rules.k_on || rules.p_on)) return;
+  if (rules.greedy() || !(rules.k_on || rules.p_on)) return;
+  if (rules.k_on && bound_serves(rules.top_k, a.tops_of_row)) return;
+  Reader<4, T> entries(row, p.from, p.to, tid, SPLIT_THREADS);
+  if (!rules.set_best(row_best(a, p.r, s.wave))) return;
   const bool masses = !rules.k_on;
   if (masses)
-    for (u32 i = tid; i < TABLE; i += SPLIT_THREADS) s.table[i] = exp2(i / (double)TABLE);
+    take_table<SPLIT_THREADS>(a.table, s.table);
   for (u32 b = tid; b < SAMPLE_BINS; b += SPLIT_THREADS) s.hist[b] = 0;
   __syncthreads();
   const double unit = ldexp(1.0, (int)a.unit);
   const float most = rules.w.most;
   auto count = [&](auto of_masses) {
-    each<4>(row, p.from, p.to, tid, SPLIT_THREADS, [&](u64, const float (&v)[V]) {
+    entries.run([&](u64, const float (&v)[V]) {
       double raw[V];
       if (of_masses)
 #pragma unroll
@@ -739,7 +881,43 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_list_kernel(SampleArgs a
   SampleState state{};
   state.kind = ROW_CUT;
   state.bin = ~0u;
-  if (rules.set_best(row_best(a, p.r, s.wave)) && !rules.greedy() && (rules.k_on || rules.p_on)) {
+  // Into LDS first, and to the row's list at once; what LDS has no room for goes there by itself.
+  auto list = [&](auto& entries, auto listed) {
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    auto put = [&](u32 at, u64 entry) {  // (too many for the list: its count alone says so)
+      if (at < a.capacity) a.list[p.r * a.capacity + at] = entry;
+    };
+    entries.run([&](u64 i, const float (&v)[V]) {
+      bool any = false;
+#pragma unroll
+      for (u32 e = 0; e < V; ++e) any |= listed(v[e]);
+      if (!any) return;
+#pragma unroll
+      for (u32 e = 0; e < V; ++e)
+        if (listed(v[e])) {
+          const u64 entry = (u64)~float_key(v[e]) << 32 | (i + e);
+          const u32 at = atomicAdd(&s.count, 1u);
+          if (at < SAMPLE_BINS)
+            s.hist[at] = entry;
+          else
+            put(atomicAdd(&a.listed[p.r], 1u), entry);
+        }
+    });
+    __syncthreads();
+    const u32 count = min(s.count, SAMPLE_BINS);
+    if (tid == 0 && count) s.place = atomicAdd(&a.listed[p.r], count);
+    __syncthreads();
+    for (u32 i = tid; i < count; i += SPLIT_THREADS) put(s.place + i, s.hist[i]);
+  };
+  if (rules.greedy() || !(rules.k_on || rules.p_on)) {
+  } else if (rules.k_on && bound_serves(rules.top_k, a.tops_of_row)) {
+    Reader<4, T> entries(row, p.from, p.to, tid, SPLIT_THREADS);
+    const float bound = a.bound[p.r];
+    state.bin = 0, state.want = rules.top_k, state.few = 1;
+    list(entries, [&](float v) { return v >= bound && v > -__builtin_inff(); });
+  } else if (rules.set_best(row_best(a, p.r, s.wave))) {
+    Reader<4, T> entries(row, p.from, p.to, tid, SPLIT_THREADS);
     u64 bin[BINS], mine = 0, upto;
 #pragma unroll
     for (u32 i = 0; i < BINS; ++i) mine += bin[i] = a.hist[p.r * SAMPLE_BINS + tid * BINS + i];
@@ -763,32 +941,12 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_list_kernel(SampleArgs a
         if (!state.few && (in_bin > a.capacity || rules.p_on)) state.kind = ROW_WHOLE;
       }
       if (state.kind == ROW_CUT) {
-        // Into LDS first, and to the row's list at once; what LDS has no room for goes there by itself.
         __syncthreads();
-        if (tid == 0) s.count = 0;
+        // the keys of the bin, an end by a wave each
+        if (tid < 128) s.word[tid / 64] = tid < 64 ? rules.last_of(state.bin + 1) + 1 : state.few ? rules.best : rules.last_of(state.bin);
         __syncthreads();
-        auto put = [&](u32 at, u64 entry) {  // (too many for the list: its count alone says so)
-          if (at < a.capacity) a.list[p.r * a.capacity + at] = entry;
-        };
-        each<4>(row, p.from, p.to, tid, SPLIT_THREADS, [&](u64 i, const float (&v)[V]) {
-#pragma unroll
-          for (u32 e = 0; e < V; ++e) {
-            const u32 b = rules.linear_bin(v[e]);
-            if (v[e] > -__builtin_inff() && (b == state.bin || (state.few && b < state.bin))) {
-              const u64 entry = (u64)~float_key(v[e]) << 32 | (i + e);
-              const u32 at = atomicAdd(&s.count, 1u);
-              if (at < SAMPLE_BINS)
-                s.hist[at] = entry;
-              else
-                put(atomicAdd(&a.listed[p.r], 1u), entry);
-            }
-          }
-        });
-        __syncthreads();
-        const u32 count = min(s.count, SAMPLE_BINS);
-        if (tid == 0 && count) s.place = atomicAdd(&a.listed[p.r], count);
-        __syncthreads();
-        for (u32 i = tid; i < count; i += SPLIT_THREADS) put(s.place + i, s.hist[i]);
+        const float low = key_float((u32)s.word[0]), top = key_float((u32)s.word[1]);
+        list(entries, [&](float v) { return v >= low && v <= top; });
       }
     }
   }
@@ -804,7 +962,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
   const u64 r = blockIdx.x;
   SampleState state = a.state[r];
   if (state.kind != ROW_CUT) return;
-  if (tid < TABLE) s.table[tid] = exp2(tid / (double)TABLE);
+  take_table<SAMPLE_THREADS>(a.table, s.table);
   RowRules rules(a, r, s.table);
   float most = tid < a.chunks ? a.most[r * a.chunks + tid] : -__builtin_inff();
 #pragma unroll
@@ -813,7 +971,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
   __syncthreads();
   for (u32 w = 0; w < SAMPLE_WAVES; ++w) most = __builtin_fmaxf(most, __uint_as_float((u32)s.wave[w]));
   __syncthreads();
-  if (!rules.set_best(most) || rules.greedy()) return;  // (the draw needs no cut)
+  if (!rules.set_best(most)) {
+    if (tid == 0 && state.few) {  // (others are left to the draw, which may not follow)
+      a.ids[r] = ANN_NONE;
+      if (a.logprobs) a.logprobs[r] = -__builtin_inff();
+      a.state[r].kind = ROW_DONE;
+    }
+    return;
+  }
+  if (rules.greedy()) return;  // (the draw needs no cut)
   u32 lowest = SAMPLE_LEAST + 1;
   state.tie_end = a.n;
   if (state.bin != ~0u) {
@@ -863,7 +1029,25 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
         some = s.count;
       } while (some > SAMPLE_FEW);
       count = some;
+      if (state.few) {
+        // (a bound's: the first `want` are drawn from, up to the one that the count reaches)
+        __syncthreads();
+        block_sort(s, count);
+        const u64 last = s.hist[state.want - state.before - 1];
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        for (u32 i = tid; i < a.listed[r]; i += SAMPLE_THREADS)
+          if (list[i] <= last) s.hist[atomicAdd(&s.count, 1u)] = list[i];
+        __syncthreads();
+        count = s.count;
+      }
       __syncthreads();
+    } else if (!left && state.few && count <= 64) {
+      __syncthreads();
+      if (tid < 64) draw_by_wave(a, r, rules, rules.top_k, count, tid < count ? list[tid] : 0, unit, s.hist);
+      if (tid == 0) a.state[r].kind = ROW_DONE;
+      return;
     } else if (!left && tid < count) {
       s.hist[tid] = list[tid];
     }
@@ -906,9 +1090,12 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_mass_kernel(SampleArgs a
   const Part p(a);
   if (a.rules && a.state[p.r].kind != ROW_CUT) return;
   const T* row = reinterpret_cast<const T*>(a.scores) + p.r * a.ld;
-  for (u32 i = tid; i < TABLE; i += SPLIT_THREADS) s.table[i] = exp2(i / (double)TABLE);
   RowRules rules(a, p.r, s.table);
-  if (!rules.set_best(row_best(a, p.r, s.wave)) || rules.greedy()) return;
+  if (rules.greedy()) return;
+  auto chunk = [&](u32 c) { return Reader<4, T>(row, (u64)c * a.chunk, min(a.n, (u64)(c + 1) * a.chunk), tid, SPLIT_THREADS); };
+  Reader<4, T> entries = chunk(p.c0);
+  take_table<SPLIT_THREADS>(a.table, s.table);
+  if (!rules.set_best(row_best(a, p.r, s.wave))) return;
   float lowest = key_float(SAMPLE_LEAST + 1);
   u64 tie_end = a.n;
   if (a.rules)
@@ -920,7 +1107,8 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_mass_kernel(SampleArgs a
   for (u32 c = p.c0; c < p.c1; ++c) {
     double mine = 0.0;
     u32 ones = 0;
-    each<4>(row, (u64)c * a.chunk, min(a.n, (u64)(c + 1) * a.chunk), tid, SPLIT_THREADS, [&](u64 i, const float (&v)[V]) {
+    if (c != p.c0) entries = chunk(c);
+    entries.run([&](u64 i, const float (&v)[V]) {
       bool keep[V], any = false;
 #pragma unroll
       for (u32 e = 0; e < V; ++e) {
@@ -962,7 +1150,7 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_draw_kernel(SampleArgs a
   state.kind = ROW_CUT;
   if (a.rules) state = a.state[r];
   if (state.kind != ROW_CUT) return;
-  for (u32 i = tid; i < TABLE; i += SPLIT_THREADS) s.table[i] = exp2(i / (double)TABLE);
+  take_table<SPLIT_THREADS>(a.table, s.table);
   RowRules rules(a, r, s.table);
   const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
   if (tid == 0) s.word[0] = ~0ull, s.word[1] = ~0ull;
@@ -1025,6 +1213,7 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_draw_kernel(SampleArgs a
 
   // 4,096 entries at a time (longer chunks have several such blocks), sixteen neighbours a thread
   float v[EACH];
+  double weight[EACH];
   auto weigh = [&](u64 from) {
     const u64 mine = from + tid * EACH;
     if (reinterpret_cast<uintptr_t>(row) % 16 == 0 && mine + EACH <= hi) {
@@ -1041,8 +1230,8 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_draw_kernel(SampleArgs a
 #pragma unroll
     for (u32 e = 0; e < EACH; ++e) {
       const bool keep = v[e] > lowest || (v[e] == lowest && mine + e < tie_end);
-      if (!keep) v[e] = -__builtin_inff();
-      sum += w.of(v[e]);
+      weight[e] = w.of(keep ? v[e] : -__builtin_inff());
+      sum += weight[e];
     }
     return sum;
   };
@@ -1071,9 +1260,8 @@ __global__ __launch_bounds__(SPLIT_THREADS) void sample_draw_kernel(SampleArgs a
     u32 which = 0;
 #pragma unroll
     for (u32 e = 0; e < EACH; ++e) {  // (the running mass before this one: the last taken is the one that passes the aim)
-      const double next = w.of(v[e]);
-      if (next > 0.0 && !(x > 0.0 && before > aim)) which = e, x = next;
-      before += next;
+      if (weight[e] > 0.0 && !(x > 0.0 && before > aim)) which = e, x = weight[e];
+      before += weight[e];
     }
     a.ids[r] = (u32)(lo + tid * EACH + which);
     if (a.logprobs) {
@@ -1135,7 +1323,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void sample_short_kernel(SampleArgs 
   const u32 tid = threadIdx.x, n = (u32)a.n, first = tid * EACH;
   const double unit = ldexp(1.0, (int)a.unit);
   auto* words = reinterpret_cast<unsigned long long*>(s.word);
-  for (u32 i = tid; i < TABLE; i += SMALL_THREADS) s.table[i] = exp2(i / (double)TABLE);
+  for (u32 i = tid; i < TABLE; i += SMALL_THREADS) s.table[i] = table_entry(i);
   for (u64 r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* row = reinterpret_cast<const T*>(a.scores) + r * a.ld;
     float v[EACH], most = -__builtin_inff();
@@ -1293,7 +1481,12 @@ u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
   a.others = reinterpret_cast<double*>(take(rows * a.chunks * 8));
   a.ones = reinterpret_cast<u32*>(take(rows * a.chunks * 4));
   a.most = reinterpret_cast<float*>(take(rows * a.chunks * 4));
+  a.top_lanes = a.chunks <= 64 ? 16 : a.chunks <= 128 ? 32 : 64;
+  a.tops_of_row = a.chunks * (SPLIT_THREADS / a.top_lanes);
+  a.tops = reinterpret_cast<float*>(take(rows * a.tops_of_row * 4));
   a.listed = reinterpret_cast<u32*>(take(rows * 4));
+  a.bound = reinterpret_cast<float*>(take(rows * 4));
+  a.table = reinterpret_cast<double*>(take(TABLE * 8));
   return at;
 }
 
@@ -1313,7 +1506,8 @@ hipError_t launch_sample(SampleArgs a, hipStream_t s) {
     const dim3 parts(a.rows * a.groups), threads(SPLIT_THREADS);
     hipLaunchKernelGGL(sample_best_kernel<T>, parts, threads, 0, s, a);
     if (a.rules) {
-      hipLaunchKernelGGL(sample_hist_kernel<T>, parts, threads, 0, s, a);
+      if (a.no_hist || a.o.top_k_dev) hipLaunchKernelGGL(sample_bound_kernel, dim3(a.rows), dim3(64), 0, s, a);
+      if (!a.no_hist) hipLaunchKernelGGL(sample_hist_kernel<T>, parts, threads, 0, s, a);
       hipLaunchKernelGGL(sample_list_kernel<T>, parts, threads, 0, s, a);
       hipLaunchKernelGGL(sample_cut_kernel<T>, dim3(a.rows), dim3(SAMPLE_THREADS), 0, s, a);
     }
@@ -1321,7 +1515,7 @@ hipError_t launch_sample(SampleArgs a, hipStream_t s) {
       hipLaunchKernelGGL(sample_mass_kernel<T>, parts, threads, 0, s, a);
       hipLaunchKernelGGL(sample_draw_kernel<T>, dim3(a.rows), threads, 0, s, a);
     }
-    if (a.rules) hipLaunchKernelGGL(sample_kernel<T>, dim3(a.rows), dim3(SAMPLE_THREADS), 0, s, a);
+    if (a.rules) hipLaunchKernelGGL(sample_kernel<T>, dim3(a.rows < 256 ? a.rows : 256), dim3(SAMPLE_THREADS), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // the next rows
@@ -1389,6 +1583,7 @@ int ann_sample(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtyp
   hipStream_t st = static_cast<hipStream_t>(stream);
   // one top-k for all rows of which their lists hold enough, but where many scores are equal or masked
   a.no_mass = !a.o.top_k_dev && a.o.top_k > 0 && a.o.top_k <= SAMPLE_FEW / 2 && a.o.top_k < n;
+  a.no_hist = a.no_mass && bound_serves(a.o.top_k, a.tops_of_row);
   if (dtype == ANN_F16)
     HIP_TRY(launch_sample<__half>(a, st));
   else if (dtype == ANN_BF16)

@@ -121,6 +121,33 @@ def test_many_candidates_around_the_cut(env):
             check(torch, A, z, uniform(torch, rng, 3), **rule)
 
 
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16"))
+@pytest.mark.parametrize("n", (5000, 50_001, 300_007))
+def test_top_k_of_rows_in_any_order(env, dtype, n):
+    """Good scores side by side, few or no candidates, as many kept as there are parts of a row: one top-k for all rows, and
+    one for each."""
+    torch, A, _ = env
+    rng = np.random.default_rng(n)
+    z = 3.0 * rng.standard_normal((9, n))
+    z[0].sort()
+    z[1] = -np.sort(-z[1])
+    z[2, 4096:] = -np.inf
+    z[3, 30:] = -np.inf
+    z[4] = -np.inf
+    z[5] = np.round(z[5])
+    z[6, :] = 1.5
+    z[7, n // 2:n // 2 + 700] += 30.0
+    z[8, ::7] = np.nan
+    scores = dev(torch, z).to(getattr(torch, dtype))
+    u = uniform(torch, rng, 9)
+    for k in (1, 7, 16, 40, 64, 65, 160, 400, 512, 513, 1100):
+        for more in ({}, dict(top_p=0.8, min_p=0.01)):
+            check(torch, A, scores, u, top_k=k, temperature=0.9, **more)
+    each = torch.tensor([3, 16, 0, 70, 12, 31, 512, 90, 1], dtype=torch.int32, device="cuda:0")
+    for shift in range(9):
+        check(torch, A, scores, u, top_k=each.roll(shift).contiguous(), top_p=0.9)
+
+
 def test_draws_do_not_depend_on_the_other_rows(env):
     torch, A, _ = env
     rng = np.random.default_rng(16)
