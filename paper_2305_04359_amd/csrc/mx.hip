@@ -76,18 +76,31 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantizeArgs a) {
       for (u32 u = 0; u < AHEAD; ++u) {
         if (!on[u]) continue;  // (whole rows or steps at a time: 16 lanes alike)
         float v[8];
-#pragma unroll
-        for (u32 e = 0; e < 8; ++e) v[e] = mx_float(static_cast<T>(in[u].v[e]));
-        if (WIDE && early[u])
-          for (u32 k = 0; k < early[u]; ++k)
-#pragma unroll
-            for (u32 e = 0; e < 7; ++e) v[e] = v[e + 1];
-#pragma unroll
-        for (u32 e = 0; e < 8; ++e) v[e] = at[u] + e < a.d ? v[e] : 0.0f;
-        // magnitudes compare like their bits, and so do NaN and infinity
         u32 most = 0;
+        if constexpr (WIDE && sizeof(T) == 1) {  // bytes: eight at once where they can be (0 is a byte of 0)
+          u64 bytes = __builtin_bit_cast(u64, in[u]) >> (8 * early[u]);
+          const u32 there = at[u] < a.d ? min(a.d - at[u], 8u) : 0;
+          bytes &= there ? ~0ull >> (64 - 8 * there) : 0ull;
+          float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+          for (u32 e = 0; e < 8; ++e) {
+            v[e] = mx_float(static_cast<T>(bytes >> (8 * e)));
+            m = __builtin_fmaxf(m, __builtin_fabsf(v[e]));
+          }
+          most = __float_as_uint(m);
+        } else {
+#pragma unroll
+          for (u32 e = 0; e < 8; ++e) v[e] = mx_float(static_cast<T>(in[u].v[e]));
+          if (WIDE && early[u])
+            for (u32 k = 0; k < early[u]; ++k)
+#pragma unroll
+              for (u32 e = 0; e < 7; ++e) v[e] = v[e + 1];
+#pragma unroll
+          for (u32 e = 0; e < 8; ++e) v[e] = at[u] + e < a.d ? v[e] : 0.0f;
+          // magnitudes compare like their bits, and so do NaN and infinity
+#pragma unroll
+          for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        }
         most = max(most, dpp<DPP_XOR1>(most));
         most = max(most, dpp<DPP_XOR2>(most));
         const bool fine = most < 0x7F800000u;
