@@ -37,7 +37,8 @@ __device__ __forceinline__ float dpp_sum(float v) {
 
 // Four lanes take 32 elements, eight each: their largest magnitude by two exchanges, then the codes.  LPR lanes
 // (16, 32 or 64: one, two or four steps) take a row, longer rows in turns; a wave asks for four such pieces of rows
-// at once.  Bound by memory: a byte in for each element at least, 17 bytes out for 32.
+// at once.  A million int8 rows of 100 take 55 us, 3.1 TB/s of the 4.9 that a copy reaches: rows of bytes are bound by
+// vector instructions (1.1 a cycle and compute unit), wider types by memory.
 // WIDE: every row has eight elements at least; eight are then read at once, past d too, but in the last row, whose
 // last eight are read where these reach its end.
 template <typename T, int LPR, bool WIDE>
@@ -180,7 +181,8 @@ struct DequantizeArgs {
   u64 ldo;
 };
 
-// A thread takes 16 bytes of a row of `out`, and the same ones of other rows in turn.  Bound by memory.
+// A thread takes 16 bytes of a row of `out`, and the same ones of other rows in turn.  Bound by memory: a million rows of
+// 100 to fp32 take 114 us, 4.1 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(DequantizeArgs a) {
   constexpr u32 E = 16 / sizeof(T), AHEAD = 4;  // elements; rows at a time

@@ -84,7 +84,8 @@ __device__ __forceinline__ Fragment load_fragment(const MxRows& m, u64 row0, u32
   return f;
 }
 
-// 128 x 128 results a workgroup, 64 x 64 a wave; both sides from memory, step by step.
+// 128 x 128 results a workgroup, 64 x 64 a wave; both sides from memory, step by step.  For products whose results are
+// most of what moves: 1,000 x 10,000 of 128 elements to fp32 take 13 us, 3.2 TB/s.
 __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 tiles_w, u64 tiles) {
   __shared__ __align__(16) char room[4 * store_room<4>()];
   const u32 wave = threadIdx.x / 64;
@@ -111,6 +112,10 @@ __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 til
 // 4-bit rows on both sides, many: 256 x 256 results a workgroup of eight waves, 128 x 64 a wave.  Pairs of steps (256
 // elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for its turn.  The
 // scales lie in LDS so that a lane reads those of all its fragments' rows at once; the instruction picks the byte.
+// 4,096 x 65,536 of 2,048 elements take 438 us, 2.5 PFLOP/s (470 us once the clock has fallen under a load that lasts):
+// the matrix cores work 28 % of that time, and the waves wait for loads, one pair of steps ahead, for which LDS and
+// registers have room.  Workgroups that stay for several tiles, with the next one's first pairs asked for before the
+// results leave, are no faster (474 to 480 us in the place of 469).
 constexpr u32 BOTH_THREADS = 512;
 constexpr u32 BOTH_ROWS = 256;  // of either side
 
@@ -314,7 +319,9 @@ __device__ __forceinline__ v8bf unpack(u32 codes, u32 scale_byte) {
 // the next AHEAD steps on their way while it multiplies the present ones.  Long rows (LONG) are summed in runs of
 // groups of AHEAD steps, which are added up in their order, by one wave or, where 4-bit rows are few, by a wave
 // each: the sums do not depend on that.  Within a step the elements are taken in the order that a lane holds
-// them (8 at a time of its 32, the same ones on both sides).
+// them (8 at a time of its 32, the same ones on both sides).  One row of 4,096 bf16 by 131,072 is bound by memory: 56 us,
+// 5.1 TB/s.  33 rows of 200 floats by 500,001 take 47 us: three bf16 numbers for each element, the matrix cores at work
+// 41 % of the time, 2.8 TB/s.
 constexpr u32 FEW_THREADS = 512;
 
 template <int G, int WF>
@@ -451,6 +458,8 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
 // step (64 elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for
 // its turn and the one after is on its way.  The codes become bf16 numbers on their way from LDS to the matrix
 // cores, four conversions for each fragment of 16 rows x 32 elements, which serves XF x PARTS products.
+// 2,048 x 16,384 of 4,096 bf16 take 246 to 270 us, 1.0 to 1.1 PFLOP/s, by the clock that the load leaves; the library's
+// product of bf16 on both sides takes 229.  The matrix cores work 53 % of the time.
 constexpr u32 MANY_THREADS = 512;
 constexpr u32 MANY_ROWS = 256;
 

