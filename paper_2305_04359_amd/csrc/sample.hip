@@ -1022,7 +1022,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_cut_kernel(SampleArgs a
         if (tid == 0) s.count = 0;
         __syncthreads();
         lo += (u64)s.bin << shift;
-        hi = min(hi, lo + ((1ull << shift) - 1));
+        hi = min(hi, lo + (((u64)1 << shift) - 1));  // (of one type: mixed ones are compared as doubles)
         state.before += s.word;
         for (u32 i = tid; i < count; i += SAMPLE_THREADS) {
           const u64 entry = list[i];

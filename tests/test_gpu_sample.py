@@ -121,6 +121,17 @@ def test_many_candidates_around_the_cut(env):
             check(torch, A, z, uniform(torch, rng, 3), **rule)
 
 
+def test_long_lists_of_equal_scores(env):
+    """Some three thousand equal candidates at the cut, of which some are kept: they are told apart by their ids alone."""
+    torch, A, _ = env
+    rng = np.random.default_rng(23)
+    z = dev(torch, rng.integers(0, 100, (4, 300_007)).astype(np.float32))
+    for rule in (dict(top_p=0.9), dict(top_p=0.9, temperature=2.0), dict(top_p=0.3, temperature=8.0), dict(top_p=0.97, temperature=8.0, min_p=1e-4),
+                 dict(top_k=4500), dict(top_k=100_000)):
+        for scores in (z, -z, z.bfloat16()):
+            check(torch, A, scores, uniform(torch, rng, 4), **rule)
+
+
 @pytest.mark.parametrize("dtype", ("float32", "bfloat16"))
 @pytest.mark.parametrize("n", (5000, 50_001, 300_007))
 def test_top_k_of_rows_in_any_order(env, dtype, n):
