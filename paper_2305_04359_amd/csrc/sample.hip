@@ -2,7 +2,8 @@
 //
 // All three rules keep a prefix of the candidates sorted by (score downwards, id), so the kept ones are told by a
 // cut: every key above it, and the first `ties` of those at it.  The cuts of top-k (by counts) and top-p (by
-// masses) are found by histograms over ever shorter ranges of keys.  Masses are sums of weights rounded to multiples
+// masses) are found by histograms over ever shorter ranges of keys, a small top-k's by a bound from the best scores of the
+// row's parts.  Masses are sums of weights rounded to multiples
 // of a power of two: whole numbers, whose sums depend on no order.  The draw sums the kept weights in fp64 in a
 // fixed order.
 #include <type_traits>
