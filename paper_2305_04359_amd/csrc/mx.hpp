@@ -82,6 +82,14 @@ __device__ __forceinline__ u32 float_key(float f) {
 }
 __device__ __forceinline__ float key_float(u32 k) { return __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k); }
 
+// Stands where lanes of one wave read from LDS what others of it wrote, and before they write there again.  The hardware
+// keeps a wave's accesses to LDS in order; this has the compiler keep them too, and takes no instruction.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 inline bool aligned_to(const void* p, u64 bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 constexpr u64 dtype_bytes(int t) { return t == ANN_F32 ? 4 : t == ANN_F16 || t == ANN_BF16 ? 2 : t == ANN_U8 || t == ANN_I8 ? 1 : 0; }
 

@@ -36,8 +36,10 @@ __device__ __forceinline__ void store_as(const ProductArgs& a, const v4f (&acc)[
 #pragma unroll
   for (int j = 0; j < XF; ++j) {
     if (x0 + 16 * j >= a.nx) break;
+    wave_exchange();
 #pragma unroll
     for (int i = 0; i < WF; ++i) *reinterpret_cast<v4f*>(room + lane % 16 * STRIDE + 16 * i + lane / 16 * 4) = acc[i][j];
+    wave_exchange();
     OUT* out = reinterpret_cast<OUT*>(a.out) + (x0 + 16 * j) * a.ldo + w0;
     const u32 xs = (u32)min((u64)16, a.nx - (x0 + 16 * j)), ws = (u32)min((u64)ROW, a.w.n - w0);
     if (a.wide && ws == ROW) {

@@ -366,14 +366,18 @@ __device__ void draw_by_wave(const SampleArgs& a, u64 r, const RowRules& rules, 
   // the lane's entry becomes the one whose rank it is, among those of the first `among` lanes
   auto sort = [&](u64 mine, u32 among) {
     using v2l = u64 __attribute__((ext_vector_type(2)));
+    wave_exchange();
     room[lane] = lane < among ? mine : ~0ull;
+    wave_exchange();
     u32 rank = 0;
 #pragma unroll 4
     for (u32 j = 0; j < among; j += 2) {
       const v2l x = *reinterpret_cast<const v2l*>(room + j);
       rank += (x[0] < mine) + (x[1] < mine);
     }
+    wave_exchange();
     if (lane < among) room[rank] = mine;
+    wave_exchange();
     return room[lane];
   };
   auto scan = [&](auto v) {
