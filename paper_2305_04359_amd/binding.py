@@ -660,10 +660,12 @@ def _run(call, t, *args):
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
     index = t.device.index
     if index == _current_device():
-        _check(call(*args, _raw_stream(index)))
+        rc = call(*args, _raw_stream(index))
     else:
         with _torch().cuda.device(index):
-            _check(call(*args, _raw_stream(index)))
+            rc = call(*args, _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def _element_code(t) -> int:

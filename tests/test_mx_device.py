@@ -33,10 +33,15 @@ class Tensor:
         return self.dtype.itemsize
 
 
+class Calls(list):
+    """(name, current device, stream) of the calls into the library, which return `rc`."""
+    rc = 0
+
+
 @pytest.fixture
 def calls(monkeypatch):
-    """[(name, current device, stream)] of the calls into the library; device 0 is current outside of them."""
-    made, now = [], [0]
+    """Device 0 is current outside of the calls."""
+    made, now = Calls(), [0]
 
     class Device:
         def __init__(self, index):
@@ -55,6 +60,7 @@ def calls(monkeypatch):
                     args[-1]._obj.value = 64
                 else:
                     made.append((name, now[0], args[-1]))
+                    return made.rc
                 return 0
             return call
 
@@ -88,7 +94,11 @@ def test_calls_run_on_the_device_of_their_tensors(calls):
 
 
 def test_the_device_comes_back_after_a_refusal(monkeypatch, calls):
-    monkeypatch.setattr(A, "_check", lambda rc: (_ for _ in ()).throw(A.AnnError(-1, "refused")))
+    def refuse(rc):
+        raise A.AnnError(rc, "refused")
+
+    monkeypatch.setattr(A, "_check", refuse)
+    calls.rc = -1
     with pytest.raises(A.AnnError):
         A.ann_mx_quantize(Tensor((5, 200)))
     assert [c[1] for c in calls] == [1]
