@@ -159,12 +159,12 @@ hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s) {
   // four rows for each place, where a turn takes a row
   const u64 per = 256 / lpr * (a.steps <= 4 ? 4 : 1), blocks = ((u64)a.n + per - 1) / per;
   const u32 grid = (u32)(blocks < (1u << 20) ? blocks : (1u << 20));
-  if (lpr == 16)
-    hipLaunchKernelGGL((mx_quantize_kernel<T, 16, WIDE>), dim3(grid), dim3(256), 0, s, a);
-  else if (lpr == 32)
-    hipLaunchKernelGGL((mx_quantize_kernel<T, 32, WIDE>), dim3(grid), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((mx_quantize_kernel<T, 64, WIDE>), dim3(grid), dim3(256), 0, s, a);
+  auto kernel = mx_quantize_kernel<T, 16, WIDE>;
+  if constexpr (WIDE) {  // (others have one step)
+    if (lpr == 32) kernel = mx_quantize_kernel<T, 32, WIDE>;
+    if (lpr == 64) kernel = mx_quantize_kernel<T, 64, WIDE>;
+  }
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>

@@ -21,6 +21,9 @@ struct ProductArgs {
 
 constexpr size_t FEW_LDS = 160 * 1024;    // of a compute unit
 constexpr size_t FEW_BATCH = 96 * 1024;   // most of it that a batch may take
+constexpr u32 LONG_STEPS = 8;             // rows of so many steps are summed in runs
+constexpr size_t few_batch(u32 nx, u32 steps, int parts) { return (size_t)nx * (steps * MX_STEP * 2 + 16) * parts; }
+static_assert(few_batch(64, 1, 3) <= FEW_BATCH);  // so that 64 rows shorter than a step always fit
 
 // The 16 WF x 16 XF results of a wave.  They lie in the matrix instruction's order (a lane holds four neighbours of a
 // row of `out`); through LDS of the wave's own they get into runs of a whole row's part, so that stores fill lines
@@ -342,8 +345,9 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
   const u32 pieces = a.w.steps * 16;
   for (u32 i = threadIdx.x; i < a.nx * pieces; i += FEW_THREADS) {
     const u32 row = i / pieces, at = i % pieces;
-    Pack<T, 8> piece = a.wide_x ? load_batch<T, true>(a, row, at * 8) : load_batch<T, false>(a, row, at * 8);
-    if (a.wide_x)
+    const bool wide = LONG || a.wide_x;
+    Pack<T, 8> piece = wide ? load_batch<T, true>(a, row, at * 8) : load_batch<T, false>(a, row, at * 8);
+    if (wide)
       mask_batch<T, true>(a, piece, at * 8);
     else
       mask_batch<T, false>(a, piece, at * 8);
@@ -706,7 +710,7 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
   constexpr int stages = 2 * (MANY_ROWS * 32 + PARTS * 64 * XF * 128) + 2 * MANY_ROWS * 4, room = MANY_THREADS / 64 * store_room<8>();
   constexpr int lds = stages > room ? stages : room;
   auto kernel = mx_product_many_kernel<T, XF, true>;
-  if constexpr (XF < 4)
+  if constexpr (XF == 2)  // (up to 64 rows of fewer than eight elements are left to the kernel of few rows)
     if (!a.wide_x) kernel = mx_product_many_kernel<T, XF, false>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
@@ -730,15 +734,16 @@ hipError_t launch_many(const ProductArgs& a, hipStream_t s) {
 template <typename T, int G>
 hipError_t launch_few_rows(const ProductArgs& a, size_t batch, hipStream_t s) {
   // runs of one group of four steps and more
-  const u32 runs = a.w.steps >= 32 ? 8 : a.w.steps >= 16 ? 4 : a.w.steps >= 8 ? 2 : 1;
-  if (runs > 1) return launch_few<T, G, G == 1 ? 1 : 2, G == 1 ? 4 : 2, true>(a, batch, runs, s);
+  if constexpr (few_batch(16 * G - 15, LONG_STEPS, parts_of<T>()) <= FEW_BATCH)  // (else no batch of long rows fits)
+    if (a.w.steps >= LONG_STEPS)
+      return launch_few<T, G, G == 1 ? 1 : 2, G == 1 ? 4 : 2, true>(a, batch, a.w.steps >= 32 ? 8 : a.w.steps >= 16 ? 4 : 2, s);
   return launch_few<T, G, G == 1 ? 2 : 4, 2, false>(a, batch, 1, s);
 }
 
 template <typename T>
 hipError_t launch_product16(const ProductArgs& a, int xdtype, hipStream_t s) {
   constexpr int PARTS = parts_of<T>();
-  const size_t batch = (size_t)a.nx * (a.w.steps * MX_STEP * 2 + 16) * PARTS;
+  const size_t batch = few_batch(a.nx, a.w.steps, PARTS);
   if (a.nx <= 64 && batch <= FEW_BATCH) {
     if (a.nx <= 16) return launch_few_rows<T, 1>(a, batch, s);
     if (a.nx <= 32) return launch_few_rows<T, 2>(a, batch, s);
