@@ -532,9 +532,13 @@ int ann_mx_product_mx(const uint8_t* xcodes_dev, const uint8_t* xscales_dev, uin
  *   ANN_MIPS  distance -s
  *   ANN_L2SQ  distance max(0, |q|^2 - 2 (s - |x|^2 / 2)), from the norms that
  *             ann_mx_quantize wrote (norms_dev, qnorms_dev; unused for MIPS)
- * ordered by (s or s - |x|^2 / 2 downwards, id).  Where the products' exponents
- * stay within 2^11 of each other, as those of rows of one kind do, all sums
- * are exact and this is the order of (distance, id).
+ * ordered by (s or s - |x|^2 / 2 downwards, id).  A product's exponent is what
+ * the scale bytes of its two elements, neither of them 0, add up to.  Where
+ * those of all products lie within r of each other and d 2^r <= 2^16, sums are
+ * exact, and this is the order of (exact distance, id); for ANN_L2SQ
+ * d 2^r <= 2^15, and products of a row and of a query with themselves count
+ * too.  Beyond that sums are rounded, and rows whose distances differ by less
+ * than the rounding may change places.
  *   ids_dev, dists_dev  nq x k uint32 / float; ANN_NONE / +inf where there are
  *               fewer than k rows.  Rows whose distance is NaN or +inf are
  *               never returned.
