@@ -648,8 +648,8 @@ _ELEMENT_CODES = {}
 _raw_stream = _current_device = None
 
 
-def _run(call, t, *args):
-    """`call` with `args` and the current stream of the device of `t`, and with that device current: the library
+def _run(call, device, *args):
+    """`call` with `args` and the current stream of `device`, the one of its tensors, and with it current: the library
     launches on the current one, and takes the handle of a default stream for the default stream there.  PyTorch's own
     short ways to both where there are any: the stream object that torch.cuda.current_stream() makes takes 3 us, a third
     of a small call."""
@@ -658,7 +658,7 @@ def _run(call, t, *args):
         torch = _torch()
         _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-    index = t.device.index
+    index = device.index
     if index == _current_device():
         rc = call(*args, _raw_stream(index))
     else:
@@ -725,14 +725,14 @@ def ann_mx_quantize(x, norms=False) -> MxRows:
     """Rows of a 2-D device tensor (uint8, int8, float32, float16 or bfloat16) as microscaled 4-bit rows."""
     torch = _torch()
     x, ld = _rows2d(x, "x")
-    n, d = x.shape
+    (n, d), device = x.shape, x.device
     steps = (d + 127) // 128
     out = MxRows.__new__(MxRows)
-    out.codes = torch.empty((n, 64 * steps), dtype=torch.uint8, device=x.device)
-    out.scales = torch.empty((n, 4 * steps), dtype=torch.uint8, device=x.device)
-    out.norms = torch.empty(n, dtype=torch.float32, device=x.device) if norms else None
+    out.codes = torch.empty((n, 64 * steps), dtype=torch.uint8, device=device)
+    out.scales = torch.empty((n, 4 * steps), dtype=torch.uint8, device=device)
+    out.norms = torch.empty(n, dtype=torch.float32, device=device) if norms else None
     out.d = d
-    _run(lib().ann_mx_quantize, x, x.data_ptr(), n, d, _element_code(x), ld, out.codes.data_ptr(), out.scales.data_ptr(),
+    _run(lib().ann_mx_quantize, device, x.data_ptr(), n, d, _element_code(x), ld, out.codes.data_ptr(), out.scales.data_ptr(),
          out.norms.data_ptr() if norms else None)
     return out
 
@@ -750,8 +750,9 @@ def _results(out, n, d, dtype, device):
 
 def ann_mx_dequantize(rows: MxRows, dtype=None, out=None):
     """The values that 4-bit rows stand for: (n, d), float32 unless `dtype` or `out` says otherwise."""
-    out, ld = _results(out, rows.codes.shape[0], rows.d, dtype, rows.codes.device)
-    _run(lib().ann_mx_dequantize, out, rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.d, out.data_ptr(),
+    n, device = rows.codes.shape[0], rows.codes.device
+    out, ld = _results(out, n, rows.d, dtype, device)
+    _run(lib().ann_mx_dequantize, device, rows.codes.data_ptr(), rows.scales.data_ptr(), n, rows.d, out.data_ptr(),
          _element_code(out), ld)
     return out
 
@@ -769,10 +770,10 @@ def ann_mx_product(x, rows: MxRows, dtype=None, out=None):
         raise ValueError("x and rows must have the same row length and device")
     out, ldo = _results(out, nx, rows.codes.shape[0], dtype, device)
     if packed:
-        _run(lib().ann_mx_product_mx, out, x.codes.data_ptr(), x.scales.data_ptr(), nx, rows.codes.data_ptr(),
+        _run(lib().ann_mx_product_mx, device, x.codes.data_ptr(), x.scales.data_ptr(), nx, rows.codes.data_ptr(),
              rows.scales.data_ptr(), rows.n, d, out.data_ptr(), _element_code(out), ldo)
     else:
-        _run(lib().ann_mx_product, out, x.data_ptr(), nx, _element_code(x), ldx, rows.codes.data_ptr(),
+        _run(lib().ann_mx_product, device, x.data_ptr(), nx, _element_code(x), ldx, rows.codes.data_ptr(),
              rows.scales.data_ptr(), rows.n, d, out.data_ptr(), _element_code(out), ldo)
     return out
 
@@ -804,7 +805,7 @@ def ann_mx_search(rows: MxRows, queries: MxRows, k, metric=L2SQ, ids_out=None, d
         ids_out = torch.empty((nq, k), dtype=torch.int32, device=device)
     if dists_out is None:
         dists_out = torch.empty((nq, k), dtype=torch.float32, device=device)
-    _run(lib().ann_mx_search, ids_out, rows.codes.data_ptr(), rows.scales.data_ptr(),
+    _run(lib().ann_mx_search, device, rows.codes.data_ptr(), rows.scales.data_ptr(),
          rows.norms.data_ptr() if rows.norms is not None else None, rows.n, rows.d, int(metric), queries.codes.data_ptr(),
          queries.scales.data_ptr(), queries.norms.data_ptr() if queries.norms is not None else None, nq, k,
          ids_out.data_ptr(), dists_out.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size())
@@ -840,6 +841,6 @@ def ann_sample(scores, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
         logprobs_out = torch.empty(rows, dtype=torch.float32, device=device)
     else:
         _one_value_per_row(logprobs_out, "logprobs_out", torch.float32, rows, device)
-    _run(lib().ann_sample, scores, scores.data_ptr(), rows, n, _element_code(scores), ld, C.byref(o), uniform.data_ptr(),
+    _run(lib().ann_sample, device, scores.data_ptr(), rows, n, _element_code(scores), ld, C.byref(o), uniform.data_ptr(),
          ids_out.data_ptr(), logprobs_out.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size())
     return ids_out, logprobs_out
