@@ -492,7 +492,9 @@ int ann_hcnng_leaf_knn(const void* points_dev, uint64_t n, uint32_t d, ann_dtype
  *   sizes       1 <= d <= 65536; rows < 2^31; a count of zero rows: ANN_OK,
  *               nothing is done and no pointer is read
  * All calls are asynchronous on `stream`, allocate nothing, keep nothing and
- * can be captured into a graph.  Arguments they cannot serve: ANN_EINVAL.
+ * can be captured into a graph.  They launch on the current device, which has to
+ * be that of the stream and of all pointers.  Arguments they cannot serve:
+ * ANN_EINVAL.
  * ------------------------------------------------------------------------ */
 
 /* Rows to 4 bits.  Of each 32 elements, with m their largest magnitude:
@@ -555,7 +557,8 @@ int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint6
  * One id drawn for each row of scores.  A row's candidates are its entries
  * other than NaN and -inf, sorted by (score downwards, id); weights are
  * w = exp((score - best) / temperature) (1 where the scores are equal, so +inf
- * shares the draw among the +inf entries), in fp64.  Kept, in this order:
+ * shares the draw among the +inf entries), in fp64; those below 1e-300 count as
+ * 0 and are never drawn.  Kept, in this order:
  *   top_k  > 0: the first top_k candidates
  *   top_p  in (0, 1): the shortest prefix of those with at least that share of
  *          their mass (the comparison is made on weights rounded to multiples
@@ -574,7 +577,9 @@ int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint6
  *                 for all rows or, where the pointer is given, a device array
  *                 with one value for each row.
  *   scratch_dev   at least what ann_sample_scratch says, 16-byte aligned
- * Asynchronous on `stream`, allocates nothing, can be captured into a graph. */
+ * Asynchronous on `stream` and on the current device, which has to be that of
+ * the stream and of all pointers; allocates nothing, can be captured into a
+ * graph.                                                                     */
 typedef struct {
   float temperature;
   uint32_t top_k;

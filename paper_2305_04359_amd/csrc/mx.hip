@@ -38,7 +38,8 @@ __device__ __forceinline__ float dpp_sum(float v) {
 // Four lanes take 32 elements, eight each: their largest magnitude by two exchanges, then the codes.  LPR lanes
 // (16, 32 or 64: one, two or four steps) take a row, longer rows in turns; a wave asks for four such pieces of rows
 // at once.  A million int8 rows of 100 take 55 us, 3.1 TB/s of the 4.9 that a copy reaches: rows of bytes are bound by
-// vector instructions (1.1 a cycle and compute unit), wider types by memory.
+// vector instructions (1.1 a cycle and compute unit), wider types by memory: fp16 60 us, 4.5 TB/s, and fp32 92 us, 5.1 TB/s
+// (250,000 rows of 1,024: bytes 131 us, 3.0 TB/s, fp16 144 us, 4.5 TB/s, fp32 211 us, 5.5 TB/s).
 // WIDE: every row has eight elements at least; eight are then read at once, past d too, but in the last row, whose
 // last eight are read where these reach its end.
 template <typename T, int LPR, bool WIDE>

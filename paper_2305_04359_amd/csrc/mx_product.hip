@@ -20,7 +20,10 @@ struct ProductArgs {
 };
 
 constexpr size_t FEW_LDS = 160 * 1024;    // of a compute unit
-constexpr size_t FEW_BATCH = 96 * 1024;   // most of it that a batch may take
+// Most of it that a batch may take: the rest is room for eight waves' sums.  By 131,072 rows of bf16, in LDS and by the
+// tiles of mx_product_many_kernel: 16 x 2,900 45 us and 81, 32 x 1,400 29 and 39, 48 x 900 32 and 32, 64 x 600 30 and 24;
+// 33 x 200 fp32 by 500,001 45 and 59, 64 x 200 bf16 48 and 44.  (More than 48 rows would be served better by the tiles.)
+constexpr size_t FEW_BATCH = 96 * 1024;
 constexpr u32 LONG_STEPS = 8;             // rows of so many steps are summed in runs
 constexpr size_t few_batch(u32 nx, u32 steps, int parts) { return (size_t)nx * (steps * MX_STEP * 2 + 16) * parts; }
 static_assert(few_batch(64, 1, 3) <= FEW_BATCH);  // so that 64 rows shorter than a step always fit
@@ -117,7 +120,7 @@ __global__ __launch_bounds__(256) void mx_product4_kernel(ProductArgs a, u32 til
 // 4-bit rows on both sides, many: 256 x 256 results a workgroup of eight waves, 128 x 64 a wave.  Pairs of steps (256
 // elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for its turn.  The
 // scales lie in LDS so that a lane reads those of all its fragments' rows at once; the instruction picks the byte.
-// 4,096 x 65,536 of 2,048 elements take 438 us, 2.5 PFLOP/s (470 us once the clock has fallen under a load that lasts):
+// 4,096 x 65,536 of 2,048 elements take 440 us, 2.5 PFLOP/s (490 us once the clock has fallen under a load that lasts):
 // the matrix cores work 28 % of that time, and the waves wait for loads, one pair of steps ahead, for which LDS and
 // registers have room.  Workgroups that stay for several tiles, with the next one's first pairs asked for before the
 // results leave, are no faster (474 to 480 us in the place of 469).
@@ -324,8 +327,8 @@ __device__ __forceinline__ v8bf unpack(u32 codes, u32 scale_byte) {
 // the next AHEAD steps on their way while it multiplies the present ones.  Long rows (LONG) are summed in runs of
 // groups of AHEAD steps, which are added up in their order, by one wave or, where 4-bit rows are few, by a wave
 // each: the sums do not depend on that.  Within a step the elements are taken in the order that a lane holds
-// them (8 at a time of its 32, the same ones on both sides).  One row of 4,096 bf16 by 131,072 is bound by memory: 56 us,
-// 5.1 TB/s.  33 rows of 200 floats by 500,001 take 47 us: three bf16 numbers for each element, the matrix cores at work
+// them (8 at a time of its 32, the same ones on both sides).  One row of 4,096 bf16 by 131,072 is bound by memory: 53 to
+// 56 us, 5.1 to 5.4 TB/s.  33 rows of 200 floats by 500,001 take 47 us: three bf16 numbers for each element, the matrix cores at work
 // 41 % of the time, 2.8 TB/s.
 constexpr u32 FEW_THREADS = 512;
 
@@ -464,8 +467,9 @@ __global__ __launch_bounds__(FEW_THREADS) void mx_product_few_kernel(ProductArgs
 // step (64 elements) pass through LDS, two at a time: while one is multiplied the next waits in registers for
 // its turn and the one after is on its way.  The codes become bf16 numbers on their way from LDS to the matrix
 // cores, four conversions for each fragment of 16 rows x 32 elements, which serves XF x PARTS products.
-// 2,048 x 16,384 of 4,096 bf16 take 246 to 270 us, 1.0 to 1.1 PFLOP/s, by the clock that the load leaves; the library's
-// product of bf16 on both sides takes 229.  The matrix cores work 53 % of the time.
+// 2,048 x 16,384 of 4,096 bf16 take 240 us as a call among others, 1.15 PFLOP/s, and 261 to 289 under a load that lasts, when
+// the clock falls; the library's product of bf16 on both sides takes 219 to 229.  The matrix cores work 53 % of the time.
+// fp16, two products for each element, takes 484 us, fp32, three, 645.
 constexpr u32 MANY_THREADS = 512;
 constexpr u32 MANY_ROWS = 256;
 
@@ -690,7 +694,9 @@ bool deep_pays(const ProductArgs& a, int xdtype) {
 template <typename T, int G, int WF, int AHEAD, bool LONG>
 hipError_t launch_few(const ProductArgs& a, size_t batch_bytes, u32 runs, hipStream_t s) {
   const u32 tiles = (u32)(((u64)a.w.n + 16 * WF - 1) / (16 * WF));
-  // waves share rows where there is less than one tile for each of 1,024 SIMDs
+  // Waves share rows where there is less than one tile for each of 1,024 SIMDs.  One row of 4,096 by 4,000, 16,000 and
+  // 20,000: 6.2 us against 14.4 without, 15.0 against 16.4, and 18.3 against 16.9; 32 rows of 1,400 by 16,000 and 40,000:
+  // 12.2 against 14.5, and 18.5 against 16.9.
   const u32 share = LONG && tiles < 1024 ? runs : 1;
   constexpr u32 WAVES = FEW_THREADS / 64;
   const size_t lds = batch_bytes + WAVES * few_room<G, WF>(share);
@@ -751,6 +757,10 @@ hipError_t launch_product16(const ProductArgs& a, int xdtype, hipStream_t s) {
     return launch_few_rows<T, 4>(a, batch, s);
   }
   if (deep_pays(a, xdtype)) return launch_deep<T>(a, s);
+  // As wide a tile as the batch fills and registers hold (four columns of fragments of one bf16 number each, two of more).
+  // bf16 by rows of 4,096, with 64, 128 and 256 rows of the batch a tile: 64 x 131,072 136 us, 153, 237; 128 x 65,536 109, 74,
+  // 116; 192 x 65,536 160, 140, 118; 256 x 65,536 214, 142, 120.  fp32, with 64 and 128: 64 x 65,536 100 and 158, 128 x 65,536 183
+  // and 164.  (Few wide tiles can leave compute units idle: 512 x 16,384 114, 74, 110.)
   if (a.nx <= 64) return launch_many<T, 1>(a, s);
   if (a.nx <= 128 || PARTS > 1 || !a.wide_x) return launch_many<T, 2>(a, s);
   if constexpr (PARTS == 1) return launch_many<T, 4>(a, s);

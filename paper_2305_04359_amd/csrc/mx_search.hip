@@ -265,7 +265,9 @@ __global__ __launch_bounds__(SEARCH_THREADS) void mx_group_many_kernel(MxSearchA
   }
 }
 
-// Rows of more steps: a wave scores 64 rows (a group) and 64 queries, step by step from memory.
+// Rows of more steps: a wave scores 64 rows (a group) and 64 queries, step by step from memory, with no step on its way ahead
+// and no LDS.  One query of a million rows of 768 and 1,024 takes 146 and 211 us with its picking (their bytes 84 and 111 at a
+// copy's rate; 66 for 512 elements, by the kernel of few queries), ten thousand 20 and 36 ms (4.1 for 512).
 __global__ __launch_bounds__(256) void mx_group_long_kernel(MxSearchArgs a, u64 tiles) {
   const u32 lane = threadIdx.x % 64;
   const u64 t = (u64)blockIdx.x * 4 + threadIdx.x / 64;
@@ -680,7 +682,9 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
   size_t room = PICK_FEW;  // (four groups of each of the first k groups of groups as well)
   while (room < (size_t)(k < a.groups ? k : a.groups) * SEARCH_GROUP) room *= 2;
   room *= 8;
-  // a thousand threads for a query where there are not enough queries for all compute units
+  // A thousand threads for a query where there are not enough queries for all compute units: with the scoring, of a million
+  // rows of 128, 1, 64 and 256 queries take 25 us against 39 with 256 threads, 29 against 43, 49 against 61; 1,000 queries
+  // 164 against 153, and of 20,000 rows 55 against 35.
   const auto pick = part <= 256 ? mx_pick_kernel<1024> : mx_pick_kernel<256>;
   const u32 pick_threads = part <= 256 ? 1024 : 256;
   HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(pick), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room));

@@ -78,8 +78,9 @@ __device__ __forceinline__ void take_table(const double* from, double* to) {
   for (u32 i = threadIdx.x; i < TABLE; i += THREADS) to[i] = from[i];
 }
 
-// exp((score - best) / temperature), within 1e-14 of itself: a power of two, times 2^(j / 512) from a table, times
-// the rest, whose logarithm is below ln 2 / 1024, by three terms of its series.  Adding 1.5 * 2^52 leaves the
+// exp((score - best) / temperature), within 1e-14 + 5e-16 |x| of itself, where x is the exponent: a power of two, times
+// 2^(j / 512) from a table, times the rest, whose logarithm is below ln 2 / 1024, by three terms of its series.  (The next term
+// makes 9e-15, the roundings of the difference, the factor and their product 2^-51 |x|.)  Below 1e-300 a weight counts as 0.  Adding 1.5 * 2^52 leaves the
 // whole number of 512ths of an octave in the low bits of the sum.
 struct Weights {
   float most;          // the best score
@@ -735,7 +736,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(SampleArgs a) {
 // Divided rows: several workgroups share each.  One launch takes the best scores of the chunks and of their parts.  Where
 // these tell the k best, the next finds the bound, else one takes the chunks' histograms (added up per row: whole
 // numbers).  One lists the candidates around the cut, one finds the cut from these or, where top-k keeps few, draws, one
-// takes the chunks' masses, and one draws.  Rows whose cut needs more than the list holds are left to the kernel above.
+// takes the chunks' masses, and one draws.  Rows whose cut needs more than the list holds are left to the kernel above, as are
+// rows with top-p whose top-k drops nothing or keeps more than some 1,000 (64 x 50,001 with top-p 0.9: top-k 1,100 114 us, 900
+// 64 us; of 600 candidates, top-k 1,000 76 us, 400 41 us) and, in calls with one top-k of up to 512 for all rows, those that
+// take the best candidate alone (one such row of 64 x 50,001: 41 us against 34).
 // Times of a launch for one row of 128,000 bf16 with top-p, and for 500 such of fp16 with settings of their own (128 MB, 26 us
 // at a copy's rate): best scores 3.6 and 24 us, bound - and 10, histograms 6 and 35, lists 5.5 and 30, cuts 5 and 35,
 // masses 8.5 and 44, draw 9 and 16, what is left whole 3.5 and 6.  One row: the chain of launches and, inside of each, of
@@ -1510,12 +1514,17 @@ u64 plan_split(SampleArgs& a, u64 rows, u64 n, char* scratch) {
   while ((n + chunk - 1) / chunk > SPLIT_CHUNKS) chunk *= 2;
   a.chunk = (u32)chunk;
   a.chunks = (u32)((n + chunk - 1) / chunk);
-  // some eight thousand workgroups
+  // Some eight thousand workgroups: 500 rows of 128,000 with settings of each take 197 us; by half and a quarter of that 198 and
+  // 219, by a workgroup for each chunk 227.  (Rows with the same settings are served better by fewer: 200 x 128,000 with top-p
+  // 158 us against 134 and 136, 3,000 x 20,000 with top-k 157 against 155 and 136.)
   const u64 groups = (8192 + rows - 1) / rows;
   a.per = (u32)(groups >= a.chunks ? 1 : (a.chunks + groups - 1) / groups);
   a.groups = (a.chunks + a.per - 1) / a.per;
-  // A bin of the histogram has about n / 200 of normal scores near their middle; sorted rows bring up to 256 entries and a
-  // bin from each of some 17 chunks.
+  // A bin of the histogram, 1/32 of max(temperature, 1) of score, has about n / 200 of scores near their middle that spread by
+  // 2.5; sorted rows bring up to 256 entries and a bin from each of some 17 chunks.  Scores that spread by little fill a list
+  // with one bin, and such rows are taken whole: 64 x 128,000 with top-p 0.9 at temperature 1 take 97 us where the standard
+  // deviation is 0.2, 232 at 0.1, 496 at 0.02 (one row at 0.1 186 us, at 0.3 50).  Lists of 16,384 for all would take 103 us in
+  // the place of 232, the same where 6,144 do, and 32 us more than these where they do not.
   a.capacity = n / 64 < SPLIT_LEAST_LIST ? SPLIT_LEAST_LIST : n / 64 < SPLIT_LIST ? (u32)(n / 64) : SPLIT_LIST;
   u64 at = 0;
   auto take = [&](u64 bytes) {
