@@ -1,0 +1,425 @@
+"""Cases of the operators on 8-bit rows, of distillation from a teacher's best entries and of beam steps, as a user's
+program calls them.
+
+Six kinds of pass:
+  quantize  rows or columns to 8-bit floating point with a scale per 128 elements, and the values read back
+  product   a batch taken to 8 bits, times all 8-bit rows: the scores of a batch
+  train     a layer's product in 8 bits and the gradients of both its sides, everything quantised within the pass
+  distill   the loss of scores against a teacher's k best entries of each row, and its gradient
+  select    one step of beam search: the best continuations of each group of beams by their running totals
+  reorder   the states of a decoder brought into the order of the beams that go on
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+TYPES = {"u8": torch.uint8, "i8": torch.int8, "f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SIZE = {"u8": 1, "i8": 1, "f32": 4, "f16": 2, "bf16": 2}
+DEV = "cuda"
+STEP = 128  # elements that share a scale; a row is stored in whole steps, its scale bytes in whole fours
+
+
+def listed():
+    return [
+        # the questions of a few users, taken to 8 bits: latency alone
+        {"name": "quantize-queries", "op": "quantize", "n": 37, "d": 200, "dtype": "f32", "columns": False, "pad": 0},
+        # a layer's weights laid out by columns, for the gradient of its inputs
+        {"name": "quantize-columns", "op": "quantize", "n": 4096, "d": 16_384, "dtype": "bf16", "columns": True, "pad": 0},
+        # one state of a decoder against all rows of its output layer
+        {"name": "product-one", "op": "product", "nx": 1, "n": 131_072, "d": 4096, "dtype": "bf16", "out": "f32", "pad": 0},
+        # a small batch of float questions against all embeddings, scores in full; rows that are slices of wider ones
+        {"name": "product-33", "op": "product", "nx": 33, "n": 500_001, "d": 200, "dtype": "f32", "out": "f32", "pad": 5},
+        # a long prompt's states through a wide layer: matrix work
+        {"name": "product-many", "op": "product", "nx": 4096, "n": 65_536, "d": 2048, "dtype": "bf16", "out": "bf16", "pad": 0},
+        # a training step of a layer
+        {"name": "train-layer", "op": "train", "nx": 2048, "n": 8192, "d": 4096, "dtype": "bf16"},
+        # a small batch of questions whose neighbours a better model has named
+        {"name": "distill-37", "op": "distill", "rows": 37, "n": 10_000, "k": 10, "dtype": "f32", "t": 2.0, "short": 0.3, "pad": 3},
+        # a batch of tokens over a whole vocabulary
+        {"name": "distill-4k", "op": "distill", "rows": 4096, "n": 128_000, "k": 64, "dtype": "bf16", "t": 1.0, "short": 0.0, "pad": 0},
+        # the next tokens of one user, and those of a serving batch with masked entries and finished beams
+        {"name": "select-one", "op": "select", "groups": 1, "beams": 4, "n": 128_000, "k": 8, "dtype": "bf16", "masked": 0.0, "finished": 0.0, "pad": 0},
+        {"name": "select-64", "op": "select", "groups": 64, "beams": 5, "n": 50_001, "k": 10, "dtype": "f32", "masked": 0.2, "finished": 0.2, "pad": 0},
+        # keys of a decoder, the part of them that is in use
+        {"name": "reorder-states", "op": "reorder", "layers": 16, "groups": 8, "beams": 8, "heads": 8, "used": 1111, "room": 2048, "width": 128, "dtype": "bf16"},
+        # the states of a small recurrent decoder: latency alone
+        {"name": "reorder-small", "op": "reorder", "layers": 2, "groups": 3, "beams": 4, "heads": 1, "used": 1, "room": 1, "width": 500, "dtype": "f32"},
+    ]
+
+
+def _log(rng, lo, hi):
+    v = int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+    return min(max(v, lo), max(lo, hi))
+
+
+def draw(rng):
+    op = rng.choice(("quantize", "product", "train", "distill", "select", "reorder"))
+    pad = rng.choice((0, 0, 3, 8))
+    if op == "quantize":
+        d = _log(rng, 16, 16_384)
+        return {"op": op, "n": _log(rng, 1, min(1_000_000, 67_000_000 // d)), "d": d, "dtype": rng.choice(sorted(TYPES)),
+                "columns": rng.random() < 0.5, "pad": pad}
+    if op == "product":
+        d = _log(rng, 16, 8192)
+        n = _log(rng, 100, min(500_000, 500_000_000 // d))
+        nx = _log(rng, 1, max(1, min(4096, 500_000_000_000 // (n * d), 268_000_000 // n)))
+        return {"op": op, "nx": nx, "n": n, "d": d, "dtype": rng.choice(sorted(TYPES)), "out": rng.choice(("f32", "bf16")), "pad": pad}
+    if op == "train":
+        n, d = _log(rng, 64, 16_384), _log(rng, 64, 8192)
+        return {"op": op, "nx": _log(rng, 16, max(16, min(4096, 68_000_000_000 // (n * d)))), "n": n, "d": d, "dtype": rng.choice(("f32", "f16", "bf16"))}
+    if op == "distill":
+        n = _log(rng, 100, 200_000)
+        return {"op": op, "rows": _log(rng, 1, min(4096, 500_000_000 // n)), "n": n, "k": _log(rng, 1, min(n, 256)), "dtype": rng.choice(("f32", "f16", "bf16")),
+                "t": rng.choice((0.5, 1.0, 2.0, 4.0)), "short": rng.choice((0.0, 0.3)), "pad": pad}
+    if op == "select":
+        n = _log(rng, 100, 200_000)
+        beams = rng.choice((1, 2, 3, 4, 5, 8, 10, 16))
+        return {"op": op, "groups": _log(rng, 1, max(1, min(128, 16_000_000 // (n * beams)))), "beams": beams, "n": n, "k": beams * rng.choice((1, 2)),
+                "dtype": rng.choice(("f32", "f16", "bf16")), "masked": rng.choice((0.0, 0.2, 0.9)), "finished": rng.choice((0.0, 0.3)), "pad": pad}
+    beams, heads, width = rng.choice((2, 3, 4, 5, 8, 16)), rng.choice((1, 2, 8)), rng.choice((64, 80, 128, 500, 1023))
+    layers, room = rng.choice((1, 4, 12, 16)), _log(rng, 1, 2048)
+    groups = _log(rng, 1, max(1, min(64, 1_000_000_000 // (beams * heads * width * layers * room))))
+    return {"op": op, "layers": layers, "groups": groups, "beams": beams, "heads": heads, "used": rng.randint(1, room), "room": room, "width": width,
+            "dtype": rng.choice(("f32", "bf16", "i8"))}
+
+
+# ---------------------------------------------------------------- inputs
+
+def _rows(g, n, d, dtype):
+    """n rows of d: bytes like image descriptors, unit embeddings of 32 bits, states of a model with a few large channels
+    for 16 bits."""
+    if n * d > 64_000_000 and n > 1:  # in parts, each drawn like the whole
+        part = max(1, 64_000_000 // d)
+        return torch.cat([_rows(g, min(n - i, part), d, dtype) for i in range(0, n, part)])
+    c = torch.Generator(device=DEV)
+    c.manual_seed(359)
+    x = torch.randn((n, d), device=DEV, generator=g)
+    if dtype == "u8":
+        return torch.clamp(torch.round(24.0 + 40.0 * x.abs()), 0, 255).to(torch.uint8)
+    if dtype == "i8":
+        return torch.clamp(torch.round(47.0 * x), -127, 127).to(torch.int8)
+    if dtype == "f32":
+        return x / x.norm(dim=1, keepdim=True)
+    x *= torch.where(torch.rand(d, device=DEV, generator=c) < 0.01, 12.0, 1.0)
+    return x.to(TYPES[dtype])
+
+
+def _wider(x, pad):
+    """The same rows as a slice of a tensor whose rows are `pad` elements longer."""
+    if not pad:
+        return x
+    wide = torch.zeros((x.shape[0], x.shape[1] + pad), dtype=x.dtype, device=x.device)
+    wide[:, :x.shape[1]] = x
+    return wide[:, :x.shape[1]]
+
+
+def _scores(g, rows, n, dtype, masked=0.0):
+    """Rows of scores with some forty good entries each, part of them masked."""
+    z = 2.5 * torch.randn((rows, n), device=DEV, generator=g)
+    top = torch.randint(0, n, (rows, 40), device=DEV, generator=g)
+    # (an entry that is drawn twice gets the larger value: which of two writes comes last is not the seed's)
+    z.scatter_reduce_(1, top, 8.0 + 4.0 * torch.rand((rows, 40), device=DEV, generator=g), "amax")
+    if masked:
+        z.masked_fill_(torch.rand((rows, n), device=DEV, generator=g) < masked, -math.inf)
+    return z.to(TYPES[dtype])
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    op = case["op"]
+    s = {"case": dict(case)}
+    if op == "quantize":
+        shape = (case["d"], case["n"]) if case["columns"] else (case["n"], case["d"])
+        s["x"] = _wider(_rows(g, *shape, case["dtype"]), case["pad"])
+    elif op == "product":
+        s["codes"], s["scales"] = _stored(_rows(g, case["n"], case["d"], case["dtype"]))
+        s["x"] = _wider(_rows(g, case["nx"], case["d"], case["dtype"]), case["pad"])
+    elif op == "train":
+        s["x"] = _rows(g, case["nx"], case["d"], case["dtype"])
+        s["w"] = (torch.randn((case["n"], case["d"]), device=DEV, generator=g) / math.sqrt(case["d"])).to(TYPES[case["dtype"]])
+        s["grad"] = (torch.randn((case["nx"], case["n"]), device=DEV, generator=g) / case["nx"]).to(TYPES[case["dtype"]])
+    elif op == "distill":
+        rows, n, k = case["rows"], case["n"], case["k"]
+        s["x"] = _wider(_scores(g, rows, n, case["dtype"]), case["pad"])
+        # k different entries of each row: a walk with a step that has no factor in common with n
+        step = next(v for v in range(max(1, int(0.381966 * n)), 2 * n + 2) if math.gcd(v, n) == 1)
+        first = torch.randint(0, n, (rows, 1), device=DEV, generator=g)
+        ids = (first + step * torch.arange(k, device=DEV)) % n
+        near = s["x"].gather(1, ids).float()
+        s["teacher"] = (6.0 + 3.0 * torch.randn((rows, k), device=DEV, generator=g) + 0.5 * near).contiguous()
+        # rows whose teacher named fewer than k
+        count = torch.where(torch.rand(rows, device=DEV, generator=g) < case["short"], torch.randint(0, k, (rows,), device=DEV, generator=g), k)
+        s["ids"] = torch.where(torch.arange(k, device=DEV) < count.unsqueeze(1), ids, -1).int().contiguous()
+        s["grad"] = torch.rand(rows, device=DEV, generator=g) / rows
+    elif op == "select":
+        rows, n = case["groups"] * case["beams"], case["n"]
+        s["x"] = _wider(_scores(g, rows, n, case["dtype"], case["masked"]), case["pad"])
+        s["totals"] = -2.0 - 3.0 * torch.rand(rows, device=DEV, generator=g)
+        s["finished"] = torch.rand(rows, device=DEV, generator=g) < case["finished"] if case["finished"] else None
+    else:
+        rows = case["groups"] * case["beams"]
+        shape = (case["layers"], rows, case["heads"], case["room"], case["width"])
+        if case["dtype"] == "i8":
+            s["states"] = torch.randint(-127, 128, shape, dtype=torch.int8, device=DEV, generator=g)
+        else:
+            s["states"] = torch.randn(shape, dtype=TYPES[case["dtype"]], device=DEV, generator=g)
+        s["spare"] = torch.zeros_like(s["states"])
+        # most beams go on from one of the better ones
+        s["parents"] = (case["beams"] * torch.rand((case["groups"], case["beams"]), device=DEV, generator=g).square()).int()
+    return s
+
+
+# ---------------------------------------------------------------- plain forms
+
+def _eights(x):
+    """What the 8-bit rows of x stand for (n, d padded to steps), and their scale bytes (n, steps), by the formulas."""
+    n, d = x.shape
+    x = torch.nn.functional.pad(x.float(), (0, -d % STEP)).view(n, -1, STEP)
+    most = x.abs().amax(2)
+    bits = most.view(torch.int32)
+    # the least e with most <= 448 * 2^e (448 is 1.75 * 2^8)
+    byte = torch.clamp((bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000).int(), min=0)
+    fine = most < math.inf
+    y = x * ((254 - byte) << 23).view(torch.float32)[..., None]  # times 2^(127 - byte)
+    spacing = torch.clamp((y.abs().view(torch.int32) >> 23) - 3, min=127 - 9) << 23
+    spacing = spacing.view(torch.float32)
+    y = torch.round(y / spacing) * spacing
+    y = torch.where(fine[..., None], y, torch.zeros_like(y))
+    byte = torch.where(fine, byte, torch.full_like(byte, 255))
+    return y, byte
+
+
+def _values(y, byte):
+    scale = torch.where(byte == 0, torch.full_like(byte, 1 << 22), byte << 23)  # 2^-127 is a subnormal number
+    scale = torch.where(byte == 255, torch.full_like(byte, 0x7FC00000), scale).view(torch.float32)
+    return (y * scale[..., None]).view(y.shape[0], -1)
+
+
+def _in_parts(f, x):
+    part = max(1, 128_000_000 // x.shape[1])
+    return [f(x[i:i + part]) for i in range(0, x.shape[0], part)]
+
+
+def _stored(x):
+    """Rows as a program holds them: a byte for each element of whole steps, scale bytes in whole fours."""
+    def one(x):
+        y, byte = _eights(x)
+        return y.view(x.shape[0], -1).to(torch.float8_e4m3fn).view(torch.uint8), torch.nn.functional.pad(byte, (0, -byte.shape[1] % 4)).to(torch.uint8)
+    return tuple(torch.cat(p).contiguous() for p in zip(*_in_parts(one, x)))
+
+
+def _unpacked(codes, scales):
+    steps = codes.shape[1] // STEP
+    return _values(codes.view(torch.float8_e4m3fn).float().view(codes.shape[0], steps, STEP), scales[:, :steps].int())
+
+
+def _read_back(x):
+    return torch.cat(_in_parts(lambda x: _values(*_eights(x)), x))
+
+
+def _plain_distill(s, case):
+    z, ids, t = s["x"].float(), s["ids"].long(), case["t"]
+    there = ids >= 0
+    shares = torch.where(there, s["teacher"].double(), -math.inf)
+    best = shares.amax(1, keepdim=True)
+    shares = torch.where(there, torch.exp((shares - best) / t), 0.0)
+    mass = shares.sum(1, keepdim=True)
+    shares = torch.where(there, shares / mass, 0.0)
+    most = z.amax(1, keepdim=True)
+    q = torch.exp((z - most) / t)
+    total = q.sum(1, keepdim=True)
+    at = torch.where(there, ids, 0)
+    logq = (z.gather(1, at).double() - most) / t - torch.log(total.double())
+    losses = t * t * torch.where(shares > 0, shares * (torch.log(shares) - logq), 0.0).sum(1)
+    some = there.any(1, keepdim=True)
+    q = torch.where(some, q / total, 0.0)
+    q.scatter_add_(1, at, -shares.float())
+    return {"losses": losses.float(), "grads": (q * (t * s["grad"].unsqueeze(1))).to(s["x"].dtype)}
+
+
+def _plain_select(s, case):
+    groups, beams, n, k = case["groups"], case["beams"], case["n"], case["k"]
+    z = s["x"].double()
+    most = z.amax(1, keepdim=True)
+    most = torch.where(most > -math.inf, most, 0.0)
+    v = s["totals"].double().unsqueeze(1) + (z - most - torch.log(torch.exp(z - most).sum(1, keepdim=True)))
+    if s["finished"] is not None:
+        v[s["finished"]] = -math.inf
+        v[:, 7] = torch.where(s["finished"], s["totals"].double(), v[:, 7])
+    v = torch.where(v.isnan(), -math.inf, v)
+    v, order = torch.sort(v.view(groups, beams * n), dim=1, descending=True, stable=True)
+    v, order = v[:, :k], order[:, :k]
+    gone = v == -math.inf
+    out = {"parents": torch.div(order, n, rounding_mode="floor"), "ids": order % n}
+    out = {name: torch.where(gone, -1, x).int() for name, x in out.items()}
+    return {**out, "totals": v.float()}
+
+
+# ---------------------------------------------------------------- one pass
+
+def run(state):
+    case = state["case"]
+    op = case["op"]
+    if own:
+        from paper_2305_04359_amd import binding as A
+        if op == "quantize":
+            return A.ann_f8_dequantize(A.ann_f8_quantize(state["x"], columns=case["columns"]))
+        if op == "product":
+            rows = A.F8Rows(state["codes"], state["scales"], case["d"])
+            return A.ann_f8_product(A.ann_f8_quantize(state["x"]), rows, dtype=TYPES[case["out"]])
+        if op == "train":
+            x, w, grad = state["x"], state["w"], state["grad"]
+            y = A.ann_f8_product(A.ann_f8_quantize(x), A.ann_f8_quantize(w), dtype=x.dtype)
+            dx = A.ann_f8_product(A.ann_f8_quantize(grad), A.ann_f8_quantize(w, columns=True), dtype=x.dtype)
+            dw = A.ann_f8_product(A.ann_f8_quantize(grad, columns=True), A.ann_f8_quantize(x, columns=True), dtype=torch.float32)
+            return {"y": y, "dx": dx, "dw": dw}
+        if op == "distill":
+            losses, stats = A.ann_distill(state["x"], state["ids"], state["teacher"], temperature=case["t"])
+            grads = A.ann_distill_grad(state["x"], state["ids"], state["teacher"], stats, grad_losses=state["grad"], temperature=case["t"])
+            return {"losses": losses, "grads": grads}
+        if op == "select":
+            parents, ids, totals = A.ann_beam_select(state["x"], state["totals"], case["beams"], case["k"], finished=state["finished"], pad_id=7)
+            return {"parents": parents, "ids": ids, "totals": totals}
+        used = case["used"]
+        return A.ann_beam_reorder(state["states"][:, :, :, :used], state["parents"], case["beams"], dim=1, out=state["spare"][:, :, :, :used])
+    if op == "quantize":
+        x = state["x"].T.contiguous() if case["columns"] else state["x"]
+        return _read_back(x)[:, :case["d"]].contiguous()
+    if op == "product":
+        return (_read_back(state["x"]) @ _unpacked(state["codes"], state["scales"]).T).to(TYPES[case["out"]])
+    if op == "train":
+        x, w, grad = state["x"], state["w"], state["grad"]
+        y = _read_back(x) @ _read_back(w).T
+        dx = _read_back(grad) @ _read_back(w.T).T
+        dw = _read_back(grad.T) @ _read_back(x.T).T
+        return {"y": y.to(x.dtype), "dx": dx.to(x.dtype), "dw": dw}
+    if op == "distill":
+        return _plain_distill(state, case)
+    if op == "select":
+        return _plain_select(state, case)
+    first = torch.arange(case["groups"], device=DEV).unsqueeze(1) * case["beams"]
+    return state["states"][:, :, :, :case["used"]].index_select(1, (first + state["parents"]).view(-1))
+
+
+def work(case):
+    op = case["op"]
+    if op == "reorder":
+        size = case["layers"] * case["groups"] * case["beams"] * case["heads"] * case["used"] * case["width"] * SIZE[case["dtype"]]
+        return {"bytes": 2 * size, "flops": 0}
+    n = case["n"]
+    if op == "distill":
+        size = case["rows"] * n * SIZE[case["dtype"]]
+        return {"bytes": 2 * size + case["rows"] * (8 * case["k"] + 8), "flops": 8 * case["rows"] * n}
+    if op == "select":
+        rows = case["groups"] * case["beams"]
+        return {"bytes": rows * (n * SIZE[case["dtype"]] + 5) + 12 * case["groups"] * case["k"], "flops": 4 * rows * n}
+    d, size = case["d"], SIZE[case["dtype"]]
+    row8 = d + -(-d // STEP)  # a byte for each element and one of scale for each step
+    if op == "quantize":
+        return {"bytes": n * (d * size + 2 * row8 + 4 * d), "flops": 3 * n * d}
+    nx = case["nx"]
+    if op == "train":
+        return {"bytes": 2 * (nx * d + n * d + nx * n) * size + n * d * (4 - size), "flops": 6 * nx * n * d}
+    return {"bytes": n * row8 + nx * d * size + nx * n * SIZE[case["out"]], "flops": 2 * nx * n * d}
+
+
+# ---------------------------------------------------------------- the definitions, in 64 bits
+
+def _exact_values(x):
+    """What the 8-bit form of rows stands for, from the definition: the scale's exponent by frexp and a comparison, and
+    the rounding by whole steps of the code's own spacing."""
+    n, d = x.shape
+    x = torch.nn.functional.pad(x.double(), (0, -d % STEP)).view(n, -1, STEP)
+    most = x.abs().amax(2, keepdim=True)
+    e = (torch.frexp(most).exponent - 9).double()
+    e = torch.where(most > 448.0 * torch.exp2(e), e + 1, e)
+    e = torch.where(most > 0, e, -127.0).clamp(min=-127.0)
+    y = x / torch.exp2(e)
+    spacing = torch.exp2((torch.frexp(y).exponent - 4).double().clamp(min=-9.0))
+    y = torch.round(y / spacing) * spacing
+    return torch.where(most < math.inf, y * torch.exp2(e), math.nan).view(n, -1)[:, :d]
+
+
+def _exact_stored(codes, scales, d):
+    b = codes.int()
+    e, m = (b >> 3 & 15).double(), (b & 7).double()
+    v = torch.where(e > 0, torch.exp2(e - 7) * (1 + m / 8), m * 2.0 ** -9) * torch.where(b >= 128, -1.0, 1.0)
+    steps = codes.shape[1] // STEP
+    return (v.view(codes.shape[0], steps, STEP) * torch.exp2(scales[:, :steps].double() - 127)[..., None]).view(codes.shape[0], -1)[:, :d]
+
+
+def _exact_distill(s, case):
+    t = case["t"]
+    logq = torch.log_softmax(s["x"].double() / t, dim=1)
+    grads = torch.exp(logq)
+    losses = torch.zeros(case["rows"], dtype=torch.float64, device=DEV)
+    ids, teacher = s["ids"], s["teacher"].double()
+    count = (ids >= 0).sum(1)
+    for k in count.unique().tolist():  # rows whose teachers named as many
+        r = (count == k).nonzero().squeeze(1)
+        if k == 0:
+            grads[r] = 0.0
+            continue
+        p = torch.log_softmax(teacher[r, :k] / t, dim=1)
+        at = ids[r, :k].long()
+        losses[r] = t * t * (p.exp() * (p - logq[r].gather(1, at))).sum(1)
+        grads[r.unsqueeze(1), at] -= p.exp()
+    return {"losses": losses, "grads": grads * (t * s["grad"].double().unsqueeze(1))}
+
+
+def _exact_select(s, case):
+    """Group by group on the host: every continuation's total, those that reach the k-th best, in order."""
+    groups, beams, n, k = case["groups"], case["beams"], case["n"], case["k"]
+    z = s["x"].double().cpu().numpy().reshape(groups, beams, n)
+    totals = s["totals"].double().cpu().numpy().reshape(groups, beams)
+    done = np.zeros((groups, beams), bool) if s["finished"] is None else s["finished"].cpu().numpy().reshape(groups, beams)
+    parents, ids, out = np.full((groups, k), -1, np.int32), np.full((groups, k), -1, np.int32), np.full((groups, k), -math.inf)
+    for g in range(groups):
+        found = []
+        for b in range(beams):
+            if done[g, b]:
+                found.append((totals[g, b:b + 1], np.full(1, b), np.array([7])))
+                continue
+            at = np.flatnonzero(z[g, b] > -math.inf)
+            if len(at):
+                zb = z[g, b, at]
+                most = zb.max()
+                found.append((totals[g, b] + (zb - (most + math.log(np.exp(zb - most).sum()))), np.full(len(at), b), at))
+        if not found:
+            continue
+        v, b, j = (np.concatenate(x) for x in zip(*found))
+        if len(v) > k:
+            near = v >= np.partition(v, len(v) - k)[len(v) - k]
+            v, b, j = v[near], b[near], j[near]
+        order = np.lexsort((j, b, -v))[:k]
+        parents[g, :len(order)], ids[g, :len(order)], out[g, :len(order)] = b[order], j[order], v[order]
+    return {"parents": torch.from_numpy(parents), "ids": torch.from_numpy(ids), "totals": torch.from_numpy(out)}
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = case["op"]
+    if op == "quantize":
+        return _exact_values(s["x"].T if case["columns"] else s["x"])
+    if op == "product":
+        return _exact_values(s["x"]) @ _exact_stored(s["codes"], s["scales"], case["d"]).T
+    if op == "train":
+        x, w, grad = s["x"], s["w"], s["grad"]
+        return {"y": _exact_values(x) @ _exact_values(w).T, "dx": _exact_values(grad) @ _exact_values(w.T).T,
+                "dw": _exact_values(grad.T) @ _exact_values(x.T).T}
+    if op == "distill":
+        return _exact_distill(s, case)
+    if op == "select":
+        return _exact_select(s, case)
+    states, parents = s["states"][:, :, :, :case["used"]], s["parents"].long()
+    out = torch.empty_like(states, memory_format=torch.contiguous_format)
+    for g in range(case["groups"]):
+        for i in range(case["beams"]):
+            out[:, g * case["beams"] + i] = states[:, g * case["beams"] + int(parents[g, i])]
+    return out
