@@ -269,15 +269,15 @@ def run(state):
     if own:
         from paper_2305_04359_amd import binding as A
         if op == "quantize":
-            return A.ann_f8_dequantize(A.ann_f8_quantize(state["x"], columns=case["columns"]))
+            return A.ann_oct_dequantize(A.ann_oct_quantize(state["x"], columns=case["columns"]))
         if op == "product":
-            rows = A.F8Rows(state["codes"], state["scales"], case["d"])
-            return A.ann_f8_product(A.ann_f8_quantize(state["x"]), rows, dtype=TYPES[case["out"]])
+            rows = A.OctRows(state["codes"], state["scales"], case["d"])
+            return A.ann_oct_product(A.ann_oct_quantize(state["x"]), rows, dtype=TYPES[case["out"]])
         if op == "train":
             x, w, grad = state["x"], state["w"], state["grad"]
-            y = A.ann_f8_product(A.ann_f8_quantize(x), A.ann_f8_quantize(w), dtype=x.dtype)
-            dx = A.ann_f8_product(A.ann_f8_quantize(grad), A.ann_f8_quantize(w, columns=True), dtype=x.dtype)
-            dw = A.ann_f8_product(A.ann_f8_quantize(grad, columns=True), A.ann_f8_quantize(x, columns=True), dtype=torch.float32)
+            y = A.ann_oct_product(A.ann_oct_quantize(x), A.ann_oct_quantize(w), dtype=x.dtype)
+            dx = A.ann_oct_product(A.ann_oct_quantize(grad), A.ann_oct_quantize(w, columns=True), dtype=x.dtype)
+            dw = A.ann_oct_product(A.ann_oct_quantize(grad, columns=True), A.ann_oct_quantize(x, columns=True), dtype=torch.float32)
             return {"y": y, "dx": dx, "dw": dw}
         if op == "distill":
             losses, stats = A.ann_distill(state["x"], state["ids"], state["teacher"], temperature=case["t"])
