@@ -554,6 +554,51 @@ int ann_mx_search(const uint8_t* codes_dev, const uint8_t* scales_dev, const flo
 int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint64_t* bytes);
 
 /* ------------------------------------------------------------------------
+ * 8-bit rows: floating-point elements with a power of two for every 128 of
+ * them, nearly as good as 16-bit rows at half the memory, and operands of the
+ * scaled matrix instructions.  Elements are E4M3 (a sign, four bits of exponent
+ * with a bias of 7, three of mantissa; up to 448; 0x7F and 0xFF are NaN); a
+ * scale is kept as an E8M0 byte b = exponent + 127.
+ *   storage     a row of d elements takes T = ceil(d / 128) steps: 128 T bytes
+ *               of codes and 4 ceil(T / 4) scale bytes, one for each step, rows
+ *               without gaps.  The padding holds codes 0 and scales 0; rows from
+ *               elsewhere must hold codes 0 there too.
+ *   alignment   codes 16 bytes, scales 4; the other matrices of these calls
+ *               that of their element, with a row stride of their own (`ld`,
+ *               in elements, at least the row's length)
+ *   sizes       1 <= d <= 1048576; rows < 2^31; a count of zero rows: ANN_OK,
+ *               nothing is done and no pointer is read
+ * All calls are asynchronous on `stream`, allocate nothing, keep nothing and
+ * can be captured into a graph.  They launch on the current device, which has to
+ * be that of the stream and of all pointers.  Arguments they cannot serve:
+ * ANN_EINVAL.
+ * ------------------------------------------------------------------------ */
+
+/* Rows to 8 bits.  Of each 128 elements, with m their largest magnitude:
+ * e = max(the least integer with m <= 448 * 2^e, -127), code = x / 2^e to the
+ * nearest E4M3 value, ties to even.  Where one of them is infinite or NaN the
+ * scale byte is 255, the codes are 0, and all 128 stand for NaN.
+ *   x_dev    columns == 0: n x d elements of any ann_dtype, rows ldx apart
+ *            else: d x n elements, rows ldx >= n apart; row i of the result is
+ *            column i of x                                                   */
+int ann_oct_quantize(const void* x_dev, uint64_t n, uint32_t d, ann_dtype dtype, uint64_t ldx, int columns, uint8_t* codes_dev,
+                    uint8_t* scales_dev, void* stream);
+
+/* The values that 8-bit rows stand for, as ANN_F32 (exact down to 2^-149), ANN_F16
+ * or ANN_BF16 (rounded once) rows of d elements, ldo elements apart.         */
+int ann_oct_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev,
+                      ann_dtype dtype, uint64_t ldo, void* stream);
+
+/* out[i][j] = sum over the d elements of value(x row i) * value(row j), summed in
+ * fp32 and rounded once to out_dtype (ANN_F32, ANN_F16 or ANN_BF16); out_dev is
+ * nx x n, rows ldo >= n apart.  The gradients of a layer's product Y = X W^T,
+ * from G = dY, are products too: dX of the rows of G with the columns of W, dW of
+ * the columns of G with the columns of X.                                    */
+int ann_oct_product(const uint8_t* xcodes_dev, const uint8_t* xscales_dev, uint64_t nx, const uint8_t* codes_dev,
+                   const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev, ann_dtype out_dtype, uint64_t ldo,
+                   void* stream);
+
+/* ------------------------------------------------------------------------
  * One id drawn for each row of scores.  A row's candidates are its entries
  * other than NaN and -inf, sorted by (score downwards, id); weights are
  * w = exp((score - best) / temperature) (1 where the scores are equal, so +inf

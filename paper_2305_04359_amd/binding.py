@@ -89,6 +89,7 @@ EXPORTS = [
     "ann_hcnng_build", "ann_hcnng_build_with", "ann_hcnng_tree_edges", "ann_hcnng_leaf_knn",
     "ann_mx_quantize", "ann_mx_dequantize", "ann_mx_product", "ann_mx_product_mx", "ann_mx_search", "ann_mx_search_scratch",
     "ann_sample", "ann_sample_scratch",
+    "ann_oct_quantize", "ann_oct_dequantize", "ann_oct_product",
 ]
 
 _lib = None
@@ -195,6 +196,12 @@ def lib():
         L.ann_sample.argtypes = [vp, u64, u64, C.c_int, u64, C.POINTER(SampleOpts), vp, vp, vp, vp, u64, vp]
         L.ann_sample_scratch.restype = C.c_int
         L.ann_sample_scratch.argtypes = [u64, u64, C.POINTER(u64)]
+        L.ann_oct_quantize.restype = C.c_int
+        L.ann_oct_quantize.argtypes = [vp, u64, u32, C.c_int, u64, C.c_int, vp, vp, vp]
+        L.ann_oct_dequantize.restype = C.c_int
+        L.ann_oct_dequantize.argtypes = [vp, vp, u64, u32, vp, C.c_int, u64, vp]
+        L.ann_oct_product.restype = C.c_int
+        L.ann_oct_product.argtypes = [vp, vp, u64, vp, vp, u64, u32, vp, C.c_int, u64, vp]
         L.ann_last_error.restype = C.c_char_p
         L.ann_last_error.argtypes = []
         _lib = L
@@ -669,7 +676,7 @@ def _run(call, device, *args):
 
 
 def _element_code(t) -> int:
-    """The ann_dtype of a tensor among the types that the calls on 4-bit rows and ann_sample take."""
+    """The ann_dtype of a tensor among the types that the calls on 4-bit and 8-bit rows and on scores take."""
     if not _ELEMENT_CODES:
         torch = _torch()
         _ELEMENT_CODES.update({torch.uint8: U8, torch.int8: I8, torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
@@ -844,3 +851,64 @@ def ann_sample(scores, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
     _run(lib().ann_sample, device, scores.data_ptr(), rows, n, _element_code(scores), ld, C.byref(o), uniform.data_ptr(),
          ids_out.data_ptr(), logprobs_out.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size())
     return ids_out, logprobs_out
+
+
+class OctRows:
+    """8-bit rows (see ann.h): codes (n, 128 T) and scales (n, 4 ceil(T / 4)), uint8, T = ceil(d / 128), and the row
+    length d."""
+
+    __slots__ = ("codes", "scales", "d")
+
+    def __init__(self, codes, scales, d):
+        steps = (int(d) + 127) // 128
+        torch = _torch()
+        for t, width, name in ((codes, 128 * steps, "codes"), (scales, (steps + 3) // 4 * 4, "scales")):
+            if not t.is_cuda or t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != width or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous (n, {width}) uint8 device tensor for rows of {d} elements")
+        if codes.shape[0] != scales.shape[0] or codes.device != scales.device:
+            raise ValueError("codes and scales must have the same rows on the same device")
+        self.codes, self.scales, self.d = codes, scales, int(d)
+
+    @property
+    def n(self) -> int:
+        return self.codes.shape[0]
+
+
+def ann_oct_quantize(x, columns=False) -> OctRows:
+    """Rows, or with `columns` the columns, of a 2-D device tensor (uint8, int8, float32, float16 or bfloat16) as 8-bit
+    rows."""
+    torch = _torch()
+    x, ld = _rows2d(x, "x")
+    n, d = x.shape
+    device = x.device
+    if columns:
+        n, d = d, n
+    steps = (d + 127) // 128
+    out = OctRows.__new__(OctRows)
+    out.codes = torch.empty((n, 128 * steps), dtype=torch.uint8, device=device)
+    out.scales = torch.empty((n, (steps + 3) // 4 * 4), dtype=torch.uint8, device=device)
+    out.d = d
+    _run(lib().ann_oct_quantize, device, x.data_ptr(), n, d, _element_code(x), ld, int(bool(columns)), out.codes.data_ptr(),
+         out.scales.data_ptr())
+    return out
+
+
+def ann_oct_dequantize(rows: OctRows, dtype=None, out=None):
+    """The values that 8-bit rows stand for: (n, d), float32 unless `dtype` or `out` says otherwise."""
+    n, device = rows.codes.shape[0], rows.codes.device
+    out, ld = _results(out, n, rows.d, dtype, device)
+    _run(lib().ann_oct_dequantize, device, rows.codes.data_ptr(), rows.scales.data_ptr(), n, rows.d, out.data_ptr(),
+         _element_code(out), ld)
+    return out
+
+
+def ann_oct_product(x: OctRows, rows: OctRows, dtype=None, out=None):
+    """Every 8-bit row of `x` times every 8-bit row of `rows`: (x.n, rows.n), float32 unless `dtype` or `out` says
+    otherwise."""
+    device = rows.codes.device
+    if x.d != rows.d or x.codes.device != device:
+        raise ValueError("x and rows must have the same row length and device")
+    out, ldo = _results(out, x.codes.shape[0], rows.codes.shape[0], dtype, device)
+    _run(lib().ann_oct_product, device, x.codes.data_ptr(), x.scales.data_ptr(), x.n, rows.codes.data_ptr(), rows.scales.data_ptr(),
+         rows.n, rows.d, out.data_ptr(), _element_code(out), ldo)
+    return out

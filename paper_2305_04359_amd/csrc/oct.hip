@@ -1,0 +1,324 @@
+// Rows or columns to 8-bit floating point with a scale for each 128 elements, and back.
+#include <type_traits>
+
+#include "oct.hpp"
+
+namespace annmi {
+
+int check_oct_rows(const char* what, const uint8_t* codes, const uint8_t* scales, u64 n, u32 d) {
+  if (n > OCT_MOST_ROWS) return fail(ANN_EINVAL, "%s: rows must stay below 2^31", what);
+  if (d < 1 || d > OCT_MOST_D) return fail(ANN_EINVAL, "%s: d must be 1 to %u", what, OCT_MOST_D);
+  if (n == 0) return ANN_OK;
+  if (!codes || !scales) return fail(ANN_EINVAL, "null argument");
+  if (!aligned_to(codes, 16)) return fail(ANN_EINVAL, "%s: codes must be 16-byte aligned", what);
+  if (!aligned_to(scales, 4)) return fail(ANN_EINVAL, "%s: scales must be 4-byte aligned", what);
+  return ANN_OK;
+}
+
+struct OctQuantizeArgs {
+  const char* x;
+  u64 ldx;
+  u32 n, d, steps;
+  uint8_t* codes;
+  u32* scales;
+};
+
+// The scale byte of 128 elements whose largest magnitude has the bits `most`: e + 127 for the least e of at least
+// -127 with most <= 448 * 2^e.  448 is 1.75 * 2^8, so that the mantissa decides whether the exponent less 8 is enough.
+__device__ __forceinline__ u32 oct_scale_byte(u32 most) {
+  if (most >= 0x7F800000u) return 255u;  // infinite or NaN
+  const u32 e = (most >> 23) + ((most & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return e > 8 ? e - 8 : 0u;
+}
+// 2^(127 - byte), exact; of no use where byte is 255
+__device__ __forceinline__ float oct_inverse(u32 byte) { return __uint_as_float((254u - byte) << 23); }
+// four elements as four codes, to the nearest, ties to even; none is above 448
+__device__ __forceinline__ u32 oct_codes(float a, float b, float c, float d) {
+  const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (u32)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, low, true);
+}
+
+// exchanges inside 16 lanes, by one instruction each
+template <int CTRL>
+__device__ __forceinline__ u32 row_max(u32 v) {
+  return max(v, (u32)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ u32 max_of_16(u32 v) {
+  v = row_max<0xB1>(v);   // the neighbour
+  v = row_max<0x4E>(v);   // two away
+  v = row_max<0x124>(v);  // four and eight around
+  return row_max<0x128>(v);
+}
+
+// Rows.  Sixteen lanes take a step, eight elements each; LPR lanes (16, 32 or 64: one, two or four steps) take a row, longer
+// rows in turns of four steps, whose scale bytes are a word.  A wave asks for four such pieces at once.
+// WIDE: every row has eight elements at least; eight are then read at once, past d too, but in the last rows, whose
+// last eight are read where these would reach past the end of the last row.
+template <typename T, int LPR, bool WIDE>
+__global__ __launch_bounds__(256) void oct_quantize_kernel(OctQuantizeArgs a) {
+  constexpr u32 AHEAD = 4, PER_BLOCK = 256 / LPR;
+  const u32 lane = threadIdx.x % LPR;
+  const u32 words = oct_words(a.steps);
+  const u32 turns = LPR < 64 ? 1 : words;
+  const bool rows_ahead = turns == 1;  // four rows at once, else four turns of a row
+  const u64 stride = (u64)gridDim.x * PER_BLOCK;
+  for (u64 r0 = (u64)blockIdx.x * PER_BLOCK + threadIdx.x / LPR; r0 < a.n; r0 += rows_ahead ? stride * AHEAD : stride) {
+    for (u32 t0 = 0; t0 < turns; t0 += AHEAD) {
+      AnyPack<T, 8> in[AHEAD];
+      u64 row[AHEAD];
+      u32 at[AHEAD], early[AHEAD];
+#pragma unroll
+      for (u32 u = 0; u < AHEAD; ++u) {
+        row[u] = rows_ahead ? r0 + stride * u : r0;
+        at[u] = (rows_ahead ? 0 : t0 + u) * (4 * OCT_STEP) + lane * 8;  // the lane's first element
+        const u64 r = min(row[u], (u64)a.n - 1);
+        const T* from = reinterpret_cast<const T*>(a.x) + r * a.ldx;
+        early[u] = 0;
+        if (WIDE) {
+          const u32 first = at[u] < a.d ? at[u] : 0;
+          early[u] = (a.n - 1 - r) * a.ldx < 7 && first + 8 > a.d ? first + 8 - a.d : 0;
+          in[u] = *reinterpret_cast<const AnyPack<T, 8>*>(from + (first - early[u]));
+        } else {
+#pragma unroll
+          for (u32 e = 0; e < 8; ++e) in[u].v[e] = from[min(at[u] + e, a.d - 1)];
+        }
+      }
+#pragma unroll
+      for (u32 u = 0; u < AHEAD; ++u) {
+        const bool on = row[u] < a.n && at[u] / (4 * OCT_STEP) < words;  // (all lanes of a row alike)
+        if (!on) continue;
+        float v[8];
+#pragma unroll
+        for (u32 e = 0; e < 8; ++e) v[e] = mx_float(static_cast<T>(in[u].v[e]));
+        if (WIDE && early[u])
+          for (u32 k = 0; k < early[u]; ++k)
+#pragma unroll
+            for (u32 e = 0; e < 7; ++e) v[e] = v[e + 1];
+        u32 most = 0;  // magnitudes compare like their bits, and so do NaN and infinity
+#pragma unroll
+        for (u32 e = 0; e < 8; ++e) {
+          v[e] = at[u] + e < a.d ? v[e] : 0.0f;
+          most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+        }
+        const u32 byte = oct_scale_byte(max_of_16(most));
+        const float inverse = oct_inverse(byte);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= inverse;
+        Pack<u32, 2> code = {{oct_codes(v[0], v[1], v[2], v[3]), oct_codes(v[4], v[5], v[6], v[7])}};
+        if (byte == 255) code = {{0, 0}};
+        const u32 step = at[u] / OCT_STEP;
+        u32 word = (step < a.steps ? byte : 0u) << (step % 4 * 8);
+        if (LPR > 16) word |= __shfl_xor(word, 16);
+        if (LPR > 32) word |= __shfl_xor(word, 32);
+        if (step < a.steps) *reinterpret_cast<Pack<u32, 2>*>(a.codes + (row[u] * a.steps + step) * OCT_STEP + lane % 16 * 8) = code;
+        if (lane == 0) a.scales[row[u] * words + step / 4] = word;
+      }
+    }
+  }
+}
+
+// Columns: row i of the result is column i of x, which has d rows.  A workgroup takes a step of COLS columns: a thread 16
+// elements of four neighbouring columns, whose maxima meet in LDS; through LDS the codes get into whole rows of 128 bytes.
+constexpr u32 COLS = 128;
+template <typename T>
+__global__ __launch_bounds__(256) void oct_columns_kernel(OctQuantizeArgs a, u32 across, u64 tiles) {
+  __shared__ u32 most_of[8][COLS];
+  __shared__ __align__(16) v4i codes[COLS][8];
+  const u32 c = threadIdx.x % 32 * 4, g = threadIdx.x / 32;
+  const u32 words = oct_words(a.steps);
+  for (u64 t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const u64 i0 = t % across * COLS;        // the first column
+    const u32 step = (u32)(t / across);
+    const u32 e0 = step * OCT_STEP + g * 16;
+    const u32 there = (u32)min((u64)COLS, a.n - i0);
+    AnyPack<T, 4> in[16];
+    if (c + 4 <= there) {
+#pragma unroll
+      for (u32 e = 0; e < 16; ++e)
+        in[e] = *reinterpret_cast<const AnyPack<T, 4>*>(reinterpret_cast<const T*>(a.x) + (u64)min(e0 + e, a.d - 1) * a.ldx + i0 + c);
+    } else {
+#pragma unroll
+      for (u32 e = 0; e < 16; ++e)
+#pragma unroll
+        for (u32 k = 0; k < 4; ++k) in[e].v[k] = reinterpret_cast<const T*>(a.x)[(u64)min(e0 + e, a.d - 1) * a.ldx + i0 + min(c + k, there - 1)];
+    }
+    float v[4][16];
+    u32 most[4] = {};
+#pragma unroll
+    for (u32 e = 0; e < 16; ++e)
+#pragma unroll
+      for (u32 k = 0; k < 4; ++k) {
+        v[k][e] = e0 + e < a.d ? mx_float(static_cast<T>(in[e].v[k])) : 0.0f;
+        most[k] = max(most[k], __float_as_uint(v[k][e]) & 0x7FFFFFFFu);
+      }
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) most_of[g][c + k] = most[k];
+    __syncthreads();
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) {
+      u32 m = 0;
+#pragma unroll
+      for (u32 o = 0; o < 8; ++o) m = max(m, most_of[o][c + k]);
+      const u32 byte = oct_scale_byte(m);
+      const float inverse = oct_inverse(byte);
+      v4i code;
+#pragma unroll
+      for (u32 q = 0; q < 4; ++q)
+        code[q] = byte == 255 ? 0
+                              : (int)oct_codes(v[k][4 * q] * inverse, v[k][4 * q + 1] * inverse, v[k][4 * q + 2] * inverse, v[k][4 * q + 3] * inverse);
+      codes[c + k][g ^ (c / 4 + k) % 8] = code;
+      if (g == 0 && c + k < there) {
+        uint8_t* to = reinterpret_cast<uint8_t*>(a.scales) + (i0 + c + k) * words * 4;
+        to[step] = (uint8_t)byte;
+        if (step + 1 == a.steps)  // the rest of the last word
+          for (u32 o = a.steps; o < words * 4; ++o) to[o] = 0;
+      }
+    }
+    __syncthreads();
+    for (u32 r = threadIdx.x / 8; r < there; r += 32) {
+      const u32 u = threadIdx.x % 8;
+      *reinterpret_cast<v4i*>(a.codes + ((i0 + r) * a.steps + step) * OCT_STEP + u * 16) = codes[r][u ^ (r / 4 + r % 4) % 8];
+    }
+    // (the next turn's maxima go where none are read any more; its codes come behind its own barrier)
+  }
+}
+
+template <typename T, bool WIDE>
+hipError_t launch_oct_rows(const OctQuantizeArgs& a, hipStream_t s) {
+  const u32 lpr = a.steps == 1 ? 16 : a.steps == 2 ? 32 : 64;
+  // four rows for each place, where a turn takes a row
+  const u64 per = 256 / lpr * (a.steps <= 4 ? 4 : 1), blocks = ((u64)a.n + per - 1) / per;
+  const u32 grid = (u32)(blocks < (1u << 20) ? blocks : (1u << 20));
+  auto kernel = oct_quantize_kernel<T, 16, WIDE>;
+  if constexpr (WIDE) {  // (others have one step)
+    if (lpr == 32) kernel = oct_quantize_kernel<T, 32, WIDE>;
+    if (lpr == 64) kernel = oct_quantize_kernel<T, 64, WIDE>;
+  }
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_oct_quantize(const OctQuantizeArgs& a, bool columns, hipStream_t s) {
+  if (!columns) return a.d >= 8 ? launch_oct_rows<T, true>(a, s) : launch_oct_rows<T, false>(a, s);
+  const u32 across = (u32)(((u64)a.n + COLS - 1) / COLS);
+  const u64 tiles = (u64)across * a.steps;
+  hipLaunchKernelGGL(oct_columns_kernel<T>, dim3((u32)(tiles < (1u << 20) ? tiles : (1u << 20))), dim3(256), 0, s, a, across, tiles);
+  return hipGetLastError();
+}
+
+struct OctDequantizeArgs {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  u64 n;
+  u32 steps, d;
+  char* out;
+  u64 ldo;
+};
+
+// A thread takes 16 bytes of a row of `out`, and the same ones of other rows in turn.
+template <typename T>
+__global__ __launch_bounds__(256) void oct_dequantize_kernel(OctDequantizeArgs a) {
+  constexpr u32 E = 16 / sizeof(T), AHEAD = 4;  // elements; rows at a time
+  using v2f = float __attribute__((ext_vector_type(2)));
+  const u32 pieces = (a.d + E - 1) / E;
+  const u32 across = pieces < 256 ? pieces : 256, rows = 256 / across;  // of a block
+  const u32 sub = threadIdx.x / across;
+  if (sub >= rows) return;
+  const u64 stride = (u64)gridDim.x * rows;
+  const u32 words = oct_words(a.steps);
+  for (u64 r0 = (u64)blockIdx.x * rows + sub; r0 < a.n; r0 += stride * AHEAD) {
+    for (u32 c = threadIdx.x % across; c < pieces; c += across) {
+      Pack<u32, E / 4> code[AHEAD];
+      float scale[AHEAD];
+#pragma unroll
+      for (u32 u = 0; u < AHEAD; ++u) {
+        const u64 r = min(r0 + stride * u, a.n - 1);
+        code[u] = *reinterpret_cast<const Pack<u32, E / 4>*>(a.codes + r * a.steps * OCT_STEP + c * E);
+        scale[u] = mx_scale(a.scales[r * words * 4 + c * E / OCT_STEP]);
+      }
+#pragma unroll
+      for (u32 u = 0; u < AHEAD; ++u) {
+        if (r0 + stride * u >= a.n) break;
+        AnyPack<T, E> o;
+#pragma unroll
+        for (u32 q = 0; q < E / 4; ++q) {
+          const v2f low = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[u].v[q], false), high = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[u].v[q], true);
+          o.v[4 * q] = mx_round<T>(low.x * scale[u]);
+          o.v[4 * q + 1] = mx_round<T>(low.y * scale[u]);
+          o.v[4 * q + 2] = mx_round<T>(high.x * scale[u]);
+          o.v[4 * q + 3] = mx_round<T>(high.y * scale[u]);
+        }
+        T* to = reinterpret_cast<T*>(a.out) + (r0 + stride * u) * a.ldo + c * E;
+        if (c * E + E <= a.d) {
+          *reinterpret_cast<AnyPack<T, E>*>(to) = o;
+        } else {
+#pragma unroll
+          for (u32 j = 0; j < E; ++j)
+            if (c * E + j < a.d) to[j] = o.v[j];
+        }
+      }
+    }
+  }
+}
+
+template <typename T>
+hipError_t launch_oct_dequantize(const OctDequantizeArgs& a, hipStream_t s) {
+  const u32 pieces = (u32)((a.d + 16 / sizeof(T) - 1) / (16 / sizeof(T))), rows = pieces < 256 ? 256 / pieces : 1;
+  const u64 blocks = (a.n + 4 * rows - 1) / (4 * rows);
+  hipLaunchKernelGGL(oct_dequantize_kernel<T>, dim3((u32)(blocks < (1u << 20) ? blocks : (1u << 20))), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace annmi
+
+using namespace annmi;
+
+extern "C" {
+
+int ann_oct_quantize(const void* x_dev, uint64_t n, uint32_t d, ann_dtype dtype, uint64_t ldx, int columns, uint8_t* codes_dev,
+                    uint8_t* scales_dev, void* stream) try {
+  const u64 esz = dtype_bytes(dtype);
+  if (esz == 0) return fail(ANN_EINVAL, "unknown dtype");
+  int rc = check_oct_rows("ann_oct_quantize", codes_dev, scales_dev, n, d);
+  if (rc) return rc;
+  if (ldx < (columns ? n : d)) return fail(ANN_EINVAL, columns ? "ldx must be at least n" : "ldx must be at least d");
+  if (n == 0) return ANN_OK;
+  if (!x_dev) return fail(ANN_EINVAL, "null argument");
+  if (!aligned_to(x_dev, esz)) return fail(ANN_EINVAL, "x not aligned to its elements");
+  OctQuantizeArgs a{static_cast<const char*>(x_dev), ldx, (u32)n, d, oct_steps(d), codes_dev, reinterpret_cast<u32*>(scales_dev)};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case ANN_U8: HIP_TRY(launch_oct_quantize<uint8_t>(a, columns, st)); break;
+    case ANN_I8: HIP_TRY(launch_oct_quantize<int8_t>(a, columns, st)); break;
+    case ANN_F16: HIP_TRY(launch_oct_quantize<__half>(a, columns, st)); break;
+    case ANN_BF16: HIP_TRY(launch_oct_quantize<__bf16>(a, columns, st)); break;
+    default: HIP_TRY(launch_oct_quantize<float>(a, columns, st)); break;
+  }
+  return ANN_OK;
+} catch (...) {
+  return annmi::on_exception();
+}
+
+int ann_oct_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev,
+                      ann_dtype dtype, uint64_t ldo, void* stream) try {
+  const u64 esz = dtype_bytes(dtype);
+  if (esz < 2) return fail(ANN_EINVAL, "the values come as ANN_F32, ANN_F16 or ANN_BF16");
+  int rc = check_oct_rows("ann_oct_dequantize", codes_dev, scales_dev, n, d);
+  if (rc) return rc;
+  if (ldo < d) return fail(ANN_EINVAL, "ldo must be at least d");
+  if (n == 0) return ANN_OK;
+  if (!out_dev) return fail(ANN_EINVAL, "null argument");
+  if (!aligned_to(out_dev, esz)) return fail(ANN_EINVAL, "out not aligned to its elements");
+  OctDequantizeArgs a{codes_dev, scales_dev, n, oct_steps(d), d, static_cast<char*>(out_dev), ldo};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case ANN_F16: HIP_TRY(launch_oct_dequantize<__half>(a, st)); break;
+    case ANN_BF16: HIP_TRY(launch_oct_dequantize<__bf16>(a, st)); break;
+    default: HIP_TRY(launch_oct_dequantize<float>(a, st)); break;
+  }
+  return ANN_OK;
+} catch (...) {
+  return annmi::on_exception();
+}
+
+}  // extern "C"
