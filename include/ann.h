@@ -640,6 +640,44 @@ int ann_sample(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtyp
                void* stream);
 int ann_sample_scratch(uint64_t rows, uint64_t n, uint64_t* bytes);
 
+/* ------------------------------------------------------------------------
+ * The loss of scores against a teacher that has named its best entries of each
+ * row (distillation; a search's k nearest and the negatives of their distances
+ * are such entries), and the gradient.  Of a row of n scores z and k entries
+ * (id_j, t_j), at a temperature T from 2^-60 to 2^60:
+ *   p = softmax(t / T) over the entries, q = softmax(z / T) over the row
+ *   loss = T^2 sum_j p_j (log p_j - log q[id_j])
+ *   d loss / d z_i = T (q_i - sum over j with id_j = i of p_j)
+ * Entries with an id of n and more (ANN_NONE) or a t of -inf are not there; an id
+ * that is named twice has both shares, each with a term of its own.  Scores of
+ * -inf (masked) have q = 0: the loss is +inf where the teacher names one of them,
+ * the gradient is as above.  Rows without entries, or without a score above -inf:
+ * loss 0, gradient 0.  NaN and +inf among the scores make the row's loss NaN and
+ * its gradients NaN.  Among the entries that are there they make the loss NaN, and
+ * the gradients of the scores that they name.
+ *   scores_dev    rows x n of ANN_F32, ANN_F16 or ANN_BF16, ld apart; n < 2^31
+ *   ids_dev       rows x k uint32; teacher_dev rows x k of ANN_F32, ANN_F16 or
+ *                 ANN_BF16; 1 <= k <= 1024
+ *   losses_dev    rows floats
+ *   stats_dev     rows x 2 floats that ann_distill writes for ann_distill_grad:
+ *                 the row's largest score m and sum exp((z - m) / T)
+ *   scratch_dev   at least what ann_distill_scratch says, 16-byte aligned
+ *   grad_losses_dev  rows floats, the gradients of the losses; NULL: 1 for each
+ *   scale         one more factor of all gradients (1 / rows for the mean)
+ *   out_dev       rows x n gradients of the scores' type, ldo apart; may be
+ *                 scores_dev itself (with its stride), and must not overlap with
+ *                 it otherwise
+ * Asynchronous on `stream` and on the current device, which has to be that of
+ * the stream and of all pointers; allocates nothing, can be captured into a
+ * graph.  The results depend on the arguments only, bit by bit.              */
+int ann_distill(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtype, uint64_t ld, const uint32_t* ids_dev,
+                const void* teacher_dev, ann_dtype teacher_dtype, uint32_t k, float temperature, float* losses_dev,
+                float* stats_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream);
+int ann_distill_scratch(uint64_t rows, uint64_t n, uint64_t* bytes);
+int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dtype, uint64_t ld, const uint32_t* ids_dev,
+                     const void* teacher_dev, ann_dtype teacher_dtype, uint32_t k, float temperature, const float* stats_dev,
+                     const float* grad_losses_dev, float scale, void* out_dev, uint64_t ldo, void* stream);
+
 /* Thread-local description of the last error on this thread ("" if none).   */
 const char* ann_last_error(void);
 

@@ -90,6 +90,7 @@ EXPORTS = [
     "ann_mx_quantize", "ann_mx_dequantize", "ann_mx_product", "ann_mx_product_mx", "ann_mx_search", "ann_mx_search_scratch",
     "ann_sample", "ann_sample_scratch",
     "ann_oct_quantize", "ann_oct_dequantize", "ann_oct_product",
+    "ann_distill", "ann_distill_scratch", "ann_distill_grad",
 ]
 
 _lib = None
@@ -202,6 +203,12 @@ def lib():
         L.ann_oct_dequantize.argtypes = [vp, vp, u64, u32, vp, C.c_int, u64, vp]
         L.ann_oct_product.restype = C.c_int
         L.ann_oct_product.argtypes = [vp, vp, u64, vp, vp, u64, u32, vp, C.c_int, u64, vp]
+        L.ann_distill.restype = C.c_int
+        L.ann_distill.argtypes = [vp, u64, u64, C.c_int, u64, vp, vp, C.c_int, u32, C.c_float, vp, vp, vp, u64, vp]
+        L.ann_distill_scratch.restype = C.c_int
+        L.ann_distill_scratch.argtypes = [u64, u64, C.POINTER(u64)]
+        L.ann_distill_grad.restype = C.c_int
+        L.ann_distill_grad.argtypes = [vp, u64, u64, C.c_int, u64, vp, vp, C.c_int, u32, C.c_float, vp, vp, C.c_float, vp, u64, vp]
         L.ann_last_error.restype = C.c_char_p
         L.ann_last_error.argtypes = []
         _lib = L
@@ -911,4 +918,62 @@ def ann_oct_product(x: OctRows, rows: OctRows, dtype=None, out=None):
     out, ldo = _results(out, x.codes.shape[0], rows.codes.shape[0], dtype, device)
     _run(lib().ann_oct_product, device, x.codes.data_ptr(), x.scales.data_ptr(), x.n, rows.codes.data_ptr(), rows.scales.data_ptr(),
          rows.n, rows.d, out.data_ptr(), _element_code(out), ldo)
+    return out
+
+
+def _teacher(scores, ids, teacher):
+    """The checks of a teacher's entries of each row of `scores`; returns rows, n, the rows' distance, k."""
+    torch = _torch()
+    scores, ld = _rows2d(scores, "scores")
+    rows, n = scores.shape
+    for t, name in ((ids, "ids"), (teacher, "teacher")):
+        if t.dim() != 2 or t.shape[0] != rows or t.device != scores.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor of {rows} rows on {scores.device}")
+    if ids.dtype != torch.int32 or ids.shape != teacher.shape:
+        raise ValueError("ids must be int32, as many in a row as the teacher's scores")
+    return rows, n, ld, ids.shape[1]
+
+
+def ann_distill(scores, ids, teacher, temperature=1.0, losses_out=None, stats_out=None, scratch=None):
+    """The loss of each row of `scores` (float32, float16 or bfloat16) against its teacher's entries `ids` (int32; -1 where
+    there are fewer) with the scores `teacher`, by the rules of ann_distill in ann.h; returns (losses, stats), the latter
+    for ann_distill_grad."""
+    torch = _torch()
+    rows, n, ld, k = _teacher(scores, ids, teacher)
+    device = scores.device
+    need = C.c_uint64(0)
+    _check(lib().ann_distill_scratch(rows, n, C.byref(need)))
+    scratch = _scratch(scratch, need.value, device)
+    if losses_out is None:
+        losses_out = torch.empty(rows, dtype=torch.float32, device=device)
+    else:
+        _one_value_per_row(losses_out, "losses_out", torch.float32, rows, device)
+    if stats_out is None:
+        stats_out = torch.empty((rows, 2), dtype=torch.float32, device=device)
+    else:
+        _stats(stats_out, rows, device)
+    _run(lib().ann_distill, device, scores.data_ptr(), rows, n, _element_code(scores), ld, ids.data_ptr(), teacher.data_ptr(),
+         _element_code(teacher), k, temperature, losses_out.data_ptr(), stats_out.data_ptr(), scratch.data_ptr(),
+         scratch.numel() * scratch.element_size())
+    return losses_out, stats_out
+
+
+def _stats(stats, rows, device):
+    if tuple(stats.shape) != (rows, 2) or stats.dtype != _torch().float32 or stats.device != device or not stats.is_contiguous():
+        raise ValueError(f"stats must be a contiguous ({rows}, 2) float32 tensor on {device}")
+
+
+def ann_distill_grad(scores, ids, teacher, stats, grad_losses=None, temperature=1.0, scale=1.0, out=None):
+    """The gradients of `scores` under the losses that ann_distill gave with `stats`: times `grad_losses`, a float32 for each
+    row, where there are any, and times `scale`.  `out` may be `scores` itself."""
+    torch = _torch()
+    rows, n, ld, k = _teacher(scores, ids, teacher)
+    device = scores.device
+    _stats(stats, rows, device)
+    if grad_losses is not None:
+        _one_value_per_row(grad_losses, "grad_losses", torch.float32, rows, device)
+    out, ldo = _results(out, rows, n, scores.dtype, device)
+    _run(lib().ann_distill_grad, device, scores.data_ptr(), rows, n, _element_code(scores), ld, ids.data_ptr(), teacher.data_ptr(),
+         _element_code(teacher), k, temperature, stats.data_ptr(), grad_losses.data_ptr() if grad_losses is not None else None,
+         scale, out.data_ptr(), ldo)
     return out
