@@ -678,6 +678,46 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
                      const void* teacher_dev, ann_dtype teacher_dtype, uint32_t k, float temperature, const float* stats_dev,
                      const float* grad_losses_dev, float scale, void* out_dev, uint64_t ldo, void* stream);
 
+/* ------------------------------------------------------------------------
+ * One step of beam search.  Each group has `beams` rows of n scores; entry j of
+ * beam b continues it and is worth
+ *   v = total_b + (score_j - log sum_i exp(score_i)), in fp64,
+ * the sum over the beam's scores that are not NaN.  Of a group's continuations
+ * the k best are kept, ordered by (v downwards, beam, score downwards, entry).
+ * Entries of NaN or -inf are none; where some are +inf, those share the beam's
+ * mass.  A beam with a total of -inf or NaN has none.  A finished beam has one:
+ * pad_id, worth its total.
+ *   scores_dev    groups * beams rows of n ANN_F32, ANN_F16 or ANN_BF16, ld apart
+ *   totals_dev    groups * beams floats
+ *   finished_dev  groups * beams bytes, other than 0 for a beam that has ended;
+ *                 may be NULL (and pad_id is unused then)
+ *   parents_dev, ids_dev, totals_out_dev  groups x k: the beam (0 to beams - 1),
+ *                 the entry and v, rounded to fp32; ANN_NONE, ANN_NONE, -inf where
+ *                 there are fewer than k
+ *   scratch_dev   at least what ann_beam_select_scratch says, 16-byte aligned
+ * 1 <= beams <= 64, 1 <= k <= 128, 1 <= n < 2^24, groups * beams < 2^31.
+ * Asynchronous on `stream` and on the current device, which has to be that of
+ * the stream and of all pointers; allocates nothing, can be captured into a
+ * graph.  The results depend on the arguments only, bit by bit.              */
+int ann_beam_select(const void* scores_dev, uint64_t groups, uint32_t beams, uint64_t n, ann_dtype dtype, uint64_t ld,
+                    const float* totals_dev, const uint8_t* finished_dev, uint32_t pad_id, uint32_t k, uint32_t* parents_dev,
+                    uint32_t* ids_dev, float* totals_out_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream);
+int ann_beam_select_scratch(uint64_t groups, uint32_t beams, uint64_t n, uint32_t k, uint64_t* bytes);
+
+/* States in the order of the beams that go on: for every outer part o, group g,
+ * i < k with a parent p = parents[g][i] below `beams`, and m < mid,
+ *   out[o][g * k + i][m] = in[o][g * beams + p][m],
+ * runs of run_bytes bytes at o * outer_ + row * row_ + m * mid_ bytes from the
+ * beginning of each side.  Rows of other parents stay as they were.  in_dev and
+ * out_dev may be one and the same, with k = beams and the same strides: rows then
+ * change places where they are.  Otherwise the two must not overlap.  Rows, runs
+ * and outer parts of a side must not overlap either.
+ * beams, k <= 64; groups < 2^25; outer, mid, run_bytes < 2^31; a count of zero:
+ * ANN_OK, nothing is done.  Streams, devices and graphs as ann_beam_select.   */
+int ann_beam_reorder(const void* in_dev, void* out_dev, const uint32_t* parents_dev, uint64_t groups, uint32_t beams, uint32_t k,
+                     uint64_t outer, uint64_t outer_in, uint64_t outer_out, uint64_t row_in, uint64_t row_out, uint64_t mid,
+                     uint64_t mid_in, uint64_t mid_out, uint64_t run_bytes, void* stream);
+
 /* Thread-local description of the last error on this thread ("" if none).   */
 const char* ann_last_error(void);
 

@@ -91,6 +91,7 @@ EXPORTS = [
     "ann_sample", "ann_sample_scratch",
     "ann_oct_quantize", "ann_oct_dequantize", "ann_oct_product",
     "ann_distill", "ann_distill_scratch", "ann_distill_grad",
+    "ann_beam_select", "ann_beam_select_scratch", "ann_beam_reorder",
 ]
 
 _lib = None
@@ -209,6 +210,12 @@ def lib():
         L.ann_distill_scratch.argtypes = [u64, u64, C.POINTER(u64)]
         L.ann_distill_grad.restype = C.c_int
         L.ann_distill_grad.argtypes = [vp, u64, u64, C.c_int, u64, vp, vp, C.c_int, u32, C.c_float, vp, vp, C.c_float, vp, u64, vp]
+        L.ann_beam_select.restype = C.c_int
+        L.ann_beam_select.argtypes = [vp, u64, u32, u64, C.c_int, u64, vp, vp, u32, u32, vp, vp, vp, vp, u64, vp]
+        L.ann_beam_select_scratch.restype = C.c_int
+        L.ann_beam_select_scratch.argtypes = [u64, u32, u64, u32, C.POINTER(u64)]
+        L.ann_beam_reorder.restype = C.c_int
+        L.ann_beam_reorder.argtypes = [vp, vp, vp, u64, u32, u32, u64, u64, u64, u64, u64, u64, u64, u64, u64, vp]
         L.ann_last_error.restype = C.c_char_p
         L.ann_last_error.argtypes = []
         _lib = L
@@ -976,4 +983,85 @@ def ann_distill_grad(scores, ids, teacher, stats, grad_losses=None, temperature=
     _run(lib().ann_distill_grad, device, scores.data_ptr(), rows, n, _element_code(scores), ld, ids.data_ptr(), teacher.data_ptr(),
          _element_code(teacher), k, temperature, stats.data_ptr(), grad_losses.data_ptr() if grad_losses is not None else None,
          scale, out.data_ptr(), ldo)
+    return out
+
+
+def ann_beam_select(scores, totals, beams, k, finished=None, pad_id=0, parents_out=None, ids_out=None, totals_out=None, scratch=None):
+    """The k best continuations of each group of `beams` rows of `scores` (float32, float16 or bfloat16) with the running
+    totals `totals` (float32, one for each row), by the rules of ann_beam_select in ann.h; returns (parents, ids, totals),
+    each (groups, k).  `finished`: bool or uint8, one for each row."""
+    torch = _torch()
+    scores, ld = _rows2d(scores, "scores")
+    rows, n = scores.shape
+    device = scores.device
+    if beams < 1 or rows % beams:
+        raise ValueError(f"scores must have whole groups of {beams} rows")
+    groups = rows // beams
+    _one_value_per_row(totals, "totals", torch.float32, rows, device)
+    if finished is not None:
+        _one_value_per_row(finished, "finished", finished.dtype if finished.dtype in (torch.bool, torch.uint8) else torch.bool, rows, device)
+    if finished is not None and not 0 <= pad_id < n:
+        raise ValueError(f"pad_id must be 0 to {n - 1}")
+    need = C.c_uint64(0)
+    _check(lib().ann_beam_select_scratch(groups, beams, n, k, C.byref(need)))
+    scratch = _scratch(scratch, need.value, device)
+    out = []
+    for t, dtype, name in ((parents_out, torch.int32, "parents_out"), (ids_out, torch.int32, "ids_out"), (totals_out, torch.float32, "totals_out")):
+        if t is None:
+            t = torch.empty((groups, k), dtype=dtype, device=device)
+        elif tuple(t.shape) != (groups, k) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous ({groups}, {k}) tensor of {dtype} on {device}")
+        out.append(t)
+    _run(lib().ann_beam_select, device, scores.data_ptr(), groups, beams, n, _element_code(scores), ld, totals.data_ptr(),
+         finished.data_ptr() if finished is not None else None, pad_id if finished is not None else 0, k, out[0].data_ptr(),
+         out[1].data_ptr(), out[2].data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size())
+    return tuple(out)
+
+
+def _joined(dims):
+    """(size, stride, stride) of neighbouring dimensions as few as they can be, those of one element left out."""
+    out = []
+    for size, a, b in dims:
+        if size == 1:
+            continue
+        if out and out[-1][1] == size * a and out[-1][2] == size * b:
+            out[-1] = (out[-1][0] * size, a, b)
+        else:
+            out.append((size, a, b))
+    return out
+
+
+def ann_beam_reorder(states, parents, beams, dim=0, out=None):
+    """`states` with the rows of dimension `dim`, groups of `beams`, in the order of `parents` ((groups, k) int32, as
+    ann_beam_select gives them): a new tensor, or `out`, which may be `states` itself.  Rows without a parent stay as they
+    were in `out` (in a new tensor they are not set).  What lies before `dim` must be one dimension with one stride, what
+    lies behind it runs of elements with one stride between them, as in slices of a cache with room for more."""
+    torch = _torch()
+    if not states.is_cuda or not 0 <= dim < states.dim():
+        raise ValueError("states must be a device tensor that has the dimension dim")
+    device = states.device
+    if parents.dim() != 2 or parents.dtype != torch.int32 or parents.device != device or not parents.is_contiguous():
+        raise ValueError(f"parents must be a contiguous (groups, k) tensor of int32 on {device}")
+    groups, k = parents.shape
+    if states.shape[dim] != groups * beams:
+        raise ValueError(f"states must have {groups} groups of {beams} rows in dimension {dim}")
+    shape = (*states.shape[:dim], groups * k, *states.shape[dim + 1:])
+    if out is None:
+        out = torch.empty(shape, dtype=states.dtype, device=device)
+    elif tuple(out.shape) != shape or out.dtype != states.dtype or out.device != device:
+        raise ValueError(f"out must be {shape} of {states.dtype} on {device}")
+    size = states.element_size()
+    dims = [(n, a * size, b * size) for n, a, b in zip(states.shape, states.stride(), out.stride())]
+    before, behind = _joined(dims[:dim]), _joined(dims[dim + 1:])
+    if 0 in shape:
+        return out
+    run = size
+    if behind and behind[-1][1:] == (size, size):
+        run *= behind.pop()[0]
+    if len(before) > 1 or len(behind) > 1:
+        raise ValueError("states or out are laid out in more parts than one before dim and one behind it")
+    outer, outer_in, outer_out = before[0] if before else (1, 0, 0)
+    mid, mid_in, mid_out = behind[0] if behind else (1, 0, 0)
+    _run(lib().ann_beam_reorder, device, states.data_ptr(), out.data_ptr(), parents.data_ptr(), groups, beams, k, outer, outer_in,
+         outer_out, dims[dim][1], dims[dim][2], mid, mid_in, mid_out, run)
     return out

@@ -1,0 +1,497 @@
+// Beam search: the best continuations of each group of beams, and the states of a decoder in the order of the beams that go on.
+//
+// The continuation of beam b by entry j is worth total_b + log q, q = softmax of the beam's scores at j.  Within a beam
+// that order is the scores' own, so that a part of a row need hand on no more than its k best scores, beside its largest
+// score and the sum of exp relative to it: one pass over the scores.  Beams are compared by their log sums, in 64 bits: the
+// order is that of the real numbers but where two differ by less than some 1e-12.
+#include <algorithm>
+
+#include "mx.hpp"
+
+namespace annmi {
+
+constexpr u32 BEAM_MOST_BEAMS = 64;
+constexpr u32 BEAM_MOST_K = 128;
+constexpr u32 BEAM_MOST_N = (1u << 24) - 1;  // an id, a score and a beam fit in one key of 64 bits
+constexpr u32 BEAM_THREADS = 256;
+constexpr u32 BEAM_EACH = 16;  // entries of a thread
+constexpr u32 BEAM_CHUNK = BEAM_THREADS * BEAM_EACH;
+
+struct BeamArgs {
+  const char* scores;
+  u64 groups;
+  u32 beams, n, k;
+  u64 ld;
+  const float* totals;
+  const uint8_t* finished;
+  u32 pad;
+  u32 chunks;  // of a row
+  u64* best;   // for each chunk its k best: score key << 32 | ~id, downwards, 0 where there are fewer
+  double* sums;
+  float* most;
+  u32* parents;
+  u32* ids;
+  float* out;
+};
+
+// exp x for x <= 0, within 1e-12 of itself; 0 below -700.  2^n and the series of e^r, |r| <= ln 2 / 2, to r^10 / 10! (the
+// next term is 2.2e-13).  Adding 1.5 * 2^52 leaves n in the low bits of the sum.
+__device__ __forceinline__ double beam_exp(double x) {
+  constexpr double MAGIC = 6755399441055744.0, LOG2E = 1.4426950408889634074, LN2 = 0.69314718055994530942;
+  const double d = __builtin_fmax(x, -700.0) * LOG2E, t = d + MAGIC;
+  const double r = (d - (t - MAGIC)) * LN2;
+  double p = 1.0 / 3628800;
+  p = __builtin_fma(p, r, 1.0 / 362880);
+  p = __builtin_fma(p, r, 1.0 / 40320);
+  p = __builtin_fma(p, r, 1.0 / 5040);
+  p = __builtin_fma(p, r, 1.0 / 720);
+  p = __builtin_fma(p, r, 1.0 / 120);
+  p = __builtin_fma(p, r, 1.0 / 24);
+  p = __builtin_fma(p, r, 1.0 / 6);
+  p = __builtin_fma(p, r, 0.5);
+  p = __builtin_fma(p, r, 1.0);
+  p = __builtin_fma(p, r, 1.0);
+  const double v = __hiloint2double(__double2hiint(p) + ((int)__double_as_longlong(t) << 20), __double2loint(p));
+  return x < -700.0 ? 0.0 : v;
+}
+// z - most, 0 among infinities
+__device__ __forceinline__ double beam_below(float z, float most) { return z == most ? 0.0 : (double)z - most; }
+
+// whether a beam goes on by its scores
+__device__ __forceinline__ bool beam_lives(const BeamArgs& a, u64 row) {
+  const float total = a.totals[row];
+  return total > -INFINITY && !(a.finished && a.finished[row]);
+}
+
+// Sorts the first `count` keys downwards, in room for the next power of two; the whole workgroup.
+template <u32 THREADS, typename Swap>
+__device__ __forceinline__ void sort_down(u32 size, Swap swap) {
+  for (u32 run = 2; run <= size; run *= 2)
+    for (u32 gap = run / 2; gap > 0; gap /= 2) {
+      for (u32 i = threadIdx.x; i < size / 2; i += THREADS) {
+        const u32 low = i / gap * (2 * gap) + i % gap, high = low + gap;
+        swap(low, high, (low & run) == 0);  // (the larger first where true)
+      }
+      __syncthreads();
+    }
+}
+__device__ __forceinline__ u32 power_of_two(u32 v) { return v <= 1 ? 1 : 1u << (32 - __clz(v - 1)); }
+
+// One chunk of a row a workgroup, 16 entries a thread, which stay in registers.  The k-th best of the threads' best ones is
+// a bound: entries above it are at least k, and few more than that in most orders; they are listed and sorted.
+template <typename T>
+__global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
+  constexpr u32 E = 16 / sizeof(T), PACKS = BEAM_EACH / E;
+  __shared__ u64 list[BEAM_CHUNK];
+  __shared__ __align__(16) u32 heads[BEAM_THREADS];
+  __shared__ double sums[BEAM_THREADS / 64];
+  __shared__ u32 bound, top, count;
+  const u64 tiles = a.groups * a.beams * a.chunks;
+  for (u64 b = blockIdx.x; b < tiles; b += gridDim.x) {
+    const u64 row = b / a.chunks;
+    if (!beam_lives(a, row)) continue;  // (nothing of it is read)
+    const u32 from = (u32)(b % a.chunks) * BEAM_CHUNK, there = min(BEAM_CHUNK, a.n - from);
+    const T* z = reinterpret_cast<const T*>(a.scores) + row * a.ld + from;
+    float v[BEAM_EACH];
+    u32 key[BEAM_EACH];
+#pragma unroll
+    for (u32 u = 0; u < PACKS; ++u) {
+      const u32 at = (threadIdx.x + BEAM_THREADS * u) * E;
+      if (at + E <= there) {
+        const AnyPack<T, E> in = *reinterpret_cast<const AnyPack<T, E>*>(z + at);
+#pragma unroll
+        for (u32 e = 0; e < E; ++e) v[u * E + e] = mx_float(static_cast<T>(in.v[e]));
+      } else {
+#pragma unroll
+        for (u32 e = 0; e < E; ++e) v[u * E + e] = at + e < there ? mx_float(z[min(at + e, there - 1)]) : -INFINITY;
+      }
+    }
+    u32 head = 0;
+#pragma unroll
+    for (u32 i = 0; i < BEAM_EACH; ++i) {
+      key[i] = v[i] > -INFINITY ? float_key(v[i]) : 0u;  // (not NaN either)
+      head = max(head, key[i]);
+    }
+    __syncthreads();  // (the last turn's readers)
+    heads[threadIdx.x] = head;
+    if (threadIdx.x == 0) count = 0, bound = 0;
+    __syncthreads();
+    u32 rank = 0;
+#pragma unroll 8
+    for (u32 i = 0; i < BEAM_THREADS; i += 4) {
+      const v4i four = *reinterpret_cast<const v4i*>(heads + i);
+#pragma unroll
+      for (u32 e = 0; e < 4; ++e) rank += (u32)four[e] > head || ((u32)four[e] == head && i + e < threadIdx.x);
+    }
+    if (rank == a.k - 1) bound = head;
+    if (rank == 0) top = head;
+    __syncthreads();
+    const float most = key_float(top);
+    if (top == 0) {  // nothing that is not masked
+      if (threadIdx.x == 0) a.sums[b] = 0.0, a.most[b] = -INFINITY;
+      for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = 0;
+      continue;
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (u32 i = 0; i < BEAM_EACH; ++i)
+      if (key[i]) sum += beam_exp(beam_below(v[i], most));
+#pragma unroll
+    for (u32 i = 0; i < BEAM_EACH; ++i)
+      if (key[i] && key[i] >= bound) {
+        const u32 id = from + (threadIdx.x + BEAM_THREADS * (i / E)) * E + i % E;
+        list[atomicAdd(&count, 1u)] = (u64)key[i] << 32 | (u32)~id;  // (in any order: the keys differ, and are sorted)
+      }
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
+    __syncthreads();
+    const u32 listed = count, size = power_of_two(max(listed, a.k));
+    for (u32 i = listed + threadIdx.x; i < size; i += BEAM_THREADS) list[i] = 0;
+    __syncthreads();
+    sort_down<BEAM_THREADS>(size, [&](u32 low, u32 high, bool down) {
+      const u64 x = list[low], y = list[high];
+      if ((x < y) == down) list[low] = y, list[high] = x;
+    });
+    for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = list[i];
+    if (threadIdx.x == 0) {
+      double all = sums[0];
+      for (u32 w = 1; w < BEAM_THREADS / 64; ++w) all += sums[w];
+      a.sums[b] = all;
+      a.most[b] = most;
+    }
+  }
+}
+
+// A group a workgroup: the beams' log sums, then the chunks' lists, first all their best ones, then all second ones, and so on,
+// a thousand at a time.  What is not better than the k-th so far is left out; when a thousand in a row, or all lists' next,
+// are, the rest is too.
+constexpr u32 PICK_THREADS = 1024, PICK_ROOM = 2048;
+__global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
+  // worth, as a key that is larger for more; and behind it beam, score and id
+  __shared__ u64 worth[PICK_ROOM], tie[PICK_ROOM];
+  __shared__ double logs[BEAM_MOST_BEAMS];
+  __shared__ float mosts[BEAM_MOST_BEAMS], totals[BEAM_MOST_BEAMS];
+  __shared__ u32 state[BEAM_MOST_BEAMS];  // 0: no continuation, 1: finished, 2: by its scores
+  __shared__ u32 count;
+  const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  auto worth_key = [](double v) {
+    const u64 bits = (u64)__double_as_longlong(v + 0.0);
+    return bits >> 63 ? ~bits : bits | 1ull << 63;
+  };
+  auto swap = [&](u32 low, u32 high, bool down) {
+    const u64 x = worth[low], y = worth[high], xt = tie[low], yt = tie[high];
+    if ((x < y || (x == y && xt < yt)) == down) worth[low] = y, worth[high] = x, tie[low] = yt, tie[high] = xt;
+  };
+  for (u64 g = blockIdx.x; g < a.groups; g += gridDim.x) {
+    __syncthreads();  // (the last group's readers)
+    for (u32 b = wave; b < a.beams; b += PICK_THREADS / 64) {
+      const u64 row = g * a.beams + b;
+      const bool lives = beam_lives(a, row);
+      float most = -INFINITY;
+      double sum = 0.0;
+      if (lives) {
+        for (u32 c = lane; c < a.chunks; c += 64) most = __builtin_fmaxf(most, a.most[row * a.chunks + c]);
+#pragma unroll
+        for (int w = 1; w < 64; w *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w));
+        for (u32 c = lane; c < a.chunks; c += 64) {
+          const double s = a.sums[row * a.chunks + c];
+          if (s > 0.0) sum += s * beam_exp(beam_below(a.most[row * a.chunks + c], most));
+        }
+#pragma unroll
+        for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
+      }
+      if (lane == 0) {
+        const float total = a.totals[row];
+        totals[b] = total;
+        mosts[b] = most;
+        logs[b] = log(sum);
+        state[b] = lives ? (most > -INFINITY ? 2 : 0) : total > -INFINITY ? 1 : 0;
+      }
+    }
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    // finished beams go on as they are
+    if (threadIdx.x < a.beams && state[threadIdx.x] == 1) {
+      const u32 at = atomicAdd(&count, 1u);
+      worth[at] = worth_key(totals[threadIdx.x]);
+      tie[at] = (u64)(63 - threadIdx.x) << 56 | (u64)(0xFFFFFFu - a.pad);
+    }
+    __syncthreads();
+    const u32 lists = a.beams * a.chunks;
+    const u64 all = (u64)lists * a.k;
+    u64 least = 0, least_tie = 0;  // the k-th so far: others have to be better
+    u32 since = 0;                 // entries in a row that were not
+    for (u64 first = 0; first < all && since < max(lists, 1u); first += PICK_THREADS) {
+      const u64 at = first + threadIdx.x;
+      u64 key = 0, key_tie = 0;
+      if (at < all) {
+        const u32 l = (u32)(at % lists), b = l / a.chunks;
+        if (state[b] == 2) {
+          const u64 e = a.best[((g * a.beams + b) * a.chunks + l % a.chunks) * a.k + at / lists];
+          if (e) {
+            const u32 score = (u32)(e >> 32), id = ~(u32)e;
+            const double v = totals[b] + (beam_below(key_float(score), mosts[b]) - logs[b]);
+            if (v > -INFINITY) {
+              key = worth_key(v);
+              key_tie = (u64)(63 - b) << 56 | (u64)score << 24 | (0xFFFFFFu - id);
+            }
+          }
+        }
+      }
+      const bool better = key > least || (key == least && key_tie > least_tie);
+      const u32 before = count;
+      __syncthreads();
+      if (better) {
+        const u32 slot = atomicAdd(&count, 1u);
+        worth[slot] = key;
+        tie[slot] = key_tie;
+      }
+      __syncthreads();
+      const u32 listed = count;
+      since = listed == before ? since + PICK_THREADS : 0;
+      const bool last = first + PICK_THREADS >= all || since >= lists;
+      if (first == 0 || last || listed + PICK_THREADS > PICK_ROOM) {
+        const u32 size = power_of_two(max(listed, a.k));
+        for (u32 i = listed + threadIdx.x; i < size; i += PICK_THREADS) worth[i] = 0, tie[i] = 0;
+        __syncthreads();
+        sort_down<PICK_THREADS>(size, swap);
+        least = worth[a.k - 1];
+        least_tie = tie[a.k - 1];
+        if (threadIdx.x == 0) count = min(listed, a.k);
+        __syncthreads();
+      }
+    }
+    for (u32 i = threadIdx.x; i < a.k; i += PICK_THREADS) {
+      const bool some = i < count;
+      const u64 key = worth[i], t = tie[i];
+      const u64 bits = key >> 63 ? key & ~(1ull << 63) : ~key;
+      a.parents[g * a.k + i] = some ? 63 - (u32)(t >> 56) : ANN_NONE;
+      a.ids[g * a.k + i] = some ? 0xFFFFFFu - (u32)(t & 0xFFFFFFu) : ANN_NONE;
+      a.out[g * a.k + i] = some ? (float)__longlong_as_double((long long)bits) : -INFINITY;
+    }
+  }
+}
+
+// A thread takes a piece of VEC bytes of the rows of all k beams that go on, so that nobody else reads or writes that piece,
+// and rows can change places where they are: it reads MOST of them before it writes any, all of them in that case.  There
+// rows that stay where they are are not touched.
+struct ReorderArgs {
+  const char* in;
+  char* out;
+  const u32* parents;
+  u64 outer, outer_in, outer_out;  // count; strides in bytes
+  u64 groups, row_in, row_out;
+  u32 beams, k;
+  u32 mid, pieces;  // runs of a row, pieces of VEC bytes of a run
+  u64 mid_in, mid_out;
+  u64 parts;  // workgroups for a row
+  u32 in_place;
+};
+template <int VEC>
+struct PieceOf;
+template <>
+struct PieceOf<16> {
+  using type = v4i;
+};
+template <>
+struct PieceOf<4> {
+  using type = int;
+};
+template <>
+struct PieceOf<1> {
+  using type = char;
+};
+
+template <int VEC, int MOST>
+__global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
+  using P = typename PieceOf<VEC>::type;
+  const u64 tiles = a.outer * a.groups * a.parts;
+  for (u64 t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const u64 og = t / a.parts, g = og % a.groups, o = og / a.groups;
+    const u64 at = t % a.parts * 256 + threadIdx.x;
+    if (at >= (u64)a.mid * a.pieces) continue;
+    const u64 m = at / a.pieces, piece = at % a.pieces * VEC;
+    const char* in = a.in + o * a.outer_in + g * a.beams * a.row_in + m * a.mid_in + piece;
+    char* out = a.out + o * a.outer_out + g * a.k * a.row_out + m * a.mid_out + piece;
+    const u32* parents = a.parents + g * a.k;
+    for (u32 first = 0; first < a.k; first += MOST) {
+      P v[MOST];
+#pragma unroll
+      for (u32 i = 0; i < MOST; ++i) {
+        if (first + i >= a.k) break;
+        const u32 p = parents[first + i];
+        if (p < a.beams && !(a.in_place && p == first + i)) v[i] = *reinterpret_cast<const P*>(in + p * a.row_in);
+      }
+#pragma unroll
+      for (u32 i = 0; i < MOST; ++i) {
+        if (first + i >= a.k) break;
+        const u32 p = parents[first + i];
+        if (p < a.beams && !(a.in_place && p == first + i)) *reinterpret_cast<P*>(out + (first + i) * a.row_out) = v[i];
+      }
+    }
+  }
+}
+
+template <int VEC>
+hipError_t launch_reorder(ReorderArgs a, u64 run_bytes, hipStream_t s) {
+  a.pieces = (u32)(run_bytes / VEC);
+  a.parts = ((u64)a.mid * a.pieces + 255) / 256;
+  const u64 tiles = a.outer * a.groups * a.parts;
+  auto kernel = beam_reorder_kernel<VEC, 8>;
+  if (a.in_place && a.k > 8) kernel = a.k <= 16 ? beam_reorder_kernel<VEC, 16> : a.k <= 32 ? beam_reorder_kernel<VEC, 32> : beam_reorder_kernel<VEC, 64>;
+  hipLaunchKernelGGL(kernel, dim3((u32)std::min<u64>(tiles, 1u << 22)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+u32 beam_chunks(u64 n) { return (u32)((n + BEAM_CHUNK - 1) / BEAM_CHUNK); }
+
+template <typename T>
+hipError_t launch_beam(const BeamArgs& a, hipStream_t s) {
+  const u64 tiles = a.groups * a.beams * a.chunks;
+  hipLaunchKernelGGL(beam_chunk_kernel<T>, dim3((u32)std::min<u64>(tiles, 1u << 22)), dim3(BEAM_THREADS), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(beam_pick_kernel, dim3((u32)std::min<u64>(a.groups, 1u << 21)), dim3(PICK_THREADS), 0, s, a);
+  return hipGetLastError();
+}
+
+int check_beams(u64 groups, u32 beams, u64 n, u32 k) {
+  if (beams < 1 || beams > BEAM_MOST_BEAMS) return fail(ANN_EINVAL, "beams must be 1 to %u", BEAM_MOST_BEAMS);
+  if (groups >= (1ull << 31) / beams) return fail(ANN_EINVAL, "groups * beams must stay below 2^31");
+  if (n < 1 || n > BEAM_MOST_N) return fail(ANN_EINVAL, "n must be 1 to %u", BEAM_MOST_N);
+  if (k < 1 || k > BEAM_MOST_K) return fail(ANN_EINVAL, "k must be 1 to %u", BEAM_MOST_K);
+  return ANN_OK;
+}
+
+}  // namespace annmi
+
+using namespace annmi;
+
+extern "C" {
+
+int ann_beam_select_scratch(uint64_t groups, uint32_t beams, uint64_t n, uint32_t k, uint64_t* bytes) try {
+  if (!bytes) return fail(ANN_EINVAL, "null argument");
+  const int rc = check_beams(groups, beams, n, k);
+  if (rc) return rc;
+  *bytes = groups * beams * beam_chunks(n) * (8ull * k + 8 + 4);
+  return ANN_OK;
+} catch (...) {
+  return annmi::on_exception();
+}
+
+int ann_beam_select(const void* scores_dev, uint64_t groups, uint32_t beams, uint64_t n, ann_dtype dtype, uint64_t ld,
+                    const float* totals_dev, const uint8_t* finished_dev, uint32_t pad_id, uint32_t k, uint32_t* parents_dev,
+                    uint32_t* ids_dev, float* totals_out_dev, void* scratch_dev, uint64_t scratch_bytes, void* stream) try {
+  const u64 esz = dtype_bytes(dtype);
+  if (esz < 2) return fail(ANN_EINVAL, "scores must be ANN_F32, ANN_F16 or ANN_BF16");
+  uint64_t need = 0;
+  const int rc = ann_beam_select_scratch(groups, beams, n, k, &need);
+  if (rc) return rc;
+  if (ld < n) return fail(ANN_EINVAL, "ld must be at least n");
+  if (finished_dev && pad_id >= n) return fail(ANN_EINVAL, "pad_id must be below n");
+  if (groups == 0) return ANN_OK;
+  if (!scores_dev || !totals_dev || !parents_dev || !ids_dev || !totals_out_dev || !scratch_dev) return fail(ANN_EINVAL, "null argument");
+  if (!aligned_to(scores_dev, esz) || !aligned_to(totals_dev, 4) || !aligned_to(parents_dev, 4) || !aligned_to(ids_dev, 4) || !aligned_to(totals_out_dev, 4))
+    return fail(ANN_EINVAL, "an array is not aligned to its elements");
+  if (scratch_bytes < need) return fail(ANN_EINVAL, "scratch must hold %llu bytes", (unsigned long long)need);
+  if (!aligned_to(scratch_dev, 16)) return fail(ANN_EINVAL, "scratch must be 16-byte aligned");
+  BeamArgs a{};
+  a.scores = static_cast<const char*>(scores_dev);
+  a.groups = groups;
+  a.beams = beams;
+  a.n = (u32)n;
+  a.k = k;
+  a.ld = ld;
+  a.totals = totals_dev;
+  a.finished = finished_dev;
+  a.pad = pad_id;
+  a.chunks = beam_chunks(n);
+  const u64 lists = groups * beams * a.chunks;
+  a.best = static_cast<u64*>(scratch_dev);
+  a.sums = reinterpret_cast<double*>(a.best + lists * k);
+  a.most = reinterpret_cast<float*>(a.sums + lists);
+  a.parents = parents_dev;
+  a.ids = ids_dev;
+  a.out = totals_out_dev;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == ANN_F32)
+    HIP_TRY(launch_beam<float>(a, st));
+  else if (dtype == ANN_F16)
+    HIP_TRY(launch_beam<__half>(a, st));
+  else
+    HIP_TRY(launch_beam<__bf16>(a, st));
+  return ANN_OK;
+} catch (...) {
+  return annmi::on_exception();
+}
+
+int ann_beam_reorder(const void* in_dev, void* out_dev, const uint32_t* parents_dev, uint64_t groups, uint32_t beams, uint32_t k,
+                     uint64_t outer, uint64_t outer_in, uint64_t outer_out, uint64_t row_in, uint64_t row_out, uint64_t mid,
+                     uint64_t mid_in, uint64_t mid_out, uint64_t run_bytes, void* stream) try {
+  if (beams < 1 || beams > BEAM_MOST_BEAMS || k < 1 || k > BEAM_MOST_BEAMS) return fail(ANN_EINVAL, "beams and k must be 1 to %u", BEAM_MOST_BEAMS);
+  if (groups >= (1ull << 31) / BEAM_MOST_BEAMS || outer >= 1ull << 31 || mid >= 1ull << 31 || run_bytes >= 1ull << 31)
+    return fail(ANN_EINVAL, "groups must stay below 2^25, outer, mid and run_bytes below 2^31");
+  if (groups == 0 || outer == 0 || mid == 0 || run_bytes == 0) return ANN_OK;
+  if (!in_dev || !out_dev || !parents_dev) return fail(ANN_EINVAL, "null argument");
+  if (!aligned_to(parents_dev, 4)) return fail(ANN_EINVAL, "parents not aligned to their elements");
+  // Where rows, their runs and the outer ones lie must be told apart by their strides, and all of it must fit in memory.
+  u64 span[2];
+  const u64 strides[2][3] = {{outer_in, row_in, mid_in}, {outer_out, row_out, mid_out}};
+  for (int side = 0; side < 2; ++side) {
+    u64 counts[3] = {outer, groups * (side ? k : beams), mid};
+    u64 step[3] = {strides[side][0], strides[side][1], strides[side][2]};
+    for (int i = 0; i < 3; ++i)  // by their strides, upwards
+      for (int j = i + 1; j < 3; ++j)
+        if (step[j] < step[i]) std::swap(step[i], step[j]), std::swap(counts[i], counts[j]);
+    unsigned __int128 end = run_bytes;
+    for (int i = 0; i < 3; ++i) {
+      if (counts[i] == 1) continue;
+      if (step[i] < end) return fail(ANN_EINVAL, "rows, their runs or outer parts overlap");
+      end += (unsigned __int128)step[i] * (counts[i] - 1);
+      if (end >= 1ull << 62) return fail(ANN_EINVAL, "strides too large");
+    }
+    span[side] = (u64)end;
+  }
+  const uintptr_t from = reinterpret_cast<uintptr_t>(in_dev), to = reinterpret_cast<uintptr_t>(out_dev);
+  ReorderArgs a{};
+  a.in_place = from == to;
+  if (a.in_place) {
+    if (k != beams || (outer > 1 && outer_in != outer_out) || (groups * k > 1 && row_in != row_out) || (mid > 1 && mid_in != mid_out))
+      return fail(ANN_EINVAL, "rows that change places where they are need k = beams and the same strides");
+  } else if (from < to + span[1] && to < from + span[0]) {
+    return fail(ANN_EINVAL, "the arrays must be one and the same or lie apart");
+  }
+  a.in = static_cast<const char*>(in_dev);
+  a.out = static_cast<char*>(out_dev);
+  a.parents = parents_dev;
+  a.outer = outer;
+  a.outer_in = outer_in;
+  a.outer_out = outer_out;
+  a.groups = groups;
+  a.row_in = row_in;
+  a.row_out = row_out;
+  a.beams = beams;
+  a.k = k;
+  a.mid = (u32)mid;
+  a.mid_in = mid_in;
+  a.mid_out = mid_out;
+  // the widest piece that all of it is a multiple of
+  u64 bits = from | to | run_bytes;
+  if (outer > 1) bits |= outer_in | outer_out;
+  if (groups * beams > 1) bits |= row_in;
+  if (groups * k > 1) bits |= row_out;
+  if (mid > 1) bits |= mid_in | mid_out;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (bits % 16 == 0)
+    HIP_TRY(launch_reorder<16>(a, run_bytes, st));
+  else if (bits % 4 == 0)
+    HIP_TRY(launch_reorder<4>(a, run_bytes, st));
+  else
+    HIP_TRY(launch_reorder<1>(a, run_bytes, st));
+  return ANN_OK;
+} catch (...) {
+  return annmi::on_exception();
+}
+
+}  // extern "C"
