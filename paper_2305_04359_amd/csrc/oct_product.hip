@@ -213,144 +213,345 @@ hipError_t launch_direct(const OctProductArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-// Many rows: 32 WF x 32 XF results a workgroup of four waves, 16 WF x 16 XF a wave.  Steps pass through LDS, two at a
-// time: while one is multiplied the next is on its way, from memory to LDS without registers between.  In LDS the eight
-// pieces of 16 bytes of a row's step change places by the row's number, so that eight lanes that read the same piece of
-// neighbouring rows meet all banks.
-constexpr u32 TILE_THREADS = 256;
+// Many rows of both sides.  Steps pass through LDS by halves (64 elements), from memory to LDS without registers between;
+// a wave takes 32 rows by 32 rows at once.  In LDS the four pieces of 16 bytes of a row's half change places by the row's
+// number, so that lanes that read the same piece of neighbouring rows meet all banks.
+constexpr u32 HALF = 64;
+using v16f = float __attribute__((ext_vector_type(16)));
+
+// 32 WF x 32 XF results of a wave: a half's fragments, and what is made of them.  Lane l holds row l & 31 of each side and
+// pieces l >> 5 and two on; its results are column (x) l & 31 and rows (w) 4 (l >> 5) and the three after of every eight.
 template <int WF, int XF>
-constexpr u32 tile_lds() {
-  constexpr u32 stages = 2 * (32 * WF + 32 * XF) * OCT_STEP, room = 4 * oct_room<WF>();
-  return stages > room ? stages : room;
-}
-
-template <int WF, int XF, bool CODED>
-__global__ __launch_bounds__(TILE_THREADS) void oct_product_tile_kernel(OctProductArgs a, u32 tiles_w, u32 tiles) {
-  constexpr u32 BW = 32 * WF, BX = 32 * XF, STAGE = (BW + BX) * OCT_STEP;
-  extern __shared__ __align__(1024) char lds[];
-  const u32 tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  // Chiplets take workgroups in turn: each gets a run of tiles that share rows.
-  const u32 per = (tiles + 7) / 8, t = blockIdx.x % 8 * per + blockIdx.x / 8;
-  if (t >= tiles) return;
-  const u32 tiles_x = tiles / tiles_w;
-  const u64 w0 = (u64)(t / tiles_x) * BW, x0 = (u64)(t % tiles_x) * BX;
-  const u32 ww = wave % 2 * (16 * WF), wx = wave / 2 * (16 * XF);  // the wave's part of the tile
-  const u32 steps = a.w.steps, words = oct_words(steps);
-  const uint8_t* side_codes[2] = {a.w.codes + w0 * steps * OCT_STEP, a.x.codes + x0 * steps * OCT_STEP};
-  const u32 last_row[2] = {(u32)min((u64)BW, a.w.n - w0) - 1, (u32)min((u64)BX, a.x.n - x0) - 1};
-
-  // What a wave brings to LDS: eight rows of a step at once, 16 bytes a lane.  Rows past the last are read as the last one:
-  // their results go nowhere.
-  u32 offset_w[WF], offset_x[XF];
-  const u32 piece = (lane % 8 ^ lane / 8) * 16;
-#pragma unroll
-  for (int i = 0; i < WF; ++i) offset_w[i] = min((wave + 4 * i) * 8 + lane / 8, last_row[0]) * steps * OCT_STEP + piece;
-#pragma unroll
-  for (int i = 0; i < XF; ++i) offset_x[i] = min((wave + 4 * i) * 8 + lane / 8, last_row[1]) * steps * OCT_STEP + piece;
-  auto fetch = [&](u32 s) {
-    char* stage = lds + s % 2 * STAGE;
-    typedef __attribute__((address_space(1))) const void* From;
-    typedef __attribute__((address_space(3))) void* To;
+struct Wave32 {
+  v8i w[WF], x[XF];
+  v16f acc[WF][XF];
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < WF; ++i)
-      __builtin_amdgcn_global_load_lds((From)(side_codes[0] + (u64)s * OCT_STEP + offset_w[i]), (To)(stage + (wave + 4 * i) * 1024), 16, 0, 0);
 #pragma unroll
-    for (int i = 0; i < XF; ++i)
-      __builtin_amdgcn_global_load_lds((From)(side_codes[1] + (u64)s * OCT_STEP + offset_x[i]), (To)(stage + BW * OCT_STEP + (wave + 4 * i) * 1024), 16, 0, 0);
-  };
-  const u32* sw[WF];
-  const u32* sx[XF];
+      for (int j = 0; j < XF; ++j) acc[i][j] = v16f{};
+  }
+  static __device__ __forceinline__ v8i fragment(const char* rows) {
+    const u32 lane = threadIdx.x % 64, at = lane % 32 * HALF + (lane / 32 ^ lane / 2 % 4) * 16;
+    return __builtin_shufflevector(*reinterpret_cast<const v4i*>(rows + at), *reinterpret_cast<const v4i*>(rows + (at ^ 32)), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  __device__ __forceinline__ void read(const char* wrows, const char* xrows) {
 #pragma unroll
-  for (int i = 0; i < WF; ++i) sw[i] = a.w.scales + min(w0 + ww + 16 * i + lane % 16, (u64)a.w.n - 1) * words;
+    for (int j = 0; j < XF; ++j) x[j] = fragment(xrows + 32 * j * HALF);
 #pragma unroll
-  for (int j = 0; j < XF; ++j) sx[j] = a.x.scales + min(x0 + wx + 16 * j + lane % 16, (u64)a.x.n - 1) * words;
-  u32 scale_w[WF], scale_x[XF];
-  v4f acc[WF][XF] = {};
-  fetch(0);
-  for (u32 s = 0; s < steps; ++s) {
-    if (s % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < WF; ++i) scale_w[i] = sw[i][s / 4];
-#pragma unroll
-      for (int j = 0; j < XF; ++j) scale_x[j] = sx[j][s / 4];
-    }
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the step's codes are in LDS
-    __syncthreads();
-    if (s + 1 < steps) fetch(s + 1);
-    const char* stage = lds + s % 2 * STAGE;
-    const u32 at = (lane / 16 ^ lane % 8) * 16 + lane % 16 * OCT_STEP;  // (the second half's piece: four on)
-    Codes x[XF];
-#pragma unroll
-    for (int j = 0; j < XF; ++j) {
-      const char* from = stage + (BW + wx + 16 * j) * OCT_STEP;
-      x[j].low = *reinterpret_cast<const v4i*>(from + at);
-      x[j].high = *reinterpret_cast<const v4i*>(from + (at ^ 64));
-    }
+    for (int i = 0; i < WF; ++i) w[i] = fragment(wrows + 32 * i * HALF);
+  }
+  // BYTE: the step's byte of the scale words
+  template <bool CODED, int BYTE>
+  __device__ __forceinline__ void multiply(const u32 (&ws)[WF], const u32 (&xs)[XF]) {
     if constexpr (CODED) {
 #pragma unroll
-      for (int i = 0; i < WF; ++i) {
-        const char* from = stage + (ww + 16 * i) * OCT_STEP;
-        const Codes w = {*reinterpret_cast<const v4i*>(from + at), *reinterpret_cast<const v4i*>(from + (at ^ 64))};
+      for (int i = 0; i < WF; ++i)
 #pragma unroll
-        for (int j = 0; j < XF; ++j) acc[i][j] = coded_mfma(w, x[j], acc[i][j], scale_w[i], scale_x[j]);
-      }
+        for (int j = 0; j < XF; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[i], x[j], acc[i][j], 0, 0, BYTE, (int)ws[i], BYTE, (int)xs[j]);
     } else {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         v8bf xv[XF];
 #pragma unroll
-        for (int j = 0; j < XF; ++j) xv[j] = oct_quarter(x[j], c, scale_x[j] & 255);
+        for (int j = 0; j < XF; ++j) xv[j] = oct_bf16((u32)x[j][2 * c], (u32)x[j][2 * c + 1], xs[j] >> (8 * BYTE) & 255);
 #pragma unroll
         for (int i = 0; i < WF; ++i) {
-          using v2i = int __attribute__((ext_vector_type(2)));
-          const v2i w = *reinterpret_cast<const v2i*>(stage + (ww + 16 * i) * OCT_STEP + (c < 2 ? at : at ^ 64) + c % 2 * 8);
-          const v8bf wv = oct_bf16((u32)w[0], (u32)w[1], scale_w[i] & 255);
+          const v8bf wv = oct_bf16((u32)w[i][2 * c], (u32)w[i][2 * c + 1], ws[i] >> (8 * BYTE) & 255);
 #pragma unroll
-          for (int j = 0; j < XF; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[j], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < XF; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv[j], acc[i][j], 0, 0, 0);
         }
       }
     }
+    // (or the compiler would gather the products of several halves behind the last one's reads)
 #pragma unroll
-    for (int i = 0; i < WF; ++i) scale_w[i] >>= 8;
+    for (int i = 0; i < WF; ++i)
 #pragma unroll
-    for (int j = 0; j < XF; ++j) scale_x[j] >>= 8;
+      for (int j = 0; j < XF; ++j) asm volatile("" : "+v"(acc[i][j]));
   }
-  __syncthreads();
-  if (w0 + ww < a.w.n) oct_store<WF, XF>(a, acc, w0 + ww, x0 + wx, lds + wave * oct_room<WF>());
+  // Results to memory, through LDS of the wave's own: 32 rows of `out` by all the wave's columns at once, so that stores
+  // fill lines, and neighbouring ones, wherever a row of `out` begins.  (128 bytes of a row at once: 4,096 x 65,536 of 2,048
+  // to bf16 639 us, 256 bytes 600.)  Pieces of 16 bytes change places by the row's number there.
+  template <typename OUT>
+  __device__ __forceinline__ void store(const OctProductArgs& a, u64 w0, u64 x0, char* room) const {
+    constexpr u32 ROW = 32 * WF * sizeof(OUT), PIECES = ROW / 16, AT_ONCE = 64 / PIECES;  // bytes; rows a store
+    constexpr u32 E = 16 / sizeof(OUT);
+    const u32 lane = threadIdx.x % 64;
+#pragma unroll
+    for (int j = 0; j < XF; ++j) {
+      wave_exchange();
+#pragma unroll
+      for (int i = 0; i < WF; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          Pack<OUT, 4> p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p.v[e] = mx_round<OUT>(acc[i][j][4 * q + e]);
+          const u32 byte = (32 * i + 8 * q + lane / 32 * 4) * sizeof(OUT);
+          *reinterpret_cast<Pack<OUT, 4>*>(room + lane % 32 * ROW + ((byte / 16 ^ lane % 8) * 16 | byte % 16)) = p;
+        }
+      wave_exchange();
+      OUT* out = reinterpret_cast<OUT*>(a.out) + (x0 + 32 * j) * a.ldo + w0;
+      const u32 xs = x0 + 32 * j < a.x.n ? (u32)min((u64)32, a.x.n - (x0 + 32 * j)) : 0;
+      if (w0 + 32 * WF <= a.w.n) {
+#pragma unroll
+        for (u32 k = 0; k < 32; k += AT_ONCE) {
+          const u32 r = k + lane / PIECES, piece = lane % PIECES;
+          const v4i p = *reinterpret_cast<const v4i*>(room + r * ROW + (piece ^ r % 8) * 16);
+          if (r < xs) __builtin_memcpy(out + r * a.ldo + piece * E, &p, 16);
+        }
+      } else {  // the last columns
+        const u32 ws = w0 < a.w.n ? (u32)(a.w.n - w0) : 0;
+#pragma unroll 1
+        for (u32 at = lane; at < 32 * 32 * WF; at += 64) {
+          const u32 r = at / (32 * WF), c = at % (32 * WF), byte = c * sizeof(OUT);
+          const OUT v = *reinterpret_cast<const OUT*>(room + r * ROW + ((byte / 16 ^ r % 8) * 16 | byte % 16));
+          if (r < xs && c < ws) out[r * a.ldo + c] = v;
+        }
+      }
+    }
+  }
+  static constexpr u32 ROOM = 32 * 32 * WF * 4;  // bytes that this takes at most
+  __device__ __forceinline__ void store(const OctProductArgs& a, u64 w0, u64 x0, char* room) const {
+    if (a.odtype == ANN_F32)
+      store<float>(a, w0, x0, room);
+    else if (a.odtype == ANN_F16)
+      store<__half>(a, w0, x0, room);
+    else
+      store<__bf16>(a, w0, x0, room);
+  }
+};
+
+// One side's rows of a tile as the WAVES waves of a workgroup bring them to LDS, 16 rows at a time a wave, 16 bytes a
+// lane.  Rows past the last are read as the last one: their results go nowhere.
+template <int ROWS, int WAVES>
+struct Side {
+  static constexpr int LOADS = ROWS / (16 * WAVES);
+  const uint8_t* codes;
+  const u32* scales;
+  u32 last;  // row
+  u32 offset[LOADS];
+  __device__ __forceinline__ void set(const OctRows& m, u64 row0) {
+    const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    codes = m.codes + row0 * m.steps * OCT_STEP;
+    scales = m.scales + row0 * oct_words(m.steps);
+    last = (u32)min((u64)ROWS, m.n - row0) - 1;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      offset[i] = min((wave + WAVES * i) * 16 + lane / 4, last) * m.steps * OCT_STEP + (lane % 4 ^ lane / 8 % 4) * 16;
+  }
+  __device__ __forceinline__ void fetch(u32 half, char* to) const {
+    typedef __attribute__((address_space(1))) const void* From;
+    typedef __attribute__((address_space(3))) void* To;
+    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      __builtin_amdgcn_global_load_lds((From)(codes + (u64)half * HALF + offset[i]), (To)(to + (wave + WAVES * i) * 1024), 16, 0, 0);
+  }
+  // scale words of the rows of N fragments from `row` of the tile on
+  template <int N>
+  __device__ __forceinline__ void fetch_scales(u32 (&to)[N], u32 row, u32 word, u32 words) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = scales[min(row + 32 * i + threadIdx.x % 32, last) * words + word];
+  }
+};
+
+// The tile of a workgroup.  Chiplets take workgroups in turn: each gets a run of tiles.  A run goes through eight tiles' rows
+// of x for one tile's rows of w before it takes the next rows of w, so that both stay in the chiplet's cache.
+struct TileAt {
+  u64 w, x;
+};
+__device__ __forceinline__ TileAt tile_at(u32 t, u32 tiles_w, u32 tiles_x) {
+  const u32 size = 8 * tiles_w, group = t / size, first = group * 8, across = min(8u, tiles_x - first), in = t % size;
+  return {in / across, first + in % across};
 }
 
-template <int WF, int XF, bool CODED>
-hipError_t launch_tile(const OctProductArgs& a, hipStream_t s) {
-  constexpr u32 BW = 32 * WF, BX = 32 * XF, LDS = tile_lds<WF, XF>();
-  const auto kernel = oct_product_tile_kernel<WF, XF, CODED>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS);
+// BW x BX results a workgroup of four waves, 64 x 64 a wave: 128 x 128, or 256 x 64 for batches of few rows.  Two
+// workgroups and more a compute unit, one of which stores or waits while another multiplies.
+constexpr u32 SMALL = 128, NARROW_W = 256, NARROW_X = 64, SMALL_BUFFERS = 3;
+template <bool CODED, int BW, int BX>
+__global__ __launch_bounds__(256, 2) void oct_product_small_kernel(OctProductArgs a, u32 tiles_w, u32 tiles) {
+  static_assert(BW * BX == 4 * 64 * 64);
+  constexpr u32 BUFFER = (BW + BX) * HALF;
+  __shared__ __align__(1024) char lds[SMALL_BUFFERS * BUFFER];
+  const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const u32 per = (tiles + 7) / 8, t = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (t >= tiles) return;
+  const TileAt at = tile_at(t, tiles_w, tiles / tiles_w);
+  const u32 ww = wave % (BW / 64) * 64, wx = wave / (BW / 64) * 64;  // the wave's part of the tile
+  const u32 steps = a.w.steps, words = oct_words(steps), halves = 2 * steps;
+  Side<BW, 4> w;
+  Side<BX, 4> x;
+  w.set(a.w, at.w * BW);
+  x.set(a.x, at.x * BX);
+  constexpr int LOADS = w.LOADS + x.LOADS;
+  auto fetch = [&](u32 h) {  // (past the last half: the last one again, which nobody reads)
+    char* to = lds + h % SMALL_BUFFERS * BUFFER;
+    w.fetch(min(h, halves - 1), to);
+    x.fetch(min(h, halves - 1), to + BW * HALF);
+  };
+  Wave32<2, 2> v;
+  v.clear();
+  u32 ws[2], xs[2], next_w[2], next_x[2];
+  w.fetch_scales(ws, ww, 0, words);
+  x.fetch_scales(xs, wx, 0, words);
+  fetch(0);
+  fetch(1);
+  auto half = [&](u32 h, auto byte) {
+    // this wave's loads of the half are in LDS, and its reads of the half before are done; then so are all waves'
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+    fetch(h + 2);
+    const char* rows = lds + h % SMALL_BUFFERS * BUFFER;
+    v.read(rows + ww * HALF, rows + (BW + wx) * HALF);
+    v.template multiply<CODED, byte>(ws, xs);
+  };
+  u32 h = 0;
+  for (; h + 8 <= halves; h += 8) {
+    w.fetch_scales(next_w, ww, min(h / 8 + 1, words - 1), words);
+    x.fetch_scales(next_x, wx, min(h / 8 + 1, words - 1), words);
+    half(h, std::integral_constant<int, 0>());
+    half(h + 1, std::integral_constant<int, 0>());
+    half(h + 2, std::integral_constant<int, 1>());
+    half(h + 3, std::integral_constant<int, 1>());
+    half(h + 4, std::integral_constant<int, 2>());
+    half(h + 5, std::integral_constant<int, 2>());
+    half(h + 6, std::integral_constant<int, 3>());
+    half(h + 7, std::integral_constant<int, 3>());
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ws[i] = next_w[i], xs[i] = next_x[i];
+  }
+  for (; h < halves; h += 2) {
+    half(h, std::integral_constant<int, 0>());
+    half(h + 1, std::integral_constant<int, 0>());
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ws[i] >>= 8, xs[i] >>= 8;
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  v.store(a, at.w * BW + ww, at.x * BX + wx, lds + wave * v.ROOM);
+}
+
+// 256 x 256 results a workgroup of eight waves, 128 x 64 a wave, two waves a SIMD, in two teams: while one team's
+// waves multiply a half the other's read theirs from LDS and ask for the half three on.
+constexpr u32 LARGE = 256, LARGE_BUFFERS = 4;
+constexpr u32 LARGE_LDS = LARGE_BUFFERS * 2 * LARGE * HALF;
+template <bool CODED>
+__global__ __launch_bounds__(512) void oct_product_large_kernel(OctProductArgs a, u32 tiles_w, u32 tiles) {
+  constexpr u32 BUFFER = 2 * LARGE * HALF;
+  extern __shared__ __align__(1024) char lds[];
+  const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const u32 per = (tiles + 7) / 8, t = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (t >= tiles) return;
+  const TileAt at = tile_at(t, tiles_w, tiles / tiles_w);
+  const u32 ww = wave % 2 * 128, wx = wave / 2 * 64;  // the wave's part of the tile
+  const bool late = wave >= 4;                        // the second team
+  const u32 steps = a.w.steps, words = oct_words(steps), halves = 2 * steps;
+  Side<LARGE, 8> w, x;
+  w.set(a.w, at.w * LARGE);
+  x.set(a.x, at.x * LARGE);
+  constexpr int LOADS = 2 * Side<LARGE, 8>::LOADS;
+  auto fetch = [&](u32 h) {  // (past the last half: the last one again, which nobody reads)
+    char* to = lds + h % LARGE_BUFFERS * BUFFER;
+    w.fetch(min(h, halves - 1), to);
+    x.fetch(min(h, halves - 1), to + LARGE * HALF);
+  };
+  Wave32<4, 2> v;
+  v.clear();
+  u32 ws[4], xs[2], next_w[4], next_x[2];
+  w.fetch_scales(ws, ww, 0, words);
+  x.fetch_scales(xs, wx, 0, words);
+  fetch(0);
+  fetch(1);
+  fetch(2);
+  // This wave's loads but those of the last two halves are in LDS, and its reads are done; then so are the others'.  The
+  // half that is read behind it was asked for three halves ago.
+  auto turn = [&]() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory"); };
+  auto half = [&](u32 h, auto byte) {
+    const char* rows = lds + h % LARGE_BUFFERS * BUFFER;
+    v.read(rows + ww * HALF, rows + (LARGE + wx) * HALF);
+    fetch(h + 3);  // (where the half before was: both teams have read it)
+    turn();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+    v.template multiply<CODED, byte>(ws, xs);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    turn();
+  };
+  turn();
+  if (late) asm volatile("s_barrier" ::: "memory");  // half a turn behind, from here to the end
+  u32 h = 0;
+  for (; h + 8 <= halves; h += 8) {
+    w.fetch_scales(next_w, ww, min(h / 8 + 1, words - 1), words);
+    x.fetch_scales(next_x, wx, min(h / 8 + 1, words - 1), words);
+    half(h, std::integral_constant<int, 0>());
+    half(h + 1, std::integral_constant<int, 0>());
+    half(h + 2, std::integral_constant<int, 1>());
+    half(h + 3, std::integral_constant<int, 1>());
+    half(h + 4, std::integral_constant<int, 2>());
+    half(h + 5, std::integral_constant<int, 2>());
+    half(h + 6, std::integral_constant<int, 3>());
+    half(h + 7, std::integral_constant<int, 3>());
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ws[i] = next_w[i];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) xs[j] = next_x[j];
+  }
+  for (; h < halves; h += 2) {
+    half(h, std::integral_constant<int, 0>());
+    half(h + 1, std::integral_constant<int, 0>());
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ws[i] >>= 8;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) xs[j] >>= 8;
+  }
+  if (!late) asm volatile("s_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");  // (no load is on its way to where results pass)
+  v.store(a, at.w * LARGE + ww, at.x * LARGE + wx, lds + wave * v.ROOM);
+}
+
+template <bool CODED>
+hipError_t launch_large(const OctProductArgs& a, hipStream_t s) {
+  const auto kernel = oct_product_large_kernel<CODED>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LARGE_LDS);
   if (e != hipSuccess) return e;
+  const u32 tiles_w = (u32)(((u64)a.w.n + LARGE - 1) / LARGE), tiles = tiles_w * (u32)(((u64)a.x.n + LARGE - 1) / LARGE);
+  hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(512), LARGE_LDS, s, a, tiles_w, tiles);
+  return hipGetLastError();
+}
+template <bool CODED, int BW, int BX>
+hipError_t launch_small(const OctProductArgs& a, hipStream_t s) {
   const u32 tiles_w = (u32)(((u64)a.w.n + BW - 1) / BW);
+  // (launches are counted in threads of 32 bits: long batches go in parts)
   u64 part = (1ull << 23) / tiles_w * BX;
   if (part == 0) part = BX;
   for (u64 at = 0; at < a.x.n; at += part) {
     const OctProductArgs b = rows_from(a, at, part);
     const u32 tiles = tiles_w * (u32)(((u64)b.x.n + BX - 1) / BX);
-    hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(TILE_THREADS), LDS, s, b, tiles_w, tiles);
-    const hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL((oct_product_small_kernel<CODED, BW, BX>), dim3((tiles + 7) / 8 * 8), dim3(256), 0, s, b, tiles_w, tiles);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-template <int WF, int XF>
-hipError_t launch_direct(const OctProductArgs& a, hipStream_t s) {
-  const u64 tiles = (((u64)a.w.n + 16 * WF - 1) / (16 * WF)) * (((u64)a.x.n + 16 * XF - 1) / (16 * XF));
-  return a.w.steps >= 8 && tiles < 1024 ? launch_direct<WF, XF, 8>(a, s) : launch_direct<WF, XF, 1>(a, s);
+template <bool CODED>
+hipError_t launch_tiles(const OctProductArgs& a, hipStream_t s) {
+  if (a.x.n <= NARROW_X) return launch_small<CODED, NARROW_W, NARROW_X>(a, s);
+  // By what a turn of workgroups over the chip takes: 256 large tiles, 256 small ones or twice as many.
+  const u64 large = (((u64)a.w.n + LARGE - 1) / LARGE) * (((u64)a.x.n + LARGE - 1) / LARGE);
+  const u64 small = (((u64)a.w.n + SMALL - 1) / SMALL) * (((u64)a.x.n + SMALL - 1) / SMALL);
+  const u64 cost_large = (large + 255) / 256 * 64, cost_small = small / 512 * 45 + (small % 512 == 0 ? 0 : small % 512 <= 256 ? 25 : 45);
+  if (a.w.steps >= 4 && large < 1u << 22 && cost_large <= cost_small) return launch_large<CODED>(a, s);
+  return launch_small<CODED, SMALL, SMALL>(a, s);
 }
 
 hipError_t launch_oct_product(const OctProductArgs& a, hipStream_t s) {
-  if (a.x.n <= 16) return launch_direct<2, 1>(a, s);
-  if (a.x.n <= 32) return launch_direct<2, 2>(a, s);
-  if (a.x.n <= 48) return launch_direct<2, 3>(a, s);
-  if (a.x.n <= 64) return launch_direct<4, 4>(a, s);
-  const bool coded = a.odtype != ANN_F32;
-  return coded ? launch_tile<4, 4, true>(a, s) : launch_tile<4, 4, false>(a, s);
+  const u64 tiles = (((u64)a.w.n + 31) / 32) * (((u64)a.x.n + 31) / 32);
+  if (a.x.n <= 16) return a.w.steps >= 8 && tiles < 1024 ? launch_direct<2, 1, 8>(a, s) : launch_direct<2, 1, 1>(a, s);
+  if (tiles <= 640) return launch_direct<2, 2, 8>(a, s);
+  // (results of 16 bits round far more coarsely than the codes' products are cut)
+  return a.odtype == ANN_F32 ? launch_tiles<false>(a, s) : launch_tiles<true>(a, s);
 }
 
 }  // namespace annmi

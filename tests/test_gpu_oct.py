@@ -84,47 +84,59 @@ def test_quantize_edges(env, columns):
     assert torch.equal(back.isnan(), torch.from_numpy(np.isnan(P.values(*want, 130))))
 
 
-def product_bound(xv, wv, out):
+def product_bound(torch, xv, wv, out):
     """Sums in fp32: each of the d additions is off by at most a step of what the sum of magnitudes allows.  Where the matrix
-    instruction takes the codes (results of 16 bits, batches above 64) it drops, of eight neighbouring products, what
+    instruction takes the codes (results of 16 bits, batches above 16) it drops, of eight neighbouring products, what
     lies below 2^(E - 13), E the largest one's exponent, of up to seven of them.  Then one rounding to the output's type."""
     d = xv.shape[1]
-    bound = d * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T)
-    if out != "float32" and len(xv) > 64:
+    x, w = xv.abs(), wv.abs()
+    bound = d * 2.0 ** -23 * (x @ w.T)
+    if out != "float32" and len(xv) > 16:
         for e in range(0, d, 8):
-            best = 0.0
-            for k in range(e, min(e + 8, d)):
-                best = np.maximum(best, np.abs(np.outer(xv[:, k], wv[:, k])))
+            best = x[:, e, None] * w[None, :, e]
+            for k in range(e + 1, min(e + 8, d)):
+                best = torch.maximum(best, x[:, k, None] * w[None, :, k])
             bound += 7 * 2.0 ** -13 * best
-    return bound, HALF[out]
+    return bound
 
 
-def check_product(torch, A, x, w, out="float32", pad=0):
-    xv = P.values(x.codes.cpu().numpy(), x.scales.cpu().numpy(), x.d)
-    wv = P.values(w.codes.cpu().numpy(), w.scales.cpu().numpy(), w.d)
+def values_of(torch, rows):
+    return dev(torch, P.values(rows.codes.cpu().numpy(), rows.scales.cpu().numpy(), rows.d))
+
+
+def check_product(torch, A, x, w, out="float32", pad=0, known=None):
+    xv, wv = values_of(torch, x), values_of(torch, w)
     want = xv @ wv.T
     room = wider(torch, torch.zeros(want.shape, dtype=getattr(torch, out), device="cuda"), pad) if pad else None
     got = A.ann_oct_product(x, w, dtype=None if pad else getattr(torch, out), out=room)
-    sums, half = product_bound(xv, wv, out)
-    off = np.abs(got.double().cpu().numpy() - want)
-    assert (off <= sums + half * (np.abs(want) + sums) + SMALLEST[out]).all(), (off.max(), np.abs(want).max())
+    sums = product_bound(torch, xv, wv, out) if known is None else known
+    off = (got.double() - want).abs()
+    assert (off <= sums + HALF[out] * (want.abs() + sums) + SMALLEST[out]).all(), (off.max().item(), want.abs().max().item())
     if pad:
         side = room._base.clone()
         side[:, pad // 2:pad // 2 + want.shape[1]] = 77
         assert (side == 77).all(), "elements beside the results changed"
-    return got
+    return sums
 
 
+# (few rows; few tiles; narrow, small and large tiles: whole ones, ends of both sides, one step and more than whole words)
 @pytest.mark.parametrize("out", ("float32", "float16", "bfloat16"))
 @pytest.mark.parametrize("nx,n,d", [(1, 1, 1), (1, 5000, 128), (2, 3, 130), (16, 64, 512), (17, 33, 640), (33, 1001, 200), (64, 500, 1000), (65, 129, 384),
-                                    (130, 70, 4097), (5, 16, 20_000), (257, 300, 96), (400, 1030, 257), (1, 40, 70_000)])
+                                    (130, 70, 4097), (5, 16, 20_000), (257, 300, 96), (400, 1030, 257), (1, 40, 70_000), (7, 40_000, 700),
+                                    (33, 10_300, 140), (64, 12_001, 96), (18, 20_500, 1500), (130, 5003, 257), (200, 8192, 1030), (129, 6000, 96),
+                                    (2100, 4000, 513), (2048, 4096, 1030), (2047, 4101, 1536)])
 def test_product(env, out, nx, n, d):
     torch, A, _ = env
     rng = np.random.default_rng(nx * n + d)
     x, w = (dev(torch, (0.3 * rng.standard_normal((r, d)) * np.exp2(rng.integers(-2, 3, (r, 1)))).astype(np.float32)) for r in (nx, n))
+    # scales of their own for every step
+    for t in (x, w):
+        for e in range(0, d, 128):
+            t[:, e:e + 128] *= 2.0 ** int(rng.integers(-3, 4))
     x, w = A.ann_oct_quantize(x), A.ann_oct_quantize(w)
+    known = None
     for pad in (0, 7, 8):
-        check_product(torch, A, x, w, out, pad)
+        known = check_product(torch, A, x, w, out, pad, known)
 
 
 def test_product_of_every_code(env):
@@ -145,6 +157,12 @@ def test_product_of_every_code(env):
     got = A.ann_oct_product(xo, wo).double().cpu().numpy()
     want = P.values(x, scales, d) @ P.values(w, scales[::-1], d).T
     assert (got == want).all()  # one product each: exact
+    # the same in every place of a step, by tiles: rows enough for the codes themselves to be multiplied
+    reps = 16
+    xo, wo = (A.OctRows(o.codes.repeat(reps, 1), o.scales.repeat(reps, 1), d) for o in (xo, wo))
+    for t in (torch.float32, torch.bfloat16):
+        got = A.ann_oct_product(xo, wo, dtype=t)
+        assert torch.equal(got, dev(torch, want).to(t).repeat(reps, reps)), t
 
 
 def test_not_a_number(env):
