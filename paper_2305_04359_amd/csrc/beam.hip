@@ -13,8 +13,8 @@ namespace annmi {
 constexpr u32 BEAM_MOST_BEAMS = 64;
 constexpr u32 BEAM_MOST_K = 128;
 constexpr u32 BEAM_MOST_N = (1u << 24) - 1;  // an id, a score and a beam fit in one key of 64 bits
-constexpr u32 BEAM_THREADS = 256;
-constexpr u32 BEAM_EACH = 16;  // entries of a thread
+constexpr u32 BEAM_THREADS = 512;
+constexpr u32 BEAM_EACH = 8;  // entries of a thread
 constexpr u32 BEAM_CHUNK = BEAM_THREADS * BEAM_EACH;
 
 struct BeamArgs {
@@ -77,15 +77,40 @@ __device__ __forceinline__ void sort_down(u32 size, Swap swap) {
 }
 __device__ __forceinline__ u32 power_of_two(u32 v) { return v <= 1 ? 1 : 1u << (32 - __clz(v - 1)); }
 
-// One chunk of a row a workgroup, 16 entries a thread, which stay in registers.  The k-th best of the threads' best ones is
-// a bound: entries above it are at least k, and few more than that in most orders; they are listed and sorted.
+// The largest of a wave, the same in every lane.
+template <int CTRL>
+__device__ __forceinline__ u32 beam_row_max(u32 v) {
+  return max(v, (u32)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ u32 wave_largest(u32 v) {
+  v = beam_row_max<0xB1>(v);   // the neighbour
+  v = beam_row_max<0x4E>(v);   // two away
+  v = beam_row_max<0x124>(v);  // four and eight around in 16 lanes
+  v = beam_row_max<0x128>(v);
+  return max(max((u32)__builtin_amdgcn_readlane((int)v, 0), (u32)__builtin_amdgcn_readlane((int)v, 16)),
+             max((u32)__builtin_amdgcn_readlane((int)v, 32), (u32)__builtin_amdgcn_readlane((int)v, 48)));
+}
+// The m-th largest of a wave's values, and the largest.
+__device__ __forceinline__ u32 wave_mth(u32 v, u32 m, u32* first) {
+  u32 best = *first = wave_largest(v);
+  for (u32 i = 1; i < m && best; ++i) {
+    const u64 holds = __ballot(v == best);
+    if (threadIdx.x % 64 == (u32)__builtin_ctzll(holds)) v = 0;  // one of those that hold it
+    best = wave_largest(v);
+  }
+  return best;
+}
+
+// One chunk of a row a workgroup, eight entries a thread, which stay in registers.  Every wave finds the ceil(k / 8)-th best
+// of its threads' best ones; the least of these is a bound that k entries reach at least, and few more in most orders;
+// they are listed and brought into order.
 template <typename T>
 __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
-  constexpr u32 E = 16 / sizeof(T), PACKS = BEAM_EACH / E;
+  constexpr u32 E = BEAM_EACH, WAVES = BEAM_THREADS / 64;
   __shared__ u64 list[BEAM_CHUNK];
-  __shared__ __align__(16) u32 heads[BEAM_THREADS];
-  __shared__ double sums[BEAM_THREADS / 64];
-  __shared__ u32 bound, top, count;
+  __shared__ double sums[BEAM_THREADS];
+  __shared__ u32 bounds[WAVES], tops[WAVES], count;
+  const u32 wave = threadIdx.x / 64;
   const u64 tiles = a.groups * a.beams * a.chunks;
   for (u64 b = blockIdx.x; b < tiles; b += gridDim.x) {
     const u64 row = b / a.chunks;
@@ -94,17 +119,15 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
     const T* z = reinterpret_cast<const T*>(a.scores) + row * a.ld + from;
     float v[BEAM_EACH];
     u32 key[BEAM_EACH];
+    // (where a chunk is not full, all waves have some of it: a wave without entries gives no bound)
+    const u32 at = (there < BEAM_CHUNK ? threadIdx.x % 64 * WAVES + wave : threadIdx.x) * E;
+    if (at + E <= there) {
+      const AnyPack<T, E> in = *reinterpret_cast<const AnyPack<T, E>*>(z + at);
 #pragma unroll
-    for (u32 u = 0; u < PACKS; ++u) {
-      const u32 at = (threadIdx.x + BEAM_THREADS * u) * E;
-      if (at + E <= there) {
-        const AnyPack<T, E> in = *reinterpret_cast<const AnyPack<T, E>*>(z + at);
+      for (u32 e = 0; e < E; ++e) v[e] = mx_float(static_cast<T>(in.v[e]));
+    } else {
 #pragma unroll
-        for (u32 e = 0; e < E; ++e) v[u * E + e] = mx_float(static_cast<T>(in.v[e]));
-      } else {
-#pragma unroll
-        for (u32 e = 0; e < E; ++e) v[u * E + e] = at + e < there ? mx_float(z[min(at + e, there - 1)]) : -INFINITY;
-      }
+      for (u32 e = 0; e < E; ++e) v[e] = at + e < there ? mx_float(z[min(at + e, there - 1)]) : -INFINITY;
     }
     u32 head = 0;
 #pragma unroll
@@ -112,80 +135,118 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
       key[i] = v[i] > -INFINITY ? float_key(v[i]) : 0u;  // (not NaN either)
       head = max(head, key[i]);
     }
+    u32 first;
+    const u32 mth = wave_mth(head, (a.k + WAVES - 1) / WAVES, &first);
     __syncthreads();  // (the last turn's readers)
-    heads[threadIdx.x] = head;
-    if (threadIdx.x == 0) count = 0, bound = 0;
+    if (threadIdx.x % 64 == 0) bounds[wave] = mth, tops[wave] = first;
+    if (threadIdx.x == 0) count = 0;
     __syncthreads();
-    u32 rank = 0;
-#pragma unroll 8
-    for (u32 i = 0; i < BEAM_THREADS; i += 4) {
-      const v4i four = *reinterpret_cast<const v4i*>(heads + i);
+    u32 bound = bounds[0], top = tops[0];
 #pragma unroll
-      for (u32 e = 0; e < 4; ++e) rank += (u32)four[e] > head || ((u32)four[e] == head && i + e < threadIdx.x);
-    }
-    if (rank == a.k - 1) bound = head;
-    if (rank == 0) top = head;
-    __syncthreads();
+    for (u32 w = 1; w < WAVES; ++w) bound = min(bound, bounds[w]), top = max(top, tops[w]);
     const float most = key_float(top);
     if (top == 0) {  // nothing that is not masked
       if (threadIdx.x == 0) a.sums[b] = 0.0, a.most[b] = -INFINITY;
       for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = 0;
       continue;
     }
-    double sum = 0.0;
-#pragma unroll
-    for (u32 i = 0; i < BEAM_EACH; ++i)
-      if (key[i]) sum += beam_exp(beam_below(v[i], most));
 #pragma unroll
     for (u32 i = 0; i < BEAM_EACH; ++i)
       if (key[i] && key[i] >= bound) {
-        const u32 id = from + (threadIdx.x + BEAM_THREADS * (i / E)) * E + i % E;
-        list[atomicAdd(&count, 1u)] = (u64)key[i] << 32 | (u32)~id;  // (in any order: the keys differ, and are sorted)
+        const u32 id = from + at + i;
+        list[atomicAdd(&count, 1u)] = (u64)key[i] << 32 | (u32)~id;  // (in any order: the keys differ)
       }
+    double sum = 0.0;
 #pragma unroll
-    for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
-    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
+    for (u32 i = 0; i < BEAM_EACH; ++i) {
+      const double w = beam_exp(beam_below(v[i], most));
+      sum += key[i] ? w : 0.0;
+    }
+    sums[threadIdx.x] = sum;
     __syncthreads();
-    const u32 listed = count, size = power_of_two(max(listed, a.k));
-    for (u32 i = listed + threadIdx.x; i < size; i += BEAM_THREADS) list[i] = 0;
-    __syncthreads();
-    sort_down<BEAM_THREADS>(size, [&](u32 low, u32 high, bool down) {
-      const u64 x = list[low], y = list[high];
-      if ((x < y) == down) list[low] = y, list[high] = x;
-    });
-    for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = list[i];
-    if (threadIdx.x == 0) {
-      double all = sums[0];
-      for (u32 w = 1; w < BEAM_THREADS / 64; ++w) all += sums[w];
-      a.sums[b] = all;
-      a.most[b] = most;
+    const u32 listed = count;
+    if (wave == WAVES - 1) {  // (the first waves have the list)
+      const u32 lane = threadIdx.x % 64;
+      double all = 0.0;
+#pragma unroll
+      for (u32 i = 0; i < BEAM_THREADS / 64; ++i) all += sums[lane + 64 * i];
+#pragma unroll
+      for (int w = 1; w < 64; w *= 2) all += __shfl_xor(all, w);
+      if (lane == 0) a.sums[b] = all, a.most[b] = most;
+    }
+    if (listed <= BEAM_THREADS) {  // an entry's place is how many are larger
+      const u32 mine = threadIdx.x;
+      if (mine < listed) {
+        const u64 entry = list[mine];
+        u32 place = 0;
+#pragma unroll 8
+        for (u32 i = 0; i < listed; ++i) place += list[i] > entry;
+        if (place < a.k) a.best[b * a.k + place] = entry;
+      } else if (mine < a.k) {
+        a.best[b * a.k + mine] = 0;
+      }
+    } else {
+      const u32 size = power_of_two(listed);
+      for (u32 i = listed + threadIdx.x; i < size; i += BEAM_THREADS) list[i] = 0;
+      __syncthreads();
+      sort_down<BEAM_THREADS>(size, [&](u32 low, u32 high, bool down) {
+        const u64 x = list[low], y = list[high];
+        if ((x < y) == down) list[low] = y, list[high] = x;
+      });
+      for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = list[i];
     }
   }
 }
 
 // A group a workgroup: the beams' log sums, then the chunks' lists, first all their best ones, then all second ones, and so on,
-// a thousand at a time.  What is not better than the k-th so far is left out; when a thousand in a row, or all lists' next,
-// are, the rest is too.
+// a thousand at a time.  What is below a bound that k of the first thousand reach, or not better than the k-th so far, is
+// left out; when all lists' next ones are, the rest is too.
 constexpr u32 PICK_THREADS = 1024, PICK_ROOM = 2048;
 __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
+  constexpr u32 WAVES = PICK_THREADS / 64;
   // worth, as a key that is larger for more; and behind it beam, score and id
   __shared__ u64 worth[PICK_ROOM], tie[PICK_ROOM];
   __shared__ double logs[BEAM_MOST_BEAMS];
   __shared__ float mosts[BEAM_MOST_BEAMS], totals[BEAM_MOST_BEAMS];
   __shared__ u32 state[BEAM_MOST_BEAMS];  // 0: no continuation, 1: finished, 2: by its scores
-  __shared__ u32 count;
+  __shared__ u32 bounds[WAVES], count;
   const u32 lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   auto worth_key = [](double v) {
     const u64 bits = (u64)__double_as_longlong(v + 0.0);
     return bits >> 63 ? ~bits : bits | 1ull << 63;
   };
-  auto swap = [&](u32 low, u32 high, bool down) {
-    const u64 x = worth[low], y = worth[high], xt = tie[low], yt = tie[high];
-    if ((x < y || (x == y && xt < yt)) == down) worth[low] = y, worth[high] = x, tie[low] = yt, tie[high] = xt;
+  // Brings the list into order downwards, as far as the first k; what lies behind its end up to there becomes empty.
+  auto order = [&](u32 listed) {
+    const u32 mine = threadIdx.x;
+    if (listed <= PICK_THREADS) {  // an entry's place is how many are larger
+      u64 entry = 0, entry_tie = 0;
+      u32 place = mine;
+      if (mine < listed) {
+        entry = worth[mine];
+        entry_tie = tie[mine];
+        place = 0;
+#pragma unroll 8
+        for (u32 i = 0; i < listed; ++i) {
+          const u64 w = worth[i], t = tie[i];
+          place += (u32)(w > entry) | ((u32)(w == entry) & (u32)(t > entry_tie));
+        }
+      }
+      __syncthreads();
+      if (place < a.k) worth[place] = entry, tie[place] = entry_tie;
+      __syncthreads();
+      return;
+    }
+    const u32 size = power_of_two(listed);
+    for (u32 i = listed + mine; i < size; i += PICK_THREADS) worth[i] = 0, tie[i] = 0;
+    __syncthreads();
+    sort_down<PICK_THREADS>(size, [&](u32 low, u32 high, bool down) {
+      const u64 x = worth[low], y = worth[high], xt = tie[low], yt = tie[high];
+      if ((x < y || (x == y && xt < yt)) == down) worth[low] = y, worth[high] = x, tie[low] = yt, tie[high] = xt;
+    });
   };
   for (u64 g = blockIdx.x; g < a.groups; g += gridDim.x) {
     __syncthreads();  // (the last group's readers)
-    for (u32 b = wave; b < a.beams; b += PICK_THREADS / 64) {
+    for (u32 b = wave; b < a.beams; b += WAVES) {
       const u64 row = g * a.beams + b;
       const bool lives = beam_lives(a, row);
       float most = -INFINITY;
@@ -217,13 +278,12 @@ __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
       worth[at] = worth_key(totals[threadIdx.x]);
       tie[at] = (u64)(63 - threadIdx.x) << 56 | (u64)(0xFFFFFFu - a.pad);
     }
-    __syncthreads();
     const u32 lists = a.beams * a.chunks;
     const u64 all = (u64)lists * a.k;
     u64 least = 0, least_tie = 0;  // the k-th so far: others have to be better
     u32 since = 0;                 // entries in a row that were not
-    for (u64 first = 0; first < all && since < max(lists, 1u); first += PICK_THREADS) {
-      const u64 at = first + threadIdx.x;
+    for (u64 first = 0; first < all && since < lists; first += PICK_THREADS) {
+      const u64 at = first + lane * WAVES + wave;  // (so that every wave has some of the lists' best ones)
       u64 key = 0, key_tie = 0;
       if (at < all) {
         const u32 l = (u32)(at % lists), b = l / a.chunks;
@@ -239,7 +299,19 @@ __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
           }
         }
       }
-      const bool better = key > least || (key == least && key_tie > least_tie);
+      bool better = key > least || (key == least && key_tie > least_tie);
+      if (first == 0) {
+        // the upper halves of the keys: the least of the waves' ceil(k / 16)-th largest ones
+        u32 top;
+        const u32 mth = wave_mth((u32)(key >> 32), (a.k + WAVES - 1) / WAVES, &top);
+        if (lane == 0) bounds[wave] = mth;
+        __syncthreads();
+        u32 bound = bounds[0];
+#pragma unroll
+        for (u32 w = 1; w < WAVES; ++w) bound = min(bound, bounds[w]);
+        better = better && (u32)(key >> 32) >= bound;
+      }
+      __syncthreads();  // (the finished ones, or the last turn's list)
       const u32 before = count;
       __syncthreads();
       if (better) {
@@ -252,10 +324,7 @@ __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
       since = listed == before ? since + PICK_THREADS : 0;
       const bool last = first + PICK_THREADS >= all || since >= lists;
       if (first == 0 || last || listed + PICK_THREADS > PICK_ROOM) {
-        const u32 size = power_of_two(max(listed, a.k));
-        for (u32 i = listed + threadIdx.x; i < size; i += PICK_THREADS) worth[i] = 0, tie[i] = 0;
-        __syncthreads();
-        sort_down<PICK_THREADS>(size, swap);
+        order(listed);
         least = worth[a.k - 1];
         least_tie = tie[a.k - 1];
         if (threadIdx.x == 0) count = min(listed, a.k);
