@@ -50,6 +50,23 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b, float c) {
   return {m, a.s * soft_exp(a.m, to, c) + b.s * soft_exp(b.m, to, c)};
 }
 
+// 16 bytes wherever they begin.  Gradients go past the caches, and scores that are more than these hold (PAST) come past
+// them, so that they do not drive out what is needed.  Loss and gradient with scores read so, and not: 4,096 x 128,000 bf16 (1 GB)
+// 165 + 414 us and 227 + 426, 4,000 x 32,000 bf16 (256 MB) 44 + 99 and 54 + 85, 700 x 50,001 fp32 (140 MB) 26 + 66 and 25 + 48.
+// Gradients written the plain way: 1,500 x 50,001 fp32 133 us, 123 so.
+constexpr u64 DISTILL_PAST = 384ull << 20;
+using Streamed = v4i __attribute__((aligned(2)));
+template <bool PAST, int E, typename T>
+__device__ __forceinline__ AnyPack<T, E> stream_in(const T* from) {
+  static_assert(E * sizeof(T) == 16);
+  if constexpr (PAST) return __builtin_bit_cast(AnyPack<T, E>, v4i(__builtin_nontemporal_load(reinterpret_cast<const Streamed*>(from))));
+  return *reinterpret_cast<const AnyPack<T, E>*>(from);
+}
+template <int E, typename T>
+__device__ __forceinline__ void stream_out(T* to, const AnyPack<T, E>& v) {
+  __builtin_nontemporal_store(__builtin_bit_cast(v4i, v), reinterpret_cast<Streamed*>(to));
+}
+
 template <typename T>
 __device__ __forceinline__ float distill_float(const char* at, u64 i) {
   return mx_float(reinterpret_cast<const T*>(at)[i]);
@@ -59,7 +76,7 @@ __device__ __forceinline__ float teacher_at(const DistillArgs& a, u64 i) {
 }
 
 // What a thread sees of entries [from, to) of a row: every 256th pack of 16 bytes, four at a time.
-template <typename T>
+template <bool PAST, typename T>
 __device__ __forceinline__ Soft soft_scan(const T* z, u32 from, u32 to, float c) {
   constexpr u32 E = 16 / sizeof(T), AHEAD = 4;
   Soft mine = {-INFINITY, 0.0f};
@@ -77,7 +94,7 @@ __device__ __forceinline__ Soft soft_scan(const T* z, u32 from, u32 to, float c)
 #pragma unroll
     for (u32 u = 0; u < AHEAD; ++u) {
       const u32 at = p + DISTILL_THREADS * u;
-      const AnyPack<T, E> in = *reinterpret_cast<const AnyPack<T, E>*>(z + from + (u64)min(at, packs - 1) * E);
+      const AnyPack<T, E> in = stream_in<PAST, E>(z + from + (u64)min(at, packs - 1) * E);
 #pragma unroll
       for (u32 e = 0; e < E; ++e) v[u * E + e] = at < packs ? mx_float(static_cast<T>(in.v[e])) : -INFINITY;
     }
@@ -133,34 +150,29 @@ struct DistillRoom {
   float most[4];
 };
 
+// the teacher's j-th score of a row, -inf where its entry is not there; and the entry
+__device__ __forceinline__ float teacher_entry(const DistillArgs& a, u64 row, u32 j, u32* id) {
+  *id = a.ids[row * a.k + j];
+  return *id < a.n ? teacher_at(a, row * a.k + j) : -INFINITY;
+}
+
 // A row's loss from its m and S, by a workgroup.
 template <typename T>
 __device__ __forceinline__ void distill_finish(const DistillArgs& a, u64 row, Soft all, DistillRoom& room) {
-  constexpr u32 PER = DISTILL_MOST_K / DISTILL_THREADS;
   const T* z = reinterpret_cast<const T*>(a.scores) + row * a.ld;
-  float t[PER], zt[PER];
+  u32 id;
   float most = -INFINITY;
-#pragma unroll
-  for (u32 u = 0; u < PER; ++u) {
-    const u32 j = threadIdx.x + DISTILL_THREADS * u;
-    t[u] = -INFINITY;
-    if (j < a.k) {
-      const u32 id = a.ids[row * a.k + j];
-      if (id < a.n) {
-        t[u] = teacher_at(a, row * a.k + j);
-        zt[u] = mx_float(z[id]);
-      }
-    }
-    most = __builtin_fmaxf(most, t[u]);
-  }
+#pragma unroll 1
+  for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) most = __builtin_fmaxf(most, teacher_entry(a, row, j, &id));
   most = block_max(most, room.most);
   double weights = 0.0, terms = 0.0;
-#pragma unroll
-  for (u32 u = 0; u < PER; ++u) {
-    if (t[u] == -INFINITY) continue;
-    const double off = ((double)t[u] - most) / a.t, w = exp(off);
+#pragma unroll 1
+  for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {
+    const float t = teacher_entry(a, row, j, &id);
+    if (t == -INFINITY) continue;
+    const double off = ((double)t - most) / a.t, w = exp(off);
     weights += w;
-    if (!(w == 0.0)) terms += w * (off - ((double)zt[u] - all.m) / a.t);
+    if (!(w == 0.0)) terms += w * (off - ((double)mx_float(z[id]) - all.m) / a.t);
   }
   weights = block_sum(weights, room.sums);
   terms = block_sum(terms, room.sums);
@@ -174,14 +186,14 @@ __device__ __forceinline__ void distill_finish(const DistillArgs& a, u64 row, So
 }
 
 // Rows by a workgroup each, or by one for each of their chunks, which leaves its part's m and S.
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool PAST>
 __global__ __launch_bounds__(DISTILL_THREADS) void distill_scan_kernel(DistillArgs a) {
   __shared__ DistillRoom room;
   for (u64 b = blockIdx.x; b < a.rows * a.chunks; b += gridDim.x) {
     const u64 row = WHOLE ? b : b / a.chunks;
     const u32 part = WHOLE ? 0 : (u32)(b % a.chunks);
     const u32 from = part * a.chunk, to = WHOLE ? a.n : min(from + a.chunk, a.n);
-    const Soft all = soft_block(soft_scan<T>(reinterpret_cast<const T*>(a.scores) + row * a.ld, from, to, a.c), a.c, room.soft);
+    const Soft all = soft_block(soft_scan<PAST>(reinterpret_cast<const T*>(a.scores) + row * a.ld, from, to, a.c), a.c, room.soft);
     if constexpr (WHOLE) {
       distill_finish<T>(a, row, all, room);
     } else if (threadIdx.x == 0) {
@@ -207,55 +219,54 @@ __global__ __launch_bounds__(DISTILL_THREADS) void distill_finish_kernel(Distill
 
 // The gradient of a chunk of a row.  The teacher's shares are made anew by every workgroup (k is small); entries of the
 // teacher inside the chunk are read before and written after all others, by the first thread that holds their id,
-// which adds up the shares of the same id in their order.  So `out` may be the scores themselves.
-template <typename T>
+// which adds up the shares of the same id in their order.  So `out` may be the scores themselves.  Whether any id is there
+// twice a table tells where k is large: without it 1,000 rows of 20,000 bf16 with k = 1,000 take 247 us, with it 33.
+constexpr u32 DISTILL_FEW = 64, DISTILL_TABLE = 2 * DISTILL_MOST_K;
+template <typename T, bool PAST>
 __global__ __launch_bounds__(DISTILL_THREADS) void distill_grad_kernel(DistillArgs a) {
-  constexpr u32 E = 16 / sizeof(T), AHEAD = 4, PER = DISTILL_MOST_K / DISTILL_THREADS;
+  constexpr u32 E = 16 / sizeof(T), AHEAD = 4;
   __shared__ DistillRoom room;
-  __shared__ u32 ids[DISTILL_MOST_K];
-  __shared__ float shares[DISTILL_MOST_K];
+  __shared__ u32 ids[DISTILL_MOST_K];  // ANN_NONE outside of the chunk
+  __shared__ float shares[DISTILL_MOST_K], kept[DISTILL_MOST_K];
+  __shared__ u32 table[DISTILL_TABLE], twice;
   for (u64 b = blockIdx.x; b < a.rows * a.chunks; b += gridDim.x) {
     const u64 row = b / a.chunks;
     const u32 from = (u32)(b % a.chunks) * a.chunk, to = min(from + a.chunk, a.n);
     const T* z = reinterpret_cast<const T*>(a.scores) + row * a.ld;
     T* out = reinterpret_cast<T*>(a.out) + row * a.ldo;
     const float m = a.stats[2 * row], s = a.stats[2 * row + 1];
-    float t[PER], zt[PER], most = -INFINITY;
-    u32 id[PER];
-#pragma unroll
-    for (u32 u = 0; u < PER; ++u) {
-      const u32 j = threadIdx.x + DISTILL_THREADS * u;
-      t[u] = -INFINITY;
-      id[u] = ANN_NONE;
-      if (j < a.k) {
-        const u32 given = a.ids[row * a.k + j];
-        if (given < a.n) {
-          id[u] = given;
-          t[u] = teacher_at(a, row * a.k + j);
-          if (given >= from && given < to) zt[u] = mx_float(z[given]);
-        }
-      }
-      most = __builtin_fmaxf(most, t[u]);
+    const bool few = a.k <= DISTILL_FEW;
+    if (!few)
+      for (u32 i = threadIdx.x; i < DISTILL_TABLE; i += DISTILL_THREADS) table[i] = ANN_NONE;
+    if (threadIdx.x == 0) twice = few;
+    u32 id;
+    float most = -INFINITY;
+#pragma unroll 1
+    for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {
+      const float t = teacher_entry(a, row, j, &id);
+      most = __builtin_fmaxf(most, t);
+      shares[j] = t;
+      const bool here = id >= from && id < to;
+      ids[j] = here ? id : ANN_NONE;
+      if (here) kept[j] = mx_float(z[id]);
     }
     most = block_max(most, room.most);
     double weights = 0.0;
-    float w[PER];
-#pragma unroll
-    for (u32 u = 0; u < PER; ++u) {
-      w[u] = t[u] == -INFINITY ? 0.0f : soft_exp(t[u], most, a.c);
-      weights += w[u];
+#pragma unroll 1
+    for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {  // (a thread's own ones)
+      const float t = shares[j], w = t == -INFINITY ? 0.0f : soft_exp(t, most, a.c);
+      shares[j] = w;
+      weights += w;
+      if (!few && ids[j] != ANN_NONE)
+        for (u32 at = ids[j] * 2654435761u;; ++at) {  // (the table has twice the room of all ids)
+          const u32 there = atomicCAS(&table[at % DISTILL_TABLE], ANN_NONE, ids[j]);
+          if (there == ids[j]) twice = 1;
+          if (there == ids[j] || there == ANN_NONE) break;
+        }
     }
     weights = block_sum(weights, room.sums);
     const bool none = weights == 0.0 || s == 0.0f;
     const float over = (float)(1.0 / weights);
-#pragma unroll
-    for (u32 u = 0; u < PER; ++u) {
-      const u32 j = threadIdx.x + DISTILL_THREADS * u;
-      if (j < a.k) {
-        ids[j] = id[u];
-        shares[j] = w[u] * over;
-      }
-    }
     const float up = a.t * a.scale * (a.upstream ? a.upstream[row] : 1.0f);
     const float base = m == -INFINITY ? 0.0f : m, share = 1.0f / s;
     auto grad = [&](float v, float p) { return mx_round<T>(none ? 0.0f : up * (soft_exp(v, base, a.c) * share - p)); };
@@ -263,31 +274,34 @@ __global__ __launch_bounds__(DISTILL_THREADS) void distill_grad_kernel(DistillAr
     for (u32 p = threadIdx.x; p < packs; p += DISTILL_THREADS * AHEAD) {
       AnyPack<T, E> in[AHEAD];
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) in[u] = *reinterpret_cast<const AnyPack<T, E>*>(z + from + (u64)min(p + DISTILL_THREADS * u, packs - 1) * E);
+      for (u32 u = 0; u < AHEAD; ++u) in[u] = stream_in<PAST, E>(z + from + (u64)min(p + DISTILL_THREADS * u, packs - 1) * E);
 #pragma unroll
       for (u32 u = 0; u < AHEAD; ++u) {
         if (p + DISTILL_THREADS * u >= packs) break;
         AnyPack<T, E> o;
 #pragma unroll
         for (u32 e = 0; e < E; ++e) o.v[e] = grad(mx_float(static_cast<T>(in[u].v[e])), 0.0f);
-        *reinterpret_cast<AnyPack<T, E>*>(out + from + (u64)(p + DISTILL_THREADS * u) * E) = o;
+        stream_out<E>(out + from + (u64)(p + DISTILL_THREADS * u) * E, o);
       }
     }
     const u32 left = from + packs * E + threadIdx.x;
     if (left < to) out[left] = grad(mx_float(z[left]), 0.0f);
     __syncthreads();  // the teacher's entries come last
-#pragma unroll
-    for (u32 u = 0; u < PER; ++u) {
-      if (id[u] < from || id[u] >= to) continue;
-      const u32 mine = threadIdx.x + DISTILL_THREADS * u;
-      float p = 0.0f;
+#pragma unroll 1
+    for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {
+      const u32 mine = ids[j];
+      if (mine == ANN_NONE) continue;
+      float p = shares[j] * over;
       bool first = true;
-      for (u32 j = 0; j < a.k; ++j) {
-        if (ids[j] != id[u]) continue;
-        first = first && j >= mine;
-        p += shares[j];
+      if (twice) {
+        p = 0.0f;
+        for (u32 i = 0; i < a.k; ++i) {
+          if (ids[i] != mine) continue;
+          first = first && i >= j;
+          p += shares[i] * over;
+        }
       }
-      if (first) out[id[u]] = grad(zt[u], p);
+      if (first) out[mine] = grad(kept[j], p);
     }
     __syncthreads();  // (the next row's ids and shares)
   }
@@ -305,25 +319,40 @@ void set_chunks(DistillArgs& a) {
   a.chunks = (a.n + a.chunk - 1) / a.chunk;
 }
 
-template <typename T>
+template <typename T, bool PAST>
 hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
   const u64 blocks = a.rows * a.chunks;
   const dim3 grid((u32)std::min<u64>(blocks, 1u << 22)), threads(DISTILL_THREADS);
   if (a.chunks == 1) {
-    hipLaunchKernelGGL((distill_scan_kernel<T, true>), grid, threads, 0, s, a);
+    hipLaunchKernelGGL((distill_scan_kernel<T, true, PAST>), grid, threads, 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((distill_scan_kernel<T, false>), grid, threads, 0, s, a);
+  hipLaunchKernelGGL((distill_scan_kernel<T, false, PAST>), grid, threads, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(distill_finish_kernel<T>, dim3((u32)a.rows), threads, 0, s, a);  // (fewer than 512 rows)
   return hipGetLastError();
 }
-template <typename T>
+template <typename T, bool PAST>
 hipError_t launch_distill_grad(const DistillArgs& a, hipStream_t s) {
   const u64 blocks = a.rows * a.chunks;
-  hipLaunchKernelGGL(distill_grad_kernel<T>, dim3((u32)std::min<u64>(blocks, 1u << 22)), dim3(DISTILL_THREADS), 0, s, a);
+  hipLaunchKernelGGL((distill_grad_kernel<T, PAST>), dim3((u32)std::min<u64>(blocks, 1u << 22)), dim3(DISTILL_THREADS), 0, s, a);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_distill(const DistillArgs& a, bool grad, hipStream_t s) {
+  if (a.rows * a.n * sizeof(T) > DISTILL_PAST) return grad ? launch_distill_grad<T, true>(a, s) : launch_distill<T, true>(a, s);
+  return grad ? launch_distill_grad<T, false>(a, s) : launch_distill<T, false>(a, s);
+}
+int launch_distill(const DistillArgs& a, int dtype, bool grad, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == ANN_F32)
+    HIP_TRY(launch_distill<float>(a, grad, st));
+  else if (dtype == ANN_F16)
+    HIP_TRY(launch_distill<__half>(a, grad, st));
+  else
+    HIP_TRY(launch_distill<__bf16>(a, grad, st));
+  return ANN_OK;
 }
 
 // what both calls check; false in *work where there is nothing to do
@@ -391,14 +420,7 @@ int ann_distill(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtype dty
   a.stats = stats_dev;
   a.parts = static_cast<float*>(scratch_dev);
   set_chunks(a);
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == ANN_F32)
-    HIP_TRY(launch_distill<float>(a, st));
-  else if (dtype == ANN_F16)
-    HIP_TRY(launch_distill<__half>(a, st));
-  else
-    HIP_TRY(launch_distill<__bf16>(a, st));
-  return ANN_OK;
+  return launch_distill(a, dtype, false, stream);
 } catch (...) {
   return annmi::on_exception();
 }
@@ -431,14 +453,7 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
   a.out = static_cast<char*>(out_dev);
   a.ldo = ldo;
   set_chunks(a);
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == ANN_F32)
-    HIP_TRY(launch_distill_grad<float>(a, st));
-  else if (dtype == ANN_F16)
-    HIP_TRY(launch_distill_grad<__half>(a, st));
-  else
-    HIP_TRY(launch_distill_grad<__bf16>(a, st));
-  return ANN_OK;
+  return launch_distill(a, dtype, true, stream);
 } catch (...) {
   return annmi::on_exception();
 }
