@@ -950,7 +950,8 @@ def ann_distill(scores, ids, teacher, temperature=1.0, losses_out=None, stats_ou
     device = scores.device
     need = C.c_uint64(0)
     _check(lib().ann_distill_scratch(rows, n, C.byref(need)))
-    scratch = _scratch(scratch, need.value, device)
+    if scratch is not None or need.value:  # (rows that are not divided need none)
+        scratch = _scratch(scratch, need.value, device)
     if losses_out is None:
         losses_out = torch.empty(rows, dtype=torch.float32, device=device)
     else:
@@ -960,8 +961,8 @@ def ann_distill(scores, ids, teacher, temperature=1.0, losses_out=None, stats_ou
     else:
         _stats(stats_out, rows, device)
     _run(lib().ann_distill, device, scores.data_ptr(), rows, n, _element_code(scores), ld, ids.data_ptr(), teacher.data_ptr(),
-         _element_code(teacher), k, temperature, losses_out.data_ptr(), stats_out.data_ptr(), scratch.data_ptr(),
-         scratch.numel() * scratch.element_size())
+         _element_code(teacher), k, temperature, losses_out.data_ptr(), stats_out.data_ptr(),
+         scratch.data_ptr() if scratch is not None else None, need.value)
     return losses_out, stats_out
 
 
@@ -986,6 +987,15 @@ def ann_distill_grad(scores, ids, teacher, stats, grad_losses=None, temperature=
     return out
 
 
+def _picked(t, name, dtype, groups, k, device):
+    """`t`, or a new (groups, k) tensor where it is None."""
+    if t is None:
+        return _torch().empty((groups, k), dtype=dtype, device=device)
+    if tuple(t.shape) != (groups, k) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous ({groups}, {k}) tensor of {dtype} on {device}")
+    return t
+
+
 def ann_beam_select(scores, totals, beams, k, finished=None, pad_id=0, parents_out=None, ids_out=None, totals_out=None, scratch=None):
     """The k best continuations of each group of `beams` rows of `scores` (float32, float16 or bfloat16) with the running
     totals `totals` (float32, one for each row), by the rules of ann_beam_select in ann.h; returns (parents, ids, totals),
@@ -999,23 +1009,19 @@ def ann_beam_select(scores, totals, beams, k, finished=None, pad_id=0, parents_o
     groups = rows // beams
     _one_value_per_row(totals, "totals", torch.float32, rows, device)
     if finished is not None:
-        _one_value_per_row(finished, "finished", finished.dtype if finished.dtype in (torch.bool, torch.uint8) else torch.bool, rows, device)
-    if finished is not None and not 0 <= pad_id < n:
-        raise ValueError(f"pad_id must be 0 to {n - 1}")
+        _one_value_per_row(finished, "finished", torch.bool if finished.dtype != torch.uint8 else torch.uint8, rows, device)
+        if not 0 <= pad_id < n:
+            raise ValueError(f"pad_id must be 0 to {n - 1}")
     need = C.c_uint64(0)
     _check(lib().ann_beam_select_scratch(groups, beams, n, k, C.byref(need)))
     scratch = _scratch(scratch, need.value, device)
-    out = []
-    for t, dtype, name in ((parents_out, torch.int32, "parents_out"), (ids_out, torch.int32, "ids_out"), (totals_out, torch.float32, "totals_out")):
-        if t is None:
-            t = torch.empty((groups, k), dtype=dtype, device=device)
-        elif tuple(t.shape) != (groups, k) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous ({groups}, {k}) tensor of {dtype} on {device}")
-        out.append(t)
+    parents_out = _picked(parents_out, "parents_out", torch.int32, groups, k, device)
+    ids_out = _picked(ids_out, "ids_out", torch.int32, groups, k, device)
+    totals_out = _picked(totals_out, "totals_out", torch.float32, groups, k, device)
     _run(lib().ann_beam_select, device, scores.data_ptr(), groups, beams, n, _element_code(scores), ld, totals.data_ptr(),
-         finished.data_ptr() if finished is not None else None, pad_id if finished is not None else 0, k, out[0].data_ptr(),
-         out[1].data_ptr(), out[2].data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size())
-    return tuple(out)
+         finished.data_ptr() if finished is not None else None, pad_id if finished is not None else 0, k, parents_out.data_ptr(),
+         ids_out.data_ptr(), totals_out.data_ptr(), scratch.data_ptr(), need.value)
+    return parents_out, ids_out, totals_out
 
 
 def _joined(dims):
