@@ -13,8 +13,8 @@ namespace annmi {
 constexpr u32 BEAM_MOST_BEAMS = 64;
 constexpr u32 BEAM_MOST_K = 128;
 constexpr u32 BEAM_MOST_N = (1u << 24) - 1;  // an id, a score and a beam fit in one key of 64 bits
-constexpr u32 BEAM_THREADS = 512;
-constexpr u32 BEAM_EACH = 8;  // entries of a thread
+constexpr u32 BEAM_THREADS = 256;
+constexpr u32 BEAM_EACH = 16;  // entries of a thread
 constexpr u32 BEAM_CHUNK = BEAM_THREADS * BEAM_EACH;
 
 struct BeamArgs {
@@ -34,25 +34,22 @@ struct BeamArgs {
   float* out;
 };
 
-// exp x for x <= 0, within 1e-12 of itself; 0 below -700.  2^n and the series of e^r, |r| <= ln 2 / 2, to r^10 / 10! (the
-// next term is 2.2e-13).  Adding 1.5 * 2^52 leaves n in the low bits of the sum.
+// exp x for x <= 0, within 1.1e-12 of itself; 1e-304 for all that is below -700, and for NaN.  2^n times 2^f, |f| <= 1/2,
+// by the polynomial that has its values at the nine Chebyshev points of that range.  Adding 1.5 * 2^52 leaves n in the low
+// bits of the sum.
 __device__ __forceinline__ double beam_exp(double x) {
-  constexpr double MAGIC = 6755399441055744.0, LOG2E = 1.4426950408889634074, LN2 = 0.69314718055994530942;
-  const double d = __builtin_fmax(x, -700.0) * LOG2E, t = d + MAGIC;
-  const double r = (d - (t - MAGIC)) * LN2;
-  double p = 1.0 / 3628800;
-  p = __builtin_fma(p, r, 1.0 / 362880);
-  p = __builtin_fma(p, r, 1.0 / 40320);
-  p = __builtin_fma(p, r, 1.0 / 5040);
-  p = __builtin_fma(p, r, 1.0 / 720);
-  p = __builtin_fma(p, r, 1.0 / 120);
-  p = __builtin_fma(p, r, 1.0 / 24);
-  p = __builtin_fma(p, r, 1.0 / 6);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
-  p = __builtin_fma(p, r, 1.0);
-  const double v = __hiloint2double(__double2hiint(p) + ((int)__double_as_longlong(t) << 20), __double2loint(p));
-  return x < -700.0 ? 0.0 : v;
+  constexpr double MAGIC = 6755399441055744.0, LOG2E = 1.4426950408889634074;
+  const double d = __builtin_fmax(x, -700.0) * LOG2E, t = d + MAGIC, f = d - (t - MAGIC);
+  double p = 0x1.63d136366db24p-20;
+  p = __builtin_fma(p, f, 0x1.00dc4a532fb8ep-16);
+  p = __builtin_fma(p, f, 0x1.4308ac85aa947p-13);
+  p = __builtin_fma(p, f, 0x1.5d8745a728441p-10);
+  p = __builtin_fma(p, f, 0x1.3b2ab7181b755p-7);
+  p = __builtin_fma(p, f, 0x1.c6b08dd6fd234p-5);
+  p = __builtin_fma(p, f, 0x1.ebfbdff823cedp-3);
+  p = __builtin_fma(p, f, 0x1.62e42fef84cf0p-1);
+  p = __builtin_fma(p, f, 1.0);
+  return __hiloint2double(__double2hiint(p) + ((int)__double_as_longlong(t) << 20), __double2loint(p));
 }
 // z - most, 0 among infinities
 __device__ __forceinline__ double beam_below(float z, float most) { return z == most ? 0.0 : (double)z - most; }
@@ -101,7 +98,7 @@ __device__ __forceinline__ u32 wave_mth(u32 v, u32 m, u32* first) {
   return best;
 }
 
-// One chunk of a row a workgroup, eight entries a thread, which stay in registers.  Every wave finds the ceil(k / 8)-th best
+// One chunk of a row a workgroup, 16 entries a thread, which stay in registers.  Every wave finds the ceil(k / 4)-th best
 // of its threads' best ones; the least of these is a bound that k entries reach at least, and few more in most orders;
 // they are listed and brought into order.
 template <typename T>
@@ -118,7 +115,6 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
     const u32 from = (u32)(b % a.chunks) * BEAM_CHUNK, there = min(BEAM_CHUNK, a.n - from);
     const T* z = reinterpret_cast<const T*>(a.scores) + row * a.ld + from;
     float v[BEAM_EACH];
-    u32 key[BEAM_EACH];
     // (where a chunk is not full, all waves have some of it: a wave without entries gives no bound)
     const u32 at = (there < BEAM_CHUNK ? threadIdx.x % 64 * WAVES + wave : threadIdx.x) * E;
     if (at + E <= there) {
@@ -129,14 +125,11 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
 #pragma unroll
       for (u32 e = 0; e < E; ++e) v[e] = at + e < there ? mx_float(z[min(at + e, there - 1)]) : -INFINITY;
     }
-    u32 head = 0;
+    float head = -INFINITY;  // (NaN is no number to fmax)
 #pragma unroll
-    for (u32 i = 0; i < BEAM_EACH; ++i) {
-      key[i] = v[i] > -INFINITY ? float_key(v[i]) : 0u;  // (not NaN either)
-      head = max(head, key[i]);
-    }
+    for (u32 i = 0; i < BEAM_EACH; ++i) head = __builtin_fmaxf(head, v[i]);
     u32 first;
-    const u32 mth = wave_mth(head, (a.k + WAVES - 1) / WAVES, &first);
+    const u32 mth = wave_mth(head > -INFINITY ? float_key(head) : 0u, (a.k + WAVES - 1) / WAVES, &first);
     __syncthreads();  // (the last turn's readers)
     if (threadIdx.x % 64 == 0) bounds[wave] = mth, tops[wave] = first;
     if (threadIdx.x == 0) count = 0;
@@ -150,17 +143,17 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
       for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = 0;
       continue;
     }
+    const float least = bound ? key_float(bound) : -__FLT_MAX__;  // (no entry is -inf or NaN)
 #pragma unroll
     for (u32 i = 0; i < BEAM_EACH; ++i)
-      if (key[i] && key[i] >= bound) {
-        const u32 id = from + at + i;
-        list[atomicAdd(&count, 1u)] = (u64)key[i] << 32 | (u32)~id;  // (in any order: the keys differ)
-      }
+      if (v[i] >= least) list[atomicAdd(&count, 1u)] = (u64)float_key(v[i]) << 32 | (u32)~(from + at + i);  // (in any order: the keys differ)
     double sum = 0.0;
+    if (most < INFINITY) {
 #pragma unroll
-    for (u32 i = 0; i < BEAM_EACH; ++i) {
-      const double w = beam_exp(beam_below(v[i], most));
-      sum += key[i] ? w : 0.0;
+      for (u32 i = 0; i < BEAM_EACH; ++i) sum += beam_exp((double)v[i] - most);  // (as good as 0 for -inf and NaN)
+    } else {
+#pragma unroll
+      for (u32 i = 0; i < BEAM_EACH; ++i) sum += v[i] == most;
     }
     sums[threadIdx.x] = sum;
     __syncthreads();
@@ -174,17 +167,15 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
       for (int w = 1; w < 64; w *= 2) all += __shfl_xor(all, w);
       if (lane == 0) a.sums[b] = all, a.most[b] = most;
     }
-    if (listed <= BEAM_THREADS) {  // an entry's place is how many are larger
-      const u32 mine = threadIdx.x;
-      if (mine < listed) {
+    if (listed <= 2 * BEAM_THREADS) {  // an entry's place is how many are larger
+      for (u32 mine = threadIdx.x; mine < listed; mine += BEAM_THREADS) {
         const u64 entry = list[mine];
         u32 place = 0;
 #pragma unroll 8
         for (u32 i = 0; i < listed; ++i) place += list[i] > entry;
         if (place < a.k) a.best[b * a.k + place] = entry;
-      } else if (mine < a.k) {
-        a.best[b * a.k + mine] = 0;
       }
+      for (u32 i = listed + threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = 0;
     } else {
       const u32 size = power_of_two(listed);
       for (u32 i = listed + threadIdx.x; i < size; i += BEAM_THREADS) list[i] = 0;
@@ -396,7 +387,7 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
       for (u32 i = 0; i < MOST; ++i) {
         if (first + i >= a.k) break;
         const u32 p = parents[first + i];
-        if (p < a.beams && !(a.in_place && p == first + i)) *reinterpret_cast<P*>(out + (first + i) * a.row_out) = v[i];
+        if (p < a.beams && !(a.in_place && p == first + i)) __builtin_nontemporal_store(v[i], reinterpret_cast<P*>(out + (first + i) * a.row_out));
       }
     }
   }

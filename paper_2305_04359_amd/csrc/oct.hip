@@ -117,67 +117,75 @@ __global__ __launch_bounds__(256) void oct_quantize_kernel(OctQuantizeArgs a) {
   }
 }
 
-// Columns: row i of the result is column i of x, which has d rows.  A workgroup takes a step of COLS columns: a thread 16
+// Columns: row i of the result is column i of x, which has d rows.  A workgroup takes a step of COLS columns: a thread EACH
 // elements of four neighbouring columns, whose maxima meet in LDS; through LDS the codes get into whole rows of 128 bytes.
 constexpr u32 COLS = 128;
+constexpr u32 COLUMN_EACH = 16, COLUMN_PARTS = OCT_STEP / COLUMN_EACH, COLUMN_THREADS = COLS / 4 * COLUMN_PARTS;
 template <typename T>
-__global__ __launch_bounds__(256) void oct_columns_kernel(OctQuantizeArgs a, u32 across, u64 tiles) {
-  __shared__ u32 most_of[8][COLS];
-  __shared__ __align__(16) v4i codes[COLS][8];
-  const u32 c = threadIdx.x % 32 * 4, g = threadIdx.x / 32;
+__global__ __launch_bounds__(COLUMN_THREADS) void oct_columns_kernel(OctQuantizeArgs a, u32 across, u64 tiles) {
+  using Part = Pack<u32, COLUMN_EACH / 4>;  // a thread's codes of a column
+  __shared__ u32 most_of[COLUMN_PARTS][COLS];
+  __shared__ __align__(16) char codes[COLS * OCT_STEP];
+  const u32 c = threadIdx.x % (COLS / 4) * 4, g = threadIdx.x / (COLS / 4);
   const u32 words = oct_words(a.steps);
   for (u64 t = blockIdx.x; t < tiles; t += gridDim.x) {
     const u64 i0 = t % across * COLS;        // the first column
     const u32 step = (u32)(t / across);
-    const u32 e0 = step * OCT_STEP + g * 16;
+    const u32 e0 = step * OCT_STEP + g * COLUMN_EACH;
     const u32 there = (u32)min((u64)COLS, a.n - i0);
-    AnyPack<T, 4> in[16];
+    AnyPack<T, 4> in[COLUMN_EACH];
     if (c + 4 <= there) {
 #pragma unroll
-      for (u32 e = 0; e < 16; ++e)
+      for (u32 e = 0; e < COLUMN_EACH; ++e)
         in[e] = *reinterpret_cast<const AnyPack<T, 4>*>(reinterpret_cast<const T*>(a.x) + (u64)min(e0 + e, a.d - 1) * a.ldx + i0 + c);
     } else {
 #pragma unroll
-      for (u32 e = 0; e < 16; ++e)
+      for (u32 e = 0; e < COLUMN_EACH; ++e)
 #pragma unroll
         for (u32 k = 0; k < 4; ++k) in[e].v[k] = reinterpret_cast<const T*>(a.x)[(u64)min(e0 + e, a.d - 1) * a.ldx + i0 + min(c + k, there - 1)];
     }
-    float v[4][16];
+    float v[4][COLUMN_EACH];
     u32 most[4] = {};
 #pragma unroll
-    for (u32 e = 0; e < 16; ++e)
+    for (u32 e = 0; e < COLUMN_EACH; ++e)
 #pragma unroll
       for (u32 k = 0; k < 4; ++k) {
         v[k][e] = e0 + e < a.d ? mx_float(static_cast<T>(in[e].v[k])) : 0.0f;
         most[k] = max(most[k], __float_as_uint(v[k][e]) & 0x7FFFFFFFu);
       }
-#pragma unroll
-    for (u32 k = 0; k < 4; ++k) most_of[g][c + k] = most[k];
+    *reinterpret_cast<Pack<u32, 4>*>(&most_of[g][c]) = {{most[0], most[1], most[2], most[3]}};
     __syncthreads();
+    // a column's maximum: each thread's four, of all parts
+    u32 m[4] = {};
+#pragma unroll
+    for (u32 o = 0; o < COLUMN_PARTS; ++o) {
+      const Pack<u32, 4> other = *reinterpret_cast<const Pack<u32, 4>*>(&most_of[o][c]);
+#pragma unroll
+      for (u32 k = 0; k < 4; ++k) m[k] = max(m[k], other.v[k]);
+    }
 #pragma unroll
     for (u32 k = 0; k < 4; ++k) {
-      u32 m = 0;
-#pragma unroll
-      for (u32 o = 0; o < 8; ++o) m = max(m, most_of[o][c + k]);
-      const u32 byte = oct_scale_byte(m);
+      const u32 byte = oct_scale_byte(m[k]);
       const float inverse = oct_inverse(byte);
-      v4i code;
+      Part code;
 #pragma unroll
-      for (u32 q = 0; q < 4; ++q)
-        code[q] = byte == 255 ? 0
-                              : (int)oct_codes(v[k][4 * q] * inverse, v[k][4 * q + 1] * inverse, v[k][4 * q + 2] * inverse, v[k][4 * q + 3] * inverse);
-      codes[c + k][g ^ (c / 4 + k) % 8] = code;
-      if (g == 0 && c + k < there) {
-        uint8_t* to = reinterpret_cast<uint8_t*>(a.scales) + (i0 + c + k) * words * 4;
+      for (u32 q = 0; q < COLUMN_EACH / 4; ++q)
+        code.v[q] = byte == 255 ? 0u : oct_codes(v[k][4 * q] * inverse, v[k][4 * q + 1] * inverse, v[k][4 * q + 2] * inverse, v[k][4 * q + 3] * inverse);
+      // pieces of 16 bytes change places by the column's number
+      const u32 r = c + k, at = g * COLUMN_EACH;
+      *reinterpret_cast<Part*>(codes + r * OCT_STEP + ((at / 16 ^ (r / 4 + r) % 8) * 16 | at % 16)) = code;
+      if (g == 0 && r < there) {
+        uint8_t* to = reinterpret_cast<uint8_t*>(a.scales) + (i0 + r) * words * 4;
         to[step] = (uint8_t)byte;
         if (step + 1 == a.steps)  // the rest of the last word
           for (u32 o = a.steps; o < words * 4; ++o) to[o] = 0;
       }
     }
     __syncthreads();
-    for (u32 r = threadIdx.x / 8; r < there; r += 32) {
+    for (u32 r = threadIdx.x / 8; r < there; r += COLUMN_THREADS / 8) {
       const u32 u = threadIdx.x % 8;
-      *reinterpret_cast<v4i*>(a.codes + ((i0 + r) * a.steps + step) * OCT_STEP + u * 16) = codes[r][u ^ (r / 4 + r % 4) % 8];
+      *reinterpret_cast<v4i*>(a.codes + ((i0 + r) * a.steps + step) * OCT_STEP + u * 16) =
+          *reinterpret_cast<const v4i*>(codes + r * OCT_STEP + (u ^ (r / 4 + r) % 8) * 16);
     }
     // (the next turn's maxima go where none are read any more; its codes come behind its own barrier)
   }
@@ -202,7 +210,7 @@ hipError_t launch_oct_quantize(const OctQuantizeArgs& a, bool columns, hipStream
   if (!columns) return a.d >= 8 ? launch_oct_rows<T, true>(a, s) : launch_oct_rows<T, false>(a, s);
   const u32 across = (u32)(((u64)a.n + COLS - 1) / COLS);
   const u64 tiles = (u64)across * a.steps;
-  hipLaunchKernelGGL(oct_columns_kernel<T>, dim3((u32)(tiles < (1u << 20) ? tiles : (1u << 20))), dim3(256), 0, s, a, across, tiles);
+  hipLaunchKernelGGL(oct_columns_kernel<T>, dim3((u32)(tiles < (1u << 20) ? tiles : (1u << 20))), dim3(COLUMN_THREADS), 0, s, a, across, tiles);
   return hipGetLastError();
 }
 
