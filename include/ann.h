@@ -566,7 +566,7 @@ int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint6
  *   alignment   codes 16 bytes, scales 4; the other matrices of these calls
  *               that of their element, with a row stride of their own (`ld`,
  *               in elements, at least the row's length)
- *   sizes       1 <= d <= 1048576; rows < 2^31; a count of zero rows: ANN_OK,
+ *   sizes       1 <= d <= 1048576; rows < 2^30; a count of zero rows: ANN_OK,
  *               nothing is done and no pointer is read
  * All calls are asynchronous on `stream`, allocate nothing, keep nothing and
  * can be captured into a graph.  They launch on the current device, which has to
@@ -591,9 +591,13 @@ int ann_oct_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint
 
 /* out[i][j] = sum over the d elements of value(x row i) * value(row j), summed in
  * fp32 and rounded once to out_dtype (ANN_F32, ANN_F16 or ANN_BF16); out_dev is
- * nx x n, rows ldo >= n apart.  The gradients of a layer's product Y = X W^T,
- * from G = dY, are products too: dX of the rows of G with the columns of W, dW of
- * the columns of G with the columns of X.                                    */
+ * nx x n, rows ldo >= n apart.  Values and products below 2^-126 may count as 0.
+ * Products are whole where the results are ANN_F32.  For ANN_F16 and ANN_BF16 they
+ * may be cut: of eight neighbouring ones (elements 8 i to 8 i + 7) what lies below
+ * 2^(E - 13), E the exponent of the largest, which is far less than the rounding of
+ * the result unless a sum nearly cancels.  The gradients of a layer's product
+ * Y = X W^T, from G = dY, are products too: dX of the rows of G with the columns of
+ * W, dW of the columns of G with the columns of X.                           */
 int ann_oct_product(const uint8_t* xcodes_dev, const uint8_t* xscales_dev, uint64_t nx, const uint8_t* codes_dev,
                    const uint8_t* scales_dev, uint64_t n, uint32_t d, void* out_dev, ann_dtype out_dtype, uint64_t ldo,
                    void* stream);
@@ -665,8 +669,8 @@ int ann_sample_scratch(uint64_t rows, uint64_t n, uint64_t* bytes);
  *   grad_losses_dev  rows floats, the gradients of the losses; NULL: 1 for each
  *   scale         one more factor of all gradients (1 / rows for the mean)
  *   out_dev       rows x n gradients of the scores' type, ldo apart; may be
- *                 scores_dev itself (with its stride), and must not overlap with
- *                 it otherwise
+ *                 scores_dev itself (with its stride); gradients that overlap with
+ *                 scores in another way are refused
  * Asynchronous on `stream` and on the current device, which has to be that of
  * the stream and of all pointers; allocates nothing, can be captured into a
  * graph.  The results depend on the arguments only, bit by bit.              */
@@ -693,7 +697,8 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
  *                 may be NULL (and pad_id is unused then)
  *   parents_dev, ids_dev, totals_out_dev  groups x k: the beam (0 to beams - 1),
  *                 the entry and v, rounded to fp32; ANN_NONE, ANN_NONE, -inf where
- *                 there are fewer than k
+ *                 there are fewer than k.  With k = beams totals_out_dev may be
+ *                 totals_dev itself
  *   scratch_dev   at least what ann_beam_select_scratch says, 16-byte aligned
  * 1 <= beams <= 64, 1 <= k <= 128, 1 <= n < 2^24, groups * beams < 2^31.
  * Asynchronous on `stream` and on the current device, which has to be that of

@@ -436,7 +436,15 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
   if (!work) return ANN_OK;
   if (!out_dev) return fail(ANN_EINVAL, "null argument");
   if (!aligned_to(out_dev, dtype_bytes(dtype)) || !aligned_to(grad_losses_dev, 4)) return fail(ANN_EINVAL, "out or grad_losses not aligned to their elements");
-  if (out_dev == scores_dev && ldo != ld && rows > 1) return fail(ANN_EINVAL, "gradients in the scores' place need the scores' row stride");
+  if (out_dev != scores_dev || (ldo != ld && rows > 1)) {
+    // apart, or side by side in rows of the same stride
+    const u64 esz = dtype_bytes(dtype);
+    const uintptr_t from = reinterpret_cast<uintptr_t>(scores_dev), to = reinterpret_cast<uintptr_t>(out_dev);
+    const u64 scores_end = from + ((rows - 1) * ld + n) * esz, out_end = to + ((rows - 1) * ldo + n) * esz;
+    const u64 off = (from < to ? to - from : from - to) % (ld * esz);
+    const bool beside = ld == ldo && off >= n * esz && off <= (ld - n) * esz;
+    if (from < out_end && to < scores_end && !beside) return fail(ANN_EINVAL, "gradients must lie in the scores' place or apart from them");
+  }
   DistillArgs a{};
   a.scores = static_cast<const char*>(scores_dev);
   a.rows = rows;

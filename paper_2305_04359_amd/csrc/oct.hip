@@ -6,7 +6,7 @@
 namespace annmi {
 
 int check_oct_rows(const char* what, const uint8_t* codes, const uint8_t* scales, u64 n, u32 d) {
-  if (n > OCT_MOST_ROWS) return fail(ANN_EINVAL, "%s: rows must stay below 2^31", what);
+  if (n > OCT_MOST_ROWS) return fail(ANN_EINVAL, "%s: rows must stay below 2^30", what);
   if (d < 1 || d > OCT_MOST_D) return fail(ANN_EINVAL, "%s: d must be 1 to %u", what, OCT_MOST_D);
   if (n == 0) return ANN_OK;
   if (!codes || !scales) return fail(ANN_EINVAL, "null argument");

@@ -6,7 +6,7 @@ namespace annmi {
 
 constexpr u32 OCT_STEP = 128;  // elements that share a scale: what one scaled matrix instruction takes of a row
 constexpr u32 OCT_MOST_D = 1u << 20;
-constexpr u64 OCT_MOST_ROWS = (1ull << 31) - 1;
+constexpr u64 OCT_MOST_ROWS = (1ull << 30) - 1;  // (their tiles are counted in workgroups, these in threads of 32 bits)
 
 constexpr u32 oct_steps(u32 d) { return (d + OCT_STEP - 1) / OCT_STEP; }
 constexpr u32 oct_words(u32 steps) { return (steps + 3) / 4; }  // of a row's scale bytes

@@ -538,10 +538,14 @@ hipError_t launch_small(const OctProductArgs& a, hipStream_t s) {
 template <bool CODED>
 hipError_t launch_tiles(const OctProductArgs& a, hipStream_t s) {
   if (a.x.n <= NARROW_X) return launch_small<CODED, NARROW_W, NARROW_X>(a, s);
-  // By what a turn of workgroups over the chip takes: 256 large tiles, 256 small ones or twice as many.
+  // By what a turn of workgroups over the chip takes: 256 large tiles, 256 small ones or twice as many.  What a tile
+  // takes besides its steps is more for large ones.  To bf16 by large tiles and by small ones: 2,048 x 8,192 of 4,096 elements
+  // 67 us and 91, 1,024 x 4,096 of 4,096 46 and 27, 2,048 x 4,096 of 8,192 97 and 93, 4,096 x 32,768 of 1,024 170 and
+  // 196, 256 x 131,072 of 1,024 47 and 53, 1,000 x 100,000 of 256 63 and 56; 1,000 x 10,000 of 1,000 to fp32 36 and 31.
   const u64 large = (((u64)a.w.n + LARGE - 1) / LARGE) * (((u64)a.x.n + LARGE - 1) / LARGE);
   const u64 small = (((u64)a.w.n + SMALL - 1) / SMALL) * (((u64)a.x.n + SMALL - 1) / SMALL);
-  const u64 cost_large = (large + 255) / 256 * 64, cost_small = small / 512 * 45 + (small % 512 == 0 ? 0 : small % 512 <= 256 ? 25 : 45);
+  const u64 cost_large = (large + 255) / 256 * (a.w.steps < 16 ? 77 : 64);
+  const u64 cost_small = small / 512 * 45 + (small % 512 == 0 ? 0 : small % 512 <= 256 ? 25 : 45);
   if (a.w.steps >= 4 && large < 1u << 22 && cost_large <= cost_small) return launch_large<CODED>(a, s);
   return launch_small<CODED, SMALL, SMALL>(a, s);
 }

@@ -18,7 +18,8 @@ BOTH = (dict(scores=None), dict(ids=None), dict(teacher=None), dict(stats=None),
 @pytest.mark.parametrize("name,good,bad", [
     *[("ann_distill", LOSS, b) for b in (*BOTH, dict(losses=None), dict(losses=PTR + 1), dict(n=100_000, ld=100_000, scratch=None),
                                          dict(n=100_000, ld=100_000, bytes=8), dict(n=100_000, ld=100_000, scratch=PTR + 8))],
-    *[("ann_distill_grad", GRAD, b) for b in (*BOTH, dict(out=None), dict(out=PTR + 2), dict(ldo=99), dict(grads=PTR + 2), dict(out=PTR, ldo=101))],
+    *[("ann_distill_grad", GRAD, b) for b in (*BOTH, dict(out=None), dict(out=PTR + 2), dict(ldo=99), dict(grads=PTR + 2), dict(out=PTR, ldo=101), dict(out=PTR + 4),
+                                               dict(out=PTR + 400, ld=150), dict(out=PTR + 800), dict(out=PTR - 4, ld=200, ldo=200), dict(out=PTR + 396, ld=200, ldo=200))],
 ])
 def test_refused(name, good, bad):
     refused(name, *{**good, **bad}.values())

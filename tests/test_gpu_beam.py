@@ -204,6 +204,16 @@ def test_reorder_beyond_32_bits(env):
     assert states.sum(dtype=torch.int64).item() == 9 + 12
 
 
+def test_totals_in_place(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(12)
+    z = scores_of(torch, rng, 400, 300, "float32")
+    totals = dev(torch, -rng.random(400).astype(np.float32))
+    want = check(torch, A, z, totals, 4, 4)
+    got = A.ann_beam_select(z, totals, 4, 4, totals_out=totals.view(100, 4))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(totals.view(100, 4), want[2])
+
+
 def test_streams_graphs_and_repeats(env):
     torch, A, _ = env
     rng = np.random.default_rng(5)

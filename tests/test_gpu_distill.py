@@ -86,7 +86,7 @@ def wider(torch, x, pad):
 
 
 @pytest.mark.parametrize("dtype", ("float32", "float16", "bfloat16"))
-@pytest.mark.parametrize("rows,n,k", [(1, 1, 1), (3, 2, 2), (2, 7, 3), (5, 8, 8), (4, 9, 20), (3, 100, 10), (7, 1025, 64), (2, 5000, 1024), (1, 8192, 5), (3, 8193, 10),
+@pytest.mark.parametrize("rows,n,k", [(1, 1, 1), (3, 2, 2), (2, 7, 3), (5, 8, 8), (4, 9, 20), (3, 100, 10), (7, 1025, 64), (2, 5000, 1024), (1, 8192, 5), (3, 8193, 10), (2, 16_384, 9), (1, 16_385, 9),
                                       (2, 16_391, 33), (600, 130, 7), (37, 10_000, 10)])
 def test_sizes(env, dtype, rows, n, k):
     torch, A, _ = env
@@ -121,6 +121,15 @@ def test_in_place_and_beside(env):
             A.ann_distill_grad(place, ids, teacher, stats, temperature=2.0, out=place)
             assert torch.equal(place, want)
         assert (strided._base[:, n:] == 77).all()
+    both = torch.zeros((5, 700), device="cuda")  # scores and gradients side by side in the same rows
+    z, ids, teacher = inputs(torch, rng, 5, 300, 4, "float32")
+    both[:, :300] = z
+    _, stats, want = check(torch, A, z, ids, teacher)
+    A.ann_distill_grad(both[:, :300], ids, teacher, stats, out=both[:, 350:650])
+    assert torch.equal(both[:, 350:650], want) and torch.equal(both[:, :300], z)
+    for out in (both[:, 299:599], both[1:, :300], both.view(-1)[200:1700].view(5, 300)):
+        with pytest.raises(A.AnnError):
+            A.ann_distill_grad(both[:len(out), :300], ids[:len(out)], teacher[:len(out)], stats[:len(out)], out=out)
 
 
 def test_same_id_twice(env):

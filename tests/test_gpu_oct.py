@@ -165,6 +165,21 @@ def test_product_of_every_code(env):
         assert torch.equal(got, dev(torch, want).to(t).repeat(reps, reps)), t
 
 
+@pytest.mark.parametrize("nx,n,d", [(3, 100, 200), (70, 300, 520), (40, 11_000, 130), (140, 5100, 300), (2048, 4096, 520)])
+def test_scales_far_from_one(env, nx, n, d):
+    """Small numbers by large ones, in steps whose scales differ by 2^30."""
+    torch, A, _ = env
+    rng = np.random.default_rng(n)
+    x, w = (dev(torch, rng.standard_normal((r, d)).astype(np.float32)) for r in (nx, n))
+    x *= 2.0 ** -100
+    w *= 2.0 ** 90
+    x[:, 128:] *= 2.0 ** 30
+    w[:, 128:] *= 2.0 ** -30
+    x, w = A.ann_oct_quantize(x), A.ann_oct_quantize(w)
+    for out in ("float32", "bfloat16"):
+        check_product(torch, A, x, w, out)
+
+
 def test_not_a_number(env):
     """A step of NaN on either side makes the results that it takes part in NaN, and no others."""
     torch, A, _ = env
@@ -177,6 +192,15 @@ def test_not_a_number(env):
     want[[3, 69]] = True
     want[:, [5, 299]] = True
     assert (np.isnan(got) == want).all()
+    for nx, n in ((40, 11_000), (140, 5100), (2048, 4096)):  # tiles
+        x, w = (torch.zeros((r, 400), device="cuda") for r in (nx, n))
+        x[3, 7], x[nx - 1, 399], w[5, 130], w[n - 1, 0] = np.nan, np.inf, -np.inf, np.nan
+        want = torch.zeros((nx, n), dtype=torch.bool, device="cuda")
+        want[[3, nx - 1]] = True
+        want[:, [5, n - 1]] = True
+        for t in (torch.float32, torch.bfloat16):
+            got = A.ann_oct_product(A.ann_oct_quantize(x), A.ann_oct_quantize(w), dtype=t)
+            assert torch.equal(got.isnan(), want), (nx, n, t)
 
 
 def test_gradients(env):
