@@ -214,8 +214,10 @@ hipError_t launch_direct(const OctProductArgs& a, hipStream_t s) {
 
 // Many rows of both sides.  Steps pass through LDS by halves (64 elements), from memory to LDS without registers between;
 // a wave takes 32 rows by 32 rows at once.  In LDS the four pieces of 16 bytes of a row's half change places by the row's
-// number, so that lanes that read the same piece of neighbouring rows meet all banks.
+// number, so that lanes that read the same piece of neighbouring rows meet all banks: of eight rows as of sixteen.  (By two
+// bits of the row's number, which serves eight, half of the time of LDS went into conflicts.)
 constexpr u32 HALF = 64;
+__device__ __forceinline__ u32 half_place(u32 row, u32 piece) { return piece ^ (row >> 2 & 1) ^ ((row >> 1 ^ row >> 3) & 1) << 1; }
 using v16f = float __attribute__((ext_vector_type(16)));
 
 // 32 WF x 32 XF results of a wave: a half's fragments, and what is made of them.  Lane l holds row l & 31 of each side and
@@ -231,7 +233,7 @@ struct Wave32 {
       for (int j = 0; j < XF; ++j) acc[i][j] = v16f{};
   }
   static __device__ __forceinline__ v8i fragment(const char* rows) {
-    const u32 lane = threadIdx.x % 64, at = lane % 32 * HALF + (lane / 32 ^ lane / 2 % 4) * 16;
+    const u32 lane = threadIdx.x % 64, at = lane % 32 * HALF + half_place(lane, lane / 32) * 16;
     return __builtin_shufflevector(*reinterpret_cast<const v4i*>(rows + at), *reinterpret_cast<const v4i*>(rows + (at ^ 32)), 0, 1, 2, 3, 4, 5, 6, 7);
   }
   __device__ __forceinline__ void read(const char* wrows, const char* xrows) {
@@ -338,7 +340,7 @@ struct Side {
     last = (u32)min((u64)ROWS, m.n - row0) - 1;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
-      offset[i] = min((wave + WAVES * i) * 16 + lane / 4, last) * m.steps * OCT_STEP + (lane % 4 ^ lane / 8 % 4) * 16;
+      offset[i] = min((wave + WAVES * i) * 16 + lane / 4, last) * m.steps * OCT_STEP + half_place(lane / 4, lane % 4) * 16;
   }
   __device__ __forceinline__ void fetch(u32 half, char* to) const {
     typedef __attribute__((address_space(1))) const void* From;
