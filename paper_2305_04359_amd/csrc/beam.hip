@@ -16,6 +16,7 @@ constexpr u32 BEAM_MOST_N = (1u << 24) - 1;  // an id, a score and a beam fit in
 constexpr u32 BEAM_THREADS = 256;
 constexpr u32 BEAM_EACH = 16;  // entries of a thread
 constexpr u32 BEAM_CHUNK = BEAM_THREADS * BEAM_EACH;
+constexpr u32 BEAM_LIST = 1024;  // entries of a chunk that are brought into order
 
 struct BeamArgs {
   const char* scores;
@@ -98,15 +99,52 @@ __device__ __forceinline__ u32 wave_mth(u32 v, u32 m, u32* first) {
   return best;
 }
 
+// how far a thread's i-th entry lies from its first one: pieces of E entries, the workgroup's next to each other
+template <u32 E>
+__device__ __forceinline__ constexpr u32 beam_step(u32 i) {
+  return i / E * (BEAM_THREADS * E) + i % E;
+}
+
+// Lists exactly the k best of a chunk that has more: the k-th best's key, of the score and the place in the chunk, is found
+// bit by bit by counting.  For chunks of many equal scores.
+template <u32 E>
+__device__ __forceinline__ u32 beam_exactly(const float (&v)[BEAM_EACH], u32 place, u32 from, u32 k, u64* list, u32 (*counts)[BEAM_THREADS / 64], u32* count) {
+  constexpr u32 BITS = 12;  // of the place
+  static_assert(BEAM_CHUNK == 1u << BITS);
+  u64 least = 0;
+  for (int bit = 31 + BITS; bit >= 0; --bit) {
+    const u64 tried = least | 1ull << bit;
+    u32 mine = 0;
+#pragma unroll
+    for (u32 i = 0; i < BEAM_EACH; ++i) mine += v[i] > -INFINITY && ((u64)float_key(v[i]) << BITS | (BEAM_CHUNK - 1 - (place + beam_step<E>(i)))) >= tried;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) mine += __shfl_xor(mine, w);
+    if (threadIdx.x % 64 == 0) counts[bit % 2][threadIdx.x / 64] = mine;
+    __syncthreads();  // (the counts before these are read by then)
+    u32 all = 0;
+#pragma unroll
+    for (u32 w = 0; w < BEAM_THREADS / 64; ++w) all += counts[bit % 2][w];
+    if (all >= k) least = tried;
+  }
+  if (threadIdx.x == 0) *count = 0;
+  __syncthreads();
+#pragma unroll
+  for (u32 i = 0; i < BEAM_EACH; ++i)
+    if (v[i] > -INFINITY && ((u64)float_key(v[i]) << BITS | (BEAM_CHUNK - 1 - (place + beam_step<E>(i)))) >= least)
+      list[atomicAdd(count, 1u)] = (u64)float_key(v[i]) << 32 | (u32)~(from + place + beam_step<E>(i));
+  __syncthreads();
+  return *count;
+}
+
 // One chunk of a row a workgroup, 16 entries a thread, which stay in registers.  Every wave finds the ceil(k / 4)-th best
 // of its threads' best ones; the least of these is a bound that k entries reach at least, and few more in most orders;
 // they are listed and brought into order.
 template <typename T>
 __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
-  constexpr u32 E = BEAM_EACH, WAVES = BEAM_THREADS / 64;
-  __shared__ u64 list[BEAM_CHUNK];
+  constexpr u32 E = 16 / sizeof(T), WAVES = BEAM_THREADS / 64;
+  __shared__ u64 list[BEAM_LIST];
   __shared__ double sums[BEAM_THREADS];
-  __shared__ u32 bounds[WAVES], tops[WAVES], count;
+  __shared__ u32 bounds[WAVES], tops[WAVES], counts[2][WAVES], count;
   const u32 wave = threadIdx.x / 64;
   const u64 tiles = a.groups * a.beams * a.chunks;
   for (u64 b = blockIdx.x; b < tiles; b += gridDim.x) {
@@ -116,14 +154,18 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
     const T* z = reinterpret_cast<const T*>(a.scores) + row * a.ld + from;
     float v[BEAM_EACH];
     // (where a chunk is not full, all waves have some of it: a wave without entries gives no bound)
-    const u32 at = (there < BEAM_CHUNK ? threadIdx.x % 64 * WAVES + wave : threadIdx.x) * E;
-    if (at + E <= there) {
-      const AnyPack<T, E> in = *reinterpret_cast<const AnyPack<T, E>*>(z + at);
+    const u32 place = (there < BEAM_CHUNK ? threadIdx.x % 64 * WAVES + wave : threadIdx.x) * E;
 #pragma unroll
-      for (u32 e = 0; e < E; ++e) v[e] = mx_float(static_cast<T>(in.v[e]));
-    } else {
+    for (u32 u = 0; u < BEAM_EACH / E; ++u) {
+      const u32 at = place + u * (BEAM_THREADS * E);
+      if (at + E <= there) {
+        const AnyPack<T, E> in = *reinterpret_cast<const AnyPack<T, E>*>(z + at);
 #pragma unroll
-      for (u32 e = 0; e < E; ++e) v[e] = at + e < there ? mx_float(z[min(at + e, there - 1)]) : -INFINITY;
+        for (u32 e = 0; e < E; ++e) v[u * E + e] = mx_float(static_cast<T>(in.v[e]));
+      } else {
+#pragma unroll
+        for (u32 e = 0; e < E; ++e) v[u * E + e] = at + e < there ? mx_float(z[min(at + e, there - 1)]) : -INFINITY;
+      }
     }
     float head = -INFINITY;  // (NaN is no number to fmax)
 #pragma unroll
@@ -144,9 +186,16 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
       continue;
     }
     const float least = bound ? key_float(bound) : -__FLT_MAX__;  // (no entry is -inf or NaN)
+    u32 mask = 0;
 #pragma unroll
-    for (u32 i = 0; i < BEAM_EACH; ++i)
-      if (v[i] >= least) list[atomicAdd(&count, 1u)] = (u64)float_key(v[i]) << 32 | (u32)~(from + at + i);  // (in any order: the keys differ)
+    for (u32 i = 0; i < BEAM_EACH; ++i) mask |= (u32)(v[i] >= least) << i;
+    if (mask) {
+      u32 slot = atomicAdd(&count, (u32)__popc(mask));  // (in any order: the keys differ)
+      for (; mask; mask &= mask - 1, ++slot) {
+        const u32 at = place + beam_step<E>(__builtin_ctz(mask));
+        if (slot < BEAM_LIST) list[slot] = (u64)float_key(mx_float(z[at])) << 32 | (u32)~(from + at);
+      }
+    }
     double sum = 0.0;
     if (most < INFINITY) {
 #pragma unroll
@@ -157,7 +206,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
     }
     sums[threadIdx.x] = sum;
     __syncthreads();
-    const u32 listed = count;
+    u32 listed = count;
     if (wave == WAVES - 1) {  // (the first waves have the list)
       const u32 lane = threadIdx.x % 64;
       double all = 0.0;
@@ -167,25 +216,16 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
       for (int w = 1; w < 64; w *= 2) all += __shfl_xor(all, w);
       if (lane == 0) a.sums[b] = all, a.most[b] = most;
     }
-    if (listed <= 2 * BEAM_THREADS) {  // an entry's place is how many are larger
-      for (u32 mine = threadIdx.x; mine < listed; mine += BEAM_THREADS) {
-        const u64 entry = list[mine];
-        u32 place = 0;
+    if (listed > BEAM_LIST) listed = beam_exactly<E>(v, place, from, a.k, list, counts, &count);
+    // an entry's place is how many are larger
+    for (u32 mine = threadIdx.x; mine < listed; mine += BEAM_THREADS) {
+      const u64 entry = list[mine];
+      u32 place = 0;
 #pragma unroll 8
-        for (u32 i = 0; i < listed; ++i) place += list[i] > entry;
-        if (place < a.k) a.best[b * a.k + place] = entry;
-      }
-      for (u32 i = listed + threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = 0;
-    } else {
-      const u32 size = power_of_two(listed);
-      for (u32 i = listed + threadIdx.x; i < size; i += BEAM_THREADS) list[i] = 0;
-      __syncthreads();
-      sort_down<BEAM_THREADS>(size, [&](u32 low, u32 high, bool down) {
-        const u64 x = list[low], y = list[high];
-        if ((x < y) == down) list[low] = y, list[high] = x;
-      });
-      for (u32 i = threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = list[i];
+      for (u32 i = 0; i < listed; ++i) place += list[i] > entry;
+      if (place < a.k) a.best[b * a.k + place] = entry;
     }
+    for (u32 i = listed + threadIdx.x; i < a.k; i += BEAM_THREADS) a.best[b * a.k + i] = 0;
   }
 }
 

@@ -81,6 +81,24 @@ def test_ties_and_orders(env, n):
     check(torch, A, z, totals[:2], 2, 20)
 
 
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16"))
+def test_many_equal_scores(env, dtype):
+    """Chunks with more entries at the bound than are listed at once, of one value and of few."""
+    torch, A, _ = env
+    rng = np.random.default_rng(15)
+    totals = dev(torch, -rng.random(6).astype(np.float32))
+    for n in (3000, 4096, 9000):
+        z = torch.zeros((6, n), dtype=getattr(torch, dtype), device="cuda")
+        for k in (1, 5, 128):
+            check(torch, A, z, totals, 3, k)
+        z[:, ::3] = 1.0
+        z[1, 5] = z[4, n - 1] = 2.0
+        z[2, :1500] = -np.inf
+        z[3] = -0.0
+        for k in (2, 100):
+            check(torch, A, z, totals, 2, k)
+
+
 def test_values_that_are_no_numbers(env):
     torch, A, _ = env
     rng = np.random.default_rng(4)
