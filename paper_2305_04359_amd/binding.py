@@ -996,10 +996,16 @@ def _picked(t, name, dtype, groups, k, device):
     return t
 
 
+def _one_value_per_beam(t, name, dtype, groups, beams, device):
+    if tuple(t.shape) not in ((groups * beams,), (groups, beams)) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {groups * beams} or ({groups}, {beams}) {dtype} on {device}")
+
+
 def ann_beam_select(scores, totals, beams, k, finished=None, pad_id=0, parents_out=None, ids_out=None, totals_out=None, scratch=None):
     """The k best continuations of each group of `beams` rows of `scores` (float32, float16 or bfloat16) with the running
     totals `totals` (float32, one for each row), by the rules of ann_beam_select in ann.h; returns (parents, ids, totals),
-    each (groups, k).  `finished`: bool or uint8, one for each row."""
+    each (groups, k).  `finished`: bool or uint8, one for each row.  Both are (rows,) or (groups, beams), so that the totals
+    returned with k = beams are the next step's as they are."""
     torch = _torch()
     scores, ld = _rows2d(scores, "scores")
     rows, n = scores.shape
@@ -1007,9 +1013,9 @@ def ann_beam_select(scores, totals, beams, k, finished=None, pad_id=0, parents_o
     if beams < 1 or rows % beams:
         raise ValueError(f"scores must have whole groups of {beams} rows")
     groups = rows // beams
-    _one_value_per_row(totals, "totals", torch.float32, rows, device)
+    _one_value_per_beam(totals, "totals", torch.float32, groups, beams, device)
     if finished is not None:
-        _one_value_per_row(finished, "finished", torch.bool if finished.dtype != torch.uint8 else torch.uint8, rows, device)
+        _one_value_per_beam(finished, "finished", torch.bool if finished.dtype != torch.uint8 else torch.uint8, groups, beams, device)
         if not 0 <= pad_id < n:
             raise ValueError(f"pad_id must be 0 to {n - 1}")
     need = C.c_uint64(0)

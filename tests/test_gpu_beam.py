@@ -232,6 +232,18 @@ def test_totals_in_place(env):
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(totals.view(100, 4), want[2])
 
 
+def test_totals_of_the_last_step(env):
+    torch, A, _ = env
+    rng = np.random.default_rng(14)
+    z = scores_of(torch, rng, 12, 300, "float32")
+    finished = dev(torch, rng.random(12) < 0.3)
+    _, _, totals = A.ann_beam_select(z, dev(torch, -rng.random(12).astype(np.float32)), 4, 4)
+    assert totals.shape == (3, 4)
+    want = A.ann_beam_select(z, totals.flatten(), 4, 4, finished=finished, pad_id=2)
+    got = A.ann_beam_select(z, totals, 4, 4, finished=finished.view(3, 4), pad_id=2)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_streams_graphs_and_repeats(env):
     torch, A, _ = env
     rng = np.random.default_rng(5)

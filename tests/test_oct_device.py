@@ -70,3 +70,15 @@ def test_shapes_and_types_are_refused(calls):  # noqa: F811
         calls.clear()
         with pytest.raises((ValueError, TypeError)):
             call()
+
+
+def test_totals_are_the_next_steps_as_they_are(calls):  # noqa: F811
+    x = Tensor((6, 200))
+    _, _, totals = A.ann_beam_select(x, Tensor(6), 3, 3)
+    A.ann_beam_select(x, totals, 3, 3, finished=Tensor((2, 3), torch.bool))
+    assert [c[0] for c in calls] == ["ann_beam_select"] * 2
+    for shape in ((3, 2), (6, 1), (2, 4), (2, 3, 1)):
+        with pytest.raises(ValueError):
+            A.ann_beam_select(x, Tensor(shape), 3, 3)
+        with pytest.raises(ValueError):
+            A.ann_beam_select(x, totals, 3, 3, finished=Tensor(shape, torch.bool))
