@@ -659,7 +659,8 @@ int ann_sample_scratch(uint64_t rows, uint64_t n, uint64_t* bytes);
  * loss 0, gradient 0.  NaN and +inf among the scores make the row's loss NaN and
  * its gradients NaN.  Among the entries that are there they make the loss NaN, and
  * the gradients of the scores that they name.
- *   scores_dev    rows x n of ANN_F32, ANN_F16 or ANN_BF16, ld apart; n < 2^31
+ *   scores_dev    rows x n of ANN_F32, ANN_F16 or ANN_BF16, ld apart; n < 2^31,
+ *                 rows * ld (and rows * ldo) at most 2^60
  *   ids_dev       rows x k uint32; teacher_dev rows x k of ANN_F32, ANN_F16 or
  *                 ANN_BF16; 1 <= k <= 1024
  *   losses_dev    rows floats

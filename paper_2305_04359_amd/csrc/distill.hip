@@ -16,6 +16,7 @@ namespace annmi {
 
 constexpr u32 DISTILL_MOST_K = 1024;
 constexpr u32 DISTILL_THREADS = 256;
+constexpr u64 DISTILL_MOST_PLACE = 1ull << 60;  // elements from a matrix's beginning: 64 bits hold their bytes
 
 struct DistillArgs {
   const char* scores;
@@ -366,6 +367,7 @@ int check_distill(const char* what, const void* scores, u64 rows, u64 n, int dty
   if (n < 1 || n >= 1ull << 31) return fail(ANN_EINVAL, "%s: n must be 1 to 2^31 - 1", what);
   if (k < 1 || k > DISTILL_MOST_K) return fail(ANN_EINVAL, "%s: k must be 1 to %u", what, DISTILL_MOST_K);
   if (ld < n) return fail(ANN_EINVAL, "%s: ld must be at least n", what);
+  if (rows && ld > DISTILL_MOST_PLACE / rows) return fail(ANN_EINVAL, "%s: rows * ld must be at most 2^60", what);
   // (log2(e) / T and T^2 then are ordinary numbers)
   if (!(temperature >= 0x1p-60f && temperature <= 0x1p60f)) return fail(ANN_EINVAL, "%s: temperature must be 2^-60 to 2^60", what);
   if (rows == 0) return ANN_OK;
@@ -433,6 +435,7 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
   int rc = check_distill("ann_distill_grad", scores_dev, rows, n, dtype, ld, ids_dev, teacher_dev, teacher_dtype, k, temperature, stats_dev, &work);
   if (rc) return rc;
   if (ldo < n) return fail(ANN_EINVAL, "ldo must be at least n");
+  if (rows && ldo > DISTILL_MOST_PLACE / rows) return fail(ANN_EINVAL, "rows * ldo must be at most 2^60");
   if (!work) return ANN_OK;
   if (!out_dev) return fail(ANN_EINVAL, "null argument");
   if (!aligned_to(out_dev, dtype_bytes(dtype)) || !aligned_to(grad_losses_dev, 4)) return fail(ANN_EINVAL, "out or grad_losses not aligned to their elements");

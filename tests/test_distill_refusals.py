@@ -47,3 +47,12 @@ def test_binding_refuses_host_tensors():
     z, i = torch.zeros(3, 4), torch.zeros((3, 2), dtype=torch.int32)
     with pytest.raises(ValueError):
         A.ann_distill(z, i, torch.zeros(3, 2))
+
+
+def test_strides_beyond_memory_are_refused():
+    # (4 * 2^62 and 4 * 3 * 2^60 leave 64 bits)
+    for rows, big in ((1, 1 << 62), (3, 1 << 60), (2, 1 << 63)):
+        refused("ann_distill", *{**LOSS, "rows": rows, "ld": big}.values())
+        refused("ann_distill_grad", *{**GRAD, "rows": rows, "ld": big}.values())
+        refused("ann_distill_grad", *{**GRAD, "rows": rows, "ldo": big}.values())
+        refused("ann_distill_grad", *{**GRAD, "rows": rows, "ld": big, "ldo": big}.values())
