@@ -699,7 +699,7 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
  *   parents_dev, ids_dev, totals_out_dev  groups x k: the beam (0 to beams - 1),
  *                 the entry and v, rounded to fp32; ANN_NONE, ANN_NONE, -inf where
  *                 there are fewer than k.  With k = beams totals_out_dev may be
- *                 totals_dev itself
+ *                 totals_dev itself; they must not overlap otherwise
  *   scratch_dev   at least what ann_beam_select_scratch says, 16-byte aligned
  * 1 <= beams <= 64, 1 <= k <= 128, 1 <= n < 2^24, groups * beams < 2^31.
  * Asynchronous on `stream` and on the current device, which has to be that of

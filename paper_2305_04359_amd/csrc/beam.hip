@@ -499,6 +499,10 @@ int ann_beam_select(const void* scores_dev, uint64_t groups, uint32_t beams, uin
     return fail(ANN_EINVAL, "an array is not aligned to its elements");
   if (scratch_bytes < need) return fail(ANN_EINVAL, "scratch must hold %llu bytes", (unsigned long long)need);
   if (!aligned_to(scratch_dev, 16)) return fail(ANN_EINVAL, "scratch must be 16-byte aligned");
+  // (one group's results may be there before another has read its beams' totals)
+  const uintptr_t from = reinterpret_cast<uintptr_t>(totals_dev), to = reinterpret_cast<uintptr_t>(totals_out_dev);
+  if (!(from == to && k == beams) && from < to + groups * k * 4 && to < from + groups * beams * 4)
+    return fail(ANN_EINVAL, "the totals must lie apart, or in one place with k = beams");
   BeamArgs a{};
   a.scores = static_cast<const char*>(scores_dev);
   a.groups = groups;

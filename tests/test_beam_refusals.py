@@ -31,6 +31,13 @@ def test_refused(name, good, bad):
     refused(name, *{**good, **bad}.values())
 
 
+def test_totals_that_overlap_are_refused():
+    # 12 totals of the beams; 3 x k of the continuations, whose groups' places are others than the beams' unless k = beams
+    apart = dict(totals=PTR, out=FAR)
+    for bad in (dict(out=PTR, k=8), dict(out=PTR, k=3), dict(out=PTR + 4, k=4), dict(out=PTR + 44, k=4), dict(out=PTR - 4 * 3 * 4 + 4, k=4), dict(out=PTR - 4 * 3 * 8 + 4, k=8)):
+        refused("ann_beam_select", *{**SELECT, **apart, **bad}.values())
+
+
 def test_nothing_to_do_reads_no_pointer():
     L = A.lib()
     assert L.ann_beam_select(*{**SELECT, "groups": 0, "scores": None, "totals": None, "parents": None, "ids": None, "out": None, "scratch": None}.values()) == 0
