@@ -119,12 +119,76 @@ __global__ __launch_bounds__(256) void oct_quantize_kernel(OctQuantizeArgs a) {
 
 // Columns: row i of the result is column i of x, which has d rows.  A workgroup takes a step of COLS columns: a thread EACH
 // elements of four neighbouring columns, whose maxima meet in LDS; through LDS the codes get into whole rows of 128 bytes.
-// From memory 16,384 columns of 4,096 fp32 take 81 us, 4.1 TB/s, and 4,096 of 16,384 bf16 68 us, 3.0 TB/s, for which eight
-// bytes are a load; sixteen, of eight columns, and half as many rows a thread take 80, for the smaller pieces in LDS.
+// Inputs stay the words that they are in memory until they are codes, with maxima of two 16-bit ones at once: held as fp32 they
+// take 188 registers, two waves a SIMD, and 67 us from memory for 4,096 columns of 16,384 bf16, so 97 and 43, 4.6 TB/s.
+// 16,384 columns of 4,096 fp32 come past the caches in 65 us, 5.2 TB/s, and through them in 81, also from a cache that has them
+// (67 MB 15 and 21); to 16-bit ones it makes no difference.
 constexpr u32 COLS = 128;
 constexpr u32 COLUMN_EACH = 16, COLUMN_PARTS = OCT_STEP / COLUMN_EACH, COLUMN_THREADS = COLS / 4 * COLUMN_PARTS;
+// four neighbouring elements of a row, as they are in memory
 template <typename T>
-__global__ __launch_bounds__(COLUMN_THREADS) void oct_columns_kernel(OctQuantizeArgs a, u32 across, u64 tiles) {
+using Four = Pack<u32, sizeof(T)>;
+template <typename T>
+__device__ __forceinline__ Four<T> four_at(const T* from) {
+  if constexpr (sizeof(T) == 4) {
+    using Streamed = v4i __attribute__((aligned(4)));
+    return __builtin_bit_cast(Four<T>, v4i(__builtin_nontemporal_load(reinterpret_cast<const Streamed*>(from))));
+  } else {
+    return __builtin_bit_cast(Four<T>, *reinterpret_cast<const AnyPack<T, 4>*>(from));
+  }
+}
+template <typename T>
+__device__ __forceinline__ float four_get(const Four<T>& four, u32 k) {
+  if constexpr (sizeof(T) == 4)
+    return __uint_as_float(four.v[k]);
+  else if constexpr (std::is_same_v<T, __bf16>)
+    return __uint_as_float(k % 2 ? four.v[k / 2] & 0xFFFF0000u : four.v[k / 2] << 16);
+  else if constexpr (sizeof(T) == 2)
+    return mx_float(__builtin_bit_cast(__half, (uint16_t)(four.v[k / 2] >> (k % 2 * 16))));
+  else if constexpr (std::is_same_v<T, int8_t>)
+    return (float)(int8_t)(four.v[0] >> (8 * k));
+  else
+    return (float)(uint8_t)(four.v[0] >> (8 * k));
+}
+// the largest magnitudes of EACH elements of four columns, as fp32's bits
+template <typename T>
+__device__ __forceinline__ Pack<u32, 4> four_most(const Four<T> (&in)[COLUMN_EACH]) {
+  Pack<u32, 4> most = {{0, 0, 0, 0}};
+  if constexpr (sizeof(T) == 2) {  // magnitudes compare like their bits: two at once
+    using v2h = uint16_t __attribute__((ext_vector_type(2)));
+    v2h low = {0, 0}, high = {0, 0};
+#pragma unroll
+    for (u32 e = 0; e < COLUMN_EACH; ++e) {
+      low = __builtin_elementwise_max(low, __builtin_bit_cast(v2h, in[e].v[0] & 0x7FFF7FFFu));
+      high = __builtin_elementwise_max(high, __builtin_bit_cast(v2h, in[e].v[1] & 0x7FFF7FFFu));
+    }
+    const Four<T> all = {{__builtin_bit_cast(u32, low), __builtin_bit_cast(u32, high)}};
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) most.v[k] = __float_as_uint(four_get<T>(all, k));
+  } else if constexpr (sizeof(T) == 1) {  // as whole numbers of 16 bits, two at once: columns 0 and 2, 1 and 3
+    using v2s = std::conditional_t<std::is_same_v<T, int8_t>, int16_t, uint16_t> __attribute__((ext_vector_type(2)));
+    v2s top[2] = {}, low[2] = {};
+#pragma unroll
+    for (u32 e = 0; e < COLUMN_EACH; ++e) {
+      const v2s both = __builtin_bit_cast(v2s, in[e].v[0]), part[2] = {(v2s)(both << 8) >> 8, both >> 8};
+#pragma unroll
+      for (u32 o = 0; o < 2; ++o) {
+        top[o] = __builtin_elementwise_max(top[o], part[o]);
+        low[o] = __builtin_elementwise_min(low[o], part[o]);
+      }
+    }
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) most.v[k] = __float_as_uint((float)max((int)top[k % 2][k / 2], -(int)low[k % 2][k / 2]));
+  } else {
+#pragma unroll
+    for (u32 e = 0; e < COLUMN_EACH; ++e)
+#pragma unroll
+      for (u32 k = 0; k < 4; ++k) most.v[k] = max(most.v[k], __float_as_uint(four_get<T>(in[e], k)) & 0x7FFFFFFFu);
+  }
+  return most;
+}
+template <typename T>
+__global__ __launch_bounds__(COLUMN_THREADS, 4) void oct_columns_kernel(OctQuantizeArgs a, u32 across, u64 tiles) {
   using Part = Pack<u32, COLUMN_EACH / 4>;  // a thread's codes of a column
   __shared__ u32 most_of[COLUMN_PARTS][COLS];
   __shared__ __align__(16) char codes[COLS * OCT_STEP];
@@ -135,27 +199,30 @@ __global__ __launch_bounds__(COLUMN_THREADS) void oct_columns_kernel(OctQuantize
     const u32 step = (u32)(t / across);
     const u32 e0 = step * OCT_STEP + g * COLUMN_EACH;
     const u32 there = (u32)min((u64)COLS, a.n - i0);
-    AnyPack<T, 4> in[COLUMN_EACH];
-    if (c + 4 <= there) {
+    const T* x = reinterpret_cast<const T*>(a.x) + i0;
+    Four<T> in[COLUMN_EACH];
+    if (there == COLS && step * OCT_STEP + OCT_STEP <= a.d) {
+      const T* from = x + (u64)e0 * a.ldx + c;
 #pragma unroll
-      for (u32 e = 0; e < COLUMN_EACH; ++e)
-        in[e] = *reinterpret_cast<const AnyPack<T, 4>*>(reinterpret_cast<const T*>(a.x) + (u64)min(e0 + e, a.d - 1) * a.ldx + i0 + c);
+      for (u32 e = 0; e < COLUMN_EACH; ++e) in[e] = four_at<T>(from + e * a.ldx);
     } else {
 #pragma unroll
-      for (u32 e = 0; e < COLUMN_EACH; ++e)
+      for (u32 e = 0; e < COLUMN_EACH; ++e) {
+        const T* from = x + (u64)min(e0 + e, a.d - 1) * a.ldx;
+        if (c + 4 <= there) {
+          in[e] = four_at<T>(from + c);
+        } else {
+          AnyPack<T, 4> four;
 #pragma unroll
-        for (u32 k = 0; k < 4; ++k) in[e].v[k] = reinterpret_cast<const T*>(a.x)[(u64)min(e0 + e, a.d - 1) * a.ldx + i0 + min(c + k, there - 1)];
-    }
-    float v[4][COLUMN_EACH];
-    u32 most[4] = {};
+          for (u32 k = 0; k < 4; ++k) four.v[k] = from[min(c + k, there - 1)];
+          in[e] = __builtin_bit_cast(Four<T>, four);
+        }
+        if (e0 + e >= a.d)
 #pragma unroll
-    for (u32 e = 0; e < COLUMN_EACH; ++e)
-#pragma unroll
-      for (u32 k = 0; k < 4; ++k) {
-        v[k][e] = e0 + e < a.d ? mx_float(static_cast<T>(in[e].v[k])) : 0.0f;
-        most[k] = max(most[k], __float_as_uint(v[k][e]) & 0x7FFFFFFFu);
+          for (u32 w = 0; w < sizeof(T); ++w) in[e].v[w] = 0;
       }
-    *reinterpret_cast<Pack<u32, 4>*>(&most_of[g][c]) = {{most[0], most[1], most[2], most[3]}};
+    }
+    *reinterpret_cast<Pack<u32, 4>*>(&most_of[g][c]) = four_most<T>(in);
     __syncthreads();
     // a column's maximum: each thread's four, of all parts
     u32 m[4] = {};
@@ -172,7 +239,9 @@ __global__ __launch_bounds__(COLUMN_THREADS) void oct_columns_kernel(OctQuantize
       Part code;
 #pragma unroll
       for (u32 q = 0; q < COLUMN_EACH / 4; ++q)
-        code.v[q] = byte == 255 ? 0u : oct_codes(v[k][4 * q] * inverse, v[k][4 * q + 1] * inverse, v[k][4 * q + 2] * inverse, v[k][4 * q + 3] * inverse);
+        code.v[q] = oct_codes(four_get<T>(in[4 * q], k) * inverse, four_get<T>(in[4 * q + 1], k) * inverse, four_get<T>(in[4 * q + 2], k) * inverse,
+                              four_get<T>(in[4 * q + 3], k) * inverse);
+      if (byte == 255) code = {};
       // pieces of 16 bytes change places by the column's number
       const u32 r = c + k, at = g * COLUMN_EACH;
       *reinterpret_cast<Part*>(codes + r * OCT_STEP + ((at / 16 ^ (r / 4 + r) % 8) * 16 | at % 16)) = code;
