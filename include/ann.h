@@ -566,8 +566,8 @@ int ann_mx_search_scratch(uint64_t n, uint32_t d, uint64_t nq, uint32_t k, uint6
  *   alignment   codes 16 bytes, scales 4; the other matrices of these calls
  *               that of their element, with a row stride of their own (`ld`,
  *               in elements, at least the row's length)
- *   sizes       1 <= d <= 1048576; rows < 2^30; a count of zero rows: ANN_OK,
- *               nothing is done and no pointer is read
+ *   sizes       1 <= d <= 1048576; rows < 2^30, steps of all rows < 2^32; a count
+ *               of zero rows: ANN_OK, nothing is done and no pointer is read
  * All calls are asynchronous on `stream`, allocate nothing, keep nothing and
  * can be captured into a graph.  They launch on the current device, which has to
  * be that of the stream and of all pointers.  Arguments they cannot serve:

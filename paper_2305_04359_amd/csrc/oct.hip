@@ -1,4 +1,5 @@
 // Rows or columns to 8-bit floating point with a scale for each 128 elements, and back.
+#include <algorithm>
 #include <type_traits>
 
 #include "oct.hpp"
@@ -8,6 +9,7 @@ namespace annmi {
 int check_oct_rows(const char* what, const uint8_t* codes, const uint8_t* scales, u64 n, u32 d) {
   if (n > OCT_MOST_ROWS) return fail(ANN_EINVAL, "%s: rows must stay below 2^30", what);
   if (d < 1 || d > OCT_MOST_D) return fail(ANN_EINVAL, "%s: d must be 1 to %u", what, OCT_MOST_D);
+  if (n * oct_steps(d) >> 32) return fail(ANN_EINVAL, "%s: rows * ceil(d / 128) must stay below 2^32", what);
   if (n == 0) return ANN_OK;
   if (!codes || !scales) return fail(ANN_EINVAL, "null argument");
   if (!aligned_to(codes, 16)) return fail(ANN_EINVAL, "%s: codes must be 16-byte aligned", what);
@@ -50,69 +52,75 @@ __device__ __forceinline__ u32 max_of_16(u32 v) {
   return row_max<0x128>(v);
 }
 
-// Rows.  Sixteen lanes take a step, eight elements each; LPR lanes (16, 32 or 64: one, two or four steps) take a row, longer
-// rows in turns of four steps, whose scale bytes are a word.  A wave asks for four such pieces at once.
+// Rows.  Sixteen lanes take a step, eight elements each, whichever row it is of: steps without gaps are where their codes lie.
+// A row a wave, four turns ahead, takes 291 us for 131,072 x 4,096 bf16, 55 for 100,000 x 640 bytes (half of its lanes have nothing),
+// 242 for 64 x 200,000 fp32 and 5 for 1 x 4,096 bf16; so 268 (5.9 TB/s), 25, 14 and 2 (200,000 x 1,000 fp32 176 and 185).
+// Stores past the caches take 260 for the first, but the products that read the codes next lose more.
 // WIDE: every row has eight elements at least; eight are then read at once, past d too, but in the last rows, whose
 // last eight are read where these would reach past the end of the last row.
-template <typename T, int LPR, bool WIDE>
-__global__ __launch_bounds__(256) void oct_quantize_kernel(OctQuantizeArgs a) {
-  constexpr u32 AHEAD = 4, PER_BLOCK = 256 / LPR;
-  const u32 lane = threadIdx.x % LPR;
+constexpr u32 ROW_STEPS = 16;
+template <typename T>
+constexpr u32 row_ahead = sizeof(T) == 1 ? 4 : 2;  // steps that a thread asks for at once (of bytes 25 us, with two 28; bf16 268, with four 287)
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(256) void oct_quantize_kernel(OctQuantizeArgs a, u64 items, u32 reciprocal) {
+  constexpr u32 ROW_AHEAD = row_ahead<T>, ROW_TILE = ROW_STEPS * ROW_AHEAD;
+  const u32 lane = threadIdx.x % 16, group = threadIdx.x / 16;
   const u32 words = oct_words(a.steps);
-  const u32 turns = LPR < 64 ? 1 : words;
-  const bool rows_ahead = turns == 1;  // four rows at once, else four turns of a row
-  const u64 stride = (u64)gridDim.x * PER_BLOCK;
-  for (u64 r0 = (u64)blockIdx.x * PER_BLOCK + threadIdx.x / LPR; r0 < a.n; r0 += rows_ahead ? stride * AHEAD : stride) {
-    for (u32 t0 = 0; t0 < turns; t0 += AHEAD) {
-      AnyPack<T, 8> in[AHEAD];
-      u64 row[AHEAD];
-      u32 at[AHEAD], early[AHEAD];
+  for (u64 base = (u64)blockIdx.x * ROW_TILE; base < items; base += (u64)gridDim.x * ROW_TILE) {
+    const u64 row0 = (u32)base / a.steps;
+    const u32 step0 = (u32)(base - row0 * a.steps);
+    AnyPack<T, 8> in[ROW_AHEAD];
+    u64 row[ROW_AHEAD];
+    u32 step[ROW_AHEAD], early[ROW_AHEAD];
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) {
-        row[u] = rows_ahead ? r0 + stride * u : r0;
-        at[u] = (rows_ahead ? 0 : t0 + u) * (4 * OCT_STEP) + lane * 8;  // the lane's first element
-        const u64 r = min(row[u], (u64)a.n - 1);
-        const T* from = reinterpret_cast<const T*>(a.x) + r * a.ldx;
-        early[u] = 0;
-        if (WIDE) {
-          const u32 first = at[u] < a.d ? at[u] : 0;
-          early[u] = (a.n - 1 - r) * a.ldx < 7 && first + 8 > a.d ? first + 8 - a.d : 0;
-          in[u] = *reinterpret_cast<const AnyPack<T, 8>*>(from + (first - early[u]));
-        } else {
+    for (u32 u = 0; u < ROW_AHEAD; ++u) {
+      const u32 from0 = step0 + u * ROW_STEPS + group;
+      const u32 rows = a.steps == 1 ? from0 : __umulhi(from0, reciprocal);
+      step[u] = from0 - rows * a.steps;
+      row[u] = row0 + rows;
+      const u64 r = min(row[u], (u64)a.n - 1);
+      const T* from = reinterpret_cast<const T*>(a.x) + r * a.ldx;
+      const u32 at = step[u] * OCT_STEP + lane * 8;  // the lane's first element
+      early[u] = 0;
+      if (WIDE) {
+        const u32 first = at < a.d ? at : 0;
+        early[u] = (a.n - 1 - r) * a.ldx < 7 && first + 8 > a.d ? first + 8 - a.d : 0;
+        in[u] = *reinterpret_cast<const AnyPack<T, 8>*>(from + (first - early[u]));
+      } else {
 #pragma unroll
-          for (u32 e = 0; e < 8; ++e) in[u].v[e] = from[min(at[u] + e, a.d - 1)];
-        }
+        for (u32 e = 0; e < 8; ++e) in[u].v[e] = from[min(at + e, a.d - 1)];
       }
+    }
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) {
-        const bool on = row[u] < a.n && at[u] / (4 * OCT_STEP) < words;  // (all lanes of a row alike)
-        if (!on) continue;
-        float v[8];
+    for (u32 u = 0; u < ROW_AHEAD; ++u) {
+      const u64 item = base + u * ROW_STEPS + group;
+      if (item >= items) break;  // (all lanes of a step alike)
+      const u32 at = step[u] * OCT_STEP + lane * 8;
+      float v[8];
 #pragma unroll
-        for (u32 e = 0; e < 8; ++e) v[e] = mx_float(static_cast<T>(in[u].v[e]));
+      for (u32 e = 0; e < 8; ++e) v[e] = mx_float(static_cast<T>(in[u].v[e]));
+      if (at + 8 > a.d) {  // the row's end
         if (WIDE && early[u])
           for (u32 k = 0; k < early[u]; ++k)
 #pragma unroll
             for (u32 e = 0; e < 7; ++e) v[e] = v[e + 1];
-        u32 most = 0;  // magnitudes compare like their bits, and so do NaN and infinity
 #pragma unroll
-        for (u32 e = 0; e < 8; ++e) {
-          v[e] = at[u] + e < a.d ? v[e] : 0.0f;
-          most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-        }
-        const u32 byte = oct_scale_byte(max_of_16(most));
-        const float inverse = oct_inverse(byte);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= inverse;
-        Pack<u32, 2> code = {{oct_codes(v[0], v[1], v[2], v[3]), oct_codes(v[4], v[5], v[6], v[7])}};
-        if (byte == 255) code = {{0, 0}};
-        const u32 step = at[u] / OCT_STEP;
-        u32 word = (step < a.steps ? byte : 0u) << (step % 4 * 8);
-        if (LPR > 16) word |= __shfl_xor(word, 16);
-        if (LPR > 32) word |= __shfl_xor(word, 32);
-        if (step < a.steps) *reinterpret_cast<Pack<u32, 2>*>(a.codes + (row[u] * a.steps + step) * OCT_STEP + lane % 16 * 8) = code;
-        if (lane == 0) a.scales[row[u] * words + step / 4] = word;
+        for (u32 e = 0; e < 8; ++e) v[e] = at + e < a.d ? v[e] : 0.0f;
       }
+      u32 most = 0;  // magnitudes compare like their bits, and so do NaN and infinity
+#pragma unroll
+      for (u32 e = 0; e < 8; ++e) most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+      const u32 byte = oct_scale_byte(max_of_16(most));
+      const float inverse = oct_inverse(byte);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= inverse;
+      Pack<u32, 2> code = {{oct_codes(v[0], v[1], v[2], v[3]), oct_codes(v[4], v[5], v[6], v[7])}};
+      if (byte == 255) code = {{0, 0}};
+      *reinterpret_cast<Pack<u32, 2>*>(a.codes + item * OCT_STEP + lane * 8) = code;
+      // the step's byte, and the rest of the last word
+      const u32 scale = step[u] + lane;
+      if (lane == 0 || (step[u] + 1 == a.steps && scale < words * 4))
+        reinterpret_cast<uint8_t*>(a.scales)[row[u] * words * 4 + scale] = lane == 0 ? (uint8_t)byte : 0;
     }
   }
 }
@@ -264,16 +272,11 @@ __global__ __launch_bounds__(COLUMN_THREADS, 4) void oct_columns_kernel(OctQuant
 
 template <typename T, bool WIDE>
 hipError_t launch_oct_rows(const OctQuantizeArgs& a, hipStream_t s) {
-  const u32 lpr = a.steps == 1 ? 16 : a.steps == 2 ? 32 : 64;
-  // four rows for each place, where a turn takes a row
-  const u64 per = 256 / lpr * (a.steps <= 4 ? 4 : 1), blocks = ((u64)a.n + per - 1) / per;
-  const u32 grid = (u32)(blocks < (1u << 20) ? blocks : (1u << 20));
-  auto kernel = oct_quantize_kernel<T, 16, WIDE>;
-  if constexpr (WIDE) {  // (others have one step)
-    if (lpr == 32) kernel = oct_quantize_kernel<T, 32, WIDE>;
-    if (lpr == 64) kernel = oct_quantize_kernel<T, 64, WIDE>;
-  }
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, a);
+  constexpr u32 ROW_TILE = ROW_STEPS * row_ahead<T>;
+  const u64 items = (u64)a.n * a.steps, blocks = (items + ROW_TILE - 1) / ROW_TILE;
+  // 2^32 / steps rounded up: from 2 to 2^13 steps and places below 2^13 + 64 their product's upper half is the quotient
+  const u32 reciprocal = (u32)(((1ull << 32) + a.steps - 1) / a.steps);
+  hipLaunchKernelGGL((oct_quantize_kernel<T, WIDE>), dim3((u32)std::min<u64>(blocks, 1u << 20)), dim3(256), 0, s, a, items, reciprocal);
   return hipGetLastError();
 }
 template <typename T>
@@ -294,48 +297,52 @@ struct OctDequantizeArgs {
   u64 ldo;
 };
 
-// A thread takes 16 bytes of a row of `out`, and the same ones of other rows in turn.  Bound by memory: 4,096 rows of 16,384 to
-// fp32 take 64 us, 5.2 TB/s.
+// Pieces of 16 bytes of `out`, its rows one after another, two for a thread.  They go past the caches, which also serves who
+// reads them next: 4,096 x 16,384 bf16 and a copy of them 87 us from memory, with plain stores 107 (67 MB that a cache holds 41
+// and 40).  A row's pieces in turn by one workgroup with plain stores: 131,072 x 4,096 bf16 442 us, so 251 (6.4 TB/s);
+// 64 x 200,000 fp32 263 and 14.
+constexpr u32 DEQUANTIZE_AHEAD = 2, DEQUANTIZE_TILE = 256 * DEQUANTIZE_AHEAD;
 template <typename T>
-__global__ __launch_bounds__(256) void oct_dequantize_kernel(OctDequantizeArgs a) {
-  constexpr u32 E = 16 / sizeof(T), AHEAD = 4;  // elements; rows at a time
+__global__ __launch_bounds__(256) void oct_dequantize_kernel(OctDequantizeArgs a, u32 pieces, u64 items) {
+  constexpr u32 E = 16 / sizeof(T), AHEAD = DEQUANTIZE_AHEAD;
   using v2f = float __attribute__((ext_vector_type(2)));
-  const u32 pieces = (a.d + E - 1) / E;
-  const u32 across = pieces < 256 ? pieces : 256, rows = 256 / across;  // of a block
-  const u32 sub = threadIdx.x / across;
-  if (sub >= rows) return;
-  const u64 stride = (u64)gridDim.x * rows;
+  using Streamed = v4i __attribute__((aligned(2)));
   const u32 words = oct_words(a.steps);
-  for (u64 r0 = (u64)blockIdx.x * rows + sub; r0 < a.n; r0 += stride * AHEAD) {
-    for (u32 c = threadIdx.x % across; c < pieces; c += across) {
-      Pack<u32, E / 4> code[AHEAD];
-      float scale[AHEAD];
+  for (u64 base = (u64)blockIdx.x * DEQUANTIZE_TILE; base < items; base += (u64)gridDim.x * DEQUANTIZE_TILE) {
+    const u64 row0 = items >> 32 ? base / pieces : (u32)base / pieces;
+    const u32 p0 = (u32)(base - row0 * pieces);
+    Pack<u32, E / 4> code[AHEAD];
+    float scale[AHEAD];
+    u64 row[AHEAD];
+    u32 c[AHEAD];
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) {
-        const u64 r = min(r0 + stride * u, a.n - 1);
-        code[u] = *reinterpret_cast<const Pack<u32, E / 4>*>(a.codes + r * a.steps * OCT_STEP + c * E);
-        scale[u] = mx_scale(a.scales[r * words * 4 + c * E / OCT_STEP]);
+    for (u32 u = 0; u < AHEAD; ++u) {
+      const u32 p = p0 + u * 256 + threadIdx.x, rows = p / pieces;
+      c[u] = p - rows * pieces;
+      row[u] = row0 + rows;
+      const u64 r = min(row[u], a.n - 1);
+      code[u] = *reinterpret_cast<const Pack<u32, E / 4>*>(a.codes + r * a.steps * OCT_STEP + c[u] * E);
+      scale[u] = mx_scale(a.scales[r * words * 4 + c[u] * E / OCT_STEP]);
+    }
+#pragma unroll
+    for (u32 u = 0; u < AHEAD; ++u) {
+      if (row[u] >= a.n) break;
+      AnyPack<T, E> o;
+#pragma unroll
+      for (u32 q = 0; q < E / 4; ++q) {
+        const v2f low = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[u].v[q], false), high = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[u].v[q], true);
+        o.v[4 * q] = mx_round<T>(low.x * scale[u]);
+        o.v[4 * q + 1] = mx_round<T>(low.y * scale[u]);
+        o.v[4 * q + 2] = mx_round<T>(high.x * scale[u]);
+        o.v[4 * q + 3] = mx_round<T>(high.y * scale[u]);
       }
+      T* to = reinterpret_cast<T*>(a.out) + row[u] * a.ldo + c[u] * E;
+      if (c[u] * E + E <= a.d) {
+        __builtin_nontemporal_store(__builtin_bit_cast(v4i, o), reinterpret_cast<Streamed*>(to));
+      } else {
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) {
-        if (r0 + stride * u >= a.n) break;
-        AnyPack<T, E> o;
-#pragma unroll
-        for (u32 q = 0; q < E / 4; ++q) {
-          const v2f low = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[u].v[q], false), high = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[u].v[q], true);
-          o.v[4 * q] = mx_round<T>(low.x * scale[u]);
-          o.v[4 * q + 1] = mx_round<T>(low.y * scale[u]);
-          o.v[4 * q + 2] = mx_round<T>(high.x * scale[u]);
-          o.v[4 * q + 3] = mx_round<T>(high.y * scale[u]);
-        }
-        T* to = reinterpret_cast<T*>(a.out) + (r0 + stride * u) * a.ldo + c * E;
-        if (c * E + E <= a.d) {
-          *reinterpret_cast<AnyPack<T, E>*>(to) = o;
-        } else {
-#pragma unroll
-          for (u32 j = 0; j < E; ++j)
-            if (c * E + j < a.d) to[j] = o.v[j];
-        }
+        for (u32 k = 0; k < E; ++k)
+          if (c[u] * E + k < a.d) to[k] = o.v[k];
       }
     }
   }
@@ -343,9 +350,9 @@ __global__ __launch_bounds__(256) void oct_dequantize_kernel(OctDequantizeArgs a
 
 template <typename T>
 hipError_t launch_oct_dequantize(const OctDequantizeArgs& a, hipStream_t s) {
-  const u32 pieces = (u32)((a.d + 16 / sizeof(T) - 1) / (16 / sizeof(T))), rows = pieces < 256 ? 256 / pieces : 1;
-  const u64 blocks = (a.n + 4 * rows - 1) / (4 * rows);
-  hipLaunchKernelGGL(oct_dequantize_kernel<T>, dim3((u32)(blocks < (1u << 20) ? blocks : (1u << 20))), dim3(256), 0, s, a);
+  const u32 pieces = (u32)((a.d + 16 / sizeof(T) - 1) / (16 / sizeof(T)));
+  const u64 items = a.n * pieces, blocks = (items + DEQUANTIZE_TILE - 1) / DEQUANTIZE_TILE;
+  hipLaunchKernelGGL(oct_dequantize_kernel<T>, dim3((u32)std::min<u64>(blocks, 1u << 23)), dim3(256), 0, s, a, pieces, items);
   return hipGetLastError();
 }
 

@@ -53,6 +53,25 @@ def test_quantize(env, dtype, n, d, columns):
         assert torch.equal(room._base, around), "elements beside the rows changed"
 
 
+@pytest.mark.parametrize("dtype", ("float32", "bfloat16", "int8"))
+@pytest.mark.parametrize("n,d", [(1, 20_000), (33, 16_384), (64, 513), (70, 385), (999, 130), (1000, 1), (40, 640), (11, 100_003), (2, 1 << 20), (300, 2000)])
+def test_steps_of_many_rows(env, dtype, n, d):
+    """Long rows, and rows that begin and end inside what a workgroup takes at once; there and back, in wider rows too."""
+    torch, A, _ = env
+    x = rows_of(torch, np.random.default_rng(n + d), n, d, dtype)
+    want = P.quantize(x.double().cpu().numpy())
+    for given in (x, wider(torch, x, 5)):
+        got = A.ann_oct_quantize(given)
+        assert (got.scales.cpu().numpy() == want[1]).all() and (got.codes.cpu().numpy() == want[0]).all()
+    exact = torch.from_numpy(P.values(*want, d))
+    for out in (torch.float32, torch.bfloat16):
+        room = wider(torch, torch.zeros((n, d), dtype=out, device=x.device), 7)
+        around = room._base.clone()
+        A.ann_oct_dequantize(got, out=room)
+        around[:, 3:3 + d] = exact.to(out).to(x.device)
+        assert torch.equal(room._base, around)
+
+
 @pytest.mark.parametrize("columns", (False, True))
 def test_quantize_edges(env, columns):
     """Every code and every middle between two, numbers at the ends of fp32, infinities and NaN in a step of their own."""
@@ -259,6 +278,24 @@ def test_offsets_beyond_32_bits(env):
     out = A.ann_oct_product(few, rows, dtype=torch.bfloat16)  # 1,100 x 4.2 million
     assert out.numel() > 1 << 32 and torch.equal(out[-1].float(), A.ann_oct_product(want, rows, dtype=torch.bfloat16)[0].float())
     assert (out[:-1, :-1] == 0).all() and (out[:-1, -1] == 0).all()
+
+
+def test_values_of_more_pieces_than_32_bits_count(env):
+    """2^27 rows and some of 127 fp32 values, 32 pieces of 16 bytes each."""
+    torch, A, _ = env
+    n = (1 << 27) + 77
+    codes = torch.zeros((n, 128), dtype=torch.uint8, device="cuda")
+    scales = torch.full((n, 4), 127, dtype=torch.uint8, device="cuda")
+    some = A.ann_oct_quantize(torch.randn((100, 127), device="cuda", generator=torch.Generator("cuda").manual_seed(4)))
+    for at in (0, 1 << 26, n - 100):
+        codes[at:at + 100], scales[at:at + 100] = some.codes, some.scales
+    out = A.ann_oct_dequantize(A.OctRows(codes, scales, 127))
+    want = A.ann_oct_dequantize(some)
+    for at in (0, 1 << 26, n - 100):
+        assert torch.equal(out[at:at + 100], want)
+        out[at:at + 100] = 0
+    for at in range(0, n, 1 << 24):
+        assert not out[at:at + (1 << 24)].any()
 
 
 def test_streams_graphs_and_repeats(env):

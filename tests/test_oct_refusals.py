@@ -24,6 +24,13 @@ def test_refused(name, good, bad):
     refused(name, *{**good, **bad}.values())
 
 
+def test_more_steps_than_32_bits_count_are_refused():
+    big = dict(n=1 << 20, d=1 << 19)  # 2^32 steps
+    for name, args in (("ann_oct_quantize", {**QUANTIZE, **big, "ldx": 1 << 20}), ("ann_oct_dequantize", {**DEQUANTIZE, **big, "ldo": 1 << 20}),
+                       ("ann_oct_product", {**PRODUCT, **big, "ldo": 1 << 20}), ("ann_oct_product", {**PRODUCT, **big, "n": 10, "nx": 1 << 20})):
+        refused(name, *args.values())
+
+
 def test_nothing_to_do_reads_no_pointer():
     L = A.lib()
     for name, args, none in (("ann_oct_quantize", QUANTIZE, dict(n=0, x=None, codes=None, scales=None)),
