@@ -106,7 +106,7 @@ OctProductArgs rows_from(const OctProductArgs& a, u64 at, u64 rows) {
 // Few rows of x, or few tiles: both sides from memory, 16 WF x 16 XF results a wave, exact.  Lane l holds row l & 15 of a
 // fragment; D's column (x) is l & 15 too, its rows (w) 4 (l >> 4) and the three after.  SHARE waves take a part of the steps
 // each; their sums meet in LDS and are added up in the order of the steps.  A step's fragments are asked for while the
-// one before is multiplied.  One row of 4,096 by 131,072 is bound by memory: 116 us, 4.6 TB/s.
+// one before is multiplied.  One row of 4,096 by 131,072 is bound by memory: 98 us, 5.5 TB/s.
 constexpr u32 DIRECT_WAVES = 8;
 template <int WF, int XF, int SHARE>
 constexpr u32 direct_room() {
@@ -273,7 +273,8 @@ struct Wave32 {
   }
   // Results to memory, through LDS of the wave's own: 32 rows of `out` by all the wave's columns at once, so that stores
   // fill lines, and neighbouring ones, wherever a row of `out` begins.  (128 bytes of a row at once: 4,096 x 65,536 of 2,048
-  // to bf16 639 us, 256 bytes 600.)  Pieces of 16 bytes change places by the row's number there.
+  // to bf16 639 us, 256 bytes 600.)  They go through the caches: past them that product takes 552 us rather than 585, but with a
+  // copy of its results behind it 845 rather than 788.  Pieces of 16 bytes change places by the row's number in LDS.
   template <typename OUT>
   __device__ __forceinline__ void store(const OctProductArgs& a, u64 w0, u64 x0, char* room) const {
     constexpr u32 ROW = 32 * WF * sizeof(OUT), PIECES = ROW / 16, AT_ONCE = 64 / PIECES;  // bytes; rows a store
@@ -559,7 +560,17 @@ hipError_t launch_tiles(const OctProductArgs& a, hipStream_t s) {
 
 hipError_t launch_oct_product(const OctProductArgs& a, hipStream_t s) {
   const u64 tiles = (((u64)a.w.n + 31) / 32) * (((u64)a.x.n + 31) / 32);
-  if (a.x.n <= 16) return a.w.steps >= 8 && tiles < 1024 ? launch_direct<2, 1, 8>(a, s) : launch_direct<2, 1, 1>(a, s);
+  if (a.x.n <= 16) {
+    // Waves that share a tile's steps read longer pieces of fewer rows at a time, and the last turn of workgroups costs less;
+    // tiles of 64 rows read the batch half as often.  Each its own tile of 32, eight sharing one of 32, four and eight one of 64:
+    // 1 row of 4,096 by 131,072 118 us, 100, 100 and 98, 16 rows 140, 145, 120 and 120; 1 by 65,600 107, 57, 70 and 60.
+    // 1 row of 1,024 by 100,000 25, 20, 24 and 24, 16 rows 28, 25, 27 and 27, by 131,072 32, 34, 31 and 35; 1 row of 200 by 65,536
+    // 5.6, 7.4, 6.2 and 8.6; 1 of 768 by 20,000 9.6, 6.4, 8.0 and 7.2, by 40,000 9.9, 9.6, 11 and 12.
+    if (tiles < (a.w.steps >= 6 ? 2048 : 1024)) return launch_direct<2, 1, 8>(a, s);
+    if (a.w.steps < 4) return launch_direct<2, 1, 1>(a, s);
+    if (a.w.steps >= 24) return launch_direct<4, 1, 8>(a, s);
+    return a.x.n <= 4 && a.w.steps >= 8 ? launch_direct<2, 1, 8>(a, s) : launch_direct<4, 1, 4>(a, s);
+  }
   if (tiles <= 640) return launch_direct<2, 2, 8>(a, s);
   // (results of 16 bits round far more coarsely than the codes' products are cut)
   return a.odtype == ANN_F32 ? launch_tiles<false>(a, s) : launch_tiles<true>(a, s);

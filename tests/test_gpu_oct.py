@@ -158,6 +158,26 @@ def test_product(env, out, nx, n, d):
         known = check_product(torch, A, x, w, out, pad, known)
 
 
+# (tiles of 32 and of 64 rows, whole steps of a wave and shared ones; the last workgroup's waves partly without a tile)
+@pytest.mark.parametrize("nx,n,d", [(1, 70_001, 300), (16, 33_000, 128), (4, 66_000, 600), (16, 65_573, 1000), (1, 65_600, 1030), (3, 131_071, 2000), (5, 65_537, 2300),
+                                    (1, 65_601, 2980), (16, 65_540, 3200), (9, 40_001, 800), (2, 20_003, 200)])
+def test_few_rows_by_many(env, nx, n, d):
+    torch, A, _ = env
+    g = torch.Generator("cuda").manual_seed(n)
+    x, w = (torch.randn((r, d), device="cuda", generator=g) * torch.exp2(torch.randint(-3, 4, (r, 1), device="cuda", generator=g)) for r in (nx, n))
+    x, w = A.ann_oct_quantize(x), A.ann_oct_quantize(w)
+    xv, wv = A.ann_oct_dequantize(x).double(), A.ann_oct_dequantize(w).double()
+    want, sums = xv @ wv.T, d * 2.0 ** -23 * (xv.abs() @ wv.abs().T)
+    for out in ("float32", "bfloat16"):
+        room = wider(torch, torch.zeros((nx, n), dtype=getattr(torch, out), device="cuda"), 5)
+        got = A.ann_oct_product(x, w, out=room)
+        assert ((got.double() - want).abs() <= sums + HALF[out] * (want.abs() + sums)).all()
+        assert torch.equal(got, A.ann_oct_product(x, w, dtype=got.dtype))
+        side = room._base.clone()
+        side[:, 2:2 + n] = 77
+        assert (side == 77).all(), "elements beside the results changed"
+
+
 def test_product_of_every_code(env):
     """All codes of one side by all of the other, in every place of a step, with scales far apart."""
     torch, A, _ = env
