@@ -220,9 +220,12 @@ __global__ __launch_bounds__(DISTILL_THREADS) void distill_finish_kernel(Distill
 
 // The gradient of a chunk of a row.  The teacher's shares are made anew by every workgroup (k is small); entries of the
 // teacher inside the chunk are read before and written after all others, by the first thread that holds their id,
-// which adds up the shares of the same id in their order.  So `out` may be the scores themselves.  Whether any id is there
-// twice a table tells where k is large: without it 1,000 rows of 20,000 bf16 with k = 1,000 take 247 us, with it 33.
-constexpr u32 DISTILL_FEW = 64, DISTILL_TABLE = 2 * DISTILL_MOST_K;
+// which adds up the shares of the same id in their order.  So `out` may be the scores themselves.  Up to 64 entries lie one a lane
+// in the first wave, which compares them while the gradients are on their way (37 rows of 10,000 fp32 with k = 64 8.0 us, from LDS
+// 10.7).  Of more a table tells whether any id is there twice: without it 1,000 rows of 20,000 bf16 with k = 1,000 take 247 us,
+// with it 33.  Of many rows a workgroup takes 32 KB: 4,096 x 128,000 bf16 374 us, 2,000 x 50,001 fp32 157; 16 KB 385 and 151,
+// 64 KB 386 and 173, whole rows 410 and 189.
+constexpr u32 DISTILL_FEW = 64, DISTILL_TABLE = 2 * DISTILL_MOST_K, GRAD_CHUNK = 32768;
 template <typename T, bool PAST>
 __global__ __launch_bounds__(DISTILL_THREADS) void distill_grad_kernel(DistillArgs a) {
   constexpr u32 E = 16 / sizeof(T), AHEAD = 4;
@@ -237,35 +240,58 @@ __global__ __launch_bounds__(DISTILL_THREADS) void distill_grad_kernel(DistillAr
     T* out = reinterpret_cast<T*>(a.out) + row * a.ldo;
     const float m = a.stats[2 * row], s = a.stats[2 * row + 1];
     const bool few = a.k <= DISTILL_FEW;
-    if (!few)
-      for (u32 i = threadIdx.x; i < DISTILL_TABLE; i += DISTILL_THREADS) table[i] = ANN_NONE;
-    if (threadIdx.x == 0) twice = few;
-    u32 id;
-    float most = -INFINITY;
-#pragma unroll 1
-    for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {
-      const float t = teacher_entry(a, row, j, &id);
-      most = __builtin_fmaxf(most, t);
-      shares[j] = t;
-      const bool here = id >= from && id < to;
-      ids[j] = here ? id : ANN_NONE;
-      if (here) kept[j] = mx_float(z[id]);
-    }
-    most = block_max(most, room.most);
     double weights = 0.0;
+    u32 id;
+    float own_kept = 0.0f, own_share = 0.0f;  // of the entry that a thread writes last, where there are few
+    u32 own_id = ANN_NONE;
+    if (few) {  // every wave makes them by itself, and holds an entry a lane
+      const u32 j = threadIdx.x % 64;
+      float t = -INFINITY;
+      u32 mine = ANN_NONE;
+      if (j < a.k) {
+        t = teacher_entry(a, row, j, &id);
+        if (id >= from && id < to) mine = id;
+        if (mine != ANN_NONE) own_kept = mx_float(z[mine]);
+      }
+      float most = t;
+#pragma unroll
+      for (int w = 1; w < 64; w *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, w));
+      const float share = t == -INFINITY ? 0.0f : soft_exp(t, most, a.c);
+      weights = share;
+#pragma unroll
+      for (int w = 1; w < 64; w *= 2) weights += __shfl_xor(weights, w);
+      own_id = mine;
+      own_share = share;
+      asm volatile("" : "+v"(own_kept));  // the scores kept are there before any wave writes where they were
+      __syncthreads();
+    } else {
+      for (u32 i = threadIdx.x; i < DISTILL_TABLE; i += DISTILL_THREADS) table[i] = ANN_NONE;
+      if (threadIdx.x == 0) twice = 0;
+      float most = -INFINITY;
 #pragma unroll 1
-    for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {  // (a thread's own ones)
-      const float t = shares[j], w = t == -INFINITY ? 0.0f : soft_exp(t, most, a.c);
-      shares[j] = w;
-      weights += w;
-      if (!few && ids[j] != ANN_NONE)
-        for (u32 at = ids[j] * 2654435761u;; ++at) {  // (the table has twice the room of all ids)
-          const u32 there = atomicCAS(&table[at % DISTILL_TABLE], ANN_NONE, ids[j]);
-          if (there == ids[j]) twice = 1;
-          if (there == ids[j] || there == ANN_NONE) break;
-        }
+      for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {
+        const float t = teacher_entry(a, row, j, &id);
+        most = __builtin_fmaxf(most, t);
+        shares[j] = t;
+        const bool here = id >= from && id < to;
+        ids[j] = here ? id : ANN_NONE;
+        if (here) kept[j] = mx_float(z[id]);
+      }
+      most = block_max(most, room.most);
+#pragma unroll 1
+      for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {  // (a thread's own ones)
+        const float t = shares[j], w = t == -INFINITY ? 0.0f : soft_exp(t, most, a.c);
+        shares[j] = w;
+        weights += w;
+        if (ids[j] != ANN_NONE)
+          for (u32 at = ids[j] * 2654435761u;; ++at) {  // (the table has twice the room of all ids)
+            const u32 there = atomicCAS(&table[at % DISTILL_TABLE], ANN_NONE, ids[j]);
+            if (there == ids[j]) twice = 1;
+            if (there == ids[j] || there == ANN_NONE) break;
+          }
+      }
+      weights = block_sum(weights, room.sums);
     }
-    weights = block_sum(weights, room.sums);
     const bool none = weights == 0.0 || s == 0.0f;
     const float over = (float)(1.0 / weights);
     const float up = a.t * a.scale * (a.upstream ? a.upstream[row] : 1.0f);
@@ -287,6 +313,20 @@ __global__ __launch_bounds__(DISTILL_THREADS) void distill_grad_kernel(DistillAr
     }
     const u32 left = from + packs * E + threadIdx.x;
     if (left < to) out[left] = grad(mx_float(z[left]), 0.0f);
+    if (few) {
+      bool first = threadIdx.x < 64 && own_id != ANN_NONE;
+      float p = 0.0f;
+      if (__any(first))  // shares of one id are added up in their order, and written by the first lane that holds it
+        for (u32 i = 0; i < a.k; ++i) {
+          const bool same = (u32)__builtin_amdgcn_readlane((int)own_id, (int)i) == own_id;
+          const float other = __uint_as_float((u32)__builtin_amdgcn_readlane((int)__float_as_uint(own_share), (int)i));
+          p += same ? other * over : 0.0f;
+          first = first && !(same && i < threadIdx.x);
+        }
+      __syncthreads();  // the teacher's entries come last
+      if (first) out[own_id] = grad(own_kept, p);
+      continue;
+    }
     __syncthreads();  // the teacher's entries come last
 #pragma unroll 1
     for (u32 j = threadIdx.x; j < a.k; j += DISTILL_THREADS) {
@@ -465,6 +505,10 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
   a.out = static_cast<char*>(out_dev);
   a.ldo = ldo;
   set_chunks(a);
+  if (rows >= 512) {  // in the rows' order: the fewer places memory is read and written at, the better
+    a.chunk = std::min(a.chunk, (u32)(GRAD_CHUNK / dtype_bytes(dtype)));
+    a.chunks = (a.n + a.chunk - 1) / a.chunk;
+  }
   return launch_distill(a, dtype, true, stream);
 } catch (...) {
   return annmi::on_exception();

@@ -132,6 +132,26 @@ def test_in_place_and_beside(env):
             A.ann_distill_grad(both[:len(out), :300], ids[:len(out)], teacher[:len(out)], stats[:len(out)], out=out)
 
 
+@pytest.mark.parametrize("dtype,n", [("float32", 8193), ("float32", 20_001), ("bfloat16", 33_000)])
+@pytest.mark.parametrize("k", (5, 64, 65, 200))
+def test_parts_of_many_rows(env, dtype, n, k):
+    """Rows of which several workgroups take a part each; the teacher's entries at the parts' ends, some named twice and more;
+    beside the scores, and in their place."""
+    torch, A, _ = env
+    rng = np.random.default_rng(n + k)
+    z, ids, teacher = inputs(torch, rng, 520, n, k, dtype, masked=0.1, short=True)
+    part = 32768 // z.element_size()
+    ends = [0, 1, part - 1, part, n - 1, n - 2, n // 2]
+    for r in range(1, 520, 3):
+        ids[r, :] = dev(torch, rng.choice(ends, k).astype(np.int32))
+    z[:, ends] = dev(torch, rng.standard_normal((520, len(ends)))).to(z.dtype)
+    up = dev(torch, rng.standard_normal(520).astype(np.float32))
+    _, stats, want = check(torch, A, z, ids, teacher, 2.0, up)
+    for _ in range(3):
+        place = z.clone()
+        assert torch.equal(A.ann_distill_grad(place, ids, teacher, stats, grad_losses=up, temperature=2.0, out=place), want)
+
+
 def test_same_id_twice(env):
     torch, A, _ = env
     rng = np.random.default_rng(8)
