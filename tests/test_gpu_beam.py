@@ -178,6 +178,19 @@ def test_reorder(env, groups, beams, k):
             assert torch.equal(states, want), (shape, dim)
 
 
+@pytest.mark.parametrize("bytes_of_a_row", (4096 * 511, 4096 * 512, 4096 * 513 + 16, 4096 * 70 + 4, 1_000_003))
+def test_reorder_of_long_rows(env, bytes_of_a_row):
+    """Rows whose pieces take whole runs of workgroups, and not."""
+    torch, A, _ = env
+    rng = np.random.default_rng(bytes_of_a_row)
+    states = states_of(torch, rng, (2, 6, bytes_of_a_row), torch.int8)
+    parents = dev(torch, rng.integers(0, 3, (2, 3)).astype(np.int32))
+    got = A.ann_beam_reorder(states, parents, 3, dim=1)
+    assert torch.equal(got, gathered(torch, states, parents, 3, 1, got))
+    A.ann_beam_reorder(states, parents, 3, dim=1, out=states)
+    assert torch.equal(states, got)
+
+
 def test_reorder_of_slices(env):
     """The used part of caches with room for more: what lies behind it stays as it was, in place and not; parents that are
     none leave their rows."""
