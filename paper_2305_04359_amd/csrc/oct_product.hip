@@ -567,7 +567,7 @@ hipError_t launch_oct_product(const OctProductArgs& a, hipStream_t s) {
     // 1 row of 1,024 by 100,000 25, 20, 24 and 24, 16 rows 28, 25, 27 and 27, by 131,072 32, 34, 31 and 35; 1 row of 200 by 65,536
     // 5.6, 7.4, 6.2 and 8.6; 1 of 768 by 20,000 9.6, 6.4, 8.0 and 7.2, by 40,000 9.9, 9.6, 11 and 12.
     if (tiles < (a.w.steps >= 6 ? 2048 : 1024)) return launch_direct<2, 1, 8>(a, s);
-    if (a.w.steps < 4) return launch_direct<2, 1, 1>(a, s);
+    if (a.w.steps < 4 || a.w.n >= 1u << 27) return launch_direct<2, 1, 1>(a, s);  // (of the others' tiles there may be too many to launch)
     if (a.w.steps >= 24) return launch_direct<4, 1, 8>(a, s);
     return a.x.n <= 4 && a.w.steps >= 8 ? launch_direct<2, 1, 8>(a, s) : launch_direct<4, 1, 4>(a, s);
   }
