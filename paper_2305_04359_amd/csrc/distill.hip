@@ -52,9 +52,9 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b, float c) {
 }
 
 // 16 bytes wherever they begin.  Gradients go past the caches, and scores that are more than these hold (PAST) come past
-// them, so that they do not drive out what is needed.  Loss and gradient with scores read so, and not: 4,096 x 128,000 bf16 (1 GB)
-// 165 + 414 us and 227 + 426, 4,000 x 32,000 bf16 (256 MB) 44 + 99 and 54 + 85, 700 x 50,001 fp32 (140 MB) 26 + 66 and 25 + 48.
-// Gradients written the plain way: 1,500 x 50,001 fp32 133 us, 123 so.
+// them, so that they do not drive out what is needed.  Loss and gradient with scores read so, and not: 4,096 x 128,000 bf16
+// (1 GB) 546 us and 627, 2,500 x 50,001 fp32 (500 MB) 269 and 285, 1,500 (300 MB) 166 and 146, 700 (140 MB) 82 and 70.  With gradients
+// written the plain way 1,500 x 50,001 fp32 take 179 us, 147 so.
 constexpr u64 DISTILL_PAST = 384ull << 20;
 using Streamed = v4i __attribute__((aligned(2)));
 template <bool PAST, int E, typename T>
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(DISTILL_THREADS) void distill_grad_kernel(DistillAr
 }
 
 // Workgroups for a row: more than one where rows are long and too few for the chip, of at least 8,192 entries each.  Loss and
-// gradient of 37 rows of 10,000 fp32 whole 11.7 us, in two 14.0; of one row of 30,000 bf16 in four 13.3 us, in two 14.8, whole 15.4.
+// gradient of 37 rows of 10,000 fp32 whole 10.7 us, in two 13.0; of one row of 30,000 bf16 in four 12.7 us, in two 13.9, whole 14.6.
 u32 distill_chunks(u64 rows, u64 n) {
   const u64 want = rows >= 512 || n <= 16384 ? 1 : 1024 / rows, most = (n + 8191) / 8192;
   return (u32)std::max<u64>(1, std::min(want, most));
