@@ -592,10 +592,11 @@ int ann_oct_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, uint
 /* out[i][j] = sum over the d elements of value(x row i) * value(row j), summed in
  * fp32 and rounded once to out_dtype (ANN_F32, ANN_F16 or ANN_BF16); out_dev is
  * nx x n, rows ldo >= n apart.  Values and products below 2^-126 may count as 0.
- * Products are whole where the results are ANN_F32.  For ANN_F16 and ANN_BF16 they
- * may be cut: of eight neighbouring ones (elements 8 i to 8 i + 7) what lies below
- * 2^(E - 13), E the exponent of the largest, which is far less than the rounding of
- * the result unless a sum nearly cancels.  The gradients of a layer's product
+ * Products are whole where the results are ANN_F32 or ANN_F16.  For ANN_BF16, in batches
+ * of more than 16 rows, they may be cut: of eight neighbouring ones (elements 8 i to
+ * 8 i + 7) what lies below 2^(E - 13), E the exponent of the largest, some twentieth of
+ * the result's rounding unless a sum nearly cancels; a row's last bits may then depend on
+ * the batch that it is in.  The gradients of a layer's product
  * Y = X W^T, from G = dY, are products too: dX of the rows of G with the columns of
  * W, dW of the columns of G with the columns of X.                           */
 int ann_oct_product(const uint8_t* xcodes_dev, const uint8_t* xscales_dev, uint64_t nx, const uint8_t* codes_dev,
