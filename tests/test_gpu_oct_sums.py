@@ -89,3 +89,26 @@ def test_what_the_cut_takes_from_bf16_results(env, nx, n, d, large):
     assert cut < 2.0 ** -12 * rms  # (a sixteenth of what bf16 may round)
     off = (A.ann_oct_product(x, w, dtype=torch.bfloat16).double() - whole.bfloat16().double()).square().mean()
     assert off <= 2.0 ** -7 * cut * rms + cut * cut, (off.sqrt() / rms, cut / rms)
+
+
+def test_large_tiles_in_a_graph(env):
+    """Captured and replayed on new contents, with eager work between."""
+    torch, A, _ = env
+    g = torch.Generator("cuda").manual_seed(9)
+    x, w = torch.randn((2048, 700), device="cuda", generator=g), torch.randn((8192, 700), device="cuda", generator=g)
+
+    def chain():
+        return [A.ann_oct_product(A.ann_oct_quantize(x), A.ann_oct_quantize(w), dtype=t) for t in (torch.float32, torch.float16, torch.bfloat16)]
+
+    chain()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = chain()
+    for turn in range(4):
+        x.copy_(torch.roll(x, 1, 0))
+        want = chain()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), turn
