@@ -690,7 +690,8 @@ int ann_distill_grad(const void* scores_dev, uint64_t rows, uint64_t n, ann_dtyp
  *   v = total_b + (score_j - log sum_i exp(score_i)), in fp64,
  * the sum over the beam's scores that are not NaN.  Of a group's continuations
  * the k best are kept, ordered by (v downwards, beam, score downwards, entry).
- * Entries of NaN or -inf are none; where some are +inf, those share the beam's
+ * Entries of NaN or -inf are none (masks of the type's lowest number are scores, and
+ * where few others are left take longer); where some are +inf, those share the beam's
  * mass.  A beam with a total of -inf or NaN has none.  A finished beam has one:
  * pad_id, worth its total.
  *   scores_dev    groups * beams rows of n ANN_F32, ANN_F16 or ANN_BF16, ld apart
@@ -718,7 +719,9 @@ int ann_beam_select_scratch(uint64_t groups, uint32_t beams, uint64_t n, uint32_
  * beginning of each side.  Rows of other parents stay as they were.  in_dev and
  * out_dev may be one and the same, with k = beams and the same strides: rows then
  * change places where they are.  Otherwise the two must not overlap.  Rows, runs
- * and outer parts of a side must not overlap either.
+ * and outer parts of a side must not overlap either.  Where the addresses, strides and
+ * run_bytes are multiples of 16 bytes, 16 move at once, of 4 bytes, 4, else one: twice
+ * and seven times slower.
  * beams, k <= 64; groups < 2^25; outer, mid, run_bytes < 2^31; a count of zero:
  * ANN_OK, nothing is done.  Streams, devices and graphs as ann_beam_select.   */
 int ann_beam_reorder(const void* in_dev, void* out_dev, const uint32_t* parents_dev, uint64_t groups, uint32_t beams, uint32_t k,

@@ -138,8 +138,10 @@ __device__ __forceinline__ u32 beam_exactly(const float (&v)[BEAM_EACH], u32 pla
 
 // One chunk of a row a workgroup, 16 entries a thread, which stay in registers.  Every wave finds the ceil(k / 4)-th best
 // of its threads' best ones; the least of these is a bound that k entries reach at least, and few more in most orders;
-// they are listed and brought into order.  64 groups of 5 beams of 50,001 fp32 take 24 us, 2.7 TB/s: a wave waits for half
-// of its life, for memory and at the barriers between bound, list and order.
+// they are listed and brought into order.  (Masks of the lowest number are scores: where so few others are left that
+// the masks are the bound beam_exactly makes the list, with 1 % left of the 50,001 in 93 us, with 0.1 % in 192.)  64 groups of 5
+// beams of 50,001 fp32 take 24 us, 2.7 TB/s: a wave waits for half of its life, for memory and at the barriers between bound,
+// list and order.
 template <typename T>
 __global__ __launch_bounds__(BEAM_THREADS) void beam_chunk_kernel(BeamArgs a) {
   constexpr u32 E = 16 / sizeof(T), WAVES = BEAM_THREADS / 64;
@@ -378,8 +380,10 @@ __global__ __launch_bounds__(PICK_THREADS) void beam_pick_kernel(BeamArgs a) {
 // A thread takes a piece of VEC bytes of the rows of all k beams that go on, so that nobody else reads or writes that piece,
 // and rows can change places where they are: it reads MOST of them before it writes any, all of them in that case.  There
 // rows that stay where they are are not touched.  Bound by memory: 16 layers of 64 rows of 2.3 MB in groups of 8 take 668 us
-// beside them and 575 in place (with stores that the caches keep 3 to 5 % more).  Chiplets take workgroups in turn: each gets runs of
-// pieces, whose rows' parts are longer (without runs 744 and 611, of 32 669 and 574, of 256 689 and 587).
+// beside them and 575 in place, on other cards up to 704 and 697 (with stores that the caches keep 3 to 5 % more).  Chiplets take
+// workgroups in turn: each gets runs of pieces, whose rows' parts are longer (without runs 744 and 611, of 32 669 and 574, of 256
+// 689 and 587).  Offsets that are multiples of four bytes only cost more than twice the time, others seven times: 2.1 GB in rows
+// of 2,046 bytes 4.8 ms, of 2,044 1.55, of 2,048 0.67.
 constexpr u64 REORDER_RUN = 64;
 struct ReorderArgs {
   const char* in;
